@@ -30,6 +30,7 @@ SOURCES = [
     "abi.cpp",
     "abi_parts.cpp",
     "abi_decode16.cpp",
+    "abi_seq.cpp",
     "ternarize_pack.hip",
     "tgemm_fwd.hip",
     "tgemm_bwd_dx.hip",
@@ -43,6 +44,11 @@ SOURCES = [
     "mixer.hip",
     "decode_stack.hip",
     "group_code_dot.hip",
+    "seq_conv.hip",
+    "seq_norm.hip",
+    "seq_scan.hip",
+    "seq_scan_bwd.hip",
+    "embed.hip",
 ]
 
 ARCH = "gfx950"

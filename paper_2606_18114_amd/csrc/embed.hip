@@ -1,0 +1,298 @@
+// Rows of an embedding, e[t] = scale W[id_t] (float32, the residual stream's
+// type), and the gradient of its weight, dW[v] = scale sum_{t: id_t = v} de[t],
+// the tokens of a row in ascending order, so that repeated calls give the same
+// bits.  An id outside [0, V) gives a row of zeros and no gradient.
+//
+// The gradient is bound by writing dW's V rows.  The tokens are sorted by id
+// into segments: a count per id, a place per segment (whichever: only the order
+// inside a segment shows in the sums), and the positions, in any order, which
+// the workgroup of a row brings into ascending order.  An id of more than
+// kEmPiece tokens (the most frequent one of a text is a tenth of it) is cut
+// into pieces of that many, whose sums meet in the row's workgroup; a piece
+// finds its tokens by going through the ids, which are few bytes.
+#include "seq.hpp"
+#include "seq_launch.hpp"
+
+namespace tmk {
+
+constexpr int kEmPiece = 64;  // tokens of a piece
+
+template <typename I>
+__device__ __forceinline__ int64_t em_id(const I* ids, int64_t t, int64_t V) {
+  const int64_t v = (int64_t)ids[t];
+  return v >= 0 && v < V ? v : -1;
+}
+
+// TYPE 0 float32, 1 bfloat16, 2 float16
+template <int TYPE>
+__device__ __forceinline__ void em_ld8(const void* w, int64_t at, float (&v)[8]) {
+  if constexpr (TYPE == 0) {
+    Zx<true>::ld8((const float*)w + at, v);
+  } else if constexpr (TYPE == 1) {
+    Zx<false>::ld8((const uint16_t*)w + at, v);
+  } else {
+    typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+    const f16x8 h = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(
+        (const u32x4_u2*)((const uint16_t*)w + at)));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)h[i];
+  }
+}
+template <int TYPE>
+__device__ __forceinline__ float em_ld(const void* w, int64_t at) {
+  if constexpr (TYPE == 0) return ((const float*)w)[at];
+  else if constexpr (TYPE == 1) return __uint_as_float((uint32_t)((const uint16_t*)w)[at] << 16);
+  else return (float)__builtin_bit_cast(_Float16, ((const uint16_t*)w)[at]);
+}
+
+// grid (T), 256 threads
+template <int TYPE, typename I>
+__global__ __launch_bounds__(256) void embed_kernel(const I* __restrict__ ids, int64_t V,
+                                                    int64_t D, const void* __restrict__ w,
+                                                    float scale, float* __restrict__ out) {
+  const int64_t t = blockIdx.x;
+  const int64_t v = em_id(ids, t, V);
+  float* o = out + t * D;
+  const int64_t D8 = D & ~(int64_t)7;
+  for (int64_t c = (int64_t)threadIdx.x * 8; c < D8; c += 256 * 8) {
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (v >= 0) {
+      em_ld8<TYPE>(w, v * D + c, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= scale;
+    }
+    Zx<true>::st8(o + c, x);
+  }
+  const int64_t c = D8 + threadIdx.x;
+  if (c < D) o[c] = v >= 0 ? em_ld<TYPE>(w, v * D + c) * scale : 0.f;
+}
+
+// the workspace: count, place, filled, first piece [V] each; cursors [2] (of
+// tokens, of pieces); sorted [T]; a piece's id and its number in its row
+// [pieces] each; pieces' sums [pieces][D]
+struct EmbedWs {
+  int *count, *place, *filled, *first, *cursor, *sorted, *pid, *pno;
+  float* psum;
+};
+static int64_t em_pieces(int64_t T) { return 2 * (T / kEmPiece) + 1; }
+static int64_t em_ints(int64_t T, int64_t V) {
+  return (4 * V + 2 + T + 2 * em_pieces(T) + 63) / 64 * 64;
+}
+static EmbedWs em_ws(void* p, int64_t T, int64_t V) {
+  EmbedWs w;
+  int* i = (int*)p;
+  w.count = i, w.place = i + V, w.filled = i + 2 * V, w.first = i + 3 * V, w.cursor = i + 4 * V;
+  w.sorted = w.cursor + 2;
+  w.pid = w.sorted + T;
+  w.pno = w.pid + em_pieces(T);
+  w.psum = (float*)(i + em_ints(T, V));
+  return w;
+}
+int64_t embed_bwd_bytes(int64_t T, int64_t V, int64_t D) {
+  return em_ints(T, V) * 4 + em_pieces(T) * D * 4;
+}
+
+__global__ __launch_bounds__(256) void embed_clear_kernel(EmbedWs w, int64_t V) {
+  const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (v < V) w.count[v] = w.filled[v] = 0;
+  if (v < 2) w.cursor[v] = 0;
+}
+
+template <typename I>
+__global__ __launch_bounds__(256) void embed_count_kernel(const I* __restrict__ ids, int64_t T,
+                                                          int64_t V, EmbedWs w) {
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (t >= T) return;
+  const int64_t v = em_id(ids, t, V);
+  if (v >= 0) atomicAdd(&w.count[v], 1);
+}
+
+// a place for every segment, and the pieces of the long ones
+__global__ __launch_bounds__(256) void embed_place_kernel(int64_t V, EmbedWs w) {
+  __shared__ int sum[2][256], base[2];
+  const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int i = threadIdx.x;
+  const int n = v < V ? w.count[v] : 0;
+  const int np = n > kEmPiece ? (n + kEmPiece - 1) / kEmPiece : 0;
+  int a = n, b = np;  // inclusive sums over the workgroup
+  sum[0][i] = a, sum[1][i] = b;
+  for (int o = 1; o < 256; o <<= 1) {
+    __syncthreads();
+    const int pa = i >= o ? sum[0][i - o] : 0, pb = i >= o ? sum[1][i - o] : 0;
+    __syncthreads();
+    sum[0][i] = a += pa, sum[1][i] = b += pb;
+  }
+  if (i == 255) {
+    base[0] = atomicAdd(&w.cursor[0], a);
+    base[1] = atomicAdd(&w.cursor[1], b);
+  }
+  __syncthreads();
+  if (v >= V) return;
+  w.place[v] = base[0] + a - n;
+  const int first = base[1] + b - np;
+  w.first[v] = first;
+  for (int k = 0; k < np; ++k) w.pid[first + k] = (int)v, w.pno[first + k] = k;
+}
+
+template <typename I>
+__global__ __launch_bounds__(256) void embed_sort_kernel(const I* __restrict__ ids, int64_t T,
+                                                         int64_t V, EmbedWs w) {
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (t >= T) return;
+  const int64_t v = em_id(ids, t, V);
+  if (v < 0 || w.count[v] > kEmPiece) return;  // the pieces find their own
+  w.sorted[w.place[v] + atomicAdd(&w.filled[v], 1)] = (int)t;
+}
+
+// sum of the rows list[0 .. n) of de, columns c .. c + 3 (all below D)
+__device__ __forceinline__ f32x4 em_sum4(const float* __restrict__ de, int64_t D, const int* list,
+                                         int n, int64_t c) {
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  int k = 0;
+  for (; k + 8 <= n; k += 8) {
+    f32x4 x[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) x[q] = *(const f32x4_u4*)(de + (int64_t)list[k + q] * D + c);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) s += x[q];
+  }
+  for (; k < n; ++k) s += *(const f32x4_u4*)(de + (int64_t)list[k] * D + c);
+  return s;
+}
+
+// grid (pieces at most): a piece's tokens, the kEmPiece occurrences of its id
+// from number kEmPiece pno on, then their sum
+template <typename I>
+__global__ __launch_bounds__(256) void embed_piece_kernel(const I* __restrict__ ids, int64_t T,
+                                                          const float* __restrict__ de, int64_t D,
+                                                          EmbedWs w) {
+  __shared__ int list[kEmPiece], wave_n[4];
+  if ((int)blockIdx.x >= w.cursor[1]) return;
+  const int64_t v = w.pid[blockIdx.x];
+  const int lo = w.pno[blockIdx.x] * kEmPiece;
+  const int total = w.count[v] - lo, n = total < kEmPiece ? total : kEmPiece;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  int seen = 0;
+  for (int64_t tb = 0; tb < T && seen < lo + n; tb += 256) {
+    const int64_t t = tb + threadIdx.x;
+    const bool hit = t < T && (int64_t)ids[t] == v;
+    const uint64_t m = __ballot(hit);
+    if (lane == 0) wave_n[wave] = __popcll(m);
+    __syncthreads();
+    int before = seen;
+    for (int k = 0; k < wave; ++k) before += wave_n[k];
+    const int at = before + __popcll(m & ((1ull << lane) - 1)) - lo;
+    if (hit && at >= 0 && at < n) list[at] = (int)t;
+    seen += wave_n[0] + wave_n[1] + wave_n[2] + wave_n[3];
+    __syncthreads();
+  }
+  float* o = w.psum + (int64_t)blockIdx.x * D;
+  const int64_t D4 = D & ~(int64_t)3;
+  for (int64_t c = (int64_t)threadIdx.x * 4; c < D4; c += 1024)
+    *(f32x4_u4*)(o + c) = em_sum4(de, D, list, n, c);
+  for (int64_t c = D4 + threadIdx.x; c < D; c += 256) {
+    float s = 0.f;
+    for (int k = 0; k < n; ++k) s += de[(int64_t)list[k] * D + c];
+    o[c] = s;
+  }
+}
+
+// grid (V): row v, zeros where no token has it
+template <bool ACC>
+__global__ __launch_bounds__(256) void embed_row_kernel(const float* __restrict__ de, int64_t D,
+                                                        float scale, float* __restrict__ dW,
+                                                        EmbedWs w) {
+  __shared__ int list[kEmPiece];
+  const int64_t v = blockIdx.x;
+  int n = w.count[v];
+  if (ACC && n == 0) return;
+  const float* src = de;
+  if (n > kEmPiece) {  // the pieces' sums instead of tokens
+    src = w.psum + (int64_t)w.first[v] * D;
+    n = (n + kEmPiece - 1) / kEmPiece;
+  } else if (n > 0) {
+    // the tokens in ascending order: each goes where as many are smaller
+    const int i = threadIdx.x;
+    const int* seg = w.sorted + w.place[v];
+    if (i < n) {
+      const int t = seg[i];
+      int at = 0;
+      for (int k = 0; k < n; ++k) at += seg[k] < t;
+      list[at] = t;
+    }
+    __syncthreads();
+  }
+  const bool pieces = src != de;
+  float* o = dW + v * D;
+  const int64_t D4 = D & ~(int64_t)3;
+  for (int64_t c = (int64_t)threadIdx.x * 4; c < D4; c += 1024) {
+    f32x4 s;
+    if (pieces) {
+      s = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+      for (int k = 0; k < n; ++k) s += *(const f32x4_u4*)(src + (int64_t)k * D + c);
+    } else {
+      s = em_sum4(src, D, list, n, c);
+    }
+    s *= scale;
+    if (ACC) s += *(const f32x4_u4*)(o + c);
+    *(f32x4_u4*)(o + c) = s;
+  }
+  for (int64_t c = D4 + threadIdx.x; c < D; c += 256) {
+    float s = 0.f;
+    for (int k = 0; k < n; ++k) s += src[(int64_t)(pieces ? k : list[k]) * D + c];
+    o[c] = ACC ? o[c] + s * scale : s * scale;
+  }
+}
+
+template <int TYPE>
+static void embed_go(const void* ids, bool ids64, int64_t T, const void* w, int64_t V, int64_t D,
+                     float scale, float* out, hipStream_t stream) {
+  if (ids64)
+    hipLaunchKernelGGL((embed_kernel<TYPE, int64_t>), dim3((unsigned)T), dim3(256), 0, stream,
+                       (const int64_t*)ids, V, D, w, scale, out);
+  else
+    hipLaunchKernelGGL((embed_kernel<TYPE, int32_t>), dim3((unsigned)T), dim3(256), 0, stream,
+                       (const int32_t*)ids, V, D, w, scale, out);
+}
+
+hipError_t launch_embed(const void* ids, bool ids64, int64_t T, const void* weight, int type,
+                        int64_t V, int64_t D, float scale, float* out, hipStream_t stream) {
+  if (type == 0) embed_go<0>(ids, ids64, T, weight, V, D, scale, out, stream);
+  else if (type == 1) embed_go<1>(ids, ids64, T, weight, V, D, scale, out, stream);
+  else embed_go<2>(ids, ids64, T, weight, V, D, scale, out, stream);
+  return hipGetLastError();
+}
+
+template <typename I>
+static hipError_t embed_bwd_go(const I* ids, int64_t T, const float* de, int64_t V, int64_t D,
+                               float scale, float* dW, bool accumulate, void* workspace,
+                               hipStream_t stream) {
+  const EmbedWs w = em_ws(workspace, T, V);
+  const unsigned vb = (unsigned)((V + 255) / 256), tb = (unsigned)((T + 255) / 256);
+  hipLaunchKernelGGL(embed_clear_kernel, dim3(vb), dim3(256), 0, stream, w, V);
+  hipLaunchKernelGGL(embed_count_kernel<I>, dim3(tb), dim3(256), 0, stream, ids, T, V, w);
+  hipLaunchKernelGGL(embed_place_kernel, dim3(vb), dim3(256), 0, stream, V, w);
+  hipLaunchKernelGGL(embed_sort_kernel<I>, dim3(tb), dim3(256), 0, stream, ids, T, V, w);
+  if (T > kEmPiece)
+    hipLaunchKernelGGL(embed_piece_kernel<I>, dim3((unsigned)em_pieces(T)), dim3(256), 0, stream,
+                       ids, T, de, D, w);
+  if (accumulate)
+    hipLaunchKernelGGL(embed_row_kernel<true>, dim3((unsigned)V), dim3(256), 0, stream, de, D,
+                       scale, dW, w);
+  else
+    hipLaunchKernelGGL(embed_row_kernel<false>, dim3((unsigned)V), dim3(256), 0, stream, de, D,
+                       scale, dW, w);
+  return hipGetLastError();
+}
+
+hipError_t launch_embed_bwd(const void* ids, bool ids64, int64_t T, const float* dout, int64_t V,
+                            int64_t D, float scale, float* dW, bool accumulate, void* workspace,
+                            hipStream_t stream) {
+  return ids64 ? embed_bwd_go((const int64_t*)ids, T, dout, V, D, scale, dW, accumulate,
+                              workspace, stream)
+               : embed_bwd_go((const int32_t*)ids, T, dout, V, D, scale, dW, accumulate,
+                              workspace, stream);
+}
+
+}  // namespace tmk

@@ -1,0 +1,434 @@
+// The selective scan over packed sequences (formulas: seq_scan_dev.hpp).
+//
+// scan_y_kernel: a workgroup of four waves walks the tiles of 64 tokens of one
+// sequence (or of a segment of it) and one head, the state in registers
+// (32 float32 a lane: wave w holds states 32 w .. + 31 of the 64 channels) and,
+// as two bfloat16 terms, in LDS for the products that read it.  Of y^T (64
+// channels x 64 tokens) wave w makes tokens 16 w .. + 15:
+//   g = B C^T (rows s, columns t: its lanes then hold exactly what the next
+//       product wants of it), times e^{c_t - c_s} dt'_s, in two terms;
+//   y^T = x^T g + e^{c_t} S C^T + D x^T.
+// The state takes the tile's e^{c_Q - c_s} dt'_s x_s B_s^T.
+//
+// Where there are too few sequences and heads to fill the chip, a sequence is
+// cut into segments: scan_state_kernel makes each segment's own state,
+// scan_pass_kernel the states that enter the segments, then scan_y_kernel
+// walks all segments at once.
+#include "seq_scan_dev.hpp"
+
+namespace tmk {
+
+// ---- tiles of 64 tokens: B or C rows (128 wide) and x or dy rows (64 wide) ----
+// staged through registers by 256 threads: 4 and 2 vectors of 16 bytes each
+struct TileRegs {
+  u32x4 m[4], v[2];
+};
+// rows t0 .. t0 + 63 of mat (128 columns) and vec (64 columns), zeros from t1 on
+__device__ __forceinline__ void tile_load(TileRegs& r, const uint16_t* mat, int64_t ldm,
+                                          const uint16_t* vec, int64_t ldv, int t0, int t1) {
+  const int tid = threadIdx.x;
+  const u32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int row = q * 16 + (tid >> 4), t = t0 + row;
+    r.m[q] = t < t1 ? ld16(mat + t * ldm + (tid & 15) * 8) : zero;
+  }
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int row = q * 32 + (tid >> 3), t = t0 + row;
+    r.v[q] = t < t1 ? ld16(vec + t * ldv + (tid & 7) * 8) : zero;
+  }
+}
+__device__ __forceinline__ void tile_store(const TileRegs& r, uint8_t* m, uint8_t* v) {
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) st16(m + (q * 16 + (tid >> 4)) * kScRowN + (tid & 15) * 16, r.m[q]);
+#pragma unroll
+  for (int q = 0; q < 2; ++q) st16(v + (q * 32 + (tid >> 3)) * kScRowP + (tid & 7) * 16, r.v[q]);
+}
+
+// The wave's state slice += sum_s coef_s vec_s mat_s^T over the tile: rows
+// (states) 32 w + 16 nb + 4 (lane / 16) + i, columns (channels) 16 pb + lane % 16.
+template <int NT>
+__device__ __forceinline__ void state_add(f32x4 (&S)[2][4], const uint8_t* m, const uint8_t* v,
+                                          const float* coef) {
+  const int wave = threadIdx.x >> 6, g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    const int r = 32 * kb + 8 * g;
+    float w[8];
+    const f32x4 w0 = *(const f32x4*)(coef + r), w1 = *(const f32x4*)(coef + r + 4);
+    w[0] = w0.x, w[1] = w0.y, w[2] = w0.z, w[3] = w0.w;
+    w[4] = w1.x, w[5] = w1.y, w[6] = w1.z, w[7] = w1.w;
+    bf16x8 a[2][NT];
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb) {
+      const bf16x8 raw = tr_op(m, kScRowN, r, r + 4, 32 * wave + 16 * nb);
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = (float)raw[i] * w[i];
+      split8<NT>(f, a[nb]);
+    }
+#pragma unroll
+    for (int pb = 0; pb < 4; ++pb) {
+      const bf16x8 b = tr_op(v, kScRowP, r, r + 4, 16 * pb);
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+        for (int q = 0; q < NT; ++q) S[nb][pb] = mfma16(a[nb][q], b, S[nb][pb]);
+    }
+  }
+}
+
+// ---- a segment's own state -------------------------------------------------
+// REV false: vec = x, mat = B, coefficient e^{c_Q - c_s} dt'_s, tiles forward:
+// the state at the segment's end from the segment alone; its sequence's last
+// segment has no use for it.  REV true: vec = dy, mat = C, coefficient e^{c_t},
+// tiles backward: the gradient with respect to the state before the segment;
+// not for the first segment.  grid (slots, nheads), 256 threads.
+template <bool F32, bool REV, int NT>
+__global__ __launch_bounds__(256) void scan_state_kernel(
+    const typename Zx<F32>::T* __restrict__ zx, const uint16_t* __restrict__ u,
+    const uint16_t* __restrict__ dy, int T, int nheads, const int* __restrict__ off, int nseq,
+    int segT, const float* __restrict__ dt_bias, const float* __restrict__ A_log,
+    float* __restrict__ state, float* __restrict__ decay) {
+  __shared__ __attribute__((aligned(16))) uint8_t m[kScQ * kScRowN], v[kScQ * kScRowP];
+  __shared__ Toks<kScQ> tk;
+  __shared__ __attribute__((aligned(16))) float coef[kScQ];
+  const int h = blockIdx.y, sl = blockIdx.x;
+  const Slot s = slot_find(off, nseq, T, segT, sl);
+  if (s.t0 >= s.t1 || (REV ? s.k == 0 : s.t1 == s.en)) return;
+  const int d = nheads * kSqP, cd = d + 2 * kSqN;
+  const int64_t Z = (int64_t)2 * d + 2 * kSqN + nheads;
+  const uint16_t* mat = u + d + (REV ? kSqN : 0);
+  const uint16_t* vec = REV ? dy + h * kSqP : u + h * kSqP;
+  const int64_t ldv = REV ? d : cd;
+  const float bias = dt_bias[h], rate = expf(A_log[h]);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  f32x4 S[2][4];
+#pragma unroll
+  for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+    for (int pb = 0; pb < 4; ++pb) S[nb][pb] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float dec = 1.f;
+  const int nt = (s.t1 - s.t0 + kScQ - 1) / kScQ;
+  for (int q = 0; q < nt; ++q) {
+    const int t0 = s.t0 + (REV ? nt - 1 - q : q) * kScQ, t1 = min(s.t1, t0 + kScQ);
+    TileRegs r;
+    tile_load(r, mat, cd, vec, ldv, t0, t1);
+    if (wave == 0) {
+      const float raw[1] = {tok_raw<F32>(zx, Z, nheads, h, min(t0 + lane, T - 1)) + bias};
+      toks_make<kScQ>(tk, raw, t1 - t0, rate);
+      // (one wave wrote and reads these)
+      coef[lane] = REV ? tk.ec[lane] : tk.eq[lane] * tk.dt[lane];
+    }
+    tile_store(r, m, v);
+    __syncthreads();
+    const float last = tk.last;
+    dec *= last;
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb) S[nb][pb] *= last;
+    state_add<NT>(S, m, v, coef);
+    __syncthreads();
+  }
+  float* o = state + ((int64_t)sl * nheads + h) * kScState;
+#pragma unroll
+  for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+    for (int pb = 0; pb < 4; ++pb)
+      *(f32x4*)(o + (16 * pb + (lane & 15)) * kSqN + 32 * wave + 16 * nb + 4 * (lane >> 4)) =
+          S[nb][pb];
+  if (threadIdx.x == 0) decay[(int64_t)sl * nheads + h] = dec;
+}
+
+// ---- the states that enter the segments, in place of the segments' own -----
+// grid (kScState / 1024, nheads, nseq), 256 threads, 4 values each.  REV false:
+// E_0 = the initial state, E_{k+1} = decay_k E_k + own_k; true: from the last
+// segment down, E_last = 0.
+template <bool REV>
+__global__ __launch_bounds__(256) void scan_pass_kernel(float* __restrict__ state,
+                                                        const float* __restrict__ decay, int T,
+                                                        int nheads, const int* __restrict__ off,
+                                                        int segT,
+                                                        const uint16_t* __restrict__ init) {
+  const int h = blockIdx.y, i = blockIdx.z;
+  const int st = off ? slot_off(off, T, i) : 0, en = off ? slot_off(off, T, i + 1) : T;
+  const int nk = en > st ? (en - st + segT - 1) / segT : 0;
+  if (nk == 0) return;
+  const int64_t base = st / segT + i;
+  const int e = (int)(blockIdx.x * 256 + threadIdx.x) * 4;
+  f32x4 E = {0.f, 0.f, 0.f, 0.f};
+  if (!REV && init) {
+    const u32x2 w = *(const u32x2*)(init + ((int64_t)i * nheads + h) * kScState + e);
+    E = f32x4{h2f((uint16_t)w.x), h2f((uint16_t)(w.x >> 16)), h2f((uint16_t)w.y),
+              h2f((uint16_t)(w.y >> 16))};
+  }
+  auto at = [&](int k) { return state + ((base + k) * nheads + h) * kScState + e; };
+  constexpr int kAhead = 4;  // segments whose loads are issued together
+  for (int kb = 0; kb < nk; kb += kAhead) {
+    f32x4 own[kAhead];
+    float dec[kAhead];
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) {
+      const int k = kb + q;
+      own[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+      dec[q] = 0.f;
+      if (k + 1 < nk) {  // the last one's own state feeds nothing
+        const int kk = REV ? nk - 1 - k : k;
+        own[q] = *(const f32x4*)at(kk);
+        dec[q] = decay[(base + kk) * nheads + h];
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) {
+      const int k = kb + q;
+      if (k >= nk) break;
+      *(f32x4*)at(REV ? nk - 1 - k : k) = E;
+      E = E * dec[q] + own[q];
+    }
+  }
+}
+
+// ---- y ---------------------------------------------------------------------
+// grid (slots, nheads), 256 threads.  enter: the states that enter the segments,
+// or NULL where every sequence is one segment.
+template <bool F32>
+__global__ __launch_bounds__(256) void scan_y_kernel(
+    const typename Zx<F32>::T* __restrict__ zx, const uint16_t* __restrict__ u, int T, int nheads,
+    const int* __restrict__ off, int nseq, int segT, const float* __restrict__ dt_bias,
+    const float* __restrict__ A_log, const float* __restrict__ Dp, const uint16_t* init,
+    const float* __restrict__ enter, uint16_t* final_, uint16_t* __restrict__ y) {
+  __shared__ __attribute__((aligned(16))) uint8_t Bt[kScQ * kScRowN], xt[kScQ * kScRowP];
+  __shared__ __attribute__((aligned(16))) uint8_t Sl[2][kSqP * kScRowN];  // the state's terms
+  __shared__ Toks<kScQ> tk;
+  __shared__ __attribute__((aligned(16))) float coef[kScQ];
+  const int h = blockIdx.y, sl = blockIdx.x;
+  const Slot s = slot_find(off, nseq, T, segT, sl);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
+  const int64_t sat = ((int64_t)s.i * nheads + h) * kScState;
+  if (s.t0 >= s.t1) {
+    // an empty sequence's state stays what it was
+    if (s.k == 0 && s.en <= s.st && final_ && final_ != init)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int e = (q * 256 + (int)threadIdx.x) * 8;
+        st16(final_ + sat + e, init ? ld16(init + sat + e) : u32x4{0, 0, 0, 0});
+      }
+    return;
+  }
+  const int d = nheads * kSqP, cd = d + 2 * kSqN;
+  const int64_t Z = (int64_t)2 * d + 2 * kSqN + nheads;
+  const float bias = dt_bias[h], rate = expf(A_log[h]), skip = Dp[h];
+  const uint16_t *Bg = u + d, *Cg = Bg + kSqN, *xg = u + h * kSqP;
+  f32x4 S[2][4];
+#pragma unroll
+  for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+    for (int pb = 0; pb < 4; ++pb) {
+      const int e = (16 * pb + col) * kSqN + 32 * wave + 16 * nb + 4 * g;
+      S[nb][pb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (s.k > 0) {
+        if (enter) S[nb][pb] = *(const f32x4*)(enter + ((int64_t)sl * nheads + h) * kScState + e);
+      } else if (init) {
+        const u32x2 w = *(const u32x2*)(init + sat + e);
+        S[nb][pb] = f32x4{h2f((uint16_t)w.x), h2f((uint16_t)(w.x >> 16)), h2f((uint16_t)w.y),
+                          h2f((uint16_t)(w.y >> 16))};
+      }
+    }
+  TileRegs r;
+  bf16x8 cn[4];
+  float raw;
+  // this wave's 16 rows of C as operands (their columns contiguous)
+  auto load = [&](int t0) {
+    const int t1 = min(s.t1, t0 + kScQ);
+    tile_load(r, Bg, cd, xg, cd, t0, t1);
+    const int t = t0 + 16 * wave + col;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      cn[k] = as_bf16x8(t < t1 ? ld16(Cg + (int64_t)t * cd + 32 * k + 8 * g) : u32x4{0, 0, 0, 0});
+    if (wave == 0) raw = tok_raw<F32>(zx, Z, nheads, h, min(t0 + lane, T - 1)) + bias;
+  };
+  load(s.t0);
+  for (int t0 = s.t0; t0 < s.t1; t0 += kScQ) {
+    const int t1 = min(s.t1, t0 + kScQ);
+    tile_store(r, Bt, xt);
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb) {
+        const float f[4] = {S[nb][pb].x, S[nb][pb].y, S[nb][pb].z, S[nb][pb].w};
+        uint32_t a[2], b[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          a[i] = bf_pack(f[2 * i], f[2 * i + 1]);
+          b[i] = bf_pack(f[2 * i] - bf_lo(a[i]), f[2 * i + 1] - bf_hi(a[i]));
+        }
+        const int at = (16 * pb + col) * kScRowN + 2 * (32 * wave + 16 * nb + 4 * g);
+        *(u32x2*)(Sl[0] + at) = u32x2{a[0], a[1]};
+        *(u32x2*)(Sl[1] + at) = u32x2{b[0], b[1]};
+      }
+    if (wave == 0) {
+      const float rr[1] = {raw};
+      toks_make<kScQ>(tk, rr, t1 - t0, rate);
+      coef[lane] = tk.eq[lane] * tk.dt[lane];
+    }
+    bf16x8 C[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) C[k] = cn[k];
+    __syncthreads();
+    if (t0 + kScQ < s.t1) load(t0 + kScQ);
+
+    // e^{c_t} S C^T first: scaled, it is what the tile's own product adds to
+    const int tt = 16 * wave + col;  // this lane's token in the tile
+    f32x4 acc[4];
+#pragma unroll
+    for (int pb = 0; pb < 4; ++pb) {
+      acc[pb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        acc[pb] = mfma16(row_op(Sl[1], kScRowN, 16 * pb, 32 * k), C[k], acc[pb]);
+        acc[pb] = mfma16(row_op(Sl[0], kScRowN, 16 * pb, 32 * k), C[k], acc[pb]);
+      }
+      acc[pb] *= tk.ec[tt];
+    }
+    // g of this wave's tokens with the s up to them, 32 at a time
+    const float thi = tk.hi[tt], tlo = tk.lo[tt];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      if (2 * kb > wave) break;
+      float gv[8];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int sb = 2 * kb + half;
+        f32x4 a = {0.f, 0.f, 0.f, 0.f};
+        if (sb <= wave)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) a = mfma16(row_op(Bt, kScRowN, 16 * sb, 32 * k), C[k], a);
+        const int s0 = 16 * sb + 4 * g;
+        const f32x4 shi = *(const f32x4*)(tk.hi + s0), slo = *(const f32x4*)(tk.lo + s0),
+                    sdt = *(const f32x4*)(tk.dt + s0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = __builtin_amdgcn_exp2f((thi - shi[i]) + (tlo - slo[i]));
+          gv[4 * half + i] = s0 + i <= tt ? a[i] * e * sdt[i] : 0.f;
+        }
+      }
+      bf16x8 gt[2];
+      split8<2>(gv, gt);
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb) {
+        const bf16x8 xo = tr_op(xt, kScRowP, 32 * kb + 4 * g, 32 * kb + 16 + 4 * g, 16 * pb);
+        acc[pb] = mfma16(xo, gt[1], acc[pb]);
+        acc[pb] = mfma16(xo, gt[0], acc[pb]);
+      }
+    }
+    if (t0 + tt < t1) {
+      uint16_t* o = y + (int64_t)(t0 + tt) * d + h * kSqP + 4 * g;
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb) {
+        const u32x2 xw = *(const u32x2*)(xt + tt * kScRowP + 2 * (16 * pb + 4 * g));
+        const f32x4 a = acc[pb];
+        *(u32x2*)(o + 16 * pb) =
+            u32x2{bf_pack(__builtin_fmaf(skip, bf_lo(xw.x), a.x), __builtin_fmaf(skip, bf_hi(xw.x), a.y)),
+                  bf_pack(__builtin_fmaf(skip, bf_lo(xw.y), a.z), __builtin_fmaf(skip, bf_hi(xw.y), a.w))};
+      }
+    }
+    // the state at the tile's end
+    const float last = tk.last;
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb) S[nb][pb] *= last;
+    state_add<2>(S, Bt, xt, coef);
+    __syncthreads();
+  }
+  if (final_ && s.t1 == s.en) {
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb) {
+        const f32x4 v = S[nb][pb];
+        *(u32x2*)(final_ + sat + (16 * pb + col) * kSqN + 32 * wave + 16 * nb + 4 * g) =
+            u32x2{(uint32_t)f2h(v.x) | ((uint32_t)f2h(v.y) << 16),
+                  (uint32_t)f2h(v.z) | ((uint32_t)f2h(v.w) << 16)};
+      }
+  }
+}
+
+// Tokens of a segment: enough segments for two workgroups on every CU.
+static int64_t scan_seg(int64_t T, int64_t nseq, int64_t nheads) {
+  const int64_t want = (512 + nheads - 1) / nheads;  // segments
+  if (nseq >= want || T <= 4 * kScQ) return T;
+  const int64_t tiles = (T + kScQ - 1) / kScQ;
+  int64_t per = tiles / (want - nseq + 1);  // T / seg + nseq >= want
+  if (per < 2) per = 2;
+  return per >= tiles ? T : per * kScQ;
+}
+
+int64_t seq_scan_bytes(int64_t T, int64_t nseq, int64_t nheads) {
+  const int64_t seg = scan_seg(T, nseq, nheads);
+  if (seg >= T) return 0;
+  return slot_count(T, nseq, seg) * nheads * (kScState + 1) * 4;
+}
+
+hipError_t launch_scan_states(const SeqIn& in, const uint16_t* u, const uint16_t* dy, bool rev,
+                              int terms, int segT, const float* dt_bias, const float* A_log,
+                              const uint16_t* init, float* state, float* decay,
+                              hipStream_t stream) {
+  const dim3 grid((unsigned)slot_count(in.T, in.nseq, segT), (unsigned)in.nheads);
+  auto go = [&](auto kern, auto zx) {
+    hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, zx, u, dy, in.T, in.nheads, in.offsets,
+                       in.nseq, segT, dt_bias, A_log, state, decay);
+  };
+  const float* zf = (const float*)in.zx;
+  const uint16_t* zb = (const uint16_t*)in.zx;
+  if (rev) {
+    if (in.f32) go(scan_state_kernel<true, true, 3>, zf);
+    else go(scan_state_kernel<false, true, 3>, zb);
+  } else if (terms == 3) {
+    if (in.f32) go(scan_state_kernel<true, false, 3>, zf);
+    else go(scan_state_kernel<false, false, 3>, zb);
+  } else {
+    if (in.f32) go(scan_state_kernel<true, false, 2>, zf);
+    else go(scan_state_kernel<false, false, 2>, zb);
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const dim3 pg(kScState / 1024, (unsigned)in.nheads, (unsigned)in.nseq);
+  if (rev)
+    hipLaunchKernelGGL(scan_pass_kernel<true>, pg, dim3(256), 0, stream, state, decay, in.T,
+                       in.nheads, in.offsets, segT, init);
+  else
+    hipLaunchKernelGGL(scan_pass_kernel<false>, pg, dim3(256), 0, stream, state, decay, in.T,
+                       in.nheads, in.offsets, segT, init);
+  return hipGetLastError();
+}
+
+hipError_t launch_seq_scan(const SeqIn& in, const uint16_t* u, const float* dt_bias,
+                           const float* A_log, const float* D, const uint16_t* ssm_in,
+                           uint16_t* ssm_out, uint16_t* y, void* workspace, hipStream_t stream) {
+  const int64_t seg = scan_seg(in.T, in.nseq, in.nheads);
+  float* enter = nullptr;
+  const int64_t slots = slot_count(in.T, in.nseq, seg);
+  if (seg < in.T) {
+    enter = (float*)workspace;
+    const hipError_t e = launch_scan_states(in, u, nullptr, false, 2, (int)seg, dt_bias, A_log,
+                                            ssm_in, enter, enter + slots * in.nheads * kScState,
+                                            stream);
+    if (e != hipSuccess) return e;
+  }
+  const dim3 grid((unsigned)slots, (unsigned)in.nheads);
+  if (in.f32)
+    hipLaunchKernelGGL(scan_y_kernel<true>, grid, dim3(256), 0, stream, (const float*)in.zx, u,
+                       in.T, in.nheads, in.offsets, in.nseq, (int)seg, dt_bias, A_log, D, ssm_in,
+                       enter, ssm_out, y);
+  else
+    hipLaunchKernelGGL(scan_y_kernel<false>, grid, dim3(256), 0, stream, (const uint16_t*)in.zx,
+                       u, in.T, in.nheads, in.offsets, in.nseq, (int)seg, dt_bias, A_log, D,
+                       ssm_in, enter, ssm_out, y);
+  return hipGetLastError();
+}
+
+}  // namespace tmk

@@ -103,6 +103,28 @@ SIGNATURES_DECODE16 = {
                                           _P, _P, _P, _P]),
 }
 
+# the calls of include/tmamba_seq.h
+SIGNATURES_SEQ = {
+    "tm_mixer_conv": (ctypes.c_int, [_P, _I32, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "tm_mixer_conv_bwd": (ctypes.c_int, [_P, _I32, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _P,
+                                         _P, _I64, _P]),
+    "tm_mixer_conv_bwd_workspace": (ctypes.c_int64, [_I64, _I32]),
+    "tm_mixer_scan": (ctypes.c_int, [_P, _P, _I32, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _P,
+                                     _P, _I64, _P]),
+    "tm_mixer_scan_workspace": (ctypes.c_int64, [_I64, _I32, _I32]),
+    "tm_mixer_scan_bwd": (ctypes.c_int, [_P, _P, _I32, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P,
+                                         _P, _P, _P, _P, _P, _I64, _P]),
+    "tm_mixer_scan_bwd_workspace": (ctypes.c_int64, [_I64, _I32, _I32]),
+    "tm_mixer_norm": (ctypes.c_int, [_P, _P, _I32, _I64, _I32, _P, ctypes.c_float, _P, _P]),
+    "tm_mixer_norm_bwd": (ctypes.c_int, [_P, _P, _I32, _I64, _I32, _P, ctypes.c_float, _P, _P, _P,
+                                         _P, _P, _I64, _P]),
+    "tm_mixer_norm_bwd_workspace": (ctypes.c_int64, [_I64, _I32]),
+    "tm_embed": (ctypes.c_int, [_P, _I32, _I64, _P, _I32, _I64, _I64, ctypes.c_float, _P, _P]),
+    "tm_embed_bwd": (ctypes.c_int, [_P, _I32, _I64, _P, _I64, _I64, ctypes.c_float, _P, _I32, _P,
+                                    _I64, _P]),
+    "tm_embed_bwd_workspace": (ctypes.c_int64, [_I64, _I64, _I64]),
+}
+
 
 class TernaryError(RuntimeError):
     def __init__(self, fn: str, status: int):
@@ -125,7 +147,7 @@ def lib() -> ctypes.CDLL:
                 "(or __graft_entry__.build()); there is no fallback implementation")
         L = ctypes.CDLL(_LIB_PATH)
         for name, (res, args) in (*SIGNATURES.items(), *SIGNATURES_PARTS.items(),
-                                  *SIGNATURES_DECODE16.items()):
+                                  *SIGNATURES_DECODE16.items(), *SIGNATURES_SEQ.items()):
             f = getattr(L, name)
             f.restype = res
             f.argtypes = args
@@ -863,3 +885,259 @@ def mamba2_decode_token(arrays: dict, g: int, eps: float, emb: torch.Tensor,
                                       workspace.numel(), _stream())
     _check("tm_mamba2_decode_token", rc)
     return x_out
+
+
+# ---- the mixer over whole sequences, and the embedding (include/tmamba_seq.h) ----
+
+_ZX = (torch.bfloat16, torch.float32)
+_IDS = (torch.int32, torch.int64)
+_EMBED_TYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _call(fn: str, device: torch.device, *args) -> None:
+    """The library call fn on the device's current stream (appended as the
+    last argument), with that device current."""
+    if device.index == torch._C._cuda_getDevice():
+        _check(fn, getattr(lib(), fn)(*args, _stream()))
+        return
+    with torch.cuda.device(device):
+        _check(fn, getattr(lib(), fn)(*args, _stream()))
+
+
+def _seq_ws(fn: str, device: torch.device, *sizes):
+    """Scratch of one call as (tensor or None, pointer, bytes)."""
+    n = int(getattr(lib(), fn)(*sizes))
+    if n < 0:
+        raise ValueError(f"{fn}: sizes {sizes} out of range")
+    if n == 0:
+        return None, None, 0
+    ws = torch.empty((n,), dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr(), n
+
+
+def _seq_in(zxbcdt: torch.Tensor, H: int, offsets: Optional[torch.Tensor]):
+    """Checks zxbcdt [T, Z] and the offsets; (device, T, nseq, d, cd, z_f32)."""
+    _need(zxbcdt, "zxbcdt", _ZX, 2)
+    dev = zxbcdt.device
+    T = zxbcdt.shape[0]
+    d = H * MIXER_HEADDIM
+    _shape(zxbcdt, "zxbcdt", (T, 2 * d + 2 * MIXER_DSTATE + H), dev)
+    nseq = 1
+    if offsets is not None:
+        _need(offsets, "offsets", (torch.int32,), 1)
+        if offsets.shape[0] < 2:
+            raise ValueError("offsets must hold the sequences' beginnings and the last one's end")
+        nseq = offsets.shape[0] - 1
+        _shape(offsets, "offsets", (nseq + 1,), dev)
+    return dev, T, nseq, d, d + 2 * MIXER_DSTATE, int(zxbcdt.dtype == torch.float32)
+
+
+def _of(t: torch.Tensor, name: str, dtypes, shape, dev) -> None:
+    _need(t, name, dtypes, len(shape))
+    _shape(t, name, shape, dev)
+
+
+def _grad_zx(dzxbcdt: torch.Tensor, zxbcdt: torch.Tensor) -> None:
+    _of(dzxbcdt, "dzxbcdt", (zxbcdt.dtype,), tuple(zxbcdt.shape), zxbcdt.device)
+
+
+def _heads_of(cd: int) -> int:
+    """Heads of a layer whose convolution has cd channels; a cd that no layer
+    has gives a count whose shapes do not fit."""
+    return max((cd - 2 * MIXER_DSTATE) // MIXER_HEADDIM, 0)
+
+
+def mixer_conv(zxbcdt: torch.Tensor, conv_w: torch.Tensor, conv_b: torch.Tensor,
+               offsets: Optional[torch.Tensor] = None,
+               conv_state: Optional[torch.Tensor] = None,
+               conv_pos: Optional[torch.Tensor] = None, *,
+               conv_out: Optional[torch.Tensor] = None,
+               u: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The mixer's causal convolution and SiLU over packed sequences
+    (tm_mixer_conv): zxbcdt [T, Z] bfloat16 or float32 -> u bfloat16
+    [T, conv_dim].  offsets int32 [nseq + 1] on the GPU (None: one sequence).
+    conv_state (float16 ring [nseq, conv_dim, 4]) gives the inputs before each
+    sequence (None: zeros) and conv_out receives the last four after it (may
+    be conv_state); both take conv_pos int32 [1], which stays as it is."""
+    _need(conv_b, "conv_b", _F32, 1)
+    dev, T, nseq, d, cd, f32 = _seq_in(zxbcdt, _heads_of(conv_b.shape[0]), offsets)
+    _of(conv_w, "conv_w", _F32, (cd, 4), dev)
+    _of(conv_b, "conv_b", _F32, (cd,), dev)
+    for t, name in ((conv_state, "conv_state"), (conv_out, "conv_out")):
+        if t is not None:
+            _of(t, name, _F16, (nseq, cd, 4), dev)
+            if conv_pos is None:
+                raise ValueError(f"{name} needs conv_pos")
+    if conv_pos is not None:
+        _of(conv_pos, "conv_pos", (torch.int32,), (1,), dev)
+    if u is None:
+        u = torch.empty((T, cd), dtype=torch.bfloat16, device=dev)
+    _of(u, "u", _BF16, (T, cd), dev)
+    if T == 0:
+        return u
+    _call("tm_mixer_conv", dev, _ptr(zxbcdt), f32, T, nseq, d // MIXER_HEADDIM, _ptr(offsets),
+          _ptr(conv_w), _ptr(conv_b), _ptr(conv_state), _ptr(conv_pos), _ptr(conv_out), _ptr(u))
+    return u
+
+
+def mixer_conv_bwd(zxbcdt: torch.Tensor, conv_w: torch.Tensor, conv_b: torch.Tensor,
+                   du: torch.Tensor, dzxbcdt: torch.Tensor,
+                   offsets: Optional[torch.Tensor] = None):
+    """Gradients of mixer_conv without states (tm_mixer_conv_bwd): writes the
+    xBC columns of dzxbcdt (zxbcdt's shape and type) and returns (dconv_w
+    [conv_dim, 4], dconv_b [conv_dim])."""
+    _need(conv_b, "conv_b", _F32, 1)
+    dev, T, nseq, d, cd, f32 = _seq_in(zxbcdt, _heads_of(conv_b.shape[0]), offsets)
+    H = d // MIXER_HEADDIM
+    _of(conv_w, "conv_w", _F32, (cd, 4), dev)
+    _of(conv_b, "conv_b", _F32, (cd,), dev)
+    _of(du, "du", _BF16, (T, cd), dev)
+    _grad_zx(dzxbcdt, zxbcdt)
+    dw = torch.empty((cd, 4), dtype=torch.float32, device=dev)
+    db = torch.empty((cd,), dtype=torch.float32, device=dev)
+    if T == 0:
+        return dw.zero_(), db.zero_()
+    ws, wp, wb = _seq_ws("tm_mixer_conv_bwd_workspace", dev, T, H)
+    _call("tm_mixer_conv_bwd", dev, _ptr(zxbcdt), f32, T, nseq, H, _ptr(offsets), _ptr(conv_w),
+          _ptr(conv_b), _ptr(du), _ptr(dzxbcdt), _ptr(dw), _ptr(db), wp, wb)
+    return dw, db
+
+
+def _scan_args(u, zxbcdt, dt_bias, A_log, D, offsets):
+    _need(A_log, "A_log", _F32, 1)
+    H = A_log.shape[0]
+    dev, T, nseq, d, cd, f32 = _seq_in(zxbcdt, H, offsets)
+    _of(u, "u", _BF16, (T, cd), dev)
+    for t, name in ((dt_bias, "dt_bias"), (A_log, "A_log"), (D, "D")):
+        _of(t, name, _F32, (H,), dev)
+    return dev, T, nseq, H, d, cd, f32
+
+
+def mixer_scan(u: torch.Tensor, zxbcdt: torch.Tensor, dt_bias: torch.Tensor, A_log: torch.Tensor,
+               D: torch.Tensor, offsets: Optional[torch.Tensor] = None,
+               ssm_state: Optional[torch.Tensor] = None, *,
+               ssm_out: Optional[torch.Tensor] = None,
+               y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The selective state space scan over packed sequences (tm_mixer_scan):
+    u bfloat16 [T, conv_dim] (mixer_conv's) and dt of zxbcdt -> y bfloat16
+    [T, d_inner].  ssm_state (float16 [nseq, nheads, 64, 128]): the states
+    before the sequences (None: zeros); ssm_out receives those after them (may
+    be ssm_state)."""
+    dev, T, nseq, H, d, cd, f32 = _scan_args(u, zxbcdt, dt_bias, A_log, D, offsets)
+    for t, name in ((ssm_state, "ssm_state"), (ssm_out, "ssm_out")):
+        if t is not None:
+            _of(t, name, _F16, (nseq, H, MIXER_HEADDIM, MIXER_DSTATE), dev)
+    if y is None:
+        y = torch.empty((T, d), dtype=torch.bfloat16, device=dev)
+    _of(y, "y", _BF16, (T, d), dev)
+    if T == 0:
+        return y
+    ws, wp, wb = _seq_ws("tm_mixer_scan_workspace", dev, T, nseq, H)
+    _call("tm_mixer_scan", dev, _ptr(u), _ptr(zxbcdt), f32, T, nseq, H, _ptr(offsets),
+          _ptr(dt_bias), _ptr(A_log), _ptr(D), _ptr(ssm_state), _ptr(ssm_out), _ptr(y), wp, wb)
+    return y
+
+
+def mixer_scan_bwd(u: torch.Tensor, zxbcdt: torch.Tensor, dt_bias: torch.Tensor,
+                   A_log: torch.Tensor, D: torch.Tensor, dy: torch.Tensor, dzxbcdt: torch.Tensor,
+                   offsets: Optional[torch.Tensor] = None, *,
+                   du: Optional[torch.Tensor] = None):
+    """Gradients of mixer_scan without states (tm_mixer_scan_bwd): writes the
+    dt columns of dzxbcdt and returns (du bfloat16 [T, conv_dim], ddt_bias,
+    dA_log, dD [nheads])."""
+    dev, T, nseq, H, d, cd, f32 = _scan_args(u, zxbcdt, dt_bias, A_log, D, offsets)
+    _of(dy, "dy", _BF16, (T, d), dev)
+    _grad_zx(dzxbcdt, zxbcdt)
+    if du is None:
+        du = torch.empty((T, cd), dtype=torch.bfloat16, device=dev)
+    _of(du, "du", _BF16, (T, cd), dev)
+    out = torch.empty((3, H), dtype=torch.float32, device=dev)
+    if T == 0:
+        return (du, *out.zero_())
+    ws, wp, wb = _seq_ws("tm_mixer_scan_bwd_workspace", dev, T, nseq, H)
+    _call("tm_mixer_scan_bwd", dev, _ptr(u), _ptr(zxbcdt), f32, T, nseq, H, _ptr(offsets),
+          _ptr(dt_bias), _ptr(A_log), _ptr(D), _ptr(dy), _ptr(dzxbcdt), _ptr(du), _ptr(out[0]),
+          _ptr(out[1]), _ptr(out[2]), wp, wb)
+    return du, out[0], out[1], out[2]
+
+
+def _norm_args(y, zxbcdt, norm_w):
+    _need(norm_w, "norm_w", _F32, 1)
+    H = norm_w.shape[0] // MIXER_HEADDIM
+    dev, T, _, d, _, f32 = _seq_in(zxbcdt, H, None)
+    _of(norm_w, "norm_w", _F32, (d,), dev)
+    _of(y, "y", _BF16, (T, d), dev)
+    return dev, T, H, d, f32
+
+
+def mixer_norm(y: torch.Tensor, zxbcdt: torch.Tensor, norm_w: torch.Tensor, eps: float = 1e-5,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gated RMS norm before out_proj, over rows (tm_mixer_norm): y
+    bfloat16 [T, d_inner] and z of zxbcdt -> out bfloat16 [T, d_inner]."""
+    dev, T, H, d, f32 = _norm_args(y, zxbcdt, norm_w)
+    if out is None:
+        out = torch.empty((T, d), dtype=torch.bfloat16, device=dev)
+    _of(out, "out", _BF16, (T, d), dev)
+    if T == 0:
+        return out
+    _call("tm_mixer_norm", dev, _ptr(y), _ptr(zxbcdt), f32, T, H, _ptr(norm_w), eps, _ptr(out))
+    return out
+
+
+def mixer_norm_bwd(y: torch.Tensor, zxbcdt: torch.Tensor, norm_w: torch.Tensor,
+                   dout: torch.Tensor, dzxbcdt: torch.Tensor, eps: float = 1e-5):
+    """Gradients of mixer_norm (tm_mixer_norm_bwd): writes the z columns of
+    dzxbcdt and returns (dy bfloat16 [T, d_inner], dnorm_w [d_inner])."""
+    dev, T, H, d, f32 = _norm_args(y, zxbcdt, norm_w)
+    _of(dout, "dout", _BF16, (T, d), dev)
+    _grad_zx(dzxbcdt, zxbcdt)
+    dy = torch.empty((T, d), dtype=torch.bfloat16, device=dev)
+    dw = torch.empty((d,), dtype=torch.float32, device=dev)
+    if T == 0:
+        return dy, dw.zero_()
+    ws, wp, wb = _seq_ws("tm_mixer_norm_bwd_workspace", dev, T, H)
+    _call("tm_mixer_norm_bwd", dev, _ptr(y), _ptr(zxbcdt), f32, T, H, _ptr(norm_w), eps,
+          _ptr(dout), _ptr(dzxbcdt), _ptr(dy), _ptr(dw), wp, wb)
+    return dy, dw
+
+
+def embed(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.0,
+          out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out float32 [T, D] = scale * weight[ids] (tm_embed): ids int32 or int64
+    [T], weight [V, D] float32, bfloat16 or float16.  An id outside the
+    weight's rows gives zeros."""
+    _need(ids, "ids", _IDS, 1)
+    _need(weight, "weight", tuple(_EMBED_TYPE), 2)
+    T, (V, D) = ids.shape[0], weight.shape
+    dev = weight.device
+    _shape(ids, "ids", (T,), dev)
+    if out is None:
+        out = torch.empty((T, D), dtype=torch.float32, device=dev)
+    _of(out, "out", _F32, (T, D), dev)
+    if T == 0:
+        return out
+    _call("tm_embed", dev, _ptr(ids), int(ids.dtype == torch.int64), T, _ptr(weight),
+          _EMBED_TYPE[weight.dtype], V, D, scale, _ptr(out))
+    return out
+
+
+def embed_bwd(ids: torch.Tensor, dout: torch.Tensor, vocab: int, scale: float = 1.0,
+              dW: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
+    """dW float32 [vocab, D] (+)= scale * the sums of dout's rows (float32
+    [T, D]) by their ids, ascending (tm_embed_bwd)."""
+    _need(ids, "ids", _IDS, 1)
+    _need(dout, "dout", _F32, 2)
+    T, D = dout.shape
+    dev = dout.device
+    _shape(ids, "ids", (T,), dev)
+    if dW is None:
+        if accumulate:
+            raise ValueError("accumulate=True needs an existing dW")
+        dW = torch.empty((vocab, D), dtype=torch.float32, device=dev)
+    _of(dW, "dW", _F32, (vocab, D), dev)
+    if T == 0:
+        return dW if accumulate else dW.zero_()
+    ws, wp, wb = _seq_ws("tm_embed_bwd_workspace", dev, T, vocab, D)
+    _call("tm_embed_bwd", dev, _ptr(ids), int(ids.dtype == torch.int64), T, _ptr(dout), vocab, D,
+          scale, _ptr(dW), int(bool(accumulate)), wp, wb)
+    return dW
