@@ -49,7 +49,7 @@ extern "C" {
  *             input (with either ring; it is not moved)
  *   ring_out  float16 [nseq, cd, 4] or NULL: the last four inputs of ring_in
  *             and the sequence, in the same slots; may be ring_in, no other
- *             overlap.  2-byte aligned, as ring_in.
+ *             overlap.  8-byte aligned, as ring_in.
  *   u         bf16 [T, cd]
  */
 tm_status tm_mixer_conv(const void* zxbcdt, int32_t z_f32, int64_t T, int32_t nseq, int32_t nheads,

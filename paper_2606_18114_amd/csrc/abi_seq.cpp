@@ -82,7 +82,7 @@ tm_status tm_mixer_conv(const void* zxbcdt, int32_t z_f32, int64_t T, int32_t ns
   if (!conv_w || !conv_b || !u) return TM_EINVAL;
   if (tm_status st = in_checked(zxbcdt, z_f32, T, nseq, nheads, offsets, &s)) return st;
   if ((ring_in || ring_out) && !ring_pos) return TM_EINVAL;
-  if (!all_aligned({conv_w, conv_b, ring_pos}, 4) || !all_aligned({ring_in, ring_out}, 2) ||
+  if (!all_aligned({conv_w, conv_b, ring_pos}, 4) || !all_aligned({ring_in, ring_out}, 8) ||
       !aligned(u, 16))
     return TM_EALIGN;
   const int64_t rb = nseq * s.cd * 8;

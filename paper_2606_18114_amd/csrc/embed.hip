@@ -161,36 +161,58 @@ __device__ __forceinline__ f32x4 em_sum4(const float* __restrict__ de, int64_t D
 }
 
 // grid (pieces at most): a piece's tokens, the kEmPiece occurrences of its id
-// from number kEmPiece pno on, then their sum
+// from number kEmPiece pno on, then their sum.  The ids are gone through 4096 at
+// a time, four a thread, so that their loads overlap and few barriers remain.
 template <typename I>
-__global__ __launch_bounds__(256) void embed_piece_kernel(const I* __restrict__ ids, int64_t T,
-                                                          const float* __restrict__ de, int64_t D,
-                                                          EmbedWs w) {
-  __shared__ int list[kEmPiece], wave_n[4];
+__global__ __launch_bounds__(1024) void embed_piece_kernel(const I* __restrict__ ids, int64_t T,
+                                                           const float* __restrict__ de, int64_t D,
+                                                           EmbedWs w) {
+  constexpr int kPer = 4, kWaves = 16;
+  __shared__ int list[kEmPiece], wave_n[2][kWaves];
   if ((int)blockIdx.x >= w.cursor[1]) return;
-  const int64_t v = w.pid[blockIdx.x];
+  const int v = w.pid[blockIdx.x];
   const int lo = w.pno[blockIdx.x] * kEmPiece;
   const int total = w.count[v] - lo, n = total < kEmPiece ? total : kEmPiece;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   int seen = 0;
-  for (int64_t tb = 0; tb < T && seen < lo + n; tb += 256) {
-    const int64_t t = tb + threadIdx.x;
-    const bool hit = t < T && (int64_t)ids[t] == v;
-    const uint64_t m = __ballot(hit);
-    if (lane == 0) wave_n[wave] = __popcll(m);
+  for (int64_t tb = 0, step = 0; tb < T && seen < lo + n; tb += 1024 * kPer, ++step) {
+    // a wave goes through 64 kPer consecutive ids, 64 at a time
+    const int64_t t0 = tb + wave * 64 * kPer + lane;
+    bool hit[kPer];
+    int before[kPer], mine = 0;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      const int64_t t = t0 + 64 * q;
+      hit[q] = t < T && (int64_t)ids[t < T ? t : T - 1] == v;
+    }
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      const uint64_t m = __ballot(hit[q]);
+      before[q] = mine + __popcll(m & ((1ull << lane) - 1));
+      mine += __popcll(m);
+    }
+    int* wn = wave_n[step & 1];  // (the other half may still be read)
+    if (lane == 0) wn[wave] = mine;
     __syncthreads();
-    int before = seen;
-    for (int k = 0; k < wave; ++k) before += wave_n[k];
-    const int at = before + __popcll(m & ((1ull << lane) - 1)) - lo;
-    if (hit && at >= 0 && at < n) list[at] = (int)t;
-    seen += wave_n[0] + wave_n[1] + wave_n[2] + wave_n[3];
-    __syncthreads();
+    int base = seen;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      const int c = wn[k];
+      base += k < wave ? c : 0;
+      seen += c;
+    }
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      const int at = base + before[q] - lo;
+      if (hit[q] && at >= 0 && at < n) list[at] = (int)(t0 + 64 * q);
+    }
   }
+  __syncthreads();
   float* o = w.psum + (int64_t)blockIdx.x * D;
   const int64_t D4 = D & ~(int64_t)3;
-  for (int64_t c = (int64_t)threadIdx.x * 4; c < D4; c += 1024)
+  for (int64_t c = (int64_t)threadIdx.x * 4; c < D4; c += 4096)
     *(f32x4_u4*)(o + c) = em_sum4(de, D, list, n, c);
-  for (int64_t c = D4 + threadIdx.x; c < D; c += 256) {
+  for (int64_t c = D4 + threadIdx.x; c < D; c += 1024) {
     float s = 0.f;
     for (int k = 0; k < n; ++k) s += de[(int64_t)list[k] * D + c];
     o[c] = s;
@@ -275,7 +297,7 @@ static hipError_t embed_bwd_go(const I* ids, int64_t T, const float* de, int64_t
   hipLaunchKernelGGL(embed_place_kernel, dim3(vb), dim3(256), 0, stream, V, w);
   hipLaunchKernelGGL(embed_sort_kernel<I>, dim3(tb), dim3(256), 0, stream, ids, T, V, w);
   if (T > kEmPiece)
-    hipLaunchKernelGGL(embed_piece_kernel<I>, dim3((unsigned)em_pieces(T)), dim3(256), 0, stream,
+    hipLaunchKernelGGL(embed_piece_kernel<I>, dim3((unsigned)em_pieces(T)), dim3(1024), 0, stream,
                        ids, T, de, D, w);
   if (accumulate)
     hipLaunchKernelGGL(embed_row_kernel<true>, dim3((unsigned)V), dim3(256), 0, stream, de, D,

@@ -23,6 +23,7 @@ constexpr int kSqTaps = 4;   // convolution taps
 // a 16-byte access at any element boundary (a row of zxbcdt begins at a
 // multiple of 16 bytes only if nheads is a multiple of 8)
 typedef u32x4 __attribute__((aligned(2))) u32x4_u2;
+typedef u32x2 __attribute__((aligned(2))) u32x2_u2;
 typedef f32x4 __attribute__((aligned(4))) f32x4_u4;
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
@@ -31,8 +32,11 @@ __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 
 __device__ __forceinline__ uint16_t bf_rne(float f) {
   return __builtin_bit_cast(uint16_t, (__bf16)f);
 }
+// two values at once: one v_cvt_pk_bf16_f32
 __device__ __forceinline__ uint32_t bf_pack(float lo, float hi) {
-  return (uint32_t)bf_rne(lo) | ((uint32_t)bf_rne(hi) << 16);
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
 }
 
 // zxbcdt's element types
@@ -50,6 +54,13 @@ struct Zx<false> {
     v[0] = bf_lo(w.x), v[1] = bf_hi(w.x), v[2] = bf_lo(w.y), v[3] = bf_hi(w.y);
     v[4] = bf_lo(w.z), v[5] = bf_hi(w.z), v[6] = bf_lo(w.w), v[7] = bf_hi(w.w);
   }
+  static __device__ __forceinline__ void ld4(const T* p, float (&v)[4]) {
+    const u32x2 w = *reinterpret_cast<const u32x2_u2*>(p);
+    v[0] = bf_lo(w.x), v[1] = bf_hi(w.x), v[2] = bf_lo(w.y), v[3] = bf_hi(w.y);
+  }
+  static __device__ __forceinline__ void st4(T* p, const float (&v)[4]) {
+    *reinterpret_cast<u32x2_u2*>(p) = u32x2{bf_pack(v[0], v[1]), bf_pack(v[2], v[3])};
+  }
   static __device__ __forceinline__ void st8(T* p, const float (&v)[8]) {
     *reinterpret_cast<u32x4_u2*>(p) = u32x4{bf_pack(v[0], v[1]), bf_pack(v[2], v[3]),
                                             bf_pack(v[4], v[5]), bf_pack(v[6], v[7])};
@@ -65,6 +76,13 @@ struct Zx<true> {
     const f32x4 b = *reinterpret_cast<const f32x4_u4*>(p + 4);
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
     v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  }
+  static __device__ __forceinline__ void ld4(const T* p, float (&v)[4]) {
+    const f32x4 a = *reinterpret_cast<const f32x4_u4*>(p);
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+  }
+  static __device__ __forceinline__ void st4(T* p, const float (&v)[4]) {
+    *reinterpret_cast<f32x4_u4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
   }
   static __device__ __forceinline__ void st8(T* p, const float (&v)[8]) {
     *reinterpret_cast<f32x4_u4*>(p) = f32x4{v[0], v[1], v[2], v[3]};

@@ -18,13 +18,15 @@ namespace tmk {
 constexpr int kCvCh = 8;       // channels of a thread
 constexpr int kCvBatch = 4;    // tokens whose loads are issued together
 constexpr int kCvBwdRun = 64;  // tokens of a backward run
+constexpr int kCvBwdCh = 4;    // its channels a thread: with 8 the sums leave two waves a SIMD
+constexpr int kCvBwdBatch = 8;
 
-// grid (runs, ceil(cd / 512)), one wave each
+// grid (runs, ceil(cd / 512)), one wave each.  ring_out: not ring, or NULL
 template <bool F32>
 __global__ __launch_bounds__(64) void seq_conv_kernel(
     const typename Zx<F32>::T* __restrict__ zx, int T, int nheads, const int* __restrict__ off,
     int nseq, int run, const float* __restrict__ conv_w, const float* __restrict__ conv_b,
-    const uint16_t* __restrict__ ring, const int* __restrict__ ring_pos,
+    const uint16_t* ring, const int* __restrict__ ring_pos, uint16_t* ring_out,
     uint16_t* __restrict__ u) {
   const int d = nheads * kSqP, cd = d + 2 * kSqN;
   const int64_t Z = (int64_t)2 * d + 2 * kSqN + nheads;
@@ -39,7 +41,18 @@ __global__ __launch_bounds__(64) void seq_conv_kernel(
 #pragma unroll
     for (int j = 0; j < kSqTaps; ++j) w[j][i] = conv_w[(int64_t)(c + i) * kSqTaps + j];
   }
-  const int pos = ring ? ring_pos[0] & 3 : 0;
+  const int pos = ring_pos ? ring_pos[0] & 3 : 0;
+  if (ring_out)  // empty sequences keep their rings
+    for (int i = blockIdx.x; i < nseq; i += gridDim.x) {
+      const int a = off ? off[i] : 0, e = off ? min(off[i + 1], T) : T;
+      if (a >= 0 && e > a) continue;
+      const u32x2 zero = {0, 0};
+      const int64_t at = ((int64_t)i * cd + c) * kSqTaps;
+#pragma unroll
+      for (int k = 0; k < kCvCh; ++k)
+        *(u32x2*)(ring_out + at + k * kSqTaps) =
+            ring ? *(const u32x2*)(ring + at + k * kSqTaps) : zero;
+    }
   SeqAt sq = seq_find(off, nseq, T, t0);
   float h[3][kCvCh];  // the three inputs before the token, oldest first
   auto past = [&](int t) {
@@ -53,10 +66,12 @@ __global__ __launch_bounds__(64) void seq_conv_kernel(
         for (int i = 0; i < kCvCh; ++i) h[j][i] = 0.f;
         if (ring && sq.i >= 0) {
           const int slot = (pos + 4 + tj - sq.st) & 3;
+          const uint16_t* r = ring + ((int64_t)sq.i * cd + c) * kSqTaps;
 #pragma unroll
-          for (int i = 0; i < kCvCh; ++i)
-            h[j][i] = (float)__builtin_bit_cast(
-                _Float16, ring[((int64_t)sq.i * cd + c + i) * kSqTaps + slot]);
+          for (int i = 0; i < kCvCh; ++i) {  // a channel's four slots are 8 bytes
+            const uint64_t q = *(const uint64_t*)(r + i * kSqTaps);
+            h[j][i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(q >> (16 * slot)));
+          }
         }
       }
     }
@@ -73,6 +88,16 @@ __global__ __launch_bounds__(64) void seq_conv_kernel(
       if (t >= sq.en) {
         sq = seq_find(off, nseq, T, t);
         past(t);
+      }
+      if (ring_out && t == sq.en - 1 && sq.i >= 0) {  // the last four inputs
+        uint64_t* r = (uint64_t*)(ring_out + ((int64_t)sq.i * cd + c) * kSqTaps);
+#pragma unroll
+        for (int i = 0; i < kCvCh; ++i) {
+          auto h16 = [](float f) { return (uint64_t)__builtin_bit_cast(uint16_t, (_Float16)f); };
+          const uint64_t n = h16(h[0][i]) | h16(h[1][i]) << 16 | h16(h[2][i]) << 32 |
+                             h16(v[q][i]) << 48;
+          r[i] = pos ? n << (16 * pos) | n >> (64 - 16 * pos) : n;  // the oldest into slot pos
+        }
       }
       float o[kCvCh];
 #pragma unroll
@@ -93,8 +118,8 @@ __global__ __launch_bounds__(64) void seq_conv_kernel(
   }
 }
 
-// The ring after the sequences, a launch of its own: in place, other
-// workgroups of the convolution may still read the old one.  grid (ceil(cd /
+// The ring after the sequences where it is updated in place, a launch of its own:
+// other workgroups of the convolution may still read the old one.  grid (ceil(cd /
 // 256), nseq); a thread takes one channel: its last four inputs, of the ring
 // where the sequence is shorter than that.
 template <bool F32>
@@ -142,55 +167,55 @@ __global__ __launch_bounds__(64) void seq_conv_bwd_kernel(
     float* __restrict__ part) {
   const int d = nheads * kSqP, cd = d + 2 * kSqN;
   const int64_t Z = (int64_t)2 * d + 2 * kSqN + nheads;
-  const int c = ((int)blockIdx.y * 64 + (int)threadIdx.x) * kCvCh;
+  const int c = ((int)blockIdx.y * 64 + (int)threadIdx.x) * kCvBwdCh;
   if (c >= cd) return;
   const int t0 = (int)blockIdx.x * kCvBwdRun, t1 = min(T, t0 + kCvBwdRun);
   const typename Zx<F32>::T* x = zx + d + c;
   typename Zx<F32>::T* dx = dzx + d + c;
-  float w[kSqTaps][kCvCh], b[kCvCh];
+  float w[kSqTaps][kCvBwdCh], b[kCvBwdCh];
 #pragma unroll
-  for (int i = 0; i < kCvCh; ++i) {
+  for (int i = 0; i < kCvBwdCh; ++i) {
     b[i] = conv_b[c + i];
 #pragma unroll
     for (int j = 0; j < kSqTaps; ++j) w[j][i] = conv_w[(int64_t)(c + i) * kSqTaps + j];
   }
   SeqAt sq = seq_find(off, nseq, T, t0);
-  float h[3][kCvCh], acc[3][kCvCh], dw[kSqTaps][kCvCh], db[kCvCh];
+  float h[3][kCvBwdCh], acc[3][kCvBwdCh], dw[kSqTaps][kCvBwdCh], db[kCvBwdCh];
 #pragma unroll
   for (int j = 0; j < 3; ++j) {
     const int tj = t0 - 3 + j;
     if (tj >= sq.st) {
-      Zx<F32>::ld8(x + tj * Z, h[j]);
+      Zx<F32>::ld4(x + tj * Z, h[j]);
     } else {
 #pragma unroll
-      for (int i = 0; i < kCvCh; ++i) h[j][i] = 0.f;
+      for (int i = 0; i < kCvBwdCh; ++i) h[j][i] = 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < kCvCh; ++i) acc[j][i] = 0.f;  // dx of t - 3, t - 2, t - 1 so far
+    for (int i = 0; i < kCvBwdCh; ++i) acc[j][i] = 0.f;  // dx of t - 3, t - 2, t - 1 so far
   }
 #pragma unroll
-  for (int i = 0; i < kCvCh; ++i) {
+  for (int i = 0; i < kCvBwdCh; ++i) {
     db[i] = 0.f;
 #pragma unroll
     for (int j = 0; j < kSqTaps; ++j) dw[j][i] = 0.f;
   }
   // stores dx of token t (in the run, in a sequence that began at st)
-  auto emit = [&](int t, int st, const float(&v)[kCvCh]) {
-    if (t >= t0 && t < t1 && t >= st) Zx<F32>::st8(dx + t * Z, v);
+  auto emit = [&](int t, int st, const float(&v)[kCvBwdCh]) {
+    if (t >= t0 && t < t1 && t >= st) Zx<F32>::st4(dx + t * Z, v);
   };
   const int te = min(T, t1 + 3);
   int t = t0;
   bool open = sq.i >= 0;
-  for (int tb = t0; tb < te; tb += kCvBatch) {
-    float v[kCvBatch][kCvCh], g[kCvBatch][kCvCh];
+  for (int tb = t0; tb < te; tb += kCvBwdBatch) {
+    float v[kCvBwdBatch][kCvBwdCh], g[kCvBwdBatch][kCvBwdCh];
 #pragma unroll
-    for (int q = 0; q < kCvBatch; ++q) {
+    for (int q = 0; q < kCvBwdBatch; ++q) {
       const int64_t tq = min(tb + q, T - 1);
-      Zx<F32>::ld8(x + tq * Z, v[q]);
-      Zx<false>::ld8(du + tq * cd + c, g[q]);
+      Zx<F32>::ld4(x + tq * Z, v[q]);
+      Zx<false>::ld4(du + tq * cd + c, g[q]);
     }
 #pragma unroll
-    for (int q = 0; q < kCvBatch; ++q) {
+    for (int q = 0; q < kCvBwdBatch; ++q) {
       t = tb + q;
       if (t >= te) break;
       if (t >= sq.en) {  // the sequence ended: its last three dx are complete
@@ -204,11 +229,11 @@ __global__ __launch_bounds__(64) void seq_conv_bwd_kernel(
 #pragma unroll
         for (int j = 0; j < 3; ++j)
 #pragma unroll
-          for (int i = 0; i < kCvCh; ++i) h[j][i] = acc[j][i] = 0.f;
+          for (int i = 0; i < kCvBwdCh; ++i) h[j][i] = acc[j][i] = 0.f;
       }
-      float now[kCvCh], first[kCvCh];
+      float now[kCvBwdCh], first[kCvBwdCh];
 #pragma unroll
-      for (int i = 0; i < kCvCh; ++i) {
+      for (int i = 0; i < kCvBwdCh; ++i) {
         float a = __builtin_fmaf(h[0][i], w[0][i], b[i]);
         a = __builtin_fmaf(h[1][i], w[1][i], a);
         a = __builtin_fmaf(h[2][i], w[2][i], a);
@@ -230,7 +255,7 @@ __global__ __launch_bounds__(64) void seq_conv_bwd_kernel(
       }
       if (open) emit(t - 3, sq.st, first);
 #pragma unroll
-      for (int i = 0; i < kCvCh; ++i) h[0][i] = h[1][i], h[1][i] = h[2][i], h[2][i] = now[i];
+      for (int i = 0; i < kCvBwdCh; ++i) h[0][i] = h[1][i], h[1][i] = h[2][i], h[2][i] = now[i];
     }
   }
   // what is left: tokens te - 3 .. te - 1 (of the run only where T ended it)
@@ -242,34 +267,35 @@ __global__ __launch_bounds__(64) void seq_conv_bwd_kernel(
   float* p = part + (int64_t)blockIdx.x * 5 * cd + c;
 #pragma unroll
   for (int j = 0; j < kSqTaps; ++j)
-#pragma unroll
-    for (int i = 0; i < kCvCh; i += 4)
-      *reinterpret_cast<f32x4*>(p + (int64_t)j * cd + i) =
-          f32x4{dw[j][i], dw[j][i + 1], dw[j][i + 2], dw[j][i + 3]};
-#pragma unroll
-  for (int i = 0; i < kCvCh; i += 4)
-    *reinterpret_cast<f32x4*>(p + (int64_t)4 * cd + i) = f32x4{db[i], db[i + 1], db[i + 2], db[i + 3]};
+    *reinterpret_cast<f32x4*>(p + (int64_t)j * cd) = f32x4{dw[j][0], dw[j][1], dw[j][2], dw[j][3]};
+  *reinterpret_cast<f32x4*>(p + (int64_t)4 * cd) = f32x4{db[0], db[1], db[2], db[3]};
 }
 
-// out[c] = sum_r part[r][c]: 64 columns a workgroup, 16 chains of rows added
-// in their order, the chains in LDS.  With ntap != 0 column q * cd + c goes to
+// out[c] = sum_r part[r][c]: COLS columns a workgroup, 1024 / COLS chains of rows
+// added in their order, the chains in LDS.  64 columns where that makes a
+// workgroup for every CU (21760 columns of 256 rows: 8 us, 11 with 16), else 16
+// (4096 of 1024: 8 us, 21 with 64).  With ntap != 0 column q * cd + c goes to
 // out[c * ntap + q] for q < ntap, to out2[c] for q == ntap.
+template <int COLS>
 __global__ __launch_bounds__(1024) void sum_rows_kernel(const float* __restrict__ part,
                                                         int64_t rows, int64_t cols,
                                                         int64_t stride, float* __restrict__ out,
                                                         int ntap, int64_t cd,
                                                         float* __restrict__ out2) {
-  __shared__ float s[16][64];
-  const int lane = threadIdx.x & 63, chain = threadIdx.x >> 6;
-  const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+  constexpr int kChains = 1024 / COLS;
+  __shared__ float s[kChains][COLS];
+  const int lane = threadIdx.x % COLS, chain = threadIdx.x / COLS;
+  const int64_t col = (int64_t)blockIdx.x * COLS + lane;
   float v = 0.f;
-  if (col < cols)
-    for (int64_t r = chain; r < rows; r += 16) v += part[r * stride + col];
+  if (col < cols) {
+#pragma unroll 4
+    for (int64_t r = chain; r < rows; r += kChains) v += part[r * stride + col];
+  }
   s[chain][lane] = v;
   __syncthreads();
   if (chain != 0 || col >= cols) return;
-#pragma unroll
-  for (int k = 1; k < 16; ++k) v += s[k][lane];
+#pragma unroll 8
+  for (int k = 1; k < kChains; ++k) v += s[k][lane];
   if (ntap == 0) {
     out[col] = v;
   } else {
@@ -279,11 +305,20 @@ __global__ __launch_bounds__(1024) void sum_rows_kernel(const float* __restrict_
   }
 }
 
+static hipError_t sum_rows(const float* part, int64_t rows, int64_t cols, int64_t stride,
+                           float* out, int ntap, int64_t cd, float* out2, hipStream_t stream) {
+  if (cols >= 256 * 64)
+    hipLaunchKernelGGL(sum_rows_kernel<64>, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0,
+                       stream, part, rows, cols, stride, out, ntap, cd, out2);
+  else
+    hipLaunchKernelGGL(sum_rows_kernel<16>, dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0,
+                       stream, part, rows, cols, stride, out, ntap, cd, out2);
+  return hipGetLastError();
+}
+
 hipError_t launch_sum_rows(const float* part, int64_t rows, int64_t cols, int64_t stride,
                            float* out, hipStream_t stream) {
-  hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, stream,
-                     part, rows, cols, stride, out, 0, (int64_t)1, nullptr);
-  return hipGetLastError();
+  return sum_rows(part, rows, cols, stride, out, 0, 1, nullptr, stream);
 }
 
 template <bool F32>
@@ -298,9 +333,10 @@ static hipError_t conv_go(const SeqIn& in, const float* conv_w, const float* con
   run = run < 1 ? 1 : run > 16 ? 16 : run;
   hipLaunchKernelGGL(seq_conv_kernel<F32>, dim3((unsigned)((in.T + run - 1) / run), (unsigned)cblk),
                      dim3(64), 0, stream, (const E*)in.zx, in.T, in.nheads, in.offsets, in.nseq,
-                     run, conv_w, conv_b, ring_in, ring_pos, u);
+                     run, conv_w, conv_b, ring_in, ring_pos,
+                     ring_out == ring_in ? nullptr : ring_out, u);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || ring_out == nullptr) return e;
+  if (e != hipSuccess || ring_out == nullptr || ring_out != ring_in) return e;
   hipLaunchKernelGGL(seq_ring_kernel<F32>, dim3((unsigned)((cd + 255) / 256), (unsigned)in.nseq),
                      dim3(256), 0, stream, (const E*)in.zx, in.T, in.nheads, in.offsets, ring_in,
                      ring_pos, ring_out);
@@ -327,15 +363,13 @@ static hipError_t conv_bwd_go(const SeqIn& in, const float* conv_w, const float*
   const int runs = (in.T + kCvBwdRun - 1) / kCvBwdRun;
   float* part = (float*)workspace;
   hipLaunchKernelGGL(seq_conv_bwd_kernel<F32>,
-                     dim3((unsigned)runs, (unsigned)((cd / kCvCh + 63) / 64)), dim3(64), 0, stream,
+                     dim3((unsigned)runs, (unsigned)((cd / kCvBwdCh + 63) / 64)), dim3(64), 0, stream,
                      (const E*)in.zx, in.T, in.nheads, in.offsets, in.nseq, conv_w, conv_b, du,
                      (E*)dzx, part);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t cols = (int64_t)5 * cd;
-  hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, stream,
-                     part, (int64_t)runs, cols, cols, dconv_w, kSqTaps, (int64_t)cd, dconv_b);
-  return hipGetLastError();
+  return sum_rows(part, runs, cols, cols, dconv_w, kSqTaps, cd, dconv_b, stream);
 }
 
 hipError_t launch_seq_conv_bwd(const SeqIn& in, const float* conv_w, const float* conv_b,

@@ -34,11 +34,12 @@ int64_t seq_scan_bytes(int64_t T, int64_t nseq, int64_t nheads);
 hipError_t launch_seq_scan(const SeqIn& in, const uint16_t* u, const float* dt_bias,
                            const float* A_log, const float* D, const uint16_t* ssm_in,
                            uint16_t* ssm_out, uint16_t* y, void* workspace, hipStream_t stream);
-// states (rev: gradients) that enter the segments of segT tokens: state [slots][nheads][64 * 128]
+// own states (rev: gradients) of the segments of segT tokens, or, with pass, those that enter
+// them: state [slots][nheads][64 * 128]
 // and decay [slots][nheads] (seq_scan_dev.hpp); terms 2 or 3 of the products (rev: 3)
 hipError_t launch_scan_states(const SeqIn& in, const uint16_t* u, const uint16_t* dy, bool rev,
                               int terms, int segT, const float* dt_bias, const float* A_log,
-                              const uint16_t* init, float* state, float* decay,
+                              const uint16_t* init, float* state, float* decay, bool pass,
                               hipStream_t stream);
 int64_t seq_scan_bwd_bytes(int64_t T, int64_t nseq, int64_t nheads);
 hipError_t launch_seq_scan_bwd(const SeqIn& in, const uint16_t* u, const float* dt_bias,
@@ -54,8 +55,7 @@ hipError_t launch_embed_bwd(const void* ids, bool ids64, int64_t T, const float*
                             int64_t D, float scale, float* dW, bool accumulate, void* workspace,
                             hipStream_t stream);
 
-// out[c * stride_out] = sum over r < rows of part[r * stride + c], c < cols, r ascending in
-// 16 interleaved chains
+// out[c] = sum over r < rows of part[r * stride + c], c < cols, in 64 interleaved chains of rows
 hipError_t launch_sum_rows(const float* part, int64_t rows, int64_t cols, int64_t stride,
                            float* out, hipStream_t stream);
 

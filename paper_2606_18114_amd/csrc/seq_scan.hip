@@ -52,7 +52,7 @@ __device__ __forceinline__ void tile_store(const TileRegs& r, uint8_t* m, uint8_
 template <int NT>
 __device__ __forceinline__ void state_add(f32x4 (&S)[2][4], const uint8_t* m, const uint8_t* v,
                                           const float* coef) {
-  const int wave = threadIdx.x >> 6, g = (threadIdx.x & 63) >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = (threadIdx.x & 63) >> 4;
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) {
     const int r = 32 * kb + 8 * g;
@@ -63,10 +63,13 @@ __device__ __forceinline__ void state_add(f32x4 (&S)[2][4], const uint8_t* m, co
     bf16x8 a[2][NT];
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb) {
-      const bf16x8 raw = tr_op(m, kScRowN, r, r + 4, 32 * wave + 16 * nb);
+      const u32x4 raw = __builtin_bit_cast(u32x4, tr_op(m, kScRowN, r, r + 4, 32 * wave + 16 * nb));
       float f[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = (float)raw[i] * w[i];
+      for (int i = 0; i < 4; ++i) {
+        f[2 * i] = bf_lo(raw[i]) * w[2 * i];
+        f[2 * i + 1] = bf_hi(raw[i]) * w[2 * i + 1];
+      }
       split8<NT>(f, a[nb]);
     }
 #pragma unroll
@@ -85,17 +88,17 @@ __device__ __forceinline__ void state_add(f32x4 (&S)[2][4], const uint8_t* m, co
 // the state at the segment's end from the segment alone; its sequence's last
 // segment has no use for it.  REV true: vec = dy, mat = C, coefficient e^{c_t},
 // tiles backward: the gradient with respect to the state before the segment;
-// not for the first segment.  grid (slots, nheads), 256 threads.
+// not for the first segment.  grid: scan_grid, 256 threads.
 template <bool F32, bool REV, int NT>
-__global__ __launch_bounds__(256) void scan_state_kernel(
+__global__ __launch_bounds__(256, 2) void scan_state_kernel(
     const typename Zx<F32>::T* __restrict__ zx, const uint16_t* __restrict__ u,
     const uint16_t* __restrict__ dy, int T, int nheads, const int* __restrict__ off, int nseq,
     int segT, const float* __restrict__ dt_bias, const float* __restrict__ A_log,
     float* __restrict__ state, float* __restrict__ decay) {
   __shared__ __attribute__((aligned(16))) uint8_t m[kScQ * kScRowN], v[kScQ * kScRowP];
-  __shared__ Toks<kScQ> tk;
-  __shared__ __attribute__((aligned(16))) float coef[kScQ];
-  const int h = blockIdx.y, sl = blockIdx.x;
+  __shared__ Toks<kScQ> tks[2];
+  __shared__ __attribute__((aligned(16))) float coefs[2][kScQ];
+  const int h = blockIdx.x, sl = blockIdx.y + blockIdx.z * gridDim.y;
   const Slot s = slot_find(off, nseq, T, segT, sl);
   if (s.t0 >= s.t1 || (REV ? s.k == 0 : s.t1 == s.en)) return;
   const int d = nheads * kSqP, cd = d + 2 * kSqN;
@@ -104,7 +107,8 @@ __global__ __launch_bounds__(256) void scan_state_kernel(
   const uint16_t* vec = REV ? dy + h * kSqP : u + h * kSqP;
   const int64_t ldv = REV ? d : cd;
   const float bias = dt_bias[h], rate = expf(A_log[h]);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   f32x4 S[2][4];
 #pragma unroll
   for (int nb = 0; nb < 2; ++nb)
@@ -112,19 +116,40 @@ __global__ __launch_bounds__(256) void scan_state_kernel(
     for (int pb = 0; pb < 4; ++pb) S[nb][pb] = f32x4{0.f, 0.f, 0.f, 0.f};
   float dec = 1.f;
   const int nt = (s.t1 - s.t0 + kScQ - 1) / kScQ;
+  TileRegs r;
+  float raw = 0.f;
+  auto tile_at = [&](int q) { return s.t0 + (REV ? nt - 1 - q : q) * kScQ; };
+  auto load = [&](int q) {
+    const int t0 = tile_at(q);
+    tile_load(r, mat, cd, vec, ldv, t0, min(s.t1, t0 + kScQ));
+  };
+  auto raw_load = [&](int q) {
+    if (q < nt) raw = tok_raw<F32>(zx, Z, nheads, h, min(tile_at(q) + lane, T - 1)) + bias;
+  };
+  auto toks = [&](int q) {  // by one wave, a tile ahead
+    const float rr[1] = {raw};
+    Toks<kScQ>& tk = tks[q & 1];
+    toks_make<kScQ>(tk, rr, min(s.t1, tile_at(q) + kScQ) - tile_at(q), rate);
+    coefs[q & 1][lane] = REV ? tk.ec[lane] : tk.eq[lane] * tk.dt[lane];
+  };
+  load(0);
+  if (wave == 0) {
+    raw_load(0);
+    toks(0);
+    raw_load(1);
+  }
   for (int q = 0; q < nt; ++q) {
-    const int t0 = s.t0 + (REV ? nt - 1 - q : q) * kScQ, t1 = min(s.t1, t0 + kScQ);
-    TileRegs r;
-    tile_load(r, mat, cd, vec, ldv, t0, t1);
-    if (wave == 0) {
-      const float raw[1] = {tok_raw<F32>(zx, Z, nheads, h, min(t0 + lane, T - 1)) + bias};
-      toks_make<kScQ>(tk, raw, t1 - t0, rate);
-      // (one wave wrote and reads these)
-      coef[lane] = REV ? tk.ec[lane] : tk.eq[lane] * tk.dt[lane];
-    }
     tile_store(r, m, v);
     __syncthreads();
-    const float last = tk.last;
+    if (q + 1 < nt) {
+      load(q + 1);
+      if (wave == 0) {
+        toks(q + 1);
+        raw_load(q + 2);
+      }
+    }
+    const float last = tks[q & 1].last;
+    const float* coef = coefs[q & 1];
     dec *= last;
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
@@ -192,21 +217,22 @@ __global__ __launch_bounds__(256) void scan_pass_kernel(float* __restrict__ stat
 }
 
 // ---- y ---------------------------------------------------------------------
-// grid (slots, nheads), 256 threads.  enter: the states that enter the segments,
-// or NULL where every sequence is one segment.
+// grid: scan_grid, 256 threads.  enter: the states that enter the segments, or,
+// with decay, the segments' own ones; NULL where every sequence is one segment.
 template <bool F32>
-__global__ __launch_bounds__(256) void scan_y_kernel(
+__global__ __launch_bounds__(256, 2) void scan_y_kernel(
     const typename Zx<F32>::T* __restrict__ zx, const uint16_t* __restrict__ u, int T, int nheads,
     const int* __restrict__ off, int nseq, int segT, const float* __restrict__ dt_bias,
     const float* __restrict__ A_log, const float* __restrict__ Dp, const uint16_t* init,
-    const float* __restrict__ enter, uint16_t* final_, uint16_t* __restrict__ y) {
+    const float* __restrict__ enter, const float* __restrict__ decay, uint16_t* final_, uint16_t* __restrict__ y) {
   __shared__ __attribute__((aligned(16))) uint8_t Bt[kScQ * kScRowN], xt[kScQ * kScRowP];
-  __shared__ __attribute__((aligned(16))) uint8_t Sl[2][kSqP * kScRowN];  // the state's terms
-  __shared__ Toks<kScQ> tk;
-  __shared__ __attribute__((aligned(16))) float coef[kScQ];
-  const int h = blockIdx.y, sl = blockIdx.x;
+  __shared__ __attribute__((aligned(16))) uint8_t Sl[2][kSqP * kScRowS];  // the state's terms
+  __shared__ Toks<kScQ> tks[2];
+  __shared__ __attribute__((aligned(16))) float coefs[2][kScQ];
+  const int h = blockIdx.x, sl = blockIdx.y + blockIdx.z * gridDim.y;
   const Slot s = slot_find(off, nseq, T, segT, sl);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
+  const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t sat = ((int64_t)s.i * nheads + h) * kScState;
   if (s.t0 >= s.t1) {
     // an empty sequence's state stays what it was
@@ -229,13 +255,25 @@ __global__ __launch_bounds__(256) void scan_y_kernel(
     for (int pb = 0; pb < 4; ++pb) {
       const int e = (16 * pb + col) * kSqN + 32 * wave + 16 * nb + 4 * g;
       S[nb][pb] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (s.k > 0) {
-        if (enter) S[nb][pb] = *(const f32x4*)(enter + ((int64_t)sl * nheads + h) * kScState + e);
+      if (s.k > 0 && enter && !decay) {
+        S[nb][pb] = *(const f32x4*)(enter + ((int64_t)sl * nheads + h) * kScState + e);
       } else if (init) {
         const u32x2 w = *(const u32x2*)(init + sat + e);
         S[nb][pb] = f32x4{h2f((uint16_t)w.x), h2f((uint16_t)(w.x >> 16)), h2f((uint16_t)w.y),
                           h2f((uint16_t)(w.y >> 16))};
       }
+    }
+  if (decay)  // the segments' own states: take those of the segments before this one
+    for (int k = s.k; k > 0; --k) {
+      const int64_t at = (int64_t)(sl - k) * nheads + h;
+      const float dec = decay[at];
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+        for (int pb = 0; pb < 4; ++pb) {
+          const int e = (16 * pb + col) * kSqN + 32 * wave + 16 * nb + 4 * g;
+          S[nb][pb] = S[nb][pb] * dec + *(const f32x4*)(enter + at * kScState + e);
+        }
     }
   TileRegs r;
   bf16x8 cn[4];
@@ -248,10 +286,25 @@ __global__ __launch_bounds__(256) void scan_y_kernel(
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       cn[k] = as_bf16x8(t < t1 ? ld16(Cg + (int64_t)t * cd + 32 * k + 8 * g) : u32x4{0, 0, 0, 0});
-    if (wave == 0) raw = tok_raw<F32>(zx, Z, nheads, h, min(t0 + lane, T - 1)) + bias;
+  };
+  // wave 0 (whose tokens have the fewest tokens before them) makes the token
+  // values a tile ahead, of dt loaded yet a tile earlier
+  auto raw_load = [&](int t0) {
+    raw = tok_raw<F32>(zx, Z, nheads, h, min(t0 + lane, T - 1)) + bias;
+  };
+  auto toks = [&](int t0, int buf) {
+    const float rr[1] = {raw};
+    toks_make<kScQ>(tks[buf], rr, min(s.t1, t0 + kScQ) - t0, rate);
+    coefs[buf][lane] = tks[buf].eq[lane] * tks[buf].dt[lane];
   };
   load(s.t0);
-  for (int t0 = s.t0; t0 < s.t1; t0 += kScQ) {
+  if (wave == 0) {
+    raw_load(s.t0);
+    toks(s.t0, 0);
+    raw_load(s.t0 + kScQ);
+  }
+  int buf = 0;
+  for (int t0 = s.t0; t0 < s.t1; t0 += kScQ, buf ^= 1) {
     const int t1 = min(s.t1, t0 + kScQ);
     tile_store(r, Bt, xt);
 #pragma unroll
@@ -265,33 +318,53 @@ __global__ __launch_bounds__(256) void scan_y_kernel(
           a[i] = bf_pack(f[2 * i], f[2 * i + 1]);
           b[i] = bf_pack(f[2 * i] - bf_lo(a[i]), f[2 * i + 1] - bf_hi(a[i]));
         }
-        const int at = (16 * pb + col) * kScRowN + 2 * (32 * wave + 16 * nb + 4 * g);
+        const int at = (16 * pb + col) * kScRowS + 2 * (32 * wave + 16 * nb + 4 * g);
         *(u32x2*)(Sl[0] + at) = u32x2{a[0], a[1]};
         *(u32x2*)(Sl[1] + at) = u32x2{b[0], b[1]};
       }
-    if (wave == 0) {
-      const float rr[1] = {raw};
-      toks_make<kScQ>(tk, rr, t1 - t0, rate);
-      coef[lane] = tk.eq[lane] * tk.dt[lane];
-    }
     bf16x8 C[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) C[k] = cn[k];
     __syncthreads();
-    if (t0 + kScQ < s.t1) load(t0 + kScQ);
+    const Toks<kScQ>& tk = tks[buf];
+    const float* coef = coefs[buf];
+    if (t0 + kScQ < s.t1) {
+      load(t0 + kScQ);
+      if (wave == 0) {
+        toks(t0 + kScQ, buf ^ 1);
+        raw_load(t0 + 2 * kScQ);
+      }
+    }
 
     // e^{c_t} S C^T first: scaled, it is what the tile's own product adds to
     const int tt = 16 * wave + col;  // this lane's token in the tile
     f32x4 acc[4];
+    {
+      // operands a step (32 states) ahead of the products that take them: left
+      // to itself the compiler waits for LDS before every other product
+      bf16x8 sf[2][4][2];
+      auto fetch = [&](int k) {
 #pragma unroll
-    for (int pb = 0; pb < 4; ++pb) {
-      acc[pb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int pb = 0; pb < 4; ++pb)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) sf[k & 1][pb][q] = row_op(Sl[q], kScRowS, 16 * pb, 32 * k);
+      };
+      fetch(0);
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb) acc[pb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        acc[pb] = mfma16(row_op(Sl[1], kScRowN, 16 * pb, 32 * k), C[k], acc[pb]);
-        acc[pb] = mfma16(row_op(Sl[0], kScRowN, 16 * pb, 32 * k), C[k], acc[pb]);
+        if (k < 3) fetch(k + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int q = 1; q >= 0; --q)
+#pragma unroll
+          for (int pb = 0; pb < 4; ++pb) acc[pb] = mfma16(sf[k & 1][pb][q], C[k], acc[pb]);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      acc[pb] *= tk.ec[tt];
+      const float et = tk.ec[tt];
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb) acc[pb] *= et;
     }
     // g of this wave's tokens with the s up to them, 32 at a time
     const float thi = tk.hi[tt], tlo = tk.lo[tt];
@@ -357,27 +430,40 @@ __global__ __launch_bounds__(256) void scan_y_kernel(
   }
 }
 
-// Tokens of a segment: enough segments for two workgroups on every CU.
-static int64_t scan_seg(int64_t T, int64_t nseq, int64_t nheads) {
-  const int64_t want = (512 + nheads - 1) / nheads;  // segments
-  if (nseq >= want || T <= 4 * kScQ) return T;
-  const int64_t tiles = (T + kScQ - 1) / kScQ;
-  int64_t per = tiles / (want - nseq + 1);  // T / seg + nseq >= want
-  if (per < 2) per = 2;
-  return per >= tiles ? T : per * kScQ;
+// Tokens of a segment: as many segments of all heads as the chip takes
+// workgroups at once (512), whatever the sequences' lengths, which the host does
+// not know.  Two sequences of 8192 tokens and 64 heads: 245 us, 455 in one
+// segment each; one of 4096: 76 and 228; eight of 2048, where one segment each
+// would do: 177 and 161.  Up to 512 tokens in one segment (300 tokens: 20 us,
+// 23 in segments of 128).
+static int64_t scan_seg(int64_t T, int64_t nheads) {
+  if (T <= 512) return T;
+  const int64_t seg = T * nheads / 512 / kScQ * kScQ;
+  return seg < 128 ? 128 : seg > T ? T : seg;
 }
+// A workgroup adds the own states of this many segments before its own up by
+// itself; with more, a launch makes the states that enter every segment.
+constexpr int kScOwn = 16;
 
 int64_t seq_scan_bytes(int64_t T, int64_t nseq, int64_t nheads) {
-  const int64_t seg = scan_seg(T, nseq, nheads);
+  const int64_t seg = scan_seg(T, nheads);
   if (seg >= T) return 0;
   return slot_count(T, nseq, seg) * nheads * (kScState + 1) * 4;
 }
 
+// Heads vary fastest: workgroups go to the eight XCDs in turn, and slots without
+// tokens (every second one where sequences are one segment long) would leave
+// XCDs idle.  y and z: the slots (65535 at most in one dimension).
+static dim3 scan_grid(int64_t slots, int64_t nheads) {
+  const int64_t y = slots < 32768 ? slots : 32768;
+  return dim3((unsigned)nheads, (unsigned)y, (unsigned)((slots + y - 1) / y));
+}
+
 hipError_t launch_scan_states(const SeqIn& in, const uint16_t* u, const uint16_t* dy, bool rev,
                               int terms, int segT, const float* dt_bias, const float* A_log,
-                              const uint16_t* init, float* state, float* decay,
+                              const uint16_t* init, float* state, float* decay, bool pass,
                               hipStream_t stream) {
-  const dim3 grid((unsigned)slot_count(in.T, in.nseq, segT), (unsigned)in.nheads);
+  const dim3 grid = scan_grid(slot_count(in.T, in.nseq, segT), in.nheads);
   auto go = [&](auto kern, auto zx) {
     hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, zx, u, dy, in.T, in.nheads, in.offsets,
                        in.nseq, segT, dt_bias, A_log, state, decay);
@@ -395,7 +481,7 @@ hipError_t launch_scan_states(const SeqIn& in, const uint16_t* u, const uint16_t
     else go(scan_state_kernel<false, false, 2>, zb);
   }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || !pass) return e;
   const dim3 pg(kScState / 1024, (unsigned)in.nheads, (unsigned)in.nseq);
   if (rev)
     hipLaunchKernelGGL(scan_pass_kernel<true>, pg, dim3(256), 0, stream, state, decay, in.T,
@@ -409,25 +495,27 @@ hipError_t launch_scan_states(const SeqIn& in, const uint16_t* u, const uint16_t
 hipError_t launch_seq_scan(const SeqIn& in, const uint16_t* u, const float* dt_bias,
                            const float* A_log, const float* D, const uint16_t* ssm_in,
                            uint16_t* ssm_out, uint16_t* y, void* workspace, hipStream_t stream) {
-  const int64_t seg = scan_seg(in.T, in.nseq, in.nheads);
-  float* enter = nullptr;
+  const int64_t seg = scan_seg(in.T, in.nheads);
+  float *enter = nullptr, *decay = nullptr;
   const int64_t slots = slot_count(in.T, in.nseq, seg);
   if (seg < in.T) {
+    const bool own = in.T / seg <= kScOwn;
     enter = (float*)workspace;
+    decay = enter + slots * in.nheads * kScState;
     const hipError_t e = launch_scan_states(in, u, nullptr, false, 2, (int)seg, dt_bias, A_log,
-                                            ssm_in, enter, enter + slots * in.nheads * kScState,
-                                            stream);
+                                            ssm_in, enter, decay, !own, stream);
     if (e != hipSuccess) return e;
+    if (!own) decay = nullptr;
   }
-  const dim3 grid((unsigned)slots, (unsigned)in.nheads);
+  const dim3 grid = scan_grid(slots, in.nheads);
   if (in.f32)
     hipLaunchKernelGGL(scan_y_kernel<true>, grid, dim3(256), 0, stream, (const float*)in.zx, u,
                        in.T, in.nheads, in.offsets, in.nseq, (int)seg, dt_bias, A_log, D, ssm_in,
-                       enter, ssm_out, y);
+                       enter, decay, ssm_out, y);
   else
     hipLaunchKernelGGL(scan_y_kernel<false>, grid, dim3(256), 0, stream, (const uint16_t*)in.zx,
                        u, in.T, in.nheads, in.offsets, in.nseq, (int)seg, dt_bias, A_log, D,
-                       ssm_in, enter, ssm_out, y);
+                       ssm_in, enter, decay, ssm_out, y);
   return hipGetLastError();
 }
 

@@ -26,10 +26,12 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr int kScQ = 64;           // tokens of a tile of the walking kernels
 constexpr int kScState = kSqP * kSqN;
-// LDS rows: 32 bytes more than the data, so that the 16 rows of an operand or
-// a transpose read spread over the banks
-constexpr int kScRowN = 2 * kSqN + 32;  // 128 states (bytes)
-constexpr int kScRowP = 2 * kSqP + 32;  // 64 channels
+// LDS rows in bytes: what transpose reads take has 32 bytes more than the data
+// (the 32-byte pieces of four rows then lie in different banks), what only row
+// reads take 16 more (the 16-byte pieces of eight rows)
+constexpr int kScRowN = 2 * kSqN + 32;  // 128 states, transpose reads
+constexpr int kScRowP = 2 * kSqP + 32;  // 64 channels, transpose reads
+constexpr int kScRowS = 2 * kSqN + 16;  // 128 states, row reads
 
 // Slot sl of the segments of segT tokens that the sequences are cut into.
 // Sequence i's segment k has slot off[i] / segT + i + k, which leaves every
@@ -91,6 +93,39 @@ __device__ __forceinline__ float tok_raw(const typename Zx<F32>::T* zx, int64_t 
   return Zx<F32>::at(zx + t * Z + (Z - nheads) + h);
 }
 
+// inclusive sums over the lanes by DPP moves (shifts inside 16 lanes, then the
+// broadcasts of lane 15 and lane 31): a tenth of the latency of going through LDS
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_f64(double v) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xF, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xF, true);
+  return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+}
+__device__ __forceinline__ double lanes_before_and_own_f64(double v) {
+  v += dpp_f64<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8: zeros come in
+  v += dpp_f64<0x112, 0xF>(v);
+  v += dpp_f64<0x114, 0xF>(v);
+  v += dpp_f64<0x118, 0xF>(v);
+  v += dpp_f64<0x142, 0xA>(v);  // lane 15 of a row to the next row (rows 1 and 3)
+  v += dpp_f64<0x143, 0xC>(v);  // lane 31 to rows 2 and 3
+  return v;
+}
+__device__ __forceinline__ double last_lane_f64(double v) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 63);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), 63);
+  return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+}
+
+// 2^c, c <= 0: the integer part into the exponent, so that what is rounded to
+// float32 before v_exp_f32 is at most 1/2 (a rounded c of -20 would be off by
+// 2^-20, and these factors stand on whole states)
+__device__ __forceinline__ float exp2_f64(double c) {
+  const double n = __builtin_rint(c);
+  return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((float)(c - n)), n < -200.0 ? -200 : (int)n);
+}
+
 // one wave: Q / 64 consecutive tokens a lane, raw[] their dt + dt_bias;
 // tokens from n on do nothing (dt' = 0)
 template <int Q>
@@ -107,13 +142,8 @@ __device__ __forceinline__ void toks_make(Toks<Q>& k, const float (&raw)[Q / 64]
     sum += r2 * (double)dt[q];
     c[q] = sum;
   }
-  double inc = sum;  // inclusive over the lanes
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double up = __shfl_up(inc, o, 64);
-    if (lane >= o) inc += up;
-  }
-  const double before = inc - sum, total = __shfl(inc, 63, 64);
+  const double inc = lanes_before_and_own_f64(sum);
+  const double before = inc - sum, total = last_lane_f64(inc);
 #pragma unroll
   for (int q = 0; q < R; ++q) {
     const int s = lane * R + q;
@@ -122,25 +152,29 @@ __device__ __forceinline__ void toks_make(Toks<Q>& k, const float (&raw)[Q / 64]
     k.hi[s] = (float)hi;
     k.lo[s] = (float)(cc - hi);
     k.dt[s] = dt[q];
-    k.ec[s] = __builtin_amdgcn_exp2f((float)cc);
-    k.eq[s] = __builtin_amdgcn_exp2f((float)(total - cc));
+    k.ec[s] = exp2_f64(cc);
+    k.eq[s] = exp2_f64(total - cc);
   }
-  if (lane == 0) k.last = __builtin_amdgcn_exp2f((float)total);
+  if (lane == 0) k.last = exp2_f64(total);
 }
 
-// eight values as bfloat16 terms
+// eight values as bfloat16 terms (two at a time: three instructions a value and
+// term, the pairs left where the matrix operand wants them)
 template <int NT>
 __device__ __forceinline__ void split8(const float (&v)[8], bf16x8 (&t)[NT]) {
+  u32x4 w[NT];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float r = v[i];
+  for (int i = 0; i < 4; ++i) {
+    float a = v[2 * i], b = v[2 * i + 1];
 #pragma unroll
     for (int q = 0; q < NT; ++q) {
-      const __bf16 b = (__bf16)r;
-      t[q][i] = b;
-      r -= (float)b;
+      const uint32_t p = bf_pack(a, b);
+      w[q][i] = p;
+      if (q + 1 < NT) a -= bf_lo(p), b -= bf_hi(p);
     }
   }
+#pragma unroll
+  for (int q = 0; q < NT; ++q) t[q] = as_bf16x8(w[q]);
 }
 
 // Operand of 16 columns (lane & 15) by 32 tokens out of token-major LDS rows,

@@ -891,17 +891,22 @@ def mamba2_decode_token(arrays: dict, g: int, eps: float, emb: torch.Tensor,
 
 _ZX = (torch.bfloat16, torch.float32)
 _IDS = (torch.int32, torch.int64)
+_INT32 = (torch.int32,)
 _EMBED_TYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 def _call(fn: str, device: torch.device, *args) -> None:
     """The library call fn on the device's current stream (appended as the
     last argument), with that device current."""
-    if device.index == torch._C._cuda_getDevice():
-        _check(fn, getattr(lib(), fn)(*args, _stream()))
-        return
-    with torch.cuda.device(device):
-        _check(fn, getattr(lib(), fn)(*args, _stream()))
+    L = _lib if _lib is not None else lib()
+    cur = torch._C._cuda_getDevice()
+    if device.index == cur:
+        st = getattr(L, fn)(*args, torch._C._cuda_getCurrentRawStream(cur))
+    else:
+        with torch.cuda.device(device):
+            st = getattr(L, fn)(*args, _stream())
+    if st:
+        raise TernaryError(fn, st)
 
 
 def _seq_ws(fn: str, device: torch.device, *sizes):
@@ -915,36 +920,45 @@ def _seq_ws(fn: str, device: torch.device, *sizes):
     return ws, ws.data_ptr(), n
 
 
+def _of(t: torch.Tensor, name: str, dtypes, shape, dev) -> None:
+    """_need and _shape in one; four attributes where nothing is wrong."""
+    try:
+        if (t.dtype in dtypes and t.shape == shape and t.device == dev and t.is_contiguous()
+                and dev.type == "cuda"):
+            return
+    except AttributeError:
+        pass
+    _need(t, name, dtypes, len(shape))
+    _shape(t, name, shape, dev)
+
+
 def _seq_in(zxbcdt: torch.Tensor, H: int, offsets: Optional[torch.Tensor]):
     """Checks zxbcdt [T, Z] and the offsets; (device, T, nseq, d, cd, z_f32)."""
-    _need(zxbcdt, "zxbcdt", _ZX, 2)
+    if not isinstance(zxbcdt, torch.Tensor) or zxbcdt.dim() != 2:
+        _need(zxbcdt, "zxbcdt", _ZX, 2)
     dev = zxbcdt.device
     T = zxbcdt.shape[0]
     d = H * MIXER_HEADDIM
-    _shape(zxbcdt, "zxbcdt", (T, 2 * d + 2 * MIXER_DSTATE + H), dev)
+    _of(zxbcdt, "zxbcdt", _ZX, (T, 2 * d + 2 * MIXER_DSTATE + H), dev)
     nseq = 1
     if offsets is not None:
-        _need(offsets, "offsets", (torch.int32,), 1)
-        if offsets.shape[0] < 2:
+        nseq = offsets.shape[0] - 1 if isinstance(offsets, torch.Tensor) and offsets.dim() else 0
+        _of(offsets, "offsets", _INT32, (nseq + 1,), dev)
+        if nseq < 1:
             raise ValueError("offsets must hold the sequences' beginnings and the last one's end")
-        nseq = offsets.shape[0] - 1
-        _shape(offsets, "offsets", (nseq + 1,), dev)
     return dev, T, nseq, d, d + 2 * MIXER_DSTATE, int(zxbcdt.dtype == torch.float32)
-
-
-def _of(t: torch.Tensor, name: str, dtypes, shape, dev) -> None:
-    _need(t, name, dtypes, len(shape))
-    _shape(t, name, shape, dev)
 
 
 def _grad_zx(dzxbcdt: torch.Tensor, zxbcdt: torch.Tensor) -> None:
     _of(dzxbcdt, "dzxbcdt", (zxbcdt.dtype,), tuple(zxbcdt.shape), zxbcdt.device)
 
 
-def _heads_of(cd: int) -> int:
-    """Heads of a layer whose convolution has cd channels; a cd that no layer
-    has gives a count whose shapes do not fit."""
-    return max((cd - 2 * MIXER_DSTATE) // MIXER_HEADDIM, 0)
+def _heads_of(conv_b: torch.Tensor) -> int:
+    """Heads of the layer whose convolution has this bias; a length that no
+    layer has gives a count whose shapes do not fit."""
+    if not isinstance(conv_b, torch.Tensor) or conv_b.dim() != 1:
+        _need(conv_b, "conv_b", _F32, 1)
+    return max((conv_b.shape[0] - 2 * MIXER_DSTATE) // MIXER_HEADDIM, 0)
 
 
 def mixer_conv(zxbcdt: torch.Tensor, conv_w: torch.Tensor, conv_b: torch.Tensor,
@@ -959,8 +973,7 @@ def mixer_conv(zxbcdt: torch.Tensor, conv_w: torch.Tensor, conv_b: torch.Tensor,
     conv_state (float16 ring [nseq, conv_dim, 4]) gives the inputs before each
     sequence (None: zeros) and conv_out receives the last four after it (may
     be conv_state); both take conv_pos int32 [1], which stays as it is."""
-    _need(conv_b, "conv_b", _F32, 1)
-    dev, T, nseq, d, cd, f32 = _seq_in(zxbcdt, _heads_of(conv_b.shape[0]), offsets)
+    dev, T, nseq, d, cd, f32 = _seq_in(zxbcdt, _heads_of(conv_b), offsets)
     _of(conv_w, "conv_w", _F32, (cd, 4), dev)
     _of(conv_b, "conv_b", _F32, (cd,), dev)
     for t, name in ((conv_state, "conv_state"), (conv_out, "conv_out")):
@@ -969,11 +982,13 @@ def mixer_conv(zxbcdt: torch.Tensor, conv_w: torch.Tensor, conv_b: torch.Tensor,
             if conv_pos is None:
                 raise ValueError(f"{name} needs conv_pos")
     if conv_pos is not None:
-        _of(conv_pos, "conv_pos", (torch.int32,), (1,), dev)
+        _of(conv_pos, "conv_pos", _INT32, (1,), dev)
     if u is None:
         u = torch.empty((T, cd), dtype=torch.bfloat16, device=dev)
-    _of(u, "u", _BF16, (T, cd), dev)
-    if T == 0:
+    else:
+        _of(u, "u", _BF16, (T, cd), dev)
+    if T == 0:  # every sequence is empty: the states stay what they were
+        _keep_state(conv_state, conv_out)
         return u
     _call("tm_mixer_conv", dev, _ptr(zxbcdt), f32, T, nseq, d // MIXER_HEADDIM, _ptr(offsets),
           _ptr(conv_w), _ptr(conv_b), _ptr(conv_state), _ptr(conv_pos), _ptr(conv_out), _ptr(u))
@@ -986,8 +1001,7 @@ def mixer_conv_bwd(zxbcdt: torch.Tensor, conv_w: torch.Tensor, conv_b: torch.Ten
     """Gradients of mixer_conv without states (tm_mixer_conv_bwd): writes the
     xBC columns of dzxbcdt (zxbcdt's shape and type) and returns (dconv_w
     [conv_dim, 4], dconv_b [conv_dim])."""
-    _need(conv_b, "conv_b", _F32, 1)
-    dev, T, nseq, d, cd, f32 = _seq_in(zxbcdt, _heads_of(conv_b.shape[0]), offsets)
+    dev, T, nseq, d, cd, f32 = _seq_in(zxbcdt, _heads_of(conv_b), offsets)
     H = d // MIXER_HEADDIM
     _of(conv_w, "conv_w", _F32, (cd, 4), dev)
     _of(conv_b, "conv_b", _F32, (cd,), dev)
@@ -1003,8 +1017,17 @@ def mixer_conv_bwd(zxbcdt: torch.Tensor, conv_w: torch.Tensor, conv_b: torch.Ten
     return dw, db
 
 
+def _keep_state(before: Optional[torch.Tensor], after: Optional[torch.Tensor]) -> None:
+    if after is not None and after is not before:
+        if before is None:
+            after.zero_()
+        else:
+            after.copy_(before)
+
+
 def _scan_args(u, zxbcdt, dt_bias, A_log, D, offsets):
-    _need(A_log, "A_log", _F32, 1)
+    if not isinstance(A_log, torch.Tensor) or A_log.dim() != 1:
+        _need(A_log, "A_log", _F32, 1)
     H = A_log.shape[0]
     dev, T, nseq, d, cd, f32 = _seq_in(zxbcdt, H, offsets)
     _of(u, "u", _BF16, (T, cd), dev)
@@ -1029,8 +1052,10 @@ def mixer_scan(u: torch.Tensor, zxbcdt: torch.Tensor, dt_bias: torch.Tensor, A_l
             _of(t, name, _F16, (nseq, H, MIXER_HEADDIM, MIXER_DSTATE), dev)
     if y is None:
         y = torch.empty((T, d), dtype=torch.bfloat16, device=dev)
-    _of(y, "y", _BF16, (T, d), dev)
+    else:
+        _of(y, "y", _BF16, (T, d), dev)
     if T == 0:
+        _keep_state(ssm_state, ssm_out)
         return y
     ws, wp, wb = _seq_ws("tm_mixer_scan_workspace", dev, T, nseq, H)
     _call("tm_mixer_scan", dev, _ptr(u), _ptr(zxbcdt), f32, T, nseq, H, _ptr(offsets),
@@ -1050,7 +1075,8 @@ def mixer_scan_bwd(u: torch.Tensor, zxbcdt: torch.Tensor, dt_bias: torch.Tensor,
     _grad_zx(dzxbcdt, zxbcdt)
     if du is None:
         du = torch.empty((T, cd), dtype=torch.bfloat16, device=dev)
-    _of(du, "du", _BF16, (T, cd), dev)
+    else:
+        _of(du, "du", _BF16, (T, cd), dev)
     out = torch.empty((3, H), dtype=torch.float32, device=dev)
     if T == 0:
         return (du, *out.zero_())
@@ -1062,7 +1088,8 @@ def mixer_scan_bwd(u: torch.Tensor, zxbcdt: torch.Tensor, dt_bias: torch.Tensor,
 
 
 def _norm_args(y, zxbcdt, norm_w):
-    _need(norm_w, "norm_w", _F32, 1)
+    if not isinstance(norm_w, torch.Tensor) or norm_w.dim() != 1:
+        _need(norm_w, "norm_w", _F32, 1)
     H = norm_w.shape[0] // MIXER_HEADDIM
     dev, T, _, d, _, f32 = _seq_in(zxbcdt, H, None)
     _of(norm_w, "norm_w", _F32, (d,), dev)
@@ -1077,7 +1104,8 @@ def mixer_norm(y: torch.Tensor, zxbcdt: torch.Tensor, norm_w: torch.Tensor, eps:
     dev, T, H, d, f32 = _norm_args(y, zxbcdt, norm_w)
     if out is None:
         out = torch.empty((T, d), dtype=torch.bfloat16, device=dev)
-    _of(out, "out", _BF16, (T, d), dev)
+    else:
+        _of(out, "out", _BF16, (T, d), dev)
     if T == 0:
         return out
     _call("tm_mixer_norm", dev, _ptr(y), _ptr(zxbcdt), f32, T, H, _ptr(norm_w), eps, _ptr(out))
@@ -1106,14 +1134,18 @@ def embed(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.0,
     """out float32 [T, D] = scale * weight[ids] (tm_embed): ids int32 or int64
     [T], weight [V, D] float32, bfloat16 or float16.  An id outside the
     weight's rows gives zeros."""
-    _need(ids, "ids", _IDS, 1)
-    _need(weight, "weight", tuple(_EMBED_TYPE), 2)
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
+        _need(weight, "weight", tuple(_EMBED_TYPE), 2)
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 1:
+        _need(ids, "ids", _IDS, 1)
     T, (V, D) = ids.shape[0], weight.shape
     dev = weight.device
-    _shape(ids, "ids", (T,), dev)
+    _of(weight, "weight", _EMBED_TYPE, (V, D), dev)
+    _of(ids, "ids", _IDS, (T,), dev)
     if out is None:
         out = torch.empty((T, D), dtype=torch.float32, device=dev)
-    _of(out, "out", _F32, (T, D), dev)
+    else:
+        _of(out, "out", _F32, (T, D), dev)
     if T == 0:
         return out
     _call("tm_embed", dev, _ptr(ids), int(ids.dtype == torch.int64), T, _ptr(weight),
@@ -1134,7 +1166,8 @@ def embed_bwd(ids: torch.Tensor, dout: torch.Tensor, vocab: int, scale: float = 
         if accumulate:
             raise ValueError("accumulate=True needs an existing dW")
         dW = torch.empty((vocab, D), dtype=torch.float32, device=dev)
-    _of(dW, "dW", _F32, (vocab, D), dev)
+    else:
+        _of(dW, "dW", _F32, (vocab, D), dev)
     if T == 0:
         return dW if accumulate else dW.zero_()
     ws, wp, wb = _seq_ws("tm_embed_bwd_workspace", dev, T, vocab, D)
