@@ -7,7 +7,7 @@
  * A layer of H = nheads heads has d = 64 H channels, 128 states and one group
  * of B and C; cd = d + 256, Z = 2 d + 256 + H.  zxbcdt [T, Z] holds in_proj's
  * output of T tokens, z | x | B | C | dt, bfloat16 (z_f32 = 0) or float32
- * (z_f32 = 1).  T 1 .. 2^30, H 1 .. 4096.
+ * (z_f32 = 1).  T 1 .. 2^23, H 1 .. 4096.
  *
  * Sequences are packed along the tokens: offsets, int32 [nseq + 1] in device
  * memory (4-byte aligned), not descending, from 0 to at most T; sequence i is
@@ -131,7 +131,7 @@ int64_t tm_mixer_norm_bwd_workspace(int64_t T, int32_t nheads);
  *   weight  [V, D], w_type 0 float32, 1 bfloat16, 2 float16; aligned to its
  *           element
  *   out     float32 [T, D] (4-byte aligned): the residual stream
- *   T 1 .. 2^30, V 1 .. 2^30, D 1 .. 2^30; scale finite
+ *   T 1 .. 2^23, V 1 .. 2^23, D 1 .. 2^30; scale finite
  */
 tm_status tm_embed(const void* ids, int32_t ids_i64, int64_t T, const void* weight, int32_t w_type,
                    int64_t V, int64_t D, float scale, float* out, tm_stream stream);

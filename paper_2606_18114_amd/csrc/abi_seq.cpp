@@ -10,7 +10,9 @@ using namespace tmk_abi;
 
 namespace {
 
-constexpr int64_t kMaxTokens = int64_t(1) << 30;
+// tokens and rows of an embedding: a workgroup of 256 threads each stays within
+// a launch's 2^32 threads
+constexpr int64_t kMaxTokens = int64_t(1) << 23;
 
 struct Sizes {
   int64_t T, H, d, cd, Z, es;  // es: bytes of an element of zxbcdt
@@ -66,7 +68,8 @@ tmk::SeqIn seq_in(const void* zx, int32_t z_f32, int64_t T, int32_t nseq, int32_
 
 bool embed_sizes(int64_t T, int64_t V, int64_t D) {
   int64_t b;
-  return T >= 1 && T <= kMaxTokens && V >= 1 && V <= kMaxTokens && D >= 1 && D <= kMaxTokens &&
+  return T >= 1 && T <= kMaxTokens && V >= 1 && V <= kMaxTokens && D >= 1 &&
+         D <= (int64_t(1) << 30) &&
          bytes_of(T, D, 4, &b) && bytes_of(V, D, 4, &b);
 }
 

@@ -12,6 +12,7 @@ runs in the library's HIP kernels.  There is no fallback: if the library is miss
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -909,11 +910,18 @@ def _call(fn: str, device: torch.device, *args) -> None:
         raise TernaryError(fn, st)
 
 
-def _seq_ws(fn: str, device: torch.device, *sizes):
-    """Scratch of one call as (tensor or None, pointer, bytes)."""
+@functools.lru_cache(maxsize=4096)
+def _ws_bytes(fn: str, *sizes) -> int:
+    """A workspace size, which is a function of the call's sizes alone."""
     n = int(getattr(lib(), fn)(*sizes))
     if n < 0:
         raise ValueError(f"{fn}: sizes {sizes} out of range")
+    return n
+
+
+def _seq_ws(fn: str, device: torch.device, *sizes):
+    """Scratch of one call as (tensor or None, pointer, bytes)."""
+    n = _ws_bytes(fn, *sizes)
     if n == 0:
         return None, None, 0
     ws = torch.empty((n,), dtype=torch.uint8, device=device)
@@ -923,8 +931,8 @@ def _seq_ws(fn: str, device: torch.device, *sizes):
 def _of(t: torch.Tensor, name: str, dtypes, shape, dev) -> None:
     """_need and _shape in one; four attributes where nothing is wrong."""
     try:
-        if (t.dtype in dtypes and t.shape == shape and t.device == dev and t.is_contiguous()
-                and dev.type == "cuda"):
+        if (t.dtype in dtypes and t.shape == shape and t.device == dev and t.is_cuda
+                and t.is_contiguous()):
             return
     except AttributeError:
         pass

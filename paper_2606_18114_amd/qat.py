@@ -27,10 +27,15 @@ Every product runs in the library's kernels; this module only wires them
 into autograd (a dtype cast of the gradient and reshapes are the only torch
 operations on the data).  ``pack_for_decode`` returns the deployment format
 (2-bit codes and float16 group scales) that ``ops.tgemv`` reads.
+
+``Mamba2Mixer`` is the unquantized part between the two projections over whole
+sequences, ``Embedding`` the residual stream's beginning; with ``TernaryLinear``
+they make up a block's training step on the library's kernels.
 """
 
 from __future__ import annotations
 
+import math
 from typing import Optional, Tuple
 
 import torch
@@ -259,10 +264,136 @@ class TernaryLinear(torch.nn.Module):
                 f"out_dtype={self.out_dtype}")
 
 
+class Mamba2MixerFn(torch.autograd.Function):
+    """The mixer between the projections over packed sequences: convolution,
+    selective scan, gated norm (``tm_mixer_conv``, ``_scan``, ``_norm``) and
+    their gradients.  zxbcdt [T, Z]; offsets int32 [nseq + 1] or None.  whole:
+    the sequences cover every row."""
+
+    @staticmethod
+    def forward(ctx, zx, conv_w, conv_b, dt_bias, A_log, D, norm_w, offsets, eps, whole):
+        new = torch.empty if whole else torch.zeros
+        T, d = zx.shape[0], norm_w.shape[0]
+        par = [p.detach().contiguous() for p in (conv_w, conv_b, dt_bias, A_log, D, norm_w)]
+        zx = zx.contiguous()
+        y = new((T, d), dtype=torch.bfloat16, device=zx.device)
+        u = ops.mixer_conv(zx, par[0], par[1], offsets)
+        ops.mixer_scan(u, zx, *par[2:5], offsets, y=y)
+        out = ops.mixer_norm(y, zx, par[5], eps)
+        ctx.save_for_backward(zx, u, y, offsets, *par)
+        ctx.eps, ctx.whole = eps, whole
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        zx, u, y, offsets, conv_w, conv_b, dt_bias, A_log, D, norm_w = ctx.saved_tensors
+        dout = dout.to(torch.bfloat16).contiguous()
+        dzx = torch.empty_like(zx) if ctx.whole else torch.zeros_like(zx)
+        dy, dnorm = ops.mixer_norm_bwd(y, zx, norm_w, dout, dzx, ctx.eps)
+        du, dbias, dalog, dd = ops.mixer_scan_bwd(u, zx, dt_bias, A_log, D, dy, dzx, offsets)
+        dw, db = ops.mixer_conv_bwd(zx, conv_w, conv_b, du, dzx, offsets)
+        grads = (dzx, dw, db, dbias, dalog, dd, dnorm)
+        return (*(g if need else None for g, need in zip(grads, ctx.needs_input_grad)),
+                None, None, None)
+
+
+class Mamba2Mixer(torch.nn.Module):
+    """What stands between in_proj and out_proj of a Mamba-2 block in training:
+    the part the paper leaves unquantized (Sec. 3.2).  nheads heads of 64
+    channels, 128 states, one group of B and C, four convolution taps.
+
+    forward(zxbcdt, offsets=None): in_proj's output, bfloat16 or float32,
+    [L, Z] or [batch, L, Z] (a sequence a row), or with offsets (int32
+    [nseq + 1] on the GPU) packed sequences [T, Z]; returns out_proj's input,
+    bfloat16 [..., d_inner].  Sequences begin with zero states; rows outside
+    the offsets come out zero and have no gradient."""
+
+    PARAMS = ("conv_w", "conv_b", "dt_bias", "A_log", "D", "norm_w")
+
+    def __init__(self, nheads: int, eps: float = 1e-5, device: Optional[torch.device] = None):
+        super().__init__()
+        if nheads < 1:
+            raise ValueError("nheads must be at least 1")
+        self.nheads, self.eps = nheads, eps
+        self.d_inner = nheads * ops.MIXER_HEADDIM
+        cd = self.d_inner + 2 * ops.MIXER_DSTATE
+        f32 = dict(dtype=torch.float32, device=device)
+        step = torch.exp(torch.empty(nheads, **f32).uniform_(math.log(1e-3), math.log(1e-1)))
+        par = dict(conv_w=torch.empty((cd, 4), **f32).uniform_(-0.5, 0.5),
+                   conv_b=torch.empty((cd,), **f32).uniform_(-0.5, 0.5),
+                   dt_bias=step + torch.log(-torch.expm1(-step)),  # softplus^-1(step)
+                   A_log=torch.log(torch.empty(nheads, **f32).uniform_(1.0, 16.0)),
+                   D=torch.ones(nheads, **f32), norm_w=torch.ones(self.d_inner, **f32))
+        for name in self.PARAMS:
+            setattr(self, name, torch.nn.Parameter(par[name]))
+
+    def forward(self, zxbcdt: torch.Tensor,
+                offsets: Optional[torch.Tensor] = None) -> torch.Tensor:
+        if zxbcdt.dim() not in (2, 3):
+            raise ValueError(f"zxbcdt must be [L, Z] or [batch, L, Z], got {tuple(zxbcdt.shape)}")
+        lead, whole = zxbcdt.shape[:-1], offsets is None
+        if offsets is not None:
+            if zxbcdt.dim() != 2:
+                raise ValueError("packed sequences (offsets) are [T, Z]")
+        elif zxbcdt.dim() == 3 and lead[0] != 1 and lead.numel():
+            offsets = torch.arange(0, lead.numel() + 1, lead[1], dtype=torch.int32,
+                                   device=zxbcdt.device)
+        out = Mamba2MixerFn.apply(zxbcdt.reshape(-1, zxbcdt.shape[-1]),
+                                  *(getattr(self, n) for n in self.PARAMS), offsets, self.eps,
+                                  whole)
+        return out.reshape(*lead, self.d_inner)
+
+    def decode_params(self) -> dict:
+        """The arrays ``Mamba2Decoder``'s mixer(l) gives."""
+        return {n: getattr(self, n).detach() for n in self.PARAMS}
+
+    def extra_repr(self) -> str:
+        return f"nheads={self.nheads}, d_inner={self.d_inner}, eps={self.eps}"
+
+
+class EmbeddingFn(torch.autograd.Function):
+    """Rows of a weight times a scale (``tm_embed``, ``tm_embed_bwd``)."""
+
+    @staticmethod
+    def forward(ctx, ids, weight, scale):
+        ctx.save_for_backward(ids)
+        ctx.vocab, ctx.scale, ctx.dtype = weight.shape[0], scale, weight.dtype
+        return ops.embed(ids, weight.detach().contiguous(), scale)
+
+    @staticmethod
+    def backward(ctx, de):
+        (ids,) = ctx.saved_tensors
+        dw = ops.embed_bwd(ids, de.to(torch.float32).contiguous(), ctx.vocab, ctx.scale)
+        return None, dw.to(ctx.dtype), None
+
+
+class Embedding(torch.nn.Module):
+    """Token embedding whose output is the float32 residual stream, scaled:
+    forward(ids int32 or int64 [...]) -> float32 [..., width].  Ids outside the
+    vocabulary are padding: rows of zeros without a gradient.  The gradient of
+    the weight adds the tokens of a row in ascending order, so that repeated
+    steps give the same bits."""
+
+    def __init__(self, vocab: int, width: int, scale: float = 1.0,
+                 device: Optional[torch.device] = None, dtype: torch.dtype = torch.float32):
+        super().__init__()
+        self.scale = scale
+        self.weight = torch.nn.Parameter(torch.empty((vocab, width), device=device, dtype=dtype))
+        torch.nn.init.normal_(self.weight, 0.0, 0.02)
+
+    def forward(self, ids: torch.Tensor) -> torch.Tensor:
+        e = EmbeddingFn.apply(ids.reshape(-1).contiguous(), self.weight, self.scale)
+        return e.reshape(*ids.shape, self.weight.shape[1])
+
+    def extra_repr(self) -> str:
+        return f"{self.weight.shape[0]}, {self.weight.shape[1]}, scale={self.scale}"
+
+
 def flops_per_step(tokens: int, layer: TernaryLinear) -> float:
     """Algorithmic flops of one forward + straight-through backward (three
     dense products of 2 * tokens * in * out each; zeros not discounted)."""
     return 3.0 * 2.0 * tokens * layer.in_features * layer.out_features
 
 
-__all__ = ["SCALE_MODES", "TernaryLinear", "TernaryLinearFn", "flops_per_step"]
+__all__ = ["SCALE_MODES", "TernaryLinear", "TernaryLinearFn", "Mamba2Mixer", "Mamba2MixerFn",
+           "Embedding", "EmbeddingFn", "flops_per_step"]

@@ -15,7 +15,7 @@ quality lost to ternarization).
 * ``Mamba2Decoder``: decode in layer order through whole Mamba-2 blocks
   (pre-norm, in_proj, the FP16 mixer step of Sec. 3.2, out_proj), one token
   capturable as a HIP graph, or the whole stack in one launch (Sec. 8:
-  small-batch decode).
+  small-batch decode); and whole prompts before it.
 
 Only argument marshalling and packing happen here; every product runs in
 the library's kernels.
@@ -231,13 +231,18 @@ class Mamba2Decoder:
     The packed weights, mixer parameters and states of all layers live in
     layer-stacked arrays (``arena``); each layer's entries are views of them,
     so every form reads and advances the same states.
+    ``prefill`` takes whole prompts through the blocks and leaves their states
+    there for the tokens that follow.  embedding: optional weight [vocab,
+    d_model] (float32, bfloat16 or float16) of ``set_ids`` and of prompts given
+    as ids, times embed_scale.
     """
 
     def __init__(self, weight: Callable[[str, int], torch.Tensor], mixer: Callable[[int], dict],
                  pre_norm: Callable[[int], torch.Tensor], n_layers: int, d_model: int,
                  nheads: int, keep: Iterable[int] = (), g: int = 128, eps: float = 1e-5,
                  batch: int = 1, device: Optional[torch.device] = None,
-                 fused: Optional[bool] = None, stack: Optional[bool] = None):
+                 fused: Optional[bool] = None, stack: Optional[bool] = None,
+                 embedding: Optional[torch.Tensor] = None, embed_scale: float = 1.0):
         dev = device or torch.device("cuda")
         self.L, self.B, self.g, self.eps = n_layers, batch, g, eps
         self.keep = set(keep)
@@ -329,7 +334,7 @@ class Mamba2Decoder:
         self.y = torch.empty((1, batch, d_model), dtype=torch.float32, device=dev)
         self.gated = torch.empty((batch, self.d_inner), dtype=torch.float32, device=dev)
         self.ws = ops.mixer_workspace(batch, nheads, dev)
-        self.x_out = torch.empty((batch, d_model), dtype=torch.bfloat16, device=dev)
+        self.x_out = torch.zeros((batch, d_model), dtype=torch.bfloat16, device=dev)
         self.arena["final_w"] = self.final_norm
         self.stack_ws = (ops.mamba2_decode_workspace(d_model, nheads, dev, batch)
                          if self.stack else None)
@@ -340,6 +345,89 @@ class Mamba2Decoder:
                                             device=dev)
             self.part_gate = torch.empty((batch, nheads), dtype=torch.float32, device=dev)
         self.graph = None
+        if embedding is not None and (embedding.dim() != 2 or embedding.shape[1] != d_model):
+            raise ValueError(f"embedding must be [vocab, {d_model}]")
+        self.embedding, self.embed_scale = embedding, embed_scale
+
+    def set_ids(self, ids: torch.Tensor) -> torch.Tensor:
+        """The next token's ids (int32 or int64 [B]) into ``emb``."""
+        if self.embedding is None:
+            raise RuntimeError("the decoder was made without an embedding")
+        if ids.shape != (self.B,):
+            raise ValueError(f"ids must be [{self.B}], got {tuple(ids.shape)}")
+        return ops.embed(ids, self.embedding, self.embed_scale, out=self.emb)
+
+    def _proj_rows(self, lay, kind: str, x: torch.Tensor, out_dtype: torch.dtype) -> torch.Tensor:
+        """A projection of many rows x bfloat16 [T, K] (tm_tgemm_fwd; the layers
+        kept in FP16 by torch's float32 product, as there is no dense kernel for
+        many rows here)."""
+        p = lay[kind]
+        if p[0] == "dense":
+            return (x.float() @ p[1][0].float().t()).to(out_dtype)
+        return ops.tgemm_fwd(x, p[1][0], p[2][0].float(), self.g, out_dtype=out_dtype)
+
+    def _norm_rows(self, residual, y, w) -> torch.Tensor:
+        """residual += y and its norm, for any number of rows."""
+        x = torch.empty(residual.shape, dtype=torch.bfloat16, device=residual.device)
+        for r in range(0, residual.shape[0], 65535):
+            rows = slice(r, r + 65535)
+            ops.residual_rmsnorm(residual[rows], None if y is None else y[rows], w, self.eps,
+                                 x=x[rows])
+        return x
+
+    def prefill(self, prompts: torch.Tensor,
+                offsets: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Prompts through every block: prompts float32 [T, d_model] (embedded)
+        or ids [T], the batch rows' tokens packed one after another, row i's
+        being offsets[i] .. offsets[i + 1] - 1 (int32 [B + 1] on the GPU; None
+        with batch 1).  Every row's states go on from what they are (zero at
+        first, or an earlier prompt's end) and are left at the prompt's end; a
+        row without tokens keeps its own.  Returns ``x_out`` (bfloat16 [B,
+        d_model]) = the final norm behind each row's last token; a row without
+        tokens keeps its own there too.
+
+        The projections write bfloat16, as a bfloat16 model stores them; the
+        states are float32 inside the call and rounded once at its end (a token
+        at a time rounds them at every token).  A multi-row normalization, a
+        product, the mixer's three calls (tm_mixer_conv, tm_mixer_scan,
+        tm_mixer_norm) and a product per block."""
+        if prompts.dim() == 1:
+            if self.embedding is None:
+                raise RuntimeError("the decoder was made without an embedding")
+            residual = ops.embed(prompts, self.embedding, self.embed_scale)
+        else:
+            if prompts.dim() != 2 or prompts.shape[1] != self.d_model:
+                raise ValueError(f"prompts must be ids [T] or float32 [T, {self.d_model}], got "
+                                 f"{tuple(prompts.shape)}")
+            if prompts.dtype != torch.float32:
+                raise TypeError(f"embedded prompts must be float32 (got {prompts.dtype})")
+            residual = prompts.clone()
+        if offsets is None:
+            if self.B != 1:
+                raise ValueError(f"a batch of {self.B} needs offsets")
+        elif offsets.shape != (self.B + 1,):
+            raise ValueError(f"offsets must be [{self.B + 1}], got {tuple(offsets.shape)}")
+        T = residual.shape[0]
+        if T == 0:
+            return self.x_out
+        y = None
+        for lay in self.layers:
+            mp = lay["mixer"]
+            x = self._norm_rows(residual, y, lay["pre"])
+            zx = self._proj_rows(lay, "in", x, torch.bfloat16)
+            u = ops.mixer_conv(zx, mp["conv_w"], mp["conv_b"], offsets, lay["conv"], lay["pos"],
+                               conv_out=lay["conv"])
+            s = ops.mixer_scan(u, zx, mp["dt_bias"], mp["A_log"], mp["D"], offsets, lay["ssm"],
+                               ssm_out=lay["ssm"])
+            m = ops.mixer_norm(s, zx, mp["norm_w"], self.eps)
+            y = self._proj_rows(lay, "out", m, torch.float32)
+        if offsets is None:
+            self.x_out.copy_(self._norm_rows(residual[-1:] + y[-1:], None, self.final_norm))
+        else:
+            last = (offsets[1:] - 1).clamp(0, T - 1).long()
+            out = self._norm_rows(residual[last] + y[last], None, self.final_norm)
+            self.x_out.copy_(torch.where((offsets[1:] > offsets[:-1])[:, None], out, self.x_out))
+        return self.x_out
 
     def set_states(self, l: int, conv: torch.Tensor, ssm: torch.Tensor, pos: int = 0) -> None:
         """Layer l's convolution ring (float16 [B, conv_dim, 4], slot (pos + j) % 4
