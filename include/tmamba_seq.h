@@ -108,7 +108,7 @@ int64_t tm_mixer_scan_bwd_workspace(int64_t T, int32_t nseq, int32_t nheads);
  * tm_mixer_norm — the gated RMS norm of every row: g = y z / (1 + e^-z),
  *   out = bf16(g / sqrt(mean(g^2) + eps) * norm_w),
  * z = columns 0 .. d - 1 of zxbcdt.  y, out bf16 [T, d]; norm_w float32 [d];
- * eps finite, >= 0.
+ * eps finite, >= 0.  All T rows, each by itself: there are no offsets here.
  */
 tm_status tm_mixer_norm(const uint16_t* y, const void* zxbcdt, int32_t z_f32, int64_t T,
                         int32_t nheads, const float* norm_w, float eps, uint16_t* out,

@@ -16,7 +16,7 @@
 namespace tmk {
 
 constexpr int kCvCh = 8;       // channels of a thread
-constexpr int kCvBatch = 4;    // tokens whose loads are issued together
+constexpr int kCvBatch = 8;    // tokens whose loads are issued together
 constexpr int kCvBwdRun = 64;  // tokens of a backward run
 constexpr int kCvBwdCh = 4;    // its channels a thread: with 8 the sums leave two waves a SIMD
 constexpr int kCvBwdBatch = 8;

@@ -34,13 +34,11 @@ int64_t seq_scan_bytes(int64_t T, int64_t nseq, int64_t nheads);
 hipError_t launch_seq_scan(const SeqIn& in, const uint16_t* u, const float* dt_bias,
                            const float* A_log, const float* D, const uint16_t* ssm_in,
                            uint16_t* ssm_out, uint16_t* y, void* workspace, hipStream_t stream);
-// own states (rev: gradients) of the segments of segT tokens, or, with pass, those that enter
-// them: state [slots][nheads][64 * 128]
-// and decay [slots][nheads] (seq_scan_dev.hpp); terms 2 or 3 of the products (rev: 3)
-hipError_t launch_scan_states(const SeqIn& in, const uint16_t* u, const uint16_t* dy, bool rev,
-                              int terms, int segT, const float* dt_bias, const float* A_log,
-                              const uint16_t* init, float* state, float* decay, bool pass,
-                              hipStream_t stream);
+// float32 states (rev: gradients) that enter the chunks of the backward pass: state
+// [slots][nheads][64 * 128], with scratch decay [slots][nheads] (seq_scan_dev.hpp)
+hipError_t launch_chunk_states(const SeqIn& in, const uint16_t* u, const uint16_t* dy, bool rev,
+                               const float* dt_bias, const float* A_log, float* state,
+                               float* decay, hipStream_t stream);
 int64_t seq_scan_bwd_bytes(int64_t T, int64_t nseq, int64_t nheads);
 hipError_t launch_seq_scan_bwd(const SeqIn& in, const uint16_t* u, const float* dt_bias,
                                const float* A_log, const float* D, const uint16_t* dy, void* dzx,

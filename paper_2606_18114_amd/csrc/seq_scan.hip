@@ -23,28 +23,33 @@ namespace tmk {
 struct TileRegs {
   u32x4 m[4], v[2];
 };
-// rows t0 .. t0 + 63 of mat (128 columns) and vec (64 columns), zeros from t1 on
+// rows t0 .. t0 + 63 of mat (128 columns) and vec (64 columns); from t1 on, row
+// t1 - 1 again: a load under a condition would make the compiler wait for every
+// one before it, so none is, and tile_store puts zeros in their place
 __device__ __forceinline__ void tile_load(TileRegs& r, const uint16_t* mat, int64_t ldm,
                                           const uint16_t* vec, int64_t ldv, int t0, int t1) {
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    r.m[q] = ld16(mat + min(t0 + q * 16 + (tid >> 4), t1 - 1) * ldm + (tid & 15) * 8);
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+    r.v[q] = ld16(vec + min(t0 + q * 32 + (tid >> 3), t1 - 1) * ldv + (tid & 7) * 8);
+}
+// n: rows that are there
+__device__ __forceinline__ void tile_store(const TileRegs& r, uint8_t* m, uint8_t* v, int n) {
   const int tid = threadIdx.x;
   const u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const int row = q * 16 + (tid >> 4), t = t0 + row;
-    r.m[q] = t < t1 ? ld16(mat + t * ldm + (tid & 15) * 8) : zero;
+    const int row = q * 16 + (tid >> 4);
+    st16(m + row * kScRowN + (tid & 15) * 16, row < n ? r.m[q] : zero);
   }
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    const int row = q * 32 + (tid >> 3), t = t0 + row;
-    r.v[q] = t < t1 ? ld16(vec + t * ldv + (tid & 7) * 8) : zero;
+    const int row = q * 32 + (tid >> 3);
+    st16(v + row * kScRowP + (tid & 7) * 16, row < n ? r.v[q] : zero);
   }
-}
-__device__ __forceinline__ void tile_store(const TileRegs& r, uint8_t* m, uint8_t* v) {
-  const int tid = threadIdx.x;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) st16(m + (q * 16 + (tid >> 4)) * kScRowN + (tid & 15) * 16, r.m[q]);
-#pragma unroll
-  for (int q = 0; q < 2; ++q) st16(v + (q * 32 + (tid >> 3)) * kScRowP + (tid & 7) * 16, r.v[q]);
 }
 
 // The wave's state slice += sum_s coef_s vec_s mat_s^T over the tile: rows
@@ -139,7 +144,7 @@ __global__ __launch_bounds__(256, 2) void scan_state_kernel(
     raw_load(1);
   }
   for (int q = 0; q < nt; ++q) {
-    tile_store(r, m, v);
+    tile_store(r, m, v, s.t1 - tile_at(q));
     __syncthreads();
     if (q + 1 < nt) {
       load(q + 1);
@@ -158,13 +163,12 @@ __global__ __launch_bounds__(256, 2) void scan_state_kernel(
     state_add<NT>(S, m, v, coef);
     __syncthreads();
   }
-  float* o = state + ((int64_t)sl * nheads + h) * kScState;
+  float* o = state + ((int64_t)sl * nheads + h) * kScState + (lane & 15) * kSqN + 32 * wave +
+             4 * (lane >> 4);
 #pragma unroll
   for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
-    for (int pb = 0; pb < 4; ++pb)
-      *(f32x4*)(o + (16 * pb + (lane & 15)) * kSqN + 32 * wave + 16 * nb + 4 * (lane >> 4)) =
-          S[nb][pb];
+    for (int pb = 0; pb < 4; ++pb) *(f32x4*)(o + 16 * pb * kSqN + 16 * nb) = S[nb][pb];
   if (threadIdx.x == 0) decay[(int64_t)sl * nheads + h] = dec;
 }
 
@@ -216,9 +220,15 @@ __global__ __launch_bounds__(256) void scan_pass_kernel(float* __restrict__ stat
   }
 }
 
+// Tokens that a segment's last tile may have for it to be taken token by token:
+// 16 sequences of one token: 21 us as tiles, 16 so (most of a tile's time is
+// its chain of products and barriers, whatever it holds)
+constexpr int kScShort = 4;
+
 // ---- y ---------------------------------------------------------------------
-// grid: scan_grid, 256 threads.  enter: the states that enter the segments, or,
-// with decay, the segments' own ones; NULL where every sequence is one segment.
+// grid: scan_grid, 256 threads.  enter: the states that enter all segments, or,
+// with decay, the segments' own ones; NULL where every sequence is one segment
+// (one workgroup a head and sequence then, which may write over init).
 template <bool F32>
 __global__ __launch_bounds__(256, 2) void scan_y_kernel(
     const typename Zx<F32>::T* __restrict__ zx, const uint16_t* __restrict__ u, int T, int nheads,
@@ -248,33 +258,6 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
   const int64_t Z = (int64_t)2 * d + 2 * kSqN + nheads;
   const float bias = dt_bias[h], rate = expf(A_log[h]), skip = Dp[h];
   const uint16_t *Bg = u + d, *Cg = Bg + kSqN, *xg = u + h * kSqP;
-  f32x4 S[2][4];
-#pragma unroll
-  for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-    for (int pb = 0; pb < 4; ++pb) {
-      const int e = (16 * pb + col) * kSqN + 32 * wave + 16 * nb + 4 * g;
-      S[nb][pb] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (s.k > 0 && enter && !decay) {
-        S[nb][pb] = *(const f32x4*)(enter + ((int64_t)sl * nheads + h) * kScState + e);
-      } else if (init) {
-        const u32x2 w = *(const u32x2*)(init + sat + e);
-        S[nb][pb] = f32x4{h2f((uint16_t)w.x), h2f((uint16_t)(w.x >> 16)), h2f((uint16_t)w.y),
-                          h2f((uint16_t)(w.y >> 16))};
-      }
-    }
-  if (decay)  // the segments' own states: take those of the segments before this one
-    for (int k = s.k; k > 0; --k) {
-      const int64_t at = (int64_t)(sl - k) * nheads + h;
-      const float dec = decay[at];
-#pragma unroll
-      for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-        for (int pb = 0; pb < 4; ++pb) {
-          const int e = (16 * pb + col) * kSqN + 32 * wave + 16 * nb + 4 * g;
-          S[nb][pb] = S[nb][pb] * dec + *(const f32x4*)(enter + at * kScState + e);
-        }
-    }
   TileRegs r;
   bf16x8 cn[4];
   float raw;
@@ -282,10 +265,10 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
   auto load = [&](int t0) {
     const int t1 = min(s.t1, t0 + kScQ);
     tile_load(r, Bg, cd, xg, cd, t0, t1);
-    const int t = t0 + 16 * wave + col;
+    // (behind the last token: its C again, for a y that is not stored)
+    const int64_t t = min(t0 + 16 * wave + col, t1 - 1);
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      cn[k] = as_bf16x8(t < t1 ? ld16(Cg + (int64_t)t * cd + 32 * k + 8 * g) : u32x4{0, 0, 0, 0});
+    for (int k = 0; k < 4; ++k) cn[k] = as_bf16x8(ld16(Cg + t * cd + 32 * k + 8 * g));
   };
   // wave 0 (whose tokens have the fewest tokens before them) makes the token
   // values a tile ahead, of dt loaded yet a tile earlier
@@ -297,16 +280,65 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
     toks_make<kScQ>(tks[buf], rr, min(s.t1, t0 + kScQ) - t0, rate);
     coefs[buf][lane] = tks[buf].eq[lane] * tks[buf].dt[lane];
   };
+  if (wave == 0) raw_load(s.t0);
   load(s.t0);
+  // C of this lane's states and the last tile's first tokens, in case it is short
+  u32x2 cv[kScShort][2];
+  const int tail = s.t0 + (s.t1 - s.t0 - 1) / kScQ * kScQ;
+#pragma unroll
+  for (int q = 0; q < kScShort; ++q)
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+      cv[q][nb] = *(const u32x2*)(Cg + (int64_t)min(tail + q, s.t1 - 1) * cd + 32 * wave +
+                                  16 * nb + 4 * g);
+  // (all of the above on their way before the state's own loads are waited for)
+  f32x4 S[2][4];
+  const int sof = col * kSqN + 32 * wave + 4 * g;  // of S[0][0] in a state
+  if (enter && !decay) {
+    const float* p = enter + ((int64_t)sl * nheads + h) * kScState + sof;
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb) S[nb][pb] = *(const f32x4*)(p + 16 * pb * kSqN + 16 * nb);
+  } else if (init) {
+    u32x2 w[2][4];
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb)
+        w[nb][pb] = *(const u32x2*)(init + sat + sof + 16 * pb * kSqN + 16 * nb);
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb)
+        S[nb][pb] = f32x4{h2f((uint16_t)w[nb][pb].x), h2f((uint16_t)(w[nb][pb].x >> 16)),
+                          h2f((uint16_t)w[nb][pb].y), h2f((uint16_t)(w[nb][pb].y >> 16))};
+  } else {
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb) S[nb][pb] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  if (decay)  // the segments' own states: take those of the segments before this one
+    for (int k = s.k; k > 0; --k) {
+      const int64_t at = (int64_t)(sl - k) * nheads + h;
+      const float dec = decay[at];
+      const float* p = enter + at * kScState + sof;
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+        for (int pb = 0; pb < 4; ++pb)
+          S[nb][pb] = S[nb][pb] * dec + *(const f32x4*)(p + 16 * pb * kSqN + 16 * nb);
+    }
   if (wave == 0) {
-    raw_load(s.t0);
     toks(s.t0, 0);
     raw_load(s.t0 + kScQ);
   }
   int buf = 0;
-  for (int t0 = s.t0; t0 < s.t1; t0 += kScQ, buf ^= 1) {
+  int t0 = s.t0;
+  for (; s.t1 - t0 > kScShort; t0 += kScQ, buf ^= 1) {
     const int t1 = min(s.t1, t0 + kScQ);
-    tile_store(r, Bt, xt);
+    tile_store(r, Bt, xt, t1 - t0);
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
@@ -417,6 +449,53 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
     state_add<2>(S, Bt, xt, coef);
     __syncthreads();
   }
+  if (t0 < s.t1) {
+    // at most kScShort tokens are left: the recurrence itself, a token at a time
+    tile_store(r, Bt, xt, s.t1 - t0);
+    __syncthreads();
+    const Toks<kScQ>& tk = tks[buf];
+    float(*red)[4][kSqP] = (float(*)[4][kSqP])Sl;  // y of a token by waves
+#pragma unroll
+    for (int q = 0; q < kScShort; ++q) {
+      if (t0 + q >= s.t1) break;
+      const float dt = tk.dt[q];
+      const float dec = q == 0 ? tk.ec[0]
+                               : __builtin_amdgcn_exp2f((tk.hi[q] - tk.hi[q - 1]) +
+                                                        (tk.lo[q] - tk.lo[q - 1]));
+      u32x2 bw[2];
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb)
+        bw[nb] = *(const u32x2*)(Bt + q * kScRowN + 2 * (32 * wave + 16 * nb + 4 * g));
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb) {
+        const float dx =
+            dt * __uint_as_float((uint32_t)*(const uint16_t*)(xt + q * kScRowP + 2 * (16 * pb + col)) << 16);
+        float v = 0.f;
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) {
+          const float bf[4] = {bf_lo(bw[nb].x), bf_hi(bw[nb].x), bf_lo(bw[nb].y), bf_hi(bw[nb].y)};
+          const float cf[4] = {bf_lo(cv[q][nb].x), bf_hi(cv[q][nb].x), bf_lo(cv[q][nb].y),
+                               bf_hi(cv[q][nb].y)};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float sn = __builtin_fmaf(S[nb][pb][i], dec, dx * bf[i]);
+            S[nb][pb][i] = sn;
+            v = __builtin_fmaf(sn, cf[i], v);
+          }
+        }
+        v += __uint_as_float(lane_xchg<16>(__float_as_uint(v)));
+        v += __uint_as_float(lane_xchg<32>(__float_as_uint(v)));
+        if (g == 0) red[q][wave][16 * pb + col] = v;
+      }
+    }
+    __syncthreads();
+    const int q = wave, p = lane;  // a wave a token
+    if (t0 + q < s.t1) {
+      const float x = __uint_as_float((uint32_t)*(const uint16_t*)(xt + q * kScRowP + 2 * p) << 16);
+      const float v = (red[q][0][p] + red[q][1][p]) + (red[q][2][p] + red[q][3][p]);
+      y[(int64_t)(t0 + q) * d + h * kSqP + p] = bf_rne(__builtin_fmaf(skip, x, v));
+    }
+  }
   if (final_ && s.t1 == s.en) {
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
@@ -459,37 +538,46 @@ static dim3 scan_grid(int64_t slots, int64_t nheads) {
   return dim3((unsigned)nheads, (unsigned)y, (unsigned)((slots + y - 1) / y));
 }
 
-hipError_t launch_scan_states(const SeqIn& in, const uint16_t* u, const uint16_t* dy, bool rev,
-                              int terms, int segT, const float* dt_bias, const float* A_log,
-                              const uint16_t* init, float* state, float* decay, bool pass,
-                              hipStream_t stream) {
-  const dim3 grid = scan_grid(slot_count(in.T, in.nseq, segT), in.nheads);
-  auto go = [&](auto kern, auto zx) {
-    hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, zx, u, dy, in.T, in.nheads, in.offsets,
-                       in.nseq, segT, dt_bias, A_log, state, decay);
-  };
-  const float* zf = (const float*)in.zx;
-  const uint16_t* zb = (const uint16_t*)in.zx;
-  if (rev) {
-    if (in.f32) go(scan_state_kernel<true, true, 3>, zf);
-    else go(scan_state_kernel<false, true, 3>, zb);
-  } else if (terms == 3) {
-    if (in.f32) go(scan_state_kernel<true, false, 3>, zf);
-    else go(scan_state_kernel<false, false, 3>, zb);
-  } else {
-    if (in.f32) go(scan_state_kernel<true, false, 2>, zf);
-    else go(scan_state_kernel<false, false, 2>, zb);
-  }
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !pass) return e;
-  const dim3 pg(kScState / 1024, (unsigned)in.nheads, (unsigned)in.nseq);
-  if (rev)
-    hipLaunchKernelGGL(scan_pass_kernel<true>, pg, dim3(256), 0, stream, state, decay, in.T,
-                       in.nheads, in.offsets, segT, init);
-  else
-    hipLaunchKernelGGL(scan_pass_kernel<false>, pg, dim3(256), 0, stream, state, decay, in.T,
-                       in.nheads, in.offsets, segT, init);
+template <bool F32, bool REV, int NT>
+static hipError_t scan_state_go(const SeqIn& in, const uint16_t* u, const uint16_t* dy, int segT,
+                                const float* dt_bias, const float* A_log, float* state,
+                                float* decay, hipStream_t stream) {
+  hipLaunchKernelGGL((scan_state_kernel<F32, REV, NT>),
+                     scan_grid(slot_count(in.T, in.nseq, segT), in.nheads), dim3(256), 0, stream,
+                     (const typename Zx<F32>::T*)in.zx, u, dy, in.T, in.nheads, in.offsets,
+                     in.nseq, segT, dt_bias, A_log, state, decay);
   return hipGetLastError();
+}
+
+template <bool REV>
+static hipError_t scan_pass_go(const SeqIn& in, int segT, float* state, const float* decay,
+                               const uint16_t* init, hipStream_t stream) {
+  hipLaunchKernelGGL(scan_pass_kernel<REV>,
+                     dim3(kScState / 1024, (unsigned)in.nheads, (unsigned)in.nseq), dim3(256), 0,
+                     stream, state, decay, in.T, in.nheads, in.offsets, segT, init);
+  return hipGetLastError();
+}
+
+// Every chunk by itself, then one launch that adds them up (96 + 78 us at 16384
+// tokens of 64 heads, by the memory's rate; workgroups that walk through the
+// sequences and write each state once took 190, too few loads in flight).
+template <bool F32, bool REV>
+static hipError_t chunk_states_go(const SeqIn& in, const uint16_t* u, const uint16_t* dy,
+                                  const float* dt_bias, const float* A_log, float* state,
+                                  float* decay, hipStream_t stream) {
+  const hipError_t e =
+      scan_state_go<F32, REV, 3>(in, u, dy, kScChunk, dt_bias, A_log, state, decay, stream);
+  return e != hipSuccess ? e : scan_pass_go<REV>(in, kScChunk, state, decay, nullptr, stream);
+}
+
+hipError_t launch_chunk_states(const SeqIn& in, const uint16_t* u, const uint16_t* dy, bool rev,
+                               const float* dt_bias, const float* A_log, float* state,
+                               float* decay, hipStream_t stream) {
+  if (in.f32)
+    return rev ? chunk_states_go<true, true>(in, u, dy, dt_bias, A_log, state, decay, stream)
+               : chunk_states_go<true, false>(in, u, dy, dt_bias, A_log, state, decay, stream);
+  return rev ? chunk_states_go<false, true>(in, u, dy, dt_bias, A_log, state, decay, stream)
+             : chunk_states_go<false, false>(in, u, dy, dt_bias, A_log, state, decay, stream);
 }
 
 hipError_t launch_seq_scan(const SeqIn& in, const uint16_t* u, const float* dt_bias,
@@ -499,13 +587,20 @@ hipError_t launch_seq_scan(const SeqIn& in, const uint16_t* u, const float* dt_b
   float *enter = nullptr, *decay = nullptr;
   const int64_t slots = slot_count(in.T, in.nseq, seg);
   if (seg < in.T) {
-    const bool own = in.T / seg <= kScOwn;
+    // in place, a workgroup that has ended may have written what another would
+    // still begin with: then only the launch in between reads the initial states
+    const bool own = in.T / seg <= kScOwn && !(ssm_in && ssm_in == ssm_out);
     enter = (float*)workspace;
     decay = enter + slots * in.nheads * kScState;
-    const hipError_t e = launch_scan_states(in, u, nullptr, false, 2, (int)seg, dt_bias, A_log,
-                                            ssm_in, enter, decay, !own, stream);
+    hipError_t e = in.f32 ? scan_state_go<true, false, 2>(in, u, nullptr, (int)seg, dt_bias, A_log,
+                                                          enter, decay, stream)
+                          : scan_state_go<false, false, 2>(in, u, nullptr, (int)seg, dt_bias, A_log,
+                                                           enter, decay, stream);
+    if (e == hipSuccess && !own) {
+      e = scan_pass_go<false>(in, (int)seg, enter, decay, ssm_in, stream);
+      decay = nullptr;
+    }
     if (e != hipSuccess) return e;
-    if (!own) decay = nullptr;
   }
   const dim3 grid = scan_grid(slots, in.nheads);
   if (in.f32)

@@ -21,7 +21,7 @@
 // dl, were off by 2 to 3e-6).
 //
 // Chunks of 128 tokens: S0 and E of every chunk and head come first
-// (launch_scan_states, float32).  Then a workgroup takes a chunk and a group of
+// (launch_chunk_states, float32).  Then a workgroup takes a chunk and a group of
 // heads, so that dB and dC, which all heads share, add up in registers:
 // scan_bwd_off_kernel everything with S0 and E that reaches a float32 gradient
 // (three bfloat16 terms), scan_bwd_to_kernel and scan_bwd_from_kernel what is
@@ -32,43 +32,53 @@
 
 namespace tmk {
 
-constexpr int kSbQ = 128;       // tokens of a chunk
+constexpr int kSbQ = kScChunk;
 constexpr int kSbThreads = 512;
 
-// rows t0 .. t0 + 127 of 64 channels in 16-byte vectors, 1024 / THREADS a thread
+// rows t0 .. t0 + 127 of 64 channels in 16-byte vectors, 1024 / THREADS a thread.
+// No load here is under a condition (the compiler would wait for every one before
+// it): behind the last token it is read again, and zeros are put in its place.
 template <int THREADS>
 struct SbTile {
   u32x4 r[1024 / THREADS];
   __device__ __forceinline__ void load(const uint16_t* src, int64_t ld, int t0, int t1) {
 #pragma unroll
     for (int q = 0; q < 1024 / THREADS; ++q) {
-      const int t = t0 + q * (THREADS / 8) + ((int)threadIdx.x >> 3);
-      r[q] = t < t1 ? ld16(src + t * ld + (threadIdx.x & 7) * 8) : u32x4{0, 0, 0, 0};
+      const int t = min(t0 + q * (THREADS / 8) + ((int)threadIdx.x >> 3), t1 - 1);
+      r[q] = ld16(src + t * ld + (threadIdx.x & 7) * 8);
     }
   }
-  __device__ __forceinline__ void store(uint8_t* dst) const {
+  __device__ __forceinline__ void store(uint8_t* dst, int n) const {  // n: tokens
+    const u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
-    for (int q = 0; q < 1024 / THREADS; ++q)
-      st16(dst + (q * (THREADS / 8) + ((int)threadIdx.x >> 3)) * kScRowP + (threadIdx.x & 7) * 16,
-           r[q]);
+    for (int q = 0; q < 1024 / THREADS; ++q) {
+      const int row = q * (THREADS / 8) + ((int)threadIdx.x >> 3);
+      st16(dst + row * kScRowP + (threadIdx.x & 7) * 16, row < n ? r[q] : zero);
+    }
   }
 };
 // the chunk's B or C rows (128 states) into LDS, by kSbThreads threads
 __device__ __forceinline__ void sb_rows(const uint16_t* src, int64_t ld, int t0, int t1,
                                         uint8_t* dst) {
+  u32x4 r[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const int row = q * 32 + ((int)threadIdx.x >> 4), t = t0 + row;
+    const int64_t t = min(t0 + q * 32 + ((int)threadIdx.x >> 4), t1 - 1);
+    r[q] = ld16(src + t * ld + (threadIdx.x & 15) * 8);
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int row = q * 32 + ((int)threadIdx.x >> 4);
     st16(dst + row * kScRowN + (threadIdx.x & 15) * 16,
-         t < t1 ? ld16(src + (int64_t)t * ld + (threadIdx.x & 15) * 8) : u32x4{0, 0, 0, 0});
+         t0 + row < t1 ? r[q] : u32x4{0, 0, 0, 0});
   }
 }
 // operands of one token a lane, straight from memory: K of 32 columns
 template <int K>
-__device__ __forceinline__ void sb_own(bf16x8 (&o)[K], const uint16_t* row, bool in) {
+__device__ __forceinline__ void sb_own(bf16x8 (&o)[K], const uint16_t* row) {
   const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
-  for (int k = 0; k < K; ++k) o[k] = as_bf16x8(in ? ld16(row + 32 * k + 8 * g) : u32x4{0, 0, 0, 0});
+  for (int k = 0; k < K; ++k) o[k] = as_bf16x8(ld16(row + 32 * k + 8 * g));
 }
 // a chunk's token values, by one wave; raw loaded a head earlier
 template <bool F32>
@@ -141,9 +151,8 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_off_kernel(
 #pragma unroll
   for (int b = 0; b < 8; ++b) {
     acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int t = s.t0 + 16 * b + col;
-    dv[b] = t < s.t1 ? *(const u32x2*)(u + (int64_t)t * cd + d + (side ? 0 : kSqN) + n0 + 4 * g)
-                     : u32x2{0, 0};
+    const int64_t t = min(s.t0 + 16 * b + col, s.t1 - 1);
+    dv[b] = *(const u32x2*)(u + t * cd + d + (side ? 0 : kSqN) + n0 + 4 * g);
   }
   const uint16_t* vec = side ? u : dy;
   const int64_t ldv = side ? cd : d;
@@ -154,11 +163,12 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_off_kernel(
   const int at = 8 * g * kSqN + n0 + col;
   auto load = [&](int h) {
     tile.load(vec + h * kSqP, ldv, s.t0, s.t1);
+    // (a slice that is zero was never written; what lies there is not used)
     const float* p = slice + ((int64_t)sl * nheads + h) * kScState;
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) a[k][j] = none ? 0.f : p[at + (32 * k + j) * kSqN];
+      for (int j = 0; j < 8; ++j) a[k][j] = p[at + (32 * k + j) * kSqN];
   };
   auto toks = [&](int h) { st.load(zx, Z, nheads, h, s.t0, T, dt_bias, A_log); };
   if (h0 < h1) {
@@ -172,7 +182,7 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_off_kernel(
   int buf = 0;
   for (int h = h0; h < h1; ++h, buf ^= 1) {
     const int64_t sh = (int64_t)sl * nheads + h;
-    tile.store(vs);
+    tile.store(vs, s.t1 - s.t0);
     if (side == 0) {  // <E, S0> of the slice
       float pv = 0.f;
       if (!first && !last) {
@@ -275,9 +285,11 @@ __global__ __launch_bounds__(kSbThreads, 4) void scan_bwd_to_kernel(
   int h0, h1;
   sb_heads(nheads, blockIdx.y, gridDim.y, h0, h1);
   const int me = 16 * wb + col, tm = s.t0 + me;  // this lane's token
+  // (behind the chunk's last one it works on that one's values, and stores nothing)
+  const int64_t tc = min(tm, s.t1 - 1);
   sb_rows(u + d, cd, s.t0, s.t1, Bs);
   bf16x8 co[4];
-  sb_own<4>(co, u + (int64_t)tm * cd + d + kSqN, tm < s.t1);
+  sb_own<4>(co, u + tc * cd + d + kSqN);
   f32x4 acc[8];
 #pragma unroll
   for (int b = 0; b < 8; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -295,8 +307,8 @@ __global__ __launch_bounds__(kSbThreads, 4) void scan_bwd_to_kernel(
     bf16x8 yo[2];
     SbTile<kSbThreads> tile;
     tile.load(u + h * kSqP, cd, s.t0, s.t1);
-    sb_own<2>(yo, dy + (int64_t)tm * d + h * kSqP, tm < s.t1);
-    tile.store(xs);
+    sb_own<2>(yo, dy + tc * d + h * kSqP);
+    tile.store(xs, s.t1 - s.t0);
     __syncthreads();
     const Toks<kSbQ>& tk = tks[buf];
     if (w == 0 && h + 1 < h1) {
@@ -375,9 +387,11 @@ __global__ __launch_bounds__(kSbThreads, 2) void scan_bwd_from_kernel(
   int h0, h1;
   sb_heads(nheads, blockIdx.y, gridDim.y, h0, h1);
   const int me = 16 * wb + col, tm = s.t0 + me;  // this lane's token
+  // (behind the chunk's last one it works on that one's values, and stores nothing)
+  const int64_t tc = min(tm, s.t1 - 1);
   sb_rows(u + d + kSqN, cd, s.t0, s.t1, Cs);
   bf16x8 bo[4], xn[2];
-  sb_own<4>(bo, u + (int64_t)tm * cd + d, tm < s.t1);
+  sb_own<4>(bo, u + tc * cd + d);
   f32x4 acc[8];
 #pragma unroll
   for (int b = 0; b < 8; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -386,7 +400,7 @@ __global__ __launch_bounds__(kSbThreads, 2) void scan_bwd_from_kernel(
   SbToks<F32> st;
   auto load = [&](int h) {
     tile.load(dy + h * kSqP, d, s.t0, s.t1);
-    sb_own<2>(xn, u + (int64_t)tm * cd + h * kSqP, tm < s.t1);
+    sb_own<2>(xn, u + tc * cd + h * kSqP);
     if (!last)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
@@ -405,7 +419,7 @@ __global__ __launch_bounds__(kSbThreads, 2) void scan_bwd_from_kernel(
   int buf = 0;
   for (int h = h0; h < h1; ++h, buf ^= 1) {
     const int64_t sh = (int64_t)sl * nheads + h;
-    tile.store(ys);
+    tile.store(ys, s.t1 - s.t0);
     const bf16x8 xo[2] = {xn[0], xn[1]};
     if (!last)
 #pragma unroll
@@ -685,7 +699,7 @@ static int sb_groups(int64_t slots, int64_t nheads) {
 
 struct ScanBwdWs {
   double *qi, *ki;
-  float *S0, *E, *dec0, *dec1, *kd, *dots, *pa, *dd, *sums, *part;
+  float *S0, *E, *dec, *kd, *dots, *pa, *dd, *sums, *part;
   int64_t bytes;
 };
 static ScanBwdWs sb_ws(void* p, int64_t T, int64_t nseq, int64_t nheads) {
@@ -699,7 +713,7 @@ static ScanBwdWs sb_ws(void* p, int64_t T, int64_t nseq, int64_t nheads) {
   };
   w.S0 = take(sh * kScState);
   w.E = take(sh * kScState);
-  w.dec0 = take(sh), w.dec1 = take(sh);
+  w.dec = take(sh);
   w.qi = (double*)take(2 * sh * kSbQ), w.ki = (double*)take(2 * sh * kSbQ);
   w.kd = take(sh * kSbQ), w.dots = take(4 * sh * kSbQ);
   w.pa = take(2 * sh), w.dd = take(sh);
@@ -723,10 +737,9 @@ static hipError_t scan_bwd_go(const SeqIn& in, const uint16_t* u, const float* d
   const ScanBwdWs w = sb_ws(workspace, in.T, in.nseq, in.nheads);
   const int64_t slots = slot_count(in.T, in.nseq, kSbQ);
   const int groups = sb_groups(slots, in.nheads);
-  hipError_t e = launch_scan_states(in, u, nullptr, false, 3, kSbQ, dt_bias, A_log, nullptr, w.S0,
-                                    w.dec0, true, stream);
+  hipError_t e = launch_chunk_states(in, u, nullptr, false, dt_bias, A_log, w.S0, w.dec, stream);
   if (e != hipSuccess) return e;
-  e = launch_scan_states(in, u, dy, true, 3, kSbQ, dt_bias, A_log, nullptr, w.E, w.dec1, true, stream);
+  e = launch_chunk_states(in, u, dy, true, dt_bias, A_log, w.E, w.dec, stream);
   if (e != hipSuccess) return e;
   const dim3 grid((unsigned)slots, (unsigned)groups);
   float* part2 = w.part + (int64_t)groups * in.T * 2 * kSqN;

@@ -25,6 +25,7 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr int kScQ = 64;           // tokens of a tile of the walking kernels
+constexpr int kScChunk = 128;      // tokens of a chunk of the backward pass
 constexpr int kScState = kSqP * kSqN;
 // LDS rows in bytes: what transpose reads take has 32 bytes more than the data
 // (the 32-byte pieces of four rows then lie in different banks), what only row
@@ -148,9 +149,9 @@ __device__ __forceinline__ void toks_make(Toks<Q>& k, const float (&raw)[Q / 64]
   for (int q = 0; q < R; ++q) {
     const int s = lane * R + q;
     const double cc = before + c[q];
-    const double hi = __builtin_rint(cc * 16.0) * 0.0625;
-    k.hi[s] = (float)hi;
-    k.lo[s] = (float)(cc - hi);
+    const float hi = (float)(__builtin_rint(cc * 16.0) * 0.0625);
+    k.hi[s] = hi;
+    k.lo[s] = (float)(cc - (double)hi);  // (of hi as it is held, where c is beyond 2^20)
     k.dt[s] = dt[q];
     k.ec[s] = exp2_f64(cc);
     k.eq[s] = exp2_f64(total - cc);

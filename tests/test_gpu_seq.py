@@ -191,6 +191,51 @@ def test_scan(offs, H, dtype, dt_shift):
     assert bool((y[offs[-1]:] == 7.0).all()), "rows behind the last sequence were written"
 
 
+# long enough for sequences to be cut into segments whose states meet: in the
+# workgroups themselves (32 heads) and by a launch in between (2 heads)
+@pytest.mark.parametrize("H,offs", [(32, [0, 700, 700, 703, 1100]), (2, [0, 2300, 2600])])
+def test_scan_segments(H, offs):
+    rng, T, prm, dev, zx, u, off, (x, B, C, dt), d, cd = _scan_case(offs, H, torch.bfloat16, H, 0.0)
+    S = len(offs) - 1
+    ssm = _t(0.5 * rng.standard_normal((S, H, P, N)), torch.float16)
+    args = (u, zx, dev["dt_bias"], dev["A_log"], dev["D"], off)
+    new, same = torch.empty_like(ssm), ssm.clone()
+    outs = [(ops.mixer_scan(*args, ssm, ssm_out=new), new),
+            (ops.mixer_scan(*args, same, ssm_out=same), same),
+            (ops.mixer_scan(*args, ssm), None)]
+    s0 = _np(ssm)
+    for i, a, b in _seqs(offs):
+        ry, rs = O.scan(x[a:b], B[a:b], C[a:b], dt[a:b], prm["dt_bias"], prm["A_log"], prm["D"],
+                        s0[i])
+        my, ms = O.scan(np.abs(x[a:b]), np.abs(B[a:b]), np.abs(C[a:b]), dt[a:b], prm["dt_bias"],
+                        prm["A_log"], np.abs(prm["D"]), np.abs(s0[i]))
+        for y, st in outs:
+            near(f"y of sequence {i}", y[a:b].reshape(-1, H, P), ry, my, 2.0 ** -14)
+            if st is not None:
+                near(f"state of sequence {i}", st[i], rs, ms, 2.0 ** -14)
+
+
+def test_scan_in_place_at_length():
+    """Many segments of many heads, more than the chip takes at once: the states
+    in place are those out of place (to the rounding of the two ways they meet)."""
+    T, H = 9000, 64
+    rng = np.random.default_rng(3)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    prm = {k: _t(v) for k, v in synth.mixer_params(rng, H).items()}
+    zx = torch.randn(T, 2 * H * P + 256 + H, generator=g, device="cuda").to(torch.bfloat16)
+    u = torch.randn(T, H * P + 256, generator=g, device="cuda").to(torch.bfloat16)
+    off = torch.tensor([0, 8000, T], dtype=torch.int32, device="cuda")
+    ssm = torch.randn(2, H, P, N, generator=g, device="cuda").to(torch.float16)
+    args = (u, zx, prm["dt_bias"], prm["A_log"], prm["D"], off)
+    new, same = torch.empty_like(ssm), ssm.clone()
+    a = ops.mixer_scan(*args, ssm, ssm_out=new)
+    b = ops.mixer_scan(*args, same, ssm_out=same)
+    # both round once; before that they differ by float32 sums in another order
+    for x, y, step in ((a, b, 2.0 ** -7), (new, same, 2.0 ** -10)):
+        x, y = x.double(), y.double()
+        assert bool(((x - y).abs() <= step * y.abs() + 2.0 ** -14 * y.abs().max()).all())
+
+
 @pytest.mark.parametrize("dt_shift", [0.0, 4.0])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("H", [1, 5])
@@ -219,6 +264,38 @@ def test_scan_bwd(offs, H, dtype, dt_shift):
     near("dD", dd, total[2], mag[2], 2.0 ** -17)
     assert bool((dzx[:, :-H] == 3.0).all()) and bool((dzx[offs[-1]:] == 3.0).all())
     assert bool((du[offs[-1]:] == 7.0).all())
+
+
+def test_scan_outlier_steps():
+    """Single tokens whose step is so long that the state before them is gone
+    (exponents of millions): the decays among the tokens behind them keep their
+    accuracy, forward and backward."""
+    offs, H = [0, 130, 300], 2
+    rng, T, prm, dev, zx, u, off, _, d, cd = _scan_case(offs, H, torch.float32, 77, 0.0)
+    for t in (20, 64, 150, 299):
+        zx[t, -H:] = 3.0e5
+    un = _np(u)
+    x, B, C, dt = (un[:, :d].reshape(T, H, P), un[:, d:d + N], un[:, d + N:], _np(zx[:, -H:]))
+    dy = _t(0.1 * rng.standard_normal((T, d)), torch.bfloat16)
+    args = (u, zx, dev["dt_bias"], dev["A_log"], dev["D"])
+    y = ops.mixer_scan(*args, off)
+    dzx = torch.empty_like(zx)
+    du, *heads = ops.mixer_scan_bwd(*args, dy, dzx, off)
+    g = _np(dy).reshape(T, H, P)
+    total, mag = 0.0, 0.0
+    for i, a, b in _seqs(offs):
+        seq = (x[a:b], B[a:b], C[a:b], dt[a:b], prm["dt_bias"], prm["A_log"], prm["D"])
+        ry, _ = O.scan(*seq)
+        my, _ = O.scan(*(np.abs(v) for v in seq[:3]), *seq[3:6], np.abs(prm["D"]))
+        near(f"y of sequence {i}", y[a:b].reshape(-1, H, P), ry, my, 2.0 ** -14)
+        r, m = O.scan_bwd(*seq, g[a:b]), O.scan_bwd(*seq, g[a:b], absolute=True)
+        near(f"dx of sequence {i}", du[a:b, :d].reshape(-1, H, P), r[0], m[0], 2.0 ** -14)
+        near(f"dB of sequence {i}", du[a:b, d:d + N], r[1], m[1], 2.0 ** -14)
+        near(f"dC of sequence {i}", du[a:b, d + N:], r[2], m[2], 2.0 ** -14)
+        near(f"ddt of sequence {i}", dzx[a:b, -H:], r[3], m[3], 2.0 ** -17)
+        total, mag = total + np.stack(r[4:]), mag + np.stack(m[4:])
+    for k, name in enumerate(("ddt_bias", "dA_log", "dD")):
+        near(name, heads[k], total[k], mag[k], 2.0 ** -17)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
