@@ -3,10 +3,11 @@
 // the tokens of a row in ascending order, so that repeated calls give the same
 // bits.  An id outside [0, V) gives a row of zeros and no gradient.
 //
-// The gradient is bound by writing dW's V rows.  The tokens are sorted by id
+// The gradient is bound by writing dW's V rows.  Few tokens are found by going
+// through the ids (embed_direct_kernel, embed_first_kernel).  Many are sorted by id
 // into segments: a count per id, a place per segment (whichever: only the order
-// inside a segment shows in the sums), and the positions, in any order, which
-// the workgroup of a row brings into ascending order.  An id of more than
+// inside a segment shows in the sums), and the positions, in any order, which the
+// workgroup of a row brings into ascending order.  An id of more than
 // kEmPiece tokens (the most frequent one of a text is a tenth of it) is cut
 // into pieces of that many, whose sums meet in the row's workgroup; a piece
 // finds its tokens by going through the ids, which are few bytes.
@@ -15,7 +16,14 @@
 
 namespace tmk {
 
-constexpr int kEmPiece = 64;  // tokens of a piece
+constexpr int kEmPiece = 64;    // tokens of a piece
+// Tokens that a row's workgroup goes through by itself: one launch (256 tokens, 1000
+// ids of 512: 7 us).
+constexpr int kEmDirect = 256, kEmDirectV = 16384;
+// Tokens that a token's workgroup does; from there on the sort's launches are less
+// than T workgroups that each read T ids (4000 tokens, 10000 ids of 1024: 29 us, 37
+// sorted).
+constexpr int kEmScan = 4096;
 
 template <typename I>
 __device__ __forceinline__ int64_t em_id(const I* ids, int64_t t, int64_t V) {
@@ -67,21 +75,21 @@ __global__ __launch_bounds__(256) void embed_kernel(const I* __restrict__ ids, i
   if (c < D) o[c] = v >= 0 ? em_ld<TYPE>(w, v * D + c) * scale : 0.f;
 }
 
-// the workspace: count, place, filled, first piece [V] each; cursors [2] (of
-// tokens, of pieces); sorted [T]; a piece's id and its number in its row
-// [pieces] each; pieces' sums [pieces][D]
+// the workspace: count, place (the first piece's number where an id is in
+// pieces), filled [V] each; cursors [2] (of tokens, of pieces); sorted [T]; a
+// piece's id and its number in its row [pieces] each; pieces' sums [pieces][D]
 struct EmbedWs {
-  int *count, *place, *filled, *first, *cursor, *sorted, *pid, *pno;
+  int *count, *place, *filled, *cursor, *sorted, *pid, *pno;
   float* psum;
 };
 static int64_t em_pieces(int64_t T) { return 2 * (T / kEmPiece) + 1; }
 static int64_t em_ints(int64_t T, int64_t V) {
-  return (4 * V + 2 + T + 2 * em_pieces(T) + 63) / 64 * 64;
+  return (3 * V + 2 + T + 2 * em_pieces(T) + 63) / 64 * 64;
 }
 static EmbedWs em_ws(void* p, int64_t T, int64_t V) {
   EmbedWs w;
   int* i = (int*)p;
-  w.count = i, w.place = i + V, w.filled = i + 2 * V, w.first = i + 3 * V, w.cursor = i + 4 * V;
+  w.count = i, w.place = i + V, w.filled = i + 2 * V, w.cursor = i + 3 * V;
   w.sorted = w.cursor + 2;
   w.pid = w.sorted + T;
   w.pno = w.pid + em_pieces(T);
@@ -89,6 +97,7 @@ static EmbedWs em_ws(void* p, int64_t T, int64_t V) {
   return w;
 }
 int64_t embed_bwd_bytes(int64_t T, int64_t V, int64_t D) {
+  if (T <= kEmScan) return 0;
   return em_ints(T, V) * 4 + em_pieces(T) * D * 4;
 }
 
@@ -105,6 +114,25 @@ __global__ __launch_bounds__(256) void embed_count_kernel(const I* __restrict__ 
   if (t >= T) return;
   const int64_t v = em_id(ids, t, V);
   if (v >= 0) atomicAdd(&w.count[v], 1);
+}
+
+// with few ids their counts queue up at few addresses: each workgroup counts its
+// 1024 tokens in LDS first (16000 tokens of 100 ids: 37 us in all, 72 otherwise)
+constexpr int kEmCountV = 16384;
+
+template <typename I>
+__global__ __launch_bounds__(1024) void embed_count_lds_kernel(const I* __restrict__ ids,
+                                                               int64_t T, int V, EmbedWs w) {
+  __shared__ int cnt[kEmCountV];
+  const int tid = threadIdx.x;
+  for (int k = tid; k < V; k += 1024) cnt[k] = 0;
+  __syncthreads();
+  const int64_t t = (int64_t)blockIdx.x * 1024 + tid;
+  const int64_t v = t < T ? em_id(ids, t, V) : -1;
+  if (v >= 0) atomicAdd(&cnt[v], 1);
+  __syncthreads();
+  for (int k = tid; k < V; k += 1024)
+    if (cnt[k]) atomicAdd(&w.count[k], cnt[k]);
 }
 
 // a place for every segment, and the pieces of the long ones
@@ -128,9 +156,8 @@ __global__ __launch_bounds__(256) void embed_place_kernel(int64_t V, EmbedWs w) 
   }
   __syncthreads();
   if (v >= V) return;
-  w.place[v] = base[0] + a - n;
   const int first = base[1] + b - np;
-  w.first[v] = first;
+  w.place[v] = np ? first : base[0] + a - n;
   for (int k = 0; k < np; ++k) w.pid[first + k] = (int)v, w.pno[first + k] = k;
 }
 
@@ -219,6 +246,134 @@ __global__ __launch_bounds__(1024) void embed_piece_kernel(const I* __restrict__
   }
 }
 
+// Few tokens (at most kEmDirect): a row's workgroup finds its own among the ids.
+// grid (V), kEmDirect threads
+
+template <typename I, bool ACC>
+__global__ __launch_bounds__(kEmDirect) void embed_direct_kernel(const I* __restrict__ ids, int T,
+                                                                 const float* __restrict__ de,
+                                                                 int64_t D, float scale,
+                                                                 float* __restrict__ dW) {
+  __shared__ int list[kEmDirect], wave_n[4];
+  const int64_t v = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const bool hit = (int64_t)ids[min(tid, T - 1)] == v && tid < T;
+  const uint64_t m = __ballot(hit);
+  if (lane == 0) wave_n[wave] = __popcll(m);
+  __syncthreads();
+  const int n = wave_n[0] + wave_n[1] + wave_n[2] + wave_n[3];
+  if (ACC && n == 0) return;
+  int at = __popcll(m & ((1ull << lane) - 1));
+  for (int k = 0; k < wave; ++k) at += wave_n[k];
+  if (hit) list[at] = tid;  // ascending
+  __syncthreads();
+  float* o = dW + v * D;
+  const int64_t D4 = D & ~(int64_t)3;
+  for (int64_t c = (int64_t)tid * 4; c < D4; c += 4 * kEmDirect) {
+    f32x4 s = em_sum4(de, D, list, n, c) * scale;
+    if (ACC) s += *(const f32x4_u4*)(o + c);
+    *(f32x4_u4*)(o + c) = s;
+  }
+  for (int64_t c = D4 + tid; c < D; c += kEmDirect) {
+    float s = 0.f;
+    for (int k = 0; k < n; ++k) s += de[(int64_t)list[k] * D + c];
+    o[c] = ACC ? o[c] + s * scale : s * scale;
+  }
+}
+
+// Up to kEmScan tokens: dW is cleared by a launch of its own, and a workgroup a
+// token goes through all ids; the one of an id's first token adds up all of them:
+// four quarters of its threads take pieces of kEmPiece tokens in turn, whose sums
+// meet in LDS.  No sort and no workspace.  grid (T), 1024 threads
+__global__ __launch_bounds__(256) void embed_zero_kernel(float* __restrict__ p, int64_t n) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i + 4 <= n) *(f32x4_u4*)(p + i) = f32x4{0.f, 0.f, 0.f, 0.f};
+  else
+    for (int64_t j = i; j < n; ++j) p[j] = 0.f;
+}
+
+template <typename I, bool ACC>
+__global__ __launch_bounds__(1024) void embed_first_kernel(const I* __restrict__ ids, int T,
+                                                           int64_t V,
+                                                           const float* __restrict__ de,
+                                                           int64_t D, float scale,
+                                                           float* __restrict__ dW) {
+  constexpr int kPer = kEmScan / 1024;
+  __shared__ int list[kEmScan], wave_n[16], before;
+  __shared__ __attribute__((aligned(16))) float part[3][1024];
+  const int t0 = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t v = em_id(ids, t0, V);
+  if (v < 0) return;
+  if (tid == 0) before = 0;
+  // a wave goes through 64 kPer consecutive ids, 64 at a time
+  const int tw = wave * 64 * kPer + lane;
+  bool hit[kPer];
+#pragma unroll
+  for (int q = 0; q < kPer; ++q)
+    hit[q] = (int64_t)ids[min(tw + 64 * q, T - 1)] == v && tw + 64 * q < T;
+  int at[kPer], mine = 0;
+  bool earlier = false;
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    const uint64_t m = __ballot(hit[q]);
+    at[q] = mine + __popcll(m & ((1ull << lane) - 1));
+    mine += __popcll(m);
+    earlier |= hit[q] && tw + 64 * q < t0;
+  }
+  __syncthreads();
+  if (lane == 0) wave_n[wave] = mine;
+  if (earlier) before = 1;
+  __syncthreads();
+  if (before) return;  // not the first
+  int base = 0, n = 0;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    base += k < wave ? wave_n[k] : 0;
+    n += wave_n[k];
+  }
+#pragma unroll
+  for (int q = 0; q < kPer; ++q)
+    if (hit[q]) list[base + at[q]] = tw + 64 * q;
+  __syncthreads();
+  float* o = dW + v * D;
+  const int quarter = tid >> 8, lc = tid & 255;
+  // all threads stay in step: a column range ends for all at once
+  for (int64_t c0 = 0; c0 < D; c0 += 1024) {
+    const int64_t c = c0 + 4 * lc;
+    const bool whole = c + 4 <= D;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int k = quarter * kEmPiece; k < n; k += 4 * kEmPiece) {
+      const int m = min(kEmPiece, n - k);
+      if (whole) {
+        s += em_sum4(de, D, list + k, m, c);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          for (int j = 0; j < m && c + i < D; ++j) s[i] += de[(int64_t)list[k + j] * D + c + i];
+      }
+    }
+    if (n > kEmPiece) {  // (else the first quarter has it all)
+      if (quarter) *(f32x4*)(part[quarter - 1] + 4 * lc) = s;
+      __syncthreads();
+      if (quarter == 0)
+#pragma unroll
+        for (int q = 0; q < 3; ++q) s += *(const f32x4*)(part[q] + 4 * lc);
+    }
+    if (quarter == 0) {
+      s *= scale;
+      if (whole) {
+        if (ACC) s += *(const f32x4_u4*)(o + c);
+        *(f32x4_u4*)(o + c) = s;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (c + i < D) o[c + i] = ACC ? o[c + i] + s[i] : s[i];
+      }
+    }
+    if (n > kEmPiece) __syncthreads();
+  }
+}
+
 // grid (V): row v, zeros where no token has it
 template <bool ACC>
 __global__ __launch_bounds__(256) void embed_row_kernel(const float* __restrict__ de, int64_t D,
@@ -230,7 +385,7 @@ __global__ __launch_bounds__(256) void embed_row_kernel(const float* __restrict_
   if (ACC && n == 0) return;
   const float* src = de;
   if (n > kEmPiece) {  // the pieces' sums instead of tokens
-    src = w.psum + (int64_t)w.first[v] * D;
+    src = w.psum + (int64_t)w.place[v] * D;
     n = (n + kEmPiece - 1) / kEmPiece;
   } else if (n > 0) {
     // the tokens in ascending order: each goes where as many are smaller
@@ -290,15 +445,44 @@ template <typename I>
 static hipError_t embed_bwd_go(const I* ids, int64_t T, const float* de, int64_t V, int64_t D,
                                float scale, float* dW, bool accumulate, void* workspace,
                                hipStream_t stream) {
+  if (T <= kEmDirect && V <= kEmDirectV) {
+    if (accumulate)
+      hipLaunchKernelGGL((embed_direct_kernel<I, true>), dim3((unsigned)V), dim3(kEmDirect), 0,
+                         stream, ids, (int)T, de, D, scale, dW);
+    else
+      hipLaunchKernelGGL((embed_direct_kernel<I, false>), dim3((unsigned)V), dim3(kEmDirect), 0,
+                         stream, ids, (int)T, de, D, scale, dW);
+    return hipGetLastError();
+  }
+  if (T <= kEmScan) {
+    if (accumulate) {
+      hipLaunchKernelGGL((embed_first_kernel<I, true>), dim3((unsigned)T), dim3(1024), 0, stream,
+                         ids, (int)T, V, de, D, scale, dW);
+    } else {
+      const int64_t n = V * D;
+      // 2^31 threads at most a launch
+      for (int64_t i = 0; i < n; i += int64_t(1) << 32) {
+        const int64_t m = n - i < (int64_t(1) << 32) ? n - i : int64_t(1) << 32;
+        hipLaunchKernelGGL(embed_zero_kernel, dim3((unsigned)((m + 1023) / 1024)), dim3(256), 0,
+                           stream, dW + i, m);
+      }
+      hipLaunchKernelGGL((embed_first_kernel<I, false>), dim3((unsigned)T), dim3(1024), 0, stream,
+                         ids, (int)T, V, de, D, scale, dW);
+    }
+    return hipGetLastError();
+  }
   const EmbedWs w = em_ws(workspace, T, V);
   const unsigned vb = (unsigned)((V + 255) / 256), tb = (unsigned)((T + 255) / 256);
   hipLaunchKernelGGL(embed_clear_kernel, dim3(vb), dim3(256), 0, stream, w, V);
-  hipLaunchKernelGGL(embed_count_kernel<I>, dim3(tb), dim3(256), 0, stream, ids, T, V, w);
+  if (V <= kEmCountV)
+    hipLaunchKernelGGL(embed_count_lds_kernel<I>, dim3((unsigned)((T + 1023) / 1024)), dim3(1024),
+                       0, stream, ids, T, (int)V, w);
+  else
+    hipLaunchKernelGGL(embed_count_kernel<I>, dim3(tb), dim3(256), 0, stream, ids, T, V, w);
   hipLaunchKernelGGL(embed_place_kernel, dim3(vb), dim3(256), 0, stream, V, w);
   hipLaunchKernelGGL(embed_sort_kernel<I>, dim3(tb), dim3(256), 0, stream, ids, T, V, w);
-  if (T > kEmPiece)
-    hipLaunchKernelGGL(embed_piece_kernel<I>, dim3((unsigned)em_pieces(T)), dim3(1024), 0, stream,
-                       ids, T, de, D, w);
+  hipLaunchKernelGGL(embed_piece_kernel<I>, dim3((unsigned)em_pieces(T)), dim3(1024), 0, stream,
+                     ids, T, de, D, w);
   if (accumulate)
     hipLaunchKernelGGL(embed_row_kernel<true>, dim3((unsigned)V), dim3(256), 0, stream, de, D,
                        scale, dW, w);

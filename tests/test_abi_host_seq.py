@@ -85,7 +85,7 @@ def _embed():
 
 
 def _embed_bwd():
-    return dict(ids=P, i64=1, T=100, dout=P + G, V=50, D=64, scale=1.0, dW=P + 2 * G, acc=0,
+    return dict(ids=P, i64=1, T=10000, dout=P + G, V=50, D=64, scale=1.0, dW=P + 2 * G, acc=0,
                 ws=P + 3 * G, wsb=BIG, stream=None)
 
 
@@ -183,7 +183,7 @@ def test_workspace_sizes(L):
     assert L.tm_mixer_scan_workspace(300, 1, 64) == 0
     assert L.tm_mixer_scan_workspace(16384, 1, 64) > 0
     assert L.tm_mixer_scan_bwd_workspace(300, 2, 64) > 0
-    assert L.tm_embed_bwd_workspace(100, 50, 64) > 0
+    assert L.tm_embed_bwd_workspace(10000, 50, 64) > 0
     for f, a in ((L.tm_mixer_conv_bwd_workspace, (0, 4)), (L.tm_mixer_conv_bwd_workspace, (10, 0)),
                  (L.tm_mixer_scan_workspace, (10, 0, 4)), (L.tm_mixer_scan_workspace, (0, 1, 4)),
                  (L.tm_mixer_scan_bwd_workspace, (10, 1, 4097)),

@@ -353,16 +353,26 @@ def test_embed(T, V, D, w_dtype, ids_dtype):
     near("rows", out, ref, ref, 0.0)
 
 
-# one id for all tokens (in pieces), exactly 64 and 65 of one, all different
+# one id for all tokens (in pieces), exactly 64 and 65 of one, all different; few
+# enough tokens for a row's workgroup to find its own (up to 256), for a token's
+# (up to 4096), and more, sorted
 @pytest.mark.parametrize("ids_dtype", [torch.int32, torch.int64])
 @pytest.mark.parametrize("D", [1, 67, 256])
-@pytest.mark.parametrize("kind", ["one", "same", "edge", "apart", "mixed"])
+@pytest.mark.parametrize("kind", ["one", "same", "edge", "apart", "mixed", "few", "few_same", "few_wide", "odd",
+                                  "most", "long", "long_same", "long_wide"])
 def test_embed_bwd(kind, D, ids_dtype):
     rng = np.random.default_rng(D)
-    V = 300
+    V = {"odd": 301, "long_wide": 74001, "few_wide": 16500}.get(kind, 300)
     ids = {"one": np.array([3]), "same": np.full(1000, 17),
            "edge": np.repeat([5, 299, 0], [64, 65, 129]),
-           "apart": rng.permutation(V), "mixed": np.minimum(rng.geometric(0.02, 3000) - 2, V)}[kind]
+           "apart": rng.permutation(V), "mixed": np.minimum(rng.geometric(0.02, 3000) - 2, V),
+           "few": rng.integers(-1, V + 1, 256), "few_same": np.full(200, 299),
+           "few_wide": rng.integers(-1, V + 1, 200),
+           "odd": rng.integers(-1, V + 1, 500),
+           "most": np.minimum(rng.geometric(0.02, 4096) - 2, V),
+           "long": np.minimum(rng.geometric(0.02, 9000) - 2, V),
+           "long_same": np.repeat([5, 299, 0, 7], [64, 65, 129, 4097]),
+           "long_wide": np.minimum(rng.geometric(0.001, 5000) * 7, V)}[kind]
     rng.shuffle(ids)
     T = len(ids)
     de = _t(rng.standard_normal((T, D)))
