@@ -17,7 +17,6 @@ namespace tmk {
 
 constexpr int kCvCh = 8;       // channels of a thread
 constexpr int kCvBatch = 8;    // tokens whose loads are issued together
-constexpr int kCvBwdRun = 64;  // tokens of a backward run
 constexpr int kCvBwdCh = 4;    // its channels a thread: with 8 the sums leave two waves a SIMD
 constexpr int kCvBwdBatch = 8;
 
@@ -155,21 +154,21 @@ __global__ __launch_bounds__(256) void seq_ring_kernel(
   for (int j = 0; j < kSqTaps; ++j) ring_out[at + ((pos + j) & 3)] = now[j];
 }
 
-// Backward, a run of kCvBwdRun tokens: da of the run's tokens and of the three
+// Backward, a run of tokens (conv_bwd_run): da of the run's tokens and of the three
 // behind it (which only feed dx of the run's last ones).  dx[t] is complete
 // once da[t + 3] is known or the sequence has ended.  part [run][5][cd]: the
 // run's sums for w (4) and b.
 template <bool F32>
 __global__ __launch_bounds__(64) void seq_conv_bwd_kernel(
     const typename Zx<F32>::T* __restrict__ zx, int T, int nheads, const int* __restrict__ off,
-    int nseq, const float* __restrict__ conv_w, const float* __restrict__ conv_b,
+    int nseq, int run, const float* __restrict__ conv_w, const float* __restrict__ conv_b,
     const uint16_t* __restrict__ du, typename Zx<F32>::T* __restrict__ dzx,
     float* __restrict__ part) {
   const int d = nheads * kSqP, cd = d + 2 * kSqN;
   const int64_t Z = (int64_t)2 * d + 2 * kSqN + nheads;
   const int c = ((int)blockIdx.y * 64 + (int)threadIdx.x) * kCvBwdCh;
   if (c >= cd) return;
-  const int t0 = (int)blockIdx.x * kCvBwdRun, t1 = min(T, t0 + kCvBwdRun);
+  const int t0 = (int)blockIdx.x * run, t1 = min(T, t0 + run);
   const typename Zx<F32>::T* x = zx + d + c;
   typename Zx<F32>::T* dx = dzx + d + c;
   float w[kSqTaps][kCvBwdCh], b[kCvBwdCh];
@@ -350,8 +349,18 @@ hipError_t launch_seq_conv(const SeqIn& in, const float* conv_w, const float* co
                 : conv_go<false>(in, conv_w, conv_b, ring_in, ring_pos, ring_out, u, stream);
 }
 
+// Tokens of a backward run: as long as three waves a SIMD are left, for the run's
+// sums are written and added up, and 8 to 64: with few tokens it is a run's walk
+// that takes the time (1000 tokens of 64 heads: 18 us, 32 in runs of 64; 16384: 115).
+static int conv_bwd_run(int64_t T, int64_t nheads) {
+  const int64_t cblk = ((nheads * kSqP + 2 * kSqN) / kCvBwdCh + 63) / 64;
+  const int64_t run = T * cblk / 3072 / 8 * 8;
+  return (int)(run < 8 ? 8 : run > 64 ? 64 : run);
+}
+
 int64_t seq_conv_bwd_bytes(int64_t T, int64_t nheads) {
-  return (T + kCvBwdRun - 1) / kCvBwdRun * 5 * (nheads * kSqP + 2 * kSqN) * 4;
+  const int run = conv_bwd_run(T, nheads);
+  return (T + run - 1) / run * 5 * (nheads * kSqP + 2 * kSqN) * 4;
 }
 
 template <bool F32>
@@ -360,12 +369,12 @@ static hipError_t conv_bwd_go(const SeqIn& in, const float* conv_w, const float*
                               void* workspace, hipStream_t stream) {
   typedef typename Zx<F32>::T E;
   const int cd = in.nheads * kSqP + 2 * kSqN;
-  const int runs = (in.T + kCvBwdRun - 1) / kCvBwdRun;
+  const int run = conv_bwd_run(in.T, in.nheads), runs = (in.T + run - 1) / run;
   float* part = (float*)workspace;
   hipLaunchKernelGGL(seq_conv_bwd_kernel<F32>,
                      dim3((unsigned)runs, (unsigned)((cd / kCvBwdCh + 63) / 64)), dim3(64), 0, stream,
-                     (const E*)in.zx, in.T, in.nheads, in.offsets, in.nseq, conv_w, conv_b, du,
-                     (E*)dzx, part);
+                     (const E*)in.zx, in.T, in.nheads, in.offsets, in.nseq, run, conv_w, conv_b,
+                     du, (E*)dzx, part);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t cols = (int64_t)5 * cd;
