@@ -108,19 +108,21 @@ int64_t tm_mixer_scan_bwd_workspace(int64_t T, int32_t nseq, int32_t nheads);
  * tm_mixer_norm — the gated RMS norm of every row: g = y z / (1 + e^-z),
  *   out = bf16(g / sqrt(mean(g^2) + eps) * norm_w),
  * z = columns 0 .. d - 1 of zxbcdt.  y, out bf16 [T, d]; norm_w float32 [d];
- * eps finite, >= 0.  All T rows, each by itself: there are no offsets here.
+ * eps finite, >= 0.  Every row by itself; the offsets only say which rows there
+ * are.
  */
 tm_status tm_mixer_norm(const uint16_t* y, const void* zxbcdt, int32_t z_f32, int64_t T,
-                        int32_t nheads, const float* norm_w, float eps, uint16_t* out,
-                        tm_stream stream);
+                        int32_t nseq, int32_t nheads, const int32_t* offsets, const float* norm_w,
+                        float eps, uint16_t* out, tm_stream stream);
 
 /*
  * tm_mixer_norm_bwd — its gradients: dy bf16 [T, d], columns z of dzxbcdt,
  * dnorm_w float32 [d].  dout bf16 [T, d].
  */
 tm_status tm_mixer_norm_bwd(const uint16_t* y, const void* zxbcdt, int32_t z_f32, int64_t T,
-                            int32_t nheads, const float* norm_w, float eps, const uint16_t* dout,
-                            void* dzxbcdt, uint16_t* dy, float* dnorm_w, void* workspace,
+                            int32_t nseq, int32_t nheads, const int32_t* offsets,
+                            const float* norm_w, float eps, const uint16_t* dout, void* dzxbcdt,
+                            uint16_t* dy, float* dnorm_w, void* workspace,
                             int64_t workspace_bytes, tm_stream stream);
 int64_t tm_mixer_norm_bwd_workspace(int64_t T, int32_t nheads);
 

@@ -191,17 +191,18 @@ tm_status tm_mixer_scan_bwd(const uint16_t* u, const void* zxbcdt, int32_t z_f32
 }
 
 tm_status tm_mixer_norm(const uint16_t* y, const void* zxbcdt, int32_t z_f32, int64_t T,
-                        int32_t nheads, const float* norm_w, float eps, uint16_t* out,
-                        tm_stream stream) {
+                        int32_t nseq, int32_t nheads, const int32_t* offsets, const float* norm_w,
+                        float eps, uint16_t* out, tm_stream stream) {
   Sizes s;
   if (!y || !norm_w || !out) return TM_EINVAL;
   if (!(eps >= 0.0f) || !std::isfinite(eps)) return TM_EINVAL;
-  if (tm_status st = in_checked(zxbcdt, z_f32, T, 1, nheads, nullptr, &s)) return st;
+  if (tm_status st = in_checked(zxbcdt, z_f32, T, nseq, nheads, offsets, &s)) return st;
   if (!aligned(norm_w, 4) || !all_aligned({y, out}, 16)) return TM_EALIGN;
-  if (!apart({span(y, T * s.d * 2), span(zxbcdt, T * s.Z * s.es), span(norm_w, s.d * 4)},
+  if (!apart({span(y, T * s.d * 2), span(zxbcdt, T * s.Z * s.es), span(norm_w, s.d * 4),
+              opt(offsets, (nseq + 1) * 4)},
              {span(out, T * s.d * 2)}))
     return TM_EINVAL;
-  return hip_status(tmk::launch_seq_norm(seq_in(zxbcdt, z_f32, T, 1, nheads, nullptr), y, norm_w,
+  return hip_status(tmk::launch_seq_norm(seq_in(zxbcdt, z_f32, T, nseq, nheads, offsets), y, norm_w,
                                          eps, out, to_hip(stream)));
 }
 
@@ -211,23 +212,25 @@ int64_t tm_mixer_norm_bwd_workspace(int64_t T, int32_t nheads) {
 }
 
 tm_status tm_mixer_norm_bwd(const uint16_t* y, const void* zxbcdt, int32_t z_f32, int64_t T,
-                            int32_t nheads, const float* norm_w, float eps, const uint16_t* dout,
-                            void* dzxbcdt, uint16_t* dy, float* dnorm_w, void* workspace,
+                            int32_t nseq, int32_t nheads, const int32_t* offsets,
+                            const float* norm_w, float eps, const uint16_t* dout, void* dzxbcdt,
+                            uint16_t* dy, float* dnorm_w, void* workspace,
                             int64_t workspace_bytes, tm_stream stream) {
   Sizes s;
   if (!y || !norm_w || !dout || !dzxbcdt || !dy || !dnorm_w) return TM_EINVAL;
   if (!(eps >= 0.0f) || !std::isfinite(eps)) return TM_EINVAL;
-  if (tm_status st = in_checked(zxbcdt, z_f32, T, 1, nheads, nullptr, &s)) return st;
+  if (tm_status st = in_checked(zxbcdt, z_f32, T, nseq, nheads, offsets, &s)) return st;
   const int64_t need = tmk::seq_norm_bwd_bytes(T, nheads);
   if (tm_status st = ws_checked(workspace, workspace_bytes, need)) return st;
   if (!all_aligned({norm_w, dnorm_w}, 4) || !all_aligned({y, dout, dy}, 16) ||
       !aligned(dzxbcdt, (uintptr_t)s.es))
     return TM_EALIGN;
   const int64_t zb = T * s.Z * s.es, yb = T * s.d * 2;
-  if (!apart({span(y, yb), span(zxbcdt, zb), span(norm_w, s.d * 4), span(dout, yb)},
+  if (!apart({span(y, yb), span(zxbcdt, zb), span(norm_w, s.d * 4), span(dout, yb),
+              opt(offsets, (nseq + 1) * 4)},
              {span(dzxbcdt, zb), span(dy, yb), span(dnorm_w, s.d * 4), span(workspace, need)}))
     return TM_EINVAL;
-  return hip_status(tmk::launch_seq_norm_bwd(seq_in(zxbcdt, z_f32, T, 1, nheads, nullptr), y,
+  return hip_status(tmk::launch_seq_norm_bwd(seq_in(zxbcdt, z_f32, T, nseq, nheads, offsets), y,
                                              norm_w, eps, dout, dzxbcdt, dy, dnorm_w, workspace,
                                              to_hip(stream)));
 }

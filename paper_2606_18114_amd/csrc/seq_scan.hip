@@ -12,8 +12,17 @@
 //
 // Where there are too few sequences and heads to fill the chip, a sequence is
 // cut into segments: scan_state_kernel makes each segment's own state,
-// scan_pass_kernel the states that enter the segments, then scan_y_kernel
-// walks all segments at once.
+// scan_pass_kernel (or the segments' workgroups themselves, where those are few)
+// the states that enter the segments, then scan_y_kernel walks all segments at
+// once.
+//
+// Why tiles of 64 and four waves: two workgroups fit a CU (69 KiB of LDS, mostly
+// the state's terms, which every wave reads), so that one computes while the
+// other waits; 128 tokens and eight waves would leave one, and more of g that is
+// thrown away.  No single thing bounds it: of 175 us for 16384 tokens of 64 heads
+// in eight sequences (3.3 times the 53 us of reading u and writing y) the matrix
+// products busy the SIMDs 30 us, the vector instructions 80, LDS 85, and what
+// they wait for each other in a tile's chain is the rest.
 #include "seq_scan_dev.hpp"
 
 namespace tmk {
@@ -111,7 +120,7 @@ __global__ __launch_bounds__(256, 2) void scan_state_kernel(
   const uint16_t* mat = u + d + (REV ? kSqN : 0);
   const uint16_t* vec = REV ? dy + h * kSqP : u + h * kSqP;
   const int64_t ldv = REV ? d : cd;
-  const float bias = dt_bias[h], rate = expf(A_log[h]);
+  const float bias = dt_bias[h], rate = sc_rate(A_log[h]);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   f32x4 S[2][4];
@@ -256,7 +265,7 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
   }
   const int d = nheads * kSqP, cd = d + 2 * kSqN;
   const int64_t Z = (int64_t)2 * d + 2 * kSqN + nheads;
-  const float bias = dt_bias[h], rate = expf(A_log[h]), skip = Dp[h];
+  const float bias = dt_bias[h], rate = sc_rate(A_log[h]), skip = Dp[h];
   const uint16_t *Bg = u + d, *Cg = Bg + kSqN, *xg = u + h * kSqP;
   TileRegs r;
   bf16x8 cn[4];

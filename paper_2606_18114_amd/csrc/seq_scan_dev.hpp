@@ -76,9 +76,21 @@ inline __host__ __device__ int64_t slot_count(int64_t T, int64_t nseq, int64_t s
   return T / segT + nseq;
 }
 
+// e^A_log, held finite: with an infinite rate the exponents of tokens that are
+// not there would be NaN (0 times it); any step that is longer than 2^-115 ends
+// every state at this one as well
+__device__ __forceinline__ float sc_rate(float A_log) {
+  const float r = expf(A_log);
+  return r > 3.402823466e38f ? 3.402823466e38f : r;
+}
+// A token's exponent of 2 at least: nothing that float32 holds is left of a state
+// that decays by 2^-4096, and a chunk's sum of such exponents has an exact hi
+constexpr double kScLeast = -4096.0;
+
 // A tile's token values in LDS.  The exponents c (base 2) are held as hi, a
-// multiple of 1/16, and the rest lo: differences of two hi are exact, so that
-// c_t - c_s keeps 2^-29 of near tokens even where c itself is in the hundreds.
+// multiple of 1/16 (at most 2^19 of them are 128 tokens': exact in float32), and
+// the rest lo: differences of two hi are exact, so that c_t - c_s keeps 2^-29 of
+// near tokens even where c itself is in the hundreds.
 template <int Q>
 struct Toks {
   float hi[Q], lo[Q];  // c_t log2(e)
@@ -140,7 +152,8 @@ __device__ __forceinline__ void toks_make(Toks<Q>& k, const float (&raw)[Q / 64]
 #pragma unroll
   for (int q = 0; q < R; ++q) {
     dt[q] = lane * R + q < n ? mx_softplus(raw[q]) : 0.f;
-    sum += r2 * (double)dt[q];
+    const double l = r2 * (double)dt[q];
+    sum += l < kScLeast ? kScLeast : l;
     c[q] = sum;
   }
   const double inc = lanes_before_and_own_f64(sum);
@@ -151,7 +164,7 @@ __device__ __forceinline__ void toks_make(Toks<Q>& k, const float (&raw)[Q / 64]
     const double cc = before + c[q];
     const float hi = (float)(__builtin_rint(cc * 16.0) * 0.0625);
     k.hi[s] = hi;
-    k.lo[s] = (float)(cc - (double)hi);  // (of hi as it is held, where c is beyond 2^20)
+    k.lo[s] = (float)(cc - (double)hi);
     k.dt[s] = dt[q];
     k.ec[s] = exp2_f64(cc);
     k.eq[s] = exp2_f64(total - cc);

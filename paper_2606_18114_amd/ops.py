@@ -116,9 +116,10 @@ SIGNATURES_SEQ = {
     "tm_mixer_scan_bwd": (ctypes.c_int, [_P, _P, _I32, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P,
                                          _P, _P, _P, _P, _P, _I64, _P]),
     "tm_mixer_scan_bwd_workspace": (ctypes.c_int64, [_I64, _I32, _I32]),
-    "tm_mixer_norm": (ctypes.c_int, [_P, _P, _I32, _I64, _I32, _P, ctypes.c_float, _P, _P]),
-    "tm_mixer_norm_bwd": (ctypes.c_int, [_P, _P, _I32, _I64, _I32, _P, ctypes.c_float, _P, _P, _P,
-                                         _P, _P, _I64, _P]),
+    "tm_mixer_norm": (ctypes.c_int, [_P, _P, _I32, _I64, _I32, _I32, _P, _P, ctypes.c_float, _P,
+                                     _P]),
+    "tm_mixer_norm_bwd": (ctypes.c_int, [_P, _P, _I32, _I64, _I32, _I32, _P, _P, ctypes.c_float,
+                                         _P, _P, _P, _P, _P, _I64, _P]),
     "tm_mixer_norm_bwd_workspace": (ctypes.c_int64, [_I64, _I32]),
     "tm_embed": (ctypes.c_int, [_P, _I32, _I64, _P, _I32, _I64, _I64, ctypes.c_float, _P, _P]),
     "tm_embed_bwd": (ctypes.c_int, [_P, _I32, _I64, _P, _I64, _I64, ctypes.c_float, _P, _I32, _P,
@@ -1095,36 +1096,40 @@ def mixer_scan_bwd(u: torch.Tensor, zxbcdt: torch.Tensor, dt_bias: torch.Tensor,
     return du, out[0], out[1], out[2]
 
 
-def _norm_args(y, zxbcdt, norm_w):
+def _norm_args(y, zxbcdt, norm_w, offsets):
     if not isinstance(norm_w, torch.Tensor) or norm_w.dim() != 1:
         _need(norm_w, "norm_w", _F32, 1)
     H = norm_w.shape[0] // MIXER_HEADDIM
-    dev, T, _, d, _, f32 = _seq_in(zxbcdt, H, None)
+    dev, T, nseq, d, _, f32 = _seq_in(zxbcdt, H, offsets)
     _of(norm_w, "norm_w", _F32, (d,), dev)
     _of(y, "y", _BF16, (T, d), dev)
-    return dev, T, H, d, f32
+    return dev, T, nseq, H, d, f32
 
 
 def mixer_norm(y: torch.Tensor, zxbcdt: torch.Tensor, norm_w: torch.Tensor, eps: float = 1e-5,
-               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+               out: Optional[torch.Tensor] = None,
+               offsets: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The gated RMS norm before out_proj, over rows (tm_mixer_norm): y
-    bfloat16 [T, d_inner] and z of zxbcdt -> out bfloat16 [T, d_inner]."""
-    dev, T, H, d, f32 = _norm_args(y, zxbcdt, norm_w)
+    bfloat16 [T, d_inner] and z of zxbcdt -> out bfloat16 [T, d_inner].  With
+    offsets, rows outside the sequences are left as they were."""
+    dev, T, nseq, H, d, f32 = _norm_args(y, zxbcdt, norm_w, offsets)
     if out is None:
         out = torch.empty((T, d), dtype=torch.bfloat16, device=dev)
     else:
         _of(out, "out", _BF16, (T, d), dev)
     if T == 0:
         return out
-    _call("tm_mixer_norm", dev, _ptr(y), _ptr(zxbcdt), f32, T, H, _ptr(norm_w), eps, _ptr(out))
+    _call("tm_mixer_norm", dev, _ptr(y), _ptr(zxbcdt), f32, T, nseq, H, _ptr(offsets),
+          _ptr(norm_w), eps, _ptr(out))
     return out
 
 
 def mixer_norm_bwd(y: torch.Tensor, zxbcdt: torch.Tensor, norm_w: torch.Tensor,
-                   dout: torch.Tensor, dzxbcdt: torch.Tensor, eps: float = 1e-5):
+                   dout: torch.Tensor, dzxbcdt: torch.Tensor, eps: float = 1e-5,
+                   offsets: Optional[torch.Tensor] = None):
     """Gradients of mixer_norm (tm_mixer_norm_bwd): writes the z columns of
     dzxbcdt and returns (dy bfloat16 [T, d_inner], dnorm_w [d_inner])."""
-    dev, T, H, d, f32 = _norm_args(y, zxbcdt, norm_w)
+    dev, T, nseq, H, d, f32 = _norm_args(y, zxbcdt, norm_w, offsets)
     _of(dout, "dout", _BF16, (T, d), dev)
     _grad_zx(dzxbcdt, zxbcdt)
     dy = torch.empty((T, d), dtype=torch.bfloat16, device=dev)
@@ -1132,8 +1137,8 @@ def mixer_norm_bwd(y: torch.Tensor, zxbcdt: torch.Tensor, norm_w: torch.Tensor,
     if T == 0:
         return dy, dw.zero_()
     ws, wp, wb = _seq_ws("tm_mixer_norm_bwd_workspace", dev, T, H)
-    _call("tm_mixer_norm_bwd", dev, _ptr(y), _ptr(zxbcdt), f32, T, H, _ptr(norm_w), eps,
-          _ptr(dout), _ptr(dzxbcdt), _ptr(dy), _ptr(dw), wp, wb)
+    _call("tm_mixer_norm_bwd", dev, _ptr(y), _ptr(zxbcdt), f32, T, nseq, H, _ptr(offsets),
+          _ptr(norm_w), eps, _ptr(dout), _ptr(dzxbcdt), _ptr(dy), _ptr(dw), wp, wb)
     return dy, dw
 
 

@@ -39,6 +39,7 @@ import math
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import ops
 
@@ -273,23 +274,23 @@ class Mamba2MixerFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, zx, conv_w, conv_b, dt_bias, A_log, D, norm_w, offsets, eps, whole):
         new = torch.empty if whole else torch.zeros
-        T, d = zx.shape[0], norm_w.shape[0]
+        out = new((zx.shape[0], norm_w.shape[0]), dtype=torch.bfloat16, device=zx.device)
         par = [p.detach().contiguous() for p in (conv_w, conv_b, dt_bias, A_log, D, norm_w)]
         zx = zx.contiguous()
-        y = new((T, d), dtype=torch.bfloat16, device=zx.device)
         u = ops.mixer_conv(zx, par[0], par[1], offsets)
-        ops.mixer_scan(u, zx, *par[2:5], offsets, y=y)
-        out = ops.mixer_norm(y, zx, par[5], eps)
+        y = ops.mixer_scan(u, zx, *par[2:5], offsets)
+        ops.mixer_norm(y, zx, par[5], eps, out, offsets)
         ctx.save_for_backward(zx, u, y, offsets, *par)
         ctx.eps, ctx.whole = eps, whole
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         zx, u, y, offsets, conv_w, conv_b, dt_bias, A_log, D, norm_w = ctx.saved_tensors
         dout = dout.to(torch.bfloat16).contiguous()
         dzx = torch.empty_like(zx) if ctx.whole else torch.zeros_like(zx)
-        dy, dnorm = ops.mixer_norm_bwd(y, zx, norm_w, dout, dzx, ctx.eps)
+        dy, dnorm = ops.mixer_norm_bwd(y, zx, norm_w, dout, dzx, ctx.eps, offsets)
         du, dbias, dalog, dd = ops.mixer_scan_bwd(u, zx, dt_bias, A_log, D, dy, dzx, offsets)
         dw, db = ops.mixer_conv_bwd(zx, conv_w, conv_b, du, dzx, offsets)
         grads = (dzx, dw, db, dbias, dalog, dd, dnorm)
@@ -361,6 +362,7 @@ class EmbeddingFn(torch.autograd.Function):
         return ops.embed(ids, weight.detach().contiguous(), scale)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, de):
         (ids,) = ctx.saved_tensors
         dw = ops.embed_bwd(ids, de.to(torch.float32).contiguous(), ctx.vocab, ctx.scale)

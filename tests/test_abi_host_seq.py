@@ -70,13 +70,13 @@ def _scan_bwd():
 
 
 def _norm():
-    return dict(y=P, zx=P + G, f32=0, T=100, H=4, w=P + 2 * G, eps=1e-5, out=P + 3 * G,
-                stream=None)
+    return dict(y=P, zx=P + G, f32=0, T=100, nseq=2, H=4, off=P + 4 * G, w=P + 2 * G, eps=1e-5,
+                out=P + 3 * G, stream=None)
 
 
 def _norm_bwd():
-    return dict(y=P, zx=P + G, f32=0, T=100, H=4, w=P + 2 * G, eps=1e-5, dout=P + 3 * G,
-                dzx=P + 4 * G, dy=P + 5 * G, dw=P + 6 * G, ws=P + 7 * G, wsb=BIG, stream=None)
+    return dict(y=P, zx=P + G, f32=0, T=100, nseq=2, H=4, off=P + 8 * G, w=P + 2 * G, eps=1e-5,
+                dout=P + 3 * G, dzx=P + 4 * G, dy=P + 5 * G, dw=P + 6 * G, ws=P + 7 * G, wsb=BIG, stream=None)
 
 
 def _embed():

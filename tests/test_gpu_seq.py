@@ -298,6 +298,86 @@ def test_scan_outlier_steps():
         near(name, heads[k], total[k], mag[k], 2.0 ** -17)
 
 
+def test_scan_steps_that_end_every_state():
+    """A_log beyond what float32's e^A_log holds, and steps of 2^-4096 and less:
+    every token stands alone, with no gradient through the state."""
+    offs, H = [0, 130, 131, 300], 2
+    rng, T, prm, dev, zx, u, off, _, d, cd = _scan_case(offs, H, torch.float32, 78, 0.0)
+    prm["A_log"] = np.array([100.0, 20.0], np.float32)
+    dev["A_log"] = _t(prm["A_log"])
+    un, dtn = _np(u), _np(zx[:, -H:])
+    x, B, C = un[:, :d].reshape(T, H, P), un[:, d:d + N], un[:, d + N:]
+    dy = _t(0.1 * rng.standard_normal((T, d)), torch.bfloat16)
+    args = (u, zx, dev["dt_bias"], dev["A_log"], dev["D"])
+    y = ops.mixer_scan(*args, off)
+    dzx = torch.empty_like(zx)
+    du, *heads = ops.mixer_scan_bwd(*args, dy, dzx, off)
+    g = _np(dy).reshape(T, H, P)
+    for i, a, b in _seqs(offs):
+        seq = (x[a:b], B[a:b], C[a:b], dtn[a:b], prm["dt_bias"], prm["A_log"], prm["D"])
+        ry, _ = O.scan(*seq)
+        my, _ = O.scan(*(np.abs(v) for v in seq[:3]), *seq[3:6], np.abs(prm["D"]))
+        near(f"y of sequence {i}", y[a:b].reshape(-1, H, P), ry, my, 2.0 ** -14)
+        r, m = O.scan_bwd(*seq, g[a:b]), O.scan_bwd(*seq, g[a:b], absolute=True)
+        near(f"dx of sequence {i}", du[a:b, :d].reshape(-1, H, P), r[0], m[0], 2.0 ** -14)
+        near(f"dB of sequence {i}", du[a:b, d:d + N], r[1], m[1], 2.0 ** -14)
+        near(f"dC of sequence {i}", du[a:b, d + N:], r[2], m[2], 2.0 ** -14)
+    assert all(bool(v.isfinite().all()) for v in heads)
+
+
+@pytest.mark.parametrize("H", [2, 300])
+@pytest.mark.parametrize("where", ["behind", "sequence"])
+def test_what_is_not_a_sequences_own_stays_out(where, H):
+    """NaN in the tokens behind the last sequence reaches nothing; NaN in all of
+    one sequence reaches no output of the others' tokens."""
+    offs = [0, 65, 130, 194]
+    rng, T, prm, dev, zx, u, off, _, d, cd = _scan_case(offs, H, torch.bfloat16, 79, 0.0)
+    dy = _t(0.1 * rng.standard_normal((T, d)), torch.bfloat16)
+    du = _t(0.1 * rng.standard_normal((T, cd)), torch.bfloat16)
+    bad = slice(offs[-1], T) if where == "behind" else slice(offs[1], offs[2])
+    keep = torch.ones(T, dtype=torch.bool, device="cuda")
+    keep[offs[-1]:] = False
+    keep[bad] = False
+
+    def run(spoil):
+        v = [t.clone() for t in (zx, u, dy, du)]
+        if spoil:
+            for t in v:
+                t[bad] = float("nan")
+        z, uu, g, gu = v
+        rows, sums = [torch.zeros_like(z)], []
+        rows.append(ops.mixer_conv(z, dev["conv_w"], dev["conv_b"], off))
+        rows.append(ops.mixer_scan(uu, z, dev["dt_bias"], dev["A_log"], dev["D"], off))
+        rows.append(torch.full_like(g, 5.0))
+        ops.mixer_norm(g, z, dev["norm_w"], 0.0, rows[-1], off)
+        a, w = ops.mixer_norm_bwd(g, z, dev["norm_w"], gu[:, :d].contiguous(), rows[0], 0.0, off)
+        rows.append(a)
+        sums.append(w)
+        a, *w = ops.mixer_scan_bwd(uu, z, dev["dt_bias"], dev["A_log"], dev["D"], g, rows[0], off)
+        rows.append(a)
+        sums += w
+        sums += ops.mixer_conv_bwd(z, dev["conv_w"], dev["conv_b"], gu, rows[0], off)
+        assert bool((rows[3][offs[-1]:] == 5.0).all()) and bool((rows[0][offs[-1]:] == 0.0).all())
+        return [r[keep] for r in rows] + (sums if where == "behind" else [])
+
+    for i, (a, b) in enumerate(zip(run(False), run(True))):
+        assert bool(a.isfinite().all()) and torch.equal(a, b), i
+
+
+@pytest.mark.parametrize("H", [1, 300])
+def test_norm_of_no_rows(H):
+    """All rows behind the last sequence: nothing is written, the sums are zero."""
+    T, d = 5, 64 * H
+    rng = np.random.default_rng(H)
+    prm, dev, zx, d, cd = _layer(rng, T, H, torch.bfloat16)
+    y = _t(rng.standard_normal((T, d)), torch.bfloat16)
+    off = torch.zeros(3, dtype=torch.int32, device="cuda")
+    out, dzx = torch.full_like(y, 5.0), torch.full_like(zx, 3.0)
+    ops.mixer_norm(y, zx, dev["norm_w"], 1e-5, out, off)
+    _, dw = ops.mixer_norm_bwd(y, zx, dev["norm_w"], y, dzx, 1e-5, off)
+    assert bool((out == 5.0).all()) and bool((dzx == 3.0).all()) and bool((dw == 0.0).all())
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("T,H", [(1, 1), (3, 5), (5, 12), (4, 24), (2, 64), (2, 100), (2, 200),
                                  (3, 300)])
