@@ -20,6 +20,7 @@ constexpr int kCvCh = 8;       // channels of a thread
 constexpr int kCvBatch = 8;    // tokens whose loads are issued together
 constexpr int kCvBwdCh = 4;    // its channels a thread: with 8 the sums leave two waves a SIMD
 constexpr int kCvBwdBatch = 8;
+constexpr int kCvSimds = 1024;  // 256 CUs
 
 // grid (runs, ceil(cd / 512)), one wave each.  ring_out: not ring, or NULL
 template <bool F32>
@@ -328,8 +329,8 @@ static hipError_t conv_go(const SeqIn& in, const float* conv_w, const float* con
   typedef typename Zx<F32>::T E;
   const int cd = in.nheads * kSqP + 2 * kSqN;
   const int cblk = (cd / kCvCh + 63) / 64;
-  // runs as long as 2048 waves are left, at most 16 tokens
-  int run = (int)((int64_t)in.T * cblk / 2048);
+  // runs as long as two waves a SIMD are left, at most 16 tokens
+  int run = (int)((int64_t)in.T * cblk / (2 * kCvSimds));
   run = run < 1 ? 1 : run > 16 ? 16 : run;
   hipLaunchKernelGGL(seq_conv_kernel<F32>, dim3((unsigned)((in.T + run - 1) / run), (unsigned)cblk),
                      dim3(64), 0, stream, (const E*)in.zx, in.T, in.nheads, in.offsets, in.nseq,
@@ -355,7 +356,7 @@ hipError_t launch_seq_conv(const SeqIn& in, const float* conv_w, const float* co
 // that takes the time (1000 tokens of 64 heads: 18 us, 32 in runs of 64; 16384: 115).
 static int conv_bwd_run(int64_t T, int64_t nheads) {
   const int64_t cblk = ((nheads * kSqP + 2 * kSqN) / kCvBwdCh + 63) / 64;
-  const int64_t run = T * cblk / 3072 / 8 * 8;
+  const int64_t run = T * cblk / (3 * kCvSimds) / 8 * 8;
   return (int)(run < 8 ? 8 : run > 64 ? 64 : run);
 }
 

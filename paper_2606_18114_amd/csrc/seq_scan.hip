@@ -19,7 +19,7 @@
 // Why tiles of 64 and four waves: two workgroups fit a CU (69 KiB of LDS, mostly
 // the state's terms, which every wave reads), so that one computes while the
 // other waits; 128 tokens and eight waves would leave one, and more of g that is
-// thrown away.  No single thing bounds it: of 175 us for 16384 tokens of 64 heads
+// thrown away.  No single thing bounds it: of 180 us for 16384 tokens of 64 heads
 // in eight sequences (3.3 times the 53 us of reading u and writing y) the matrix
 // products busy the SIMDs 30 us, the vector instructions 80, LDS 85, and what
 // they wait for each other in a tile's chain is the rest.
@@ -104,7 +104,7 @@ __device__ __forceinline__ void state_add(f32x4 (&S)[2][4], const uint8_t* m, co
 // tiles backward: the gradient with respect to the state before the segment;
 // not for the first segment.  grid: scan_grid, 256 threads.
 template <bool F32, bool REV, int NT>
-__global__ __launch_bounds__(256, 2) void scan_state_kernel(
+__global__ __launch_bounds__(256, 4) void scan_state_kernel(
     const typename Zx<F32>::T* __restrict__ zx, const uint16_t* __restrict__ u,
     const uint16_t* __restrict__ dy, int T, int nheads, const int* __restrict__ off, int nseq,
     int segT, const float* __restrict__ dt_bias, const float* __restrict__ A_log,
@@ -567,7 +567,7 @@ static hipError_t scan_pass_go(const SeqIn& in, int segT, float* state, const fl
   return hipGetLastError();
 }
 
-// Every chunk by itself, then one launch that adds them up (96 + 78 us at 16384
+// Every chunk by itself, then one launch that adds them up (102 + 77 us at 16384
 // tokens of 64 heads, by the memory's rate; workgroups that walk through the
 // sequences and write each state once took 190, too few loads in flight).
 template <bool F32, bool REV>

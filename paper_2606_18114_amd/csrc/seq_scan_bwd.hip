@@ -29,8 +29,8 @@
 // are made in both orientations, so that the lanes of a product hold what the
 // next one takes of it.  scan_bwd_fin_kernel makes dt's gradient of the sums above.
 //
-// 16384 tokens of 64 heads, eight sequences: states 96 + 78 us each way (0.94 GB
-// written, read and written again), off 315 (1.1 to 1.4 GB), to 175, from 265
+// 16384 tokens of 64 heads, eight sequences: states 102 + 77 us each way (0.94 GB
+// written, read and written again), off 325 (1.1 to 1.4 GB), to 180, from 270
 // (0.7 GB), bc 37, fin 21.  The float32 states of the chunks, half a gigabyte, are
 // most of the traffic; shorter ones would be more of it, longer ones more work
 // inside the chunk, which grows with its length.

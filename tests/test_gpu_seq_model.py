@@ -123,17 +123,15 @@ def test_mixer_module_repeats_its_bits_and_skips_unneeded_gradients():
 
 
 def test_a_second_derivative_is_refused():
-    m = Mamba2Mixer(1, device="cuda")
+    m, e = Mamba2Mixer(1, device="cuda"), Embedding(5, 8, device="cuda")
     zx = torch.randn((3, 385), device="cuda", requires_grad=True)
-    (g,) = torch.autograd.grad(m(zx).float().sum(), zx, create_graph=True)
-    with pytest.raises(RuntimeError, match="once_differentiable"):
-        g.sum().backward()
-    e = Embedding(5, 8, device="cuda")
     ids = torch.tensor([1, 7, 1], device="cuda")
-    w = torch.ones((3, 8), device="cuda", requires_grad=True)
-    (g,) = torch.autograd.grad((e(ids) * w).sum(), e.weight, create_graph=True)
-    with pytest.raises(RuntimeError, match="once_differentiable"):
-        g.sum().backward()
+    for f, leaf in ((lambda: m(zx).float(), zx), (lambda: e(ids), e.weight)):
+        out = f()
+        w = torch.ones_like(out, requires_grad=True)
+        (g,) = torch.autograd.grad((out * w).sum(), leaf, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            g.sum().backward()
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, BF])
