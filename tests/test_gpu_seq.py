@@ -266,6 +266,22 @@ def test_scan_bwd(offs, H, dtype, dt_shift):
     assert bool((du[offs[-1]:] == 7.0).all())
 
 
+@pytest.mark.parametrize("T", [1, 100, 128])
+def test_scan_bwd_of_one_chunk(T):
+    """Up to 128 tokens there are no states between chunks; the same tokens in a
+    longer batch give the same bits."""
+    rng, n, prm, dev, zx, u, off, _, d, cd = _scan_case([0, T, T + 130], 1, torch.float32, T, 0.0)
+    dy = _t(0.1 * rng.standard_normal((n, d)), torch.bfloat16)
+    par = (dev["dt_bias"], dev["A_log"], dev["D"])
+    dzx, short = torch.zeros_like(zx), torch.zeros_like(zx[:T])
+    du, *_ = ops.mixer_scan_bwd(u, zx, *par, dy, dzx, off)
+    got, *heads = ops.mixer_scan_bwd(u[:T], zx[:T], *par, dy[:T], short)
+    assert torch.equal(got, du[:T]) and torch.equal(short, dzx[:T])
+    alone = torch.tensor([0, T, T], dtype=torch.int32, device="cuda")
+    _, *same = ops.mixer_scan_bwd(u, zx, *par, dy, dzx, alone)
+    assert all(torch.equal(a, b) for a, b in zip(heads, same))
+
+
 def test_scan_outlier_steps():
     """Single tokens whose step is so long that the state before them is gone
     (exponents of millions): the decays among the tokens behind them keep their
