@@ -141,7 +141,8 @@ tm_status tm_embed(const void* ids, int32_t ids_i64, int64_t T, const void* weig
 /*
  * tm_embed_bwd — the gradient of its weight: dW[v] = scale * the sum of dout[t]
  * over the tokens t with id v, in ascending order of t (in float32; beyond 64
- * tokens, sums of 64 each are added up); accumulate 1: dW += that.
+ * tokens, sums of 64 each are added up, to 4096 tokens of a batch in float32, in
+ * longer ones in float64); accumulate 1: dW += that.
  *   dout float32 [T, D], dW float32 [V, D] (4-byte aligned)
  */
 tm_status tm_embed_bwd(const void* ids, int32_t ids_i64, int64_t T, const float* dout, int64_t V,

@@ -4,14 +4,19 @@
 // bits.  An id outside [0, V) gives a row of zeros and no gradient.
 //
 // The gradient is bound by writing dW's V rows.  Few tokens are found by going
-// through the ids (embed_direct_kernel, embed_first_kernel).  Many are sorted by id
+// through the ids (embed_direct_kernel, embed_first_kernel).  More are sorted by id
 // into segments: a count per id, a place per segment (whichever: only the order
 // inside a segment shows in the sums), and the positions, in any order, which the
 // workgroup of a row brings into ascending order.  An id of more than
 // kEmPiece tokens (the most frequent one of a text is a tenth of it) is cut
-// into pieces of that many, whose sums meet in the row's workgroup; a piece
-// finds its tokens by going through the ids, which are few bytes.  16384 tokens,
+// into pieces of that many, whose sums meet, in float64, in the row's workgroup; a
+// piece finds its tokens by going through the ids, which are few bytes.  16384 tokens,
 // 50000 ids of 2048 columns: 149 us, 100 of them for the rows (4.8 TB/s).
+//
+// That search grows with the square of the tokens: above kEmSearch of them the sort
+// is a stable one by digits of the id (embed_digit_*), which leaves every
+// segment ascending, so that a piece takes its tokens from where they lie, and 64
+// pieces' sums are added up by a workgroup of their own (embed_fold_kernel).
 #include "seq.hpp"
 #include "seq_launch.hpp"
 
@@ -25,6 +30,14 @@ constexpr int kEmDirect = 256, kEmDirectV = 16384;
 // than T workgroups that each read T ids (4000 tokens, 10000 ids of 1024: 29 us, 37
 // sorted).
 constexpr int kEmScan = 4096;
+// Tokens up to which pieces search for their own.  98304 tokens of 50000 ids of 2048
+// columns, as a text has them: 349 us so, 334 with the sort by digits; all of one id
+// 648, 342; hardly any twice 260, 279.  65536: 252, 276; 448, 275; 209, 231.  2^20
+// of 512 columns: 15.4 ms, 0.54; 18.3, 0.56; 0.57, 0.52.
+constexpr int64_t kEmSearch = 98304;
+constexpr int kEmDigit = 8;         // bits of a digit
+constexpr int kEmBlock = 4096;      // tokens of a workgroup that places them
+constexpr int kEmTotals = 3 << kEmDigit;  // of the digits of the (at most 3) passes
 
 template <typename I>
 __device__ __forceinline__ int64_t em_id(const I* ids, int64_t t, int64_t V) {
@@ -77,29 +90,43 @@ __global__ __launch_bounds__(256) void embed_kernel(const I* __restrict__ ids, i
 }
 
 // the workspace: count, place (the first piece's number where an id is in
-// pieces), filled [V] each; cursors [2] (of tokens, of pieces); sorted [T]; a
-// piece's id and its number in its row [pieces] each; pieces' sums [pieces][D]
+// pieces), filled (sorted by digits: where its segment begins) [V] each; cursors
+// [2] (of tokens, of pieces); sorted [T]; a piece's id and its number in its row
+// [pieces] each; pieces' sums [pieces][D].  Sorted by digits also: the other
+// positions and two arrays of ids [T] each, digits' counts [passes][2^kEmDigit], and of
+// a pass by block [2^kEmDigit][blocks]
 struct EmbedWs {
-  int *count, *place, *filled, *cursor, *sorted, *pid, *pno;
+  int *count, *place, *filled, *cursor, *sorted, *pid, *pno, *other, *key[2], *total, *digits;
   float* psum;
+  int fold;  // sums that a piece's stands for in a row of more pieces than that
 };
 static int64_t em_pieces(int64_t T) { return 2 * (T / kEmPiece) + 1; }
+static int64_t em_blocks(int64_t T) { return (T + kEmBlock - 1) / kEmBlock; }
 static int64_t em_ints(int64_t T, int64_t V) {
-  return (3 * V + 2 + T + 2 * em_pieces(T) + 63) / 64 * 64;
+  const int64_t n = 3 * V + 2 + T + 2 * em_pieces(T) +
+                    (T > kEmSearch ? 3 * T + kEmTotals + (em_blocks(T) << kEmDigit) : 0);
+  return (n + 63) / 64 * 64;
 }
 static EmbedWs em_ws(void* p, int64_t T, int64_t V) {
-  EmbedWs w;
+  EmbedWs w = {};
   int* i = (int*)p;
   w.count = i, w.place = i + V, w.filled = i + 2 * V, w.cursor = i + 3 * V;
   w.sorted = w.cursor + 2;
   w.pid = w.sorted + T;
   w.pno = w.pid + em_pieces(T);
+  w.fold = 1;
+  if (T > kEmSearch) {
+    w.other = w.pno + em_pieces(T);
+    w.key[0] = w.other + T, w.key[1] = w.key[0] + T;
+    w.total = w.key[1] + T;
+    w.digits = w.total + kEmTotals;
+    w.fold = kEmPiece;
+  }
   w.psum = (float*)(i + em_ints(T, V));
   return w;
 }
 int64_t embed_bwd_bytes(int64_t T, int64_t V, int64_t D) {
-  if (T <= kEmScan) return 0;
-  return em_ints(T, V) * 4 + em_pieces(T) * D * 4;
+  return T <= kEmScan ? 0 : em_ints(T, V) * 4 + em_pieces(T) * D * 4;
 }
 
 __global__ __launch_bounds__(256) void embed_clear_kernel(EmbedWs w, int64_t V) {
@@ -384,6 +411,214 @@ __global__ __launch_bounds__(1024) void embed_first_kernel(const I* __restrict__
   }
 }
 
+// ---- more than kEmSearch tokens: a stable sort by the ids' digits --------------
+// A pass: the digits' counts of every block of kEmBlock tokens, the places that
+// follow from them (digit by digit, block by block), and the tokens to their
+// places.  An id without a row is sorted as V, behind the others.
+
+__global__ __launch_bounds__(256) void embed_digit_clear_kernel(EmbedWs w, int64_t V,
+                                                                int64_t pieces) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < V) w.filled[i] = w.place[i] = 0;
+  if (i < pieces) w.pid[i] = -1;
+  if (i < kEmTotals) w.total[i] = 0;
+}
+
+// FIRST: of the ids; else of key, with positions pos
+template <typename I, bool FIRST>
+__device__ __forceinline__ int em_key(const I* __restrict__ ids, const int* __restrict__ key,
+                                      int64_t t, int64_t V) {
+  if constexpr (FIRST) {
+    const int64_t v = em_id(ids, t, V);
+    return (int)(v < 0 ? V : v);
+  } else {
+    return key[t];
+  }
+}
+
+// grid (blocks), 1024 threads
+template <typename I, bool FIRST>
+__global__ __launch_bounds__(1024) void embed_digit_count_kernel(
+    const I* __restrict__ ids, const int* __restrict__ key, int64_t T, int64_t V, int shift,
+    int* __restrict__ digits, int* __restrict__ total) {
+  __shared__ int cnt[1 << kEmDigit];
+  const int tid = threadIdx.x;
+  if (tid < 1 << kEmDigit) cnt[tid] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < kEmBlock / 1024; ++q) {
+    const int64_t t = (int64_t)blockIdx.x * kEmBlock + q * 1024 + tid;
+    if (t < T)
+      atomicAdd(&cnt[em_key<I, FIRST>(ids, key, t, V) >> shift & ((1 << kEmDigit) - 1)], 1);
+  }
+  __syncthreads();
+  if (tid < 1 << kEmDigit) {
+    digits[(int64_t)tid * gridDim.x + blockIdx.x] = cnt[tid];
+    if (cnt[tid]) atomicAdd(&total[tid], cnt[tid]);
+  }
+}
+
+// Places, in place: a digit's workgroup adds up what lies before it, all of the lower
+// digits (total) and the blocks before.  grid (2^kEmDigit), 256 threads, each of which
+// takes blocks / 256 of them in a row
+__global__ __launch_bounds__(256) void embed_digit_scan_kernel(int* __restrict__ digits,
+                                                               const int* __restrict__ total,
+                                                               int blocks) {
+  __shared__ int sum[256];
+  const int i = threadIdx.x, per = (blocks + 255) / 256;
+  const int lo = min(blocks, i * per), hi = min(blocks, lo + per);
+  int* row = digits + (int64_t)blockIdx.x * blocks;
+  auto sums = [&](int a) {  // up to this thread's and with it
+    sum[i] = a;
+    for (int o = 1; o < 256; o <<= 1) {
+      __syncthreads();
+      const int p = i >= o ? sum[i - o] : 0;
+      __syncthreads();
+      sum[i] = a += p;
+    }
+    __syncthreads();
+    return a;
+  };
+  sums(i < (int)blockIdx.x ? total[i] : 0);
+  const int below = sum[255];
+  __syncthreads();
+  int own = 0;
+  for (int k = lo; k < hi; ++k) own += row[k];
+  int a = below + sums(own) - own;
+  for (int k = lo; k < hi; ++k) {
+    const int d = row[k];
+    row[k] = a;
+    a += d;
+  }
+}
+
+// grid (blocks), 1024 threads: a wave takes kEmBlock / 16 tokens in a row, 64 at a
+// time.  A token's place: its digit's in the block, the waves before, the wave's
+// earlier ones (cnt so far), the lanes below with the same digit.
+template <typename I, bool FIRST>
+__global__ __launch_bounds__(1024) void embed_digit_place_kernel(
+    const I* __restrict__ ids, const int* __restrict__ key, const int* __restrict__ pos, int64_t T,
+    int64_t V, int shift, const int* __restrict__ digits, int* __restrict__ key_out,
+    int* __restrict__ pos_out) {
+  constexpr int kPer = kEmBlock / 1024, kDig = 1 << kEmDigit;
+  __shared__ int cnt[16][kDig];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int k = tid; k < 16 * kDig; k += 1024) cnt[k / kDig][k % kDig] = 0;
+  int v[kPer], at[kPer];
+  bool in[kPer];
+  const int64_t t0 = (int64_t)blockIdx.x * kEmBlock + wave * 64 * kPer + lane;
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    const int64_t t = t0 + 64 * q;
+    in[q] = t < T;
+    v[q] = em_key<I, FIRST>(ids, key, t < T ? t : T - 1, V);
+  }
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    __syncthreads();  // cnt is clear; the step before has been counted
+    const int dig = v[q] >> shift & (kDig - 1);
+    uint64_t same = __ballot(in[q]);
+#pragma unroll
+    for (int b = 0; b < kEmDigit; ++b) {
+      const uint64_t set = __ballot(dig >> b & 1);
+      same &= dig >> b & 1 ? set : ~set;
+    }
+    at[q] = cnt[wave][dig] + __popcll(same & ((1ull << lane) - 1));
+    __syncthreads();
+    if (in[q] && lane == __builtin_ctzll(same)) cnt[wave][dig] += __popcll(same);
+  }
+  __syncthreads();
+  if (tid < kDig) {  // what lies before every wave's
+    int a = digits[(int64_t)tid * gridDim.x + blockIdx.x];
+    for (int k = 0; k < 16; ++k) {
+      const int n = cnt[k][tid];
+      cnt[k][tid] = a;
+      a += n;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    if (!in[q]) continue;
+    const int p = cnt[wave][v[q] >> shift & (kDig - 1)] + at[q];
+    key_out[p] = v[q];
+    pos_out[p] = FIRST ? (int)(t0 + 64 * q) : pos[t0 + 64 * q];
+  }
+}
+
+// where the segments begin (filled) and end (place)
+__global__ __launch_bounds__(256) void embed_digit_ends_kernel(const int* __restrict__ key,
+                                                               int64_t T, int64_t V, EmbedWs w) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= T) return;
+  const int v = key[i];
+  if (v >= V) return;
+  if (i == 0 || key[i - 1] != v) w.filled[v] = (int)i;
+  if (i == T - 1 || key[i + 1] != v) w.place[v] = (int)i + 1;
+}
+
+// A segment's count and place.  Pieces: from number 2 (begin / kEmPiece) on.  One
+// of n > kEmPiece tokens has np >= 2 of them; the next one begins n > kEmPiece (np -
+// 1) tokens later, so at a number higher by 2 (np - 1) >= np; the last number is at most
+// 2 (T / kEmPiece).
+__global__ __launch_bounds__(256) void embed_digit_rows_kernel(int64_t V, EmbedWs w) {
+  const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (v >= V) return;
+  const int begin = w.filled[v], n = w.place[v] - begin;
+  w.count[v] = n;
+  w.place[v] = n > kEmPiece ? 2 * (begin / kEmPiece) : begin;
+}
+
+// which pieces there are
+__global__ __launch_bounds__(256) void embed_digit_pieces_kernel(const int* __restrict__ key,
+                                                                 int64_t T, int64_t V, EmbedWs w) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= T) return;
+  const int v = key[i];
+  if (v >= V || w.count[v] <= kEmPiece) return;
+  const int k = (int)i - w.filled[v];
+  if (k % kEmPiece) return;
+  const int p = w.place[v] + k / kEmPiece;
+  w.pid[p] = v, w.pno[p] = k / kEmPiece;
+}
+
+// grid (pieces at most), 256 threads: a piece's sum
+__global__ __launch_bounds__(256) void embed_digit_sum_kernel(const float* __restrict__ de,
+                                                              int64_t D, EmbedWs w) {
+  __shared__ int list[kEmPiece];
+  const int v = w.pid[blockIdx.x];
+  if (v < 0) return;
+  const int lo = w.pno[blockIdx.x] * kEmPiece, n = min(kEmPiece, w.count[v] - lo);
+  if ((int)threadIdx.x < n) list[threadIdx.x] = w.sorted[w.filled[v] + lo + threadIdx.x];
+  __syncthreads();
+  float* o = w.psum + (int64_t)blockIdx.x * D;
+  const int64_t D4 = D & ~(int64_t)3;
+  for (int64_t c = (int64_t)threadIdx.x * 4; c < D4; c += 1024)
+    *(f32x4_u4*)(o + c) = em_sum4(de, D, list, n, c);
+  for (int64_t c = D4 + threadIdx.x; c < D; c += 256) {
+    float s = 0.f;
+    for (int k = 0; k < n; ++k) s += de[(int64_t)list[k] * D + c];
+    o[c] = s;
+  }
+}
+
+// grid (pieces at most), 256 threads: where a row has more than kEmPiece pieces, the
+// sums of as many into the first one's
+__global__ __launch_bounds__(256) void embed_fold_kernel(int64_t D, EmbedWs w) {
+  const int v = w.pid[blockIdx.x];
+  if (v < 0) return;
+  const int k = w.pno[blockIdx.x], np = (w.count[v] + kEmPiece - 1) / kEmPiece;
+  if (k % kEmPiece || np <= kEmPiece) return;
+  const int n = min(kEmPiece, np - k);
+  float* o = w.psum + (int64_t)blockIdx.x * D;
+  for (int64_t c = threadIdx.x; c < D; c += 256) {
+    double a = 0.0;
+#pragma unroll 16
+    for (int q = 0; q < n; ++q) a += (double)o[q * D + c];
+    o[c] = (float)a;
+  }
+}
+
 // grid (V): row v, zeros where no token has it
 template <bool ACC>
 __global__ __launch_bounds__(256) void embed_row_kernel(const float* __restrict__ de, int64_t D,
@@ -394,9 +629,11 @@ __global__ __launch_bounds__(256) void embed_row_kernel(const float* __restrict_
   int n = w.count[v];
   if (ACC && n == 0) return;
   const float* src = de;
+  int64_t step = D;
   if (n > kEmPiece) {  // the pieces' sums instead of tokens
     src = w.psum + (int64_t)w.place[v] * D;
     n = (n + kEmPiece - 1) / kEmPiece;
+    if (w.fold > 1 && n > w.fold) n = (n + w.fold - 1) / w.fold, step = w.fold * D;
   } else if (n > 0) {
     // the tokens in ascending order: each goes where as many are smaller
     const int i = threadIdx.x;
@@ -415,9 +652,14 @@ __global__ __launch_bounds__(256) void embed_row_kernel(const float* __restrict_
   for (int64_t c = (int64_t)threadIdx.x * 4; c < D4; c += 1024) {
     f32x4 s;
     if (pieces) {
-      s = f32x4{0.f, 0.f, 0.f, 0.f};
+      double a[4] = {0.0, 0.0, 0.0, 0.0};  // (thousands of them in a long batch)
 #pragma unroll 8
-      for (int k = 0; k < n; ++k) s += *(const f32x4_u4*)(src + (int64_t)k * D + c);
+      for (int k = 0; k < n; ++k) {
+        const f32x4 x = *(const f32x4_u4*)(src + k * step + c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] += (double)x[i];
+      }
+      s = f32x4{(float)a[0], (float)a[1], (float)a[2], (float)a[3]};
     } else {
       s = em_sum4(src, D, list, n, c);
     }
@@ -427,7 +669,13 @@ __global__ __launch_bounds__(256) void embed_row_kernel(const float* __restrict_
   }
   for (int64_t c = D4 + threadIdx.x; c < D; c += 256) {
     float s = 0.f;
-    for (int k = 0; k < n; ++k) s += src[(int64_t)(pieces ? k : list[k]) * D + c];
+    if (pieces) {
+      double a = 0.0;
+      for (int k = 0; k < n; ++k) a += (double)src[k * step + c];
+      s = (float)a;
+    } else {
+      for (int k = 0; k < n; ++k) s += src[(int64_t)list[k] * D + c];
+    }
     o[c] = ACC ? o[c] + s * scale : s * scale;
   }
 }
@@ -449,6 +697,54 @@ hipError_t launch_embed(const void* ids, bool ids64, int64_t T, const void* weig
   else if (type == 1) embed_go<1>(ids, ids64, T, weight, V, D, scale, out, stream);
   else embed_go<2>(ids, ids64, T, weight, V, D, scale, out, stream);
   return hipGetLastError();
+}
+
+static hipError_t embed_rows(const float* de, int64_t V, int64_t D, float scale, float* dW,
+                             bool accumulate, const EmbedWs& w, hipStream_t stream) {
+  if (accumulate)
+    hipLaunchKernelGGL(embed_row_kernel<true>, dim3((unsigned)V), dim3(256), 0, stream, de, D,
+                       scale, dW, w);
+  else
+    hipLaunchKernelGGL(embed_row_kernel<false>, dim3((unsigned)V), dim3(256), 0, stream, de, D,
+                       scale, dW, w);
+  return hipGetLastError();
+}
+
+// the positions by id (w.sorted), the rows' counts and places, and their pieces
+template <typename I>
+static void embed_digits(const I* ids, int64_t T, int64_t V, EmbedWs& w, hipStream_t stream) {
+  const int64_t pieces = em_pieces(T), most = V > pieces ? V : pieces;
+  const unsigned blocks = (unsigned)em_blocks(T), tb = (unsigned)((T + 255) / 256);
+  hipLaunchKernelGGL(embed_digit_clear_kernel, dim3((unsigned)((most + 255) / 256)), dim3(256), 0,
+                     stream, w, V, pieces);
+  int* pos[2] = {w.sorted, w.other};
+  int in = 1;
+  for (int shift = 0; V >> shift != 0; shift += kEmDigit, in ^= 1) {
+    const int *k = w.key[in], *p = pos[in];
+    int *ko = w.key[in ^ 1], *po = pos[in ^ 1], *total = w.total + (shift / kEmDigit << kEmDigit);
+    if (shift == 0) {
+      hipLaunchKernelGGL((embed_digit_count_kernel<I, true>), dim3(blocks), dim3(1024), 0, stream,
+                         ids, k, T, V, shift, w.digits, total);
+    } else {
+      hipLaunchKernelGGL((embed_digit_count_kernel<I, false>), dim3(blocks), dim3(1024), 0, stream,
+                         ids, k, T, V, shift, w.digits, total);
+    }
+    hipLaunchKernelGGL(embed_digit_scan_kernel, dim3(1 << kEmDigit), dim3(256), 0, stream,
+                       w.digits, total, (int)blocks);
+    if (shift == 0) {
+      hipLaunchKernelGGL((embed_digit_place_kernel<I, true>), dim3(blocks), dim3(1024), 0, stream,
+                         ids, k, p, T, V, shift, w.digits, ko, po);
+    } else {
+      hipLaunchKernelGGL((embed_digit_place_kernel<I, false>), dim3(blocks), dim3(1024), 0, stream,
+                         ids, k, p, T, V, shift, w.digits, ko, po);
+    }
+  }
+  w.sorted = pos[in];
+  const int* key = w.key[in];
+  hipLaunchKernelGGL(embed_digit_ends_kernel, dim3(tb), dim3(256), 0, stream, key, T, V, w);
+  hipLaunchKernelGGL(embed_digit_rows_kernel, dim3((unsigned)((V + 255) / 256)), dim3(256), 0,
+                     stream, V, w);
+  hipLaunchKernelGGL(embed_digit_pieces_kernel, dim3(tb), dim3(256), 0, stream, key, T, V, w);
 }
 
 template <typename I>
@@ -481,8 +777,15 @@ static hipError_t embed_bwd_go(const I* ids, int64_t T, const float* de, int64_t
     }
     return hipGetLastError();
   }
-  const EmbedWs w = em_ws(workspace, T, V);
+  EmbedWs w = em_ws(workspace, T, V);
   const unsigned vb = (unsigned)((V + 255) / 256), tb = (unsigned)((T + 255) / 256);
+  const unsigned pieces = (unsigned)em_pieces(T);
+  if (T > kEmSearch) {
+    embed_digits(ids, T, V, w, stream);
+    hipLaunchKernelGGL(embed_digit_sum_kernel, dim3(pieces), dim3(256), 0, stream, de, D, w);
+    hipLaunchKernelGGL(embed_fold_kernel, dim3(pieces), dim3(256), 0, stream, D, w);
+    return embed_rows(de, V, D, scale, dW, accumulate, w, stream);
+  }
   hipLaunchKernelGGL(embed_clear_kernel, dim3(vb), dim3(256), 0, stream, w, V);
   if (V <= kEmCountV)
     hipLaunchKernelGGL(embed_count_lds_kernel<I>, dim3((unsigned)((T + 1023) / 1024)), dim3(1024),
@@ -491,15 +794,8 @@ static hipError_t embed_bwd_go(const I* ids, int64_t T, const float* de, int64_t
     hipLaunchKernelGGL(embed_count_kernel<I>, dim3(tb), dim3(256), 0, stream, ids, T, V, w);
   hipLaunchKernelGGL(embed_place_kernel, dim3(vb), dim3(256), 0, stream, V, w);
   hipLaunchKernelGGL(embed_sort_kernel<I>, dim3(tb), dim3(256), 0, stream, ids, T, V, w);
-  hipLaunchKernelGGL(embed_piece_kernel<I>, dim3((unsigned)em_pieces(T)), dim3(1024), 0, stream,
-                     ids, T, de, D, w);
-  if (accumulate)
-    hipLaunchKernelGGL(embed_row_kernel<true>, dim3((unsigned)V), dim3(256), 0, stream, de, D,
-                       scale, dW, w);
-  else
-    hipLaunchKernelGGL(embed_row_kernel<false>, dim3((unsigned)V), dim3(256), 0, stream, de, D,
-                       scale, dW, w);
-  return hipGetLastError();
+  hipLaunchKernelGGL(embed_piece_kernel<I>, dim3(pieces), dim3(1024), 0, stream, ids, T, de, D, w);
+  return embed_rows(de, V, D, scale, dW, accumulate, w, stream);
 }
 
 hipError_t launch_embed_bwd(const void* ids, bool ids64, int64_t T, const float* dout, int64_t V,

@@ -174,6 +174,36 @@ def test_embed_bwd_wide(kind, D, accumulate):
     near("dW", dW, ref, O.embed_bwd(ids, np.abs(_np(de)), V, 0.5) + add, 2.0 ** -17)
 
 
+# more tokens than pieces search through: sorted by one, two and three digits of the
+# id, at the digits' borders; pieces that are folded.  Equal rows make the roundings
+# of a chain of additions add up: the longest one, 64 tokens, with the roundings of
+# the sums that are added in float64, the scale and the first value is below 2^-17
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("ids_dtype", [torch.int32, torch.int64])
+@pytest.mark.parametrize("kind", ["one id", "uniform", "text", "wide", 255, 256, 65535, 65536])
+def test_embed_bwd_of_many_tokens(kind, ids_dtype, accumulate):
+    rng = np.random.default_rng(6)
+    T, V, D = {"one id": ((1 << 20) + 37, 5, 4), "uniform": (200003, 3000, 6),
+               "text": (98305, 20000, 33), "wide": (99001, 300000, 1)}.get(kind, (100000, kind, 3))
+    if kind == "one id":
+        ids, de = np.full(T, 2), torch.full((T, D), 0.1, device="cuda")
+    else:
+        ids = (rng.integers(-1, V + 1, T) if kind != "text"
+               else np.minimum(np.exp(rng.uniform(0, np.log(V), T)).astype(np.int64), V))
+        ids[:2] = 0, V - 1
+        de = _t(rng.standard_normal((T, D)))
+    t = torch.from_numpy(ids).to(ids_dtype).cuda()
+
+    def run():
+        base = torch.ones((V, D), device="cuda") if accumulate else None
+        return ops.embed_bwd(t, de, V, 0.5, dW=base, accumulate=accumulate)
+
+    dW, add = run(), 1.0 if accumulate else 0.0
+    near("dW", dW, O.embed_bwd(ids, _np(de), V, 0.5) + add,
+         O.embed_bwd(ids, np.abs(_np(de)), V, 0.5) + add, 2.0 ** -17)
+    assert torch.equal(dW, run()), "repeated calls differ"
+
+
 def test_gradients_of_steps_that_end_every_state():
     """No gradient reaches a step through a state that is over: dt's is that of
     the token's own input, A_log's is zero, whatever the rate."""
