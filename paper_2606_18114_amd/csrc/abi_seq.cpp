@@ -131,7 +131,7 @@ tm_status tm_mixer_conv_bwd(const void* zxbcdt, int32_t z_f32, int64_t T, int32_
 
 int64_t tm_mixer_scan_workspace(int64_t T, int32_t nseq, int32_t nheads) {
   Sizes s;
-  return seq_sizes(T, nseq, nheads, 1, &s) ? tmk::seq_scan_bytes(T, nseq, nheads) : -1;
+  return seq_sizes(T, nseq, nheads, 1, &s) ? tmk::seq_scan_bytes(T, nheads) : -1;
 }
 
 tm_status tm_mixer_scan(const uint16_t* u, const void* zxbcdt, int32_t z_f32, int64_t T,
@@ -142,7 +142,7 @@ tm_status tm_mixer_scan(const uint16_t* u, const void* zxbcdt, int32_t z_f32, in
   Sizes s;
   if (!u || !dt_bias || !A_log || !D || !y) return TM_EINVAL;
   if (tm_status st = in_checked(zxbcdt, z_f32, T, nseq, nheads, offsets, &s)) return st;
-  const int64_t need = tmk::seq_scan_bytes(T, nseq, nheads);
+  const int64_t need = tmk::seq_scan_bytes(T, nheads);
   if (tm_status st = ws_checked(workspace, workspace_bytes, need)) return st;
   if (!all_aligned({dt_bias, A_log, D}, 4) || !all_aligned({u, y, ssm_in, ssm_out}, 16))
     return TM_EALIGN;

@@ -30,12 +30,13 @@ hipError_t launch_seq_norm_bwd(const SeqIn& in, const uint16_t* y, const float* 
                                const uint16_t* dout, void* dzx, uint16_t* dy, float* dnorm_w,
                                void* workspace, hipStream_t stream);
 
-int64_t seq_scan_bytes(int64_t T, int64_t nseq, int64_t nheads);
+int64_t seq_scan_bytes(int64_t T, int64_t nheads);
 hipError_t launch_seq_scan(const SeqIn& in, const uint16_t* u, const float* dt_bias,
                            const float* A_log, const float* D, const uint16_t* ssm_in,
                            uint16_t* ssm_out, uint16_t* y, void* workspace, hipStream_t stream);
-// float32 states (rev: gradients) that enter the chunks of the backward pass: state
-// [slots][nheads][64 * 128], with scratch decay [slots][nheads] (seq_scan_dev.hpp)
+// float32 states behind the chunks of the backward pass that another one follows
+// (rev: their gradients): state [T / 128 + 1][nheads][64 * 128], with scratch decay
+// [T / 128 + 1][nheads] (places: seq_scan_dev.hpp)
 hipError_t launch_chunk_states(const SeqIn& in, const uint16_t* u, const uint16_t* dy, bool rev,
                                const float* dt_bias, const float* A_log, float* state,
                                float* decay, hipStream_t stream);

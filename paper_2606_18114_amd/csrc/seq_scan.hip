@@ -13,8 +13,7 @@
 // Where there are too few sequences and heads to fill the chip, a sequence is
 // cut into segments: scan_state_kernel makes each segment's own state,
 // scan_pass_kernel (or the segments' workgroups themselves, where those are few)
-// the states that enter the segments, then scan_y_kernel walks all segments at
-// once.
+// the states between the segments, then scan_y_kernel walks all segments at once.
 //
 // Why tiles of 64 and four waves: two workgroups fit a CU (69 KiB of LDS, mostly
 // the state's terms, which every wave reads), so that one computes while the
@@ -99,10 +98,11 @@ __device__ __forceinline__ void state_add(f32x4 (&S)[2][4], const uint8_t* m, co
 
 // ---- a segment's own state -------------------------------------------------
 // REV false: vec = x, mat = B, coefficient e^{c_Q - c_s} dt'_s, tiles forward:
-// the state at the segment's end from the segment alone; its sequence's last
-// segment has no use for it.  REV true: vec = dy, mat = C, coefficient e^{c_t},
-// tiles backward: the gradient with respect to the state before the segment;
-// not for the first segment.  grid: scan_grid, 256 threads.
+// the state at the segment's end from the segment alone, at its place; its
+// sequence's last segment has no use for it.  REV true: vec = dy, mat = C,
+// coefficient e^{c_t}, tiles backward: the gradient with respect to the state before
+// the segment, at the place of the one before; not for the first segment.  grid:
+// scan_grid, 256 threads.
 template <bool F32, bool REV, int NT>
 __global__ __launch_bounds__(256, 4) void scan_state_kernel(
     const typename Zx<F32>::T* __restrict__ zx, const uint16_t* __restrict__ u,
@@ -172,60 +172,71 @@ __global__ __launch_bounds__(256, 4) void scan_state_kernel(
     state_add<NT>(S, m, v, coef);
     __syncthreads();
   }
-  float* o = state + ((int64_t)sl * nheads + h) * kScState + (lane & 15) * kSqN + 32 * wave +
-             4 * (lane >> 4);
+  const int64_t at = (int64_t)(sl - s.i - (REV ? 1 : 0)) * nheads + h;
+  float* o = state + at * kScState + (lane & 15) * kSqN + 32 * wave + 4 * (lane >> 4);
 #pragma unroll
   for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
     for (int pb = 0; pb < 4; ++pb) *(f32x4*)(o + 16 * pb * kSqN + 16 * nb) = S[nb][pb];
-  if (threadIdx.x == 0) decay[(int64_t)sl * nheads + h] = dec;
+  if (threadIdx.x == 0) decay[at] = dec;
 }
 
-// ---- the states that enter the segments, in place of the segments' own -----
-// grid (kScState / 1024, nheads, nseq), 256 threads, 4 values each.  REV false:
-// E_0 = the initial state, E_{k+1} = decay_k E_k + own_k; true: from the last
-// segment down, E_last = 0.
+// ---- the states between the segments, in place of the segments' own ---------
+// grid (kScState / 1024, nheads, nseq), 256 threads, 4 values each.  REV false: at a
+// segment's place, the state behind it, from init on; true: the gradient of that
+// state, from zero behind the last segment.  first: receives init of sequences of
+// more than one segment, at the first one's place (float16), or NULL.
 template <bool REV>
 __global__ __launch_bounds__(256) void scan_pass_kernel(float* __restrict__ state,
                                                         const float* __restrict__ decay, int T,
                                                         int nheads, const int* __restrict__ off,
                                                         int segT,
-                                                        const uint16_t* __restrict__ init) {
+                                                        const uint16_t* __restrict__ init,
+                                                        uint16_t* __restrict__ first) {
   const int h = blockIdx.y, i = blockIdx.z;
   const int st = off ? slot_off(off, T, i) : 0, en = off ? slot_off(off, T, i + 1) : T;
   const int nk = en > st ? (en - st + segT - 1) / segT : 0;
-  if (nk == 0) return;
-  const int64_t base = st / segT + i;
+  if (nk <= 1) return;
+  const int64_t base = st / segT;
   const int e = (int)(blockIdx.x * 256 + threadIdx.x) * 4;
   f32x4 E = {0.f, 0.f, 0.f, 0.f};
   if (!REV && init) {
     const u32x2 w = *(const u32x2*)(init + ((int64_t)i * nheads + h) * kScState + e);
+    if (first) *(u32x2*)(first + (base * nheads + h) * kScState + e) = w;
     E = f32x4{h2f((uint16_t)w.x), h2f((uint16_t)(w.x >> 16)), h2f((uint16_t)w.y),
               h2f((uint16_t)(w.y >> 16))};
   }
   auto at = [&](int k) { return state + ((base + k) * nheads + h) * kScState + e; };
-  constexpr int kAhead = 4;  // segments whose loads are issued together
-  for (int kb = 0; kb < nk; kb += kAhead) {
-    f32x4 own[kAhead];
-    float dec[kAhead];
+  // two segments' loads are issued together, and before the two before them are
+  // stored, as a wait for loads is one for older stores too (one prompt of 16384
+  // tokens backward, two passes: 1140 us in all, four at a time 1163; its scan with 8
+  // heads: 61, 58, and 67 one at a time)
+  constexpr int kAhead = 2;
+  f32x4 own[2][kAhead];
+  float dec[2][kAhead];
+  auto load = [&](int b, int kb) {
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) {
+      const int k = min(kb + q, nk - 2), kk = REV ? nk - 2 - k : k;
+      own[b][q] = *(const f32x4*)at(kk);
+      dec[b][q] = decay[(base + kk) * nheads + h];
+    }
+  };
+  auto walk = [&](int b, int kb) {
 #pragma unroll
     for (int q = 0; q < kAhead; ++q) {
       const int k = kb + q;
-      own[q] = f32x4{0.f, 0.f, 0.f, 0.f};
-      dec[q] = 0.f;
-      if (k + 1 < nk) {  // the last one's own state feeds nothing
-        const int kk = REV ? nk - 1 - k : k;
-        own[q] = *(const f32x4*)at(kk);
-        dec[q] = decay[(base + kk) * nheads + h];
-      }
+      if (k >= nk - 1) break;
+      E = E * dec[b][q] + own[b][q];
+      *(f32x4*)at(REV ? nk - 2 - k : k) = E;
     }
-#pragma unroll
-    for (int q = 0; q < kAhead; ++q) {
-      const int k = kb + q;
-      if (k >= nk) break;
-      *(f32x4*)at(REV ? nk - 1 - k : k) = E;
-      E = E * dec[q] + own[q];
-    }
+  };
+  load(0, 0);
+  for (int kb = 0; kb < nk - 1; kb += 2 * kAhead) {
+    load(1, kb + kAhead);
+    walk(0, kb);
+    load(0, kb + 2 * kAhead);
+    walk(1, kb + kAhead);
   }
 }
 
@@ -235,15 +246,17 @@ __global__ __launch_bounds__(256) void scan_pass_kernel(float* __restrict__ stat
 constexpr int kScShort = 4;
 
 // ---- y ---------------------------------------------------------------------
-// grid: scan_grid, 256 threads.  enter: the states that enter all segments, or,
-// with decay, the segments' own ones; NULL where every sequence is one segment
-// (one workgroup a head and sequence then, which may write over init).
+// grid: scan_grid, 256 threads.  state: the states behind the segments, or, with
+// decay, the segments' own ones; NULL where every sequence is one segment (one
+// workgroup a head and sequence then, which may write over init).  first: init of the
+// sequences of more segments, where it is written over, or NULL.
 template <bool F32>
 __global__ __launch_bounds__(256, 2) void scan_y_kernel(
     const typename Zx<F32>::T* __restrict__ zx, const uint16_t* __restrict__ u, int T, int nheads,
     const int* __restrict__ off, int nseq, int segT, const float* __restrict__ dt_bias,
     const float* __restrict__ A_log, const float* __restrict__ Dp, const uint16_t* init,
-    const float* __restrict__ enter, const float* __restrict__ decay, uint16_t* final_, uint16_t* __restrict__ y) {
+    const uint16_t* __restrict__ first, const float* __restrict__ state,
+    const float* __restrict__ decay, uint16_t* final_, uint16_t* __restrict__ y) {
   __shared__ __attribute__((aligned(16))) uint8_t Bt[kScQ * kScRowN], xt[kScQ * kScRowP];
   __shared__ __attribute__((aligned(16))) uint8_t Sl[2][kSqP * kScRowS];  // the state's terms
   __shared__ Toks<kScQ> tks[2];
@@ -303,19 +316,22 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
   // (all of the above on their way before the state's own loads are waited for)
   f32x4 S[2][4];
   const int sof = col * kSqN + 32 * wave + 4 * g;  // of S[0][0] in a state
-  if (enter && !decay) {
-    const float* p = enter + ((int64_t)sl * nheads + h) * kScState + sof;
+  const int place = sl - s.i;  // of this segment's state
+  if (state && !decay && s.k > 0) {
+    const float* p = state + ((int64_t)(place - 1) * nheads + h) * kScState + sof;
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
       for (int pb = 0; pb < 4; ++pb) S[nb][pb] = *(const f32x4*)(p + 16 * pb * kSqN + 16 * nb);
   } else if (init) {
+    const uint16_t* p = first && s.t1 < s.en
+                            ? first + ((int64_t)place * nheads + h) * kScState + sof
+                            : init + sat + sof;
     u32x2 w[2][4];
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
-      for (int pb = 0; pb < 4; ++pb)
-        w[nb][pb] = *(const u32x2*)(init + sat + sof + 16 * pb * kSqN + 16 * nb);
+      for (int pb = 0; pb < 4; ++pb) w[nb][pb] = *(const u32x2*)(p + 16 * pb * kSqN + 16 * nb);
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
@@ -330,9 +346,9 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
   }
   if (decay)  // the segments' own states: take those of the segments before this one
     for (int k = s.k; k > 0; --k) {
-      const int64_t at = (int64_t)(sl - k) * nheads + h;
+      const int64_t at = (int64_t)(place - k) * nheads + h;
       const float dec = decay[at];
-      const float* p = enter + at * kScState + sof;
+      const float* p = state + at * kScState + sof;
 #pragma unroll
       for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
@@ -530,13 +546,14 @@ static int64_t scan_seg(int64_t T, int64_t nheads) {
   return seg < 128 ? 128 : seg > T ? T : seg;
 }
 // A workgroup adds the own states of this many segments before its own up by
-// itself; with more, a launch makes the states that enter every segment.
+// itself; with more, a launch makes the states between the segments.
 constexpr int kScOwn = 16;
 
-int64_t seq_scan_bytes(int64_t T, int64_t nseq, int64_t nheads) {
+int64_t seq_scan_bytes(int64_t T, int64_t nheads) {
   const int64_t seg = scan_seg(T, nheads);
   if (seg >= T) return 0;
-  return slot_count(T, nseq, seg) * nheads * (kScState + 1) * 4;
+  // the states and decays in float32, the first segments' initial states in float16
+  return state_count(T, seg) * nheads * (kScState * 6 + 4) + 16;
 }
 
 // Heads vary fastest: workgroups go to the eight XCDs in turn, and slots without
@@ -560,10 +577,10 @@ static hipError_t scan_state_go(const SeqIn& in, const uint16_t* u, const uint16
 
 template <bool REV>
 static hipError_t scan_pass_go(const SeqIn& in, int segT, float* state, const float* decay,
-                               const uint16_t* init, hipStream_t stream) {
+                               const uint16_t* init, uint16_t* first, hipStream_t stream) {
   hipLaunchKernelGGL(scan_pass_kernel<REV>,
                      dim3(kScState / 1024, (unsigned)in.nheads, (unsigned)in.nseq), dim3(256), 0,
-                     stream, state, decay, in.T, in.nheads, in.offsets, segT, init);
+                     stream, state, decay, in.T, in.nheads, in.offsets, segT, init, first);
   return hipGetLastError();
 }
 
@@ -576,7 +593,7 @@ static hipError_t chunk_states_go(const SeqIn& in, const uint16_t* u, const uint
                                   float* decay, hipStream_t stream) {
   const hipError_t e =
       scan_state_go<F32, REV, 3>(in, u, dy, kScChunk, dt_bias, A_log, state, decay, stream);
-  return e != hipSuccess ? e : scan_pass_go<REV>(in, kScChunk, state, decay, nullptr, stream);
+  return e != hipSuccess ? e : scan_pass_go<REV>(in, kScChunk, state, decay, nullptr, nullptr, stream);
 }
 
 hipError_t launch_chunk_states(const SeqIn& in, const uint16_t* u, const uint16_t* dy, bool rev,
@@ -593,20 +610,23 @@ hipError_t launch_seq_scan(const SeqIn& in, const uint16_t* u, const float* dt_b
                            const float* A_log, const float* D, const uint16_t* ssm_in,
                            uint16_t* ssm_out, uint16_t* y, void* workspace, hipStream_t stream) {
   const int64_t seg = scan_seg(in.T, in.nheads);
-  float *enter = nullptr, *decay = nullptr;
+  float *state = nullptr, *decay = nullptr;
+  uint16_t* first = nullptr;
   const int64_t slots = slot_count(in.T, in.nseq, seg);
   if (seg < in.T) {
     // in place, a workgroup that has ended may have written what another would
-    // still begin with: then only the launch in between reads the initial states
-    const bool own = in.T / seg <= kScOwn && !(ssm_in && ssm_in == ssm_out);
-    enter = (float*)workspace;
-    decay = enter + slots * in.nheads * kScState;
+    // still begin with: then the launch in between keeps the initial states
+    const bool over = ssm_in && ssm_in == ssm_out, own = in.T / seg <= kScOwn && !over;
+    const int64_t n = state_count(in.T, seg) * in.nheads;
+    state = (float*)workspace;
+    decay = state + n * kScState;
     hipError_t e = in.f32 ? scan_state_go<true, false, 2>(in, u, nullptr, (int)seg, dt_bias, A_log,
-                                                          enter, decay, stream)
+                                                          state, decay, stream)
                           : scan_state_go<false, false, 2>(in, u, nullptr, (int)seg, dt_bias, A_log,
-                                                           enter, decay, stream);
+                                                           state, decay, stream);
     if (e == hipSuccess && !own) {
-      e = scan_pass_go<false>(in, (int)seg, enter, decay, ssm_in, stream);
+      if (over) first = (uint16_t*)(decay + (n + 3) / 4 * 4);
+      e = scan_pass_go<false>(in, (int)seg, state, decay, ssm_in, first, stream);
       decay = nullptr;
     }
     if (e != hipSuccess) return e;
@@ -615,11 +635,11 @@ hipError_t launch_seq_scan(const SeqIn& in, const uint16_t* u, const float* dt_b
   if (in.f32)
     hipLaunchKernelGGL(scan_y_kernel<true>, grid, dim3(256), 0, stream, (const float*)in.zx, u,
                        in.T, in.nheads, in.offsets, in.nseq, (int)seg, dt_bias, A_log, D, ssm_in,
-                       enter, decay, ssm_out, y);
+                       first, state, decay, ssm_out, y);
   else
     hipLaunchKernelGGL(scan_y_kernel<false>, grid, dim3(256), 0, stream, (const uint16_t*)in.zx,
                        u, in.T, in.nheads, in.offsets, in.nseq, (int)seg, dt_bias, A_log, D,
-                       ssm_in, enter, decay, ssm_out, y);
+                       ssm_in, first, state, decay, ssm_out, y);
   return hipGetLastError();
 }
 

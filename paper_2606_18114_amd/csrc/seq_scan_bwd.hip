@@ -124,8 +124,8 @@ __device__ __forceinline__ float over_groups(float v) {
 // from memory straight to registers; dC^T or dB^T (rows states, columns tokens)
 // add up over the heads there.  The next head's values are on their way
 // meanwhile, and wave 0 makes its token values.
-// part [groups][T][256] (dB, dC); dots [2 halves][2: qo, ko without
-// dt'][slots][nheads][128], pa [2 halves][slots][nheads]
+// part [groups][T][256] (dB, dC); dots [2 halves][2: qo, ko without dt'][nheads][T],
+// pa [2 halves][slots][nheads]
 template <bool F32>
 __global__ __launch_bounds__(256, 2) void scan_bwd_off_kernel(
     const typename Zx<F32>::T* __restrict__ zx, const uint16_t* __restrict__ u,
@@ -167,10 +167,12 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_off_kernel(
   float a[2][8];  // the slice: channels 32 k + 8 g + j, state n0 + col
   SbToks<F32> st;
   const int at = 8 * g * kSqN + n0 + col;
+  // the places of the states before and behind the chunk
+  const int64_t behind = sl - s.i, before = max(sl - s.i - 1, 0);
   auto load = [&](int h) {
     tile.load(vec + h * kSqP, ldv, s.t0, s.t1);
-    // (a slice that is zero was never written; what lies there is not used)
-    const float* p = slice + ((int64_t)sl * nheads + h) * kScState;
+    // (a slice that is zero has no place; what is loaded is not used)
+    const float* p = slice + ((side ? behind : before) * nheads + h) * kScState;
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -192,7 +194,7 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_off_kernel(
     if (side == 0) {  // <E, S0> of the slice
       float pv = 0.f;
       if (!first && !last) {
-        const float* e = E + sh * kScState;
+        const float* e = E + (behind * nheads + h) * kScState;
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -255,8 +257,9 @@ __global__ __launch_bounds__(256, 2) void scan_bwd_off_kernel(
     __syncthreads();
     if (threadIdx.x < kSbQ) {
       const int t = threadIdx.x;
-      dots[(((int64_t)(half * 2 + side) * slots + sl) * nheads + h) * kSbQ + t] =
-          (dw[0][t] + dw[1][t]) + (dw[2][t] + dw[3][t]);
+      if (s.t0 + t < s.t1)
+        dots[((int64_t)(half * 2 + side) * nheads + h) * T + s.t0 + t] =
+            (dw[0][t] + dw[1][t]) + (dw[2][t] + dw[3][t]);
     } else if (threadIdx.x == kSbQ && side == 0) {
       pa[(int64_t)half * slots * nheads + sh] = ((pp[0] + pp[1]) + (pp[2] + pp[3])) * tk.last;
     }
@@ -308,7 +311,6 @@ __global__ __launch_bounds__(kSbThreads, 4) void scan_bwd_to_kernel(
   }
   int buf = 0;
   for (int h = h0; h < h1; ++h, buf ^= 1) {
-    const int64_t sh = (int64_t)sl * nheads + h;
     // (no values ahead of the head: two workgroups share a CU, 128 registers a lane)
     bf16x8 yo[2];
     SbTile<kSbThreads> tile;
@@ -358,7 +360,7 @@ __global__ __launch_bounds__(kSbThreads, 4) void scan_bwd_to_kernel(
     }
     q += lane_xchg_f64<16>(q);
     q += lane_xchg_f64<32>(q);
-    if (g == 0) qi[sh * kSbQ + me] = q;
+    if (g == 0 && tm < s.t1) qi[(int64_t)h * T + tm] = q;
     __syncthreads();
   }
   if (tm < s.t1) {
@@ -410,7 +412,8 @@ __global__ __launch_bounds__(kSbThreads, 2) void scan_bwd_from_kernel(
     if (!last)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        re[q] = *(const f32x4*)(E + ((int64_t)sl * nheads + h) * kScState + (q * kSbThreads + tid) * 4);
+        re[q] = *(const f32x4*)(E + ((int64_t)(sl - s.i) * nheads + h) * kScState +
+                                (q * kSbThreads + tid) * 4);
   };
   auto toks = [&](int h) { st.load(zx, Z, nheads, h, s.t0, T, dt_bias, A_log); };
   constexpr int kTokWave = 4;  // block 7: one block of t
@@ -539,9 +542,9 @@ __global__ __launch_bounds__(kSbThreads, 2) void scan_bwd_from_kernel(
     }
     kk += lane_xchg_f64<16>(kk);
     kk += lane_xchg_f64<32>(kk);
-    if (g == 0) ki[sh * kSbQ + me] = kk;
+    if (g == 0 && tm < s.t1) ki[(int64_t)h * T + tm] = kk;
     own = over_groups(own);
-    if (g == 0) kd[sh * kSbQ + me] = own;
+    if (g == 0 && tm < s.t1) kd[(int64_t)h * T + tm] = own;
     diag = wave_sum(diag);
     if (lane == 0) ddp[w] = diag;
     if (tm < s.t1) {
@@ -619,7 +622,7 @@ __global__ __launch_bounds__(256) void scan_bwd_fin_kernel(
   const int d = nheads * kSqP;
   const int64_t Z = (int64_t)2 * d + 2 * kSqN + nheads, sh = (int64_t)sl * nheads + h;
   const float rate = sc_rate(A_log[h]), bias = dt_bias[h];
-  const int64_t per = (int64_t)gridDim.x * nheads * kSbQ;
+  const int64_t per = (int64_t)nheads * T, ht = (int64_t)h * T + s.t0;
   float raw[2], dt[2], kout[2], own[2];
   double a[2], b[2];  // what the sums over t >= s and over s' < s take
 #pragma unroll
@@ -631,12 +634,12 @@ __global__ __launch_bounds__(256) void scan_bwd_fin_kernel(
     float qout = 0.f;  // the halves of the states
     kout[q] = 0.f;
     if (in) {
-      const float* p = dots + sh * kSbQ + i;
+      const float* p = dots + ht + i;
       qout = p[0] + p[2 * per];
       kout[q] = p[per] + p[3 * per];
     }
-    own[q] = in ? kd[sh * kSbQ + i] : 0.f;
-    a[q] = in ? qi[sh * kSbQ + i] - ki[sh * kSbQ + i] + (double)qout : 0.0;
+    own[q] = in ? kd[ht + i] : 0.f;
+    a[q] = in ? qi[ht + i] - ki[ht + i] + (double)qout : 0.0;
     b[q] = (double)dt[q] * kout[q];
   }
   double ai = a[0] + a[1], bi = b[0] + b[1];  // from this lane up, up to this lane
@@ -709,7 +712,8 @@ struct ScanBwdWs {
   int64_t bytes;
 };
 static ScanBwdWs sb_ws(void* p, int64_t T, int64_t nseq, int64_t nheads) {
-  const int64_t slots = slot_count(T, nseq, kSbQ), sh = slots * nheads;
+  const int64_t slots = slot_count(T, nseq, kSbQ), sh = slots * nheads, th = T * nheads;
+  const int64_t states = state_count(T, kSbQ) * nheads;
   ScanBwdWs w;
   float* f = (float*)p;
   auto take = [&](int64_t n) {
@@ -717,11 +721,11 @@ static ScanBwdWs sb_ws(void* p, int64_t T, int64_t nseq, int64_t nheads) {
     f += (n + 63) / 64 * 64;
     return r;
   };
-  w.S0 = take(sh * kScState);
-  w.E = take(sh * kScState);
-  w.dec = take(sh);
-  w.qi = (double*)take(2 * sh * kSbQ), w.ki = (double*)take(2 * sh * kSbQ);
-  w.kd = take(sh * kSbQ), w.dots = take(4 * sh * kSbQ);
+  w.S0 = take(states * kScState);
+  w.E = take(states * kScState);
+  w.dec = take(states);
+  w.qi = (double*)take(2 * th), w.ki = (double*)take(2 * th);
+  w.kd = take(th), w.dots = take(4 * th);
   w.pa = take(2 * sh), w.dd = take(sh);
   w.sums = take(3 * sh);
   w.part = take(2 * sb_groups(slots, nheads) * T * 2 * kSqN);

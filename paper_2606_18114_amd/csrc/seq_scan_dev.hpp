@@ -38,6 +38,11 @@ constexpr int kScRowS = 2 * kSqN + 16;  // 128 states, row reads
 // Sequence i's segment k has slot off[i] / segT + i + k, which leaves every
 // sequence at least as many slots as it has segments without adding lengths
 // up; T / segT + nseq slots in all.  t0 >= t1: no tokens.
+//
+// States that segments hand on lie at sl - i = off[i] / segT + k, for the segments
+// k that another one of their sequence follows: those have off[i] + (k + 1) segT <
+// off[i + 1], so that the places of later sequences are higher, and the last place
+// is at most (T - 1) / segT, however many sequences there are.
 struct Slot {
   int i, k, t0, t1;  // sequence, segment, the segment's tokens
   int st, en;        // the sequence's tokens
@@ -75,6 +80,7 @@ __device__ __forceinline__ Slot slot_find(const int* __restrict__ off, int nseq,
 inline __host__ __device__ int64_t slot_count(int64_t T, int64_t nseq, int64_t segT) {
   return T / segT + nseq;
 }
+inline __host__ __device__ int64_t state_count(int64_t T, int64_t segT) { return T / segT + 1; }
 
 // e^A_log, held finite: with an infinite rate the exponents of tokens that are
 // not there would be NaN (0 times it); any step that is longer than 2^-115 ends

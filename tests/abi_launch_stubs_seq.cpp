@@ -33,7 +33,7 @@ hipError_t launch_seq_norm_bwd(const SeqIn&, const uint16_t*, const float*, floa
                                void*, uint16_t*, float*, void*, hipStream_t) {
   reached("seq_norm_bwd");
 }
-int64_t seq_scan_bytes(int64_t T, int64_t, int64_t nheads) {
+int64_t seq_scan_bytes(int64_t T, int64_t nheads) {
   return T > 512 ? 256 * (T + nheads) : 0;
 }
 hipError_t launch_seq_scan(const SeqIn&, const uint16_t*, const float*, const float*, const float*,

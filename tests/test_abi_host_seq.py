@@ -192,6 +192,19 @@ def test_workspace_sizes(L):
         assert f(*a) == -1, a
 
 
+def test_workspaces_of_many_sequences(L):
+    """States lie between the segments of a sequence: tokens bound their number,
+    not sequences (a state of 64 heads is 2 MiB)."""
+    if os.environ.get("TM_ABI_SEQ_LIB"):
+        pytest.skip("sizes of the kernels' own")
+    T, H, S = 65535, 64, 65535
+    assert L.tm_mixer_scan_workspace(T, S, H) == L.tm_mixer_scan_workspace(T, 1, H)
+    one, many = L.tm_mixer_scan_bwd_workspace(T, 1, H), L.tm_mixer_scan_bwd_workspace(T, S, H)
+    # per sequence and head: six float32 of a chunk's sums
+    assert many <= one + 6 * 4 * S * H + 4096
+    assert L.tm_mixer_scan_bwd_workspace(16384, 1024, H) < 2 * 130 * H * 8192 * 4 + 2 ** 28
+
+
 def test_checks_under_sanitizers(tmp_path):
     if os.environ.get("TM_ABI_SEQ_LIB"):
         pytest.skip("already the sanitizer build")

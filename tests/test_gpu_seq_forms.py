@@ -68,6 +68,36 @@ def test_scan_bwd_of_several_heads_a_workgroup(lengths, dtype):
     assert bool((du[e:] == 7.0).all())
 
 
+# sequences of several segments beside many of one: their states meet in the
+# workgroups themselves (H = 2: segments of 128 tokens, 12 of them) and in a launch
+# in between (24 of them; and always in place)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lengths", [[1] * 100 + [300, 0, 700] + [2] * 60 + [259],
+                                     [900] + [3] * 200 + [128, 256, 0, 1000] + [1] * 50])
+def test_scan_of_many_sequences(lengths, dtype):
+    offs, H = _packed(lengths), 2
+    rng, T, prm, dev, zx, u, off, (x, B, C, dt), d, cd = _scan_case(
+        offs, H, dtype, len(lengths), 0.0)
+    S = len(offs) - 1
+    ssm = _t(0.5 * rng.standard_normal((S, H, P, N)), torch.float16)
+    args = (u, zx, dev["dt_bias"], dev["A_log"], dev["D"], off)
+    new, same, from0 = torch.full_like(ssm, 9.0), ssm.clone(), torch.full_like(ssm, 9.0)
+    got = [(ops.mixer_scan(*args, ssm, ssm_out=new), new),
+           (ops.mixer_scan(*args, same, ssm_out=same), same),
+           (ops.mixer_scan(*args, ssm_out=from0), from0)]
+    s0 = _np(ssm)
+    for (y, st), start in zip(got, (s0, s0, 0.0 * s0)):
+        ry, my, rs, ms = np.zeros((T, H, P)), np.zeros((T, H, P)), start.copy(), np.abs(start)
+        for i, a, b in _seqs(offs):
+            seq = (dt[a:b], prm["dt_bias"], prm["A_log"])
+            ry[a:b], rs[i] = O.scan(x[a:b], B[a:b], C[a:b], *seq, prm["D"], start[i])
+            my[a:b], ms[i] = O.scan(np.abs(x[a:b]), np.abs(B[a:b]), np.abs(C[a:b]), *seq,
+                                    np.abs(prm["D"]), np.abs(start[i]))
+        e = offs[-1]
+        near("y", y[:e].reshape(-1, H, P), ry[:e], my[:e], 2.0 ** -14)
+        near("states", st, rs, ms, 2.0 ** -14)
+
+
 def _conv_lengths(rng, T):
     """Ragged lengths that add up to T: empty ones, single tokens, less than the
     taps, ends anywhere in a run and on its border."""
