@@ -575,8 +575,8 @@ __global__ __launch_bounds__(kSbThreads, 2) void scan_bwd_from_kernel(
   }
 }
 
-// du's B and C columns: the sums over the head groups (both kernels'), in a
-// fixed order.  grid (ceil(T / 4)), 256 threads: a wave a token, four columns a lane
+// du's B and C columns: the sums over the head groups (of what lies outside the
+// chunks, and inside), in a fixed order.  grid (ceil(T / 4)), 256 threads: a wave a token, four columns a lane
 __global__ __launch_bounds__(256) void scan_bwd_bc_kernel(const float* __restrict__ part,
                                                           int groups, int T, int nheads,
                                                           const int* __restrict__ off, int nseq,
@@ -602,8 +602,8 @@ __global__ __launch_bounds__(256) void scan_bwd_bc_kernel(const float* __restric
 }
 
 // A wave a chunk and head, two tokens a lane: dl, dt's gradient, and the
-// chunk's sums for dt_bias, A_log and D (sums [slots][3][nheads]).
-// grid (slots, ceil(nheads / 4)), 256 threads
+// chunk's sums for dt_bias, A_log and D (sums [slots][3][nheads]).  dots, pa NULL:
+// nothing from outside the chunks.  grid (slots, ceil(nheads / 4)), 256 threads
 template <bool F32>
 __global__ __launch_bounds__(256) void scan_bwd_fin_kernel(
     const typename Zx<F32>::T* __restrict__ zx, int T, int nheads, const int* __restrict__ off,
@@ -633,7 +633,7 @@ __global__ __launch_bounds__(256) void scan_bwd_fin_kernel(
     dt[q] = in ? mx_softplus(raw[q]) : 0.f;
     float qout = 0.f;  // the halves of the states
     kout[q] = 0.f;
-    if (in) {
+    if (in && dots) {
       const float* p = dots + ht + i;
       qout = p[0] + p[2 * per];
       kout[q] = p[per] + p[3 * per];
@@ -651,7 +651,7 @@ __global__ __launch_bounds__(256) void scan_bwd_fin_kernel(
     if (lane >= k) bi += y;
   }
   const double above = ai - a2, before = bi - b2,
-               through = (double)pa[sh] + (double)pa[(int64_t)gridDim.x * nheads + sh];
+               through = pa ? (double)pa[sh] + (double)pa[(int64_t)gridDim.x * nheads + sh] : 0.0;
   const double dl[2] = {above + a[1] + a[0] + before + through,
                         above + a[1] + before + b[0] + through};
   double sb = 0.0, sa = 0.0;  // (many small terms of either sign)
@@ -706,6 +706,11 @@ static int sb_groups(int64_t slots, int64_t nheads) {
   return (int)((nheads + per - 1) / per);
 }
 
+// Whether there may be states between chunks: up to 128 tokens a sequence is one
+// chunk, and the launches for what lies outside of one are left out (four sequences
+// of 64 heads in 128 tokens: 41 us, 55 with the launch by chunks; in 129: 65)
+static bool sb_states(int64_t T) { return T > kSbQ; }
+
 struct ScanBwdWs {
   double *qi, *ki;
   float *S0, *E, *dec, *kd, *dots, *pa, *dd, *sums, *part;
@@ -721,14 +726,17 @@ static ScanBwdWs sb_ws(void* p, int64_t T, int64_t nseq, int64_t nheads) {
     f += (n + 63) / 64 * 64;
     return r;
   };
-  w.S0 = take(states * kScState);
-  w.E = take(states * kScState);
-  w.dec = take(states);
+  w.S0 = w.E = w.dec = w.dots = w.pa = nullptr;
+  if (sb_states(T)) {
+    w.S0 = take(states * kScState);
+    w.E = take(states * kScState);
+    w.dec = take(states);
+    w.dots = take(4 * th), w.pa = take(2 * sh);
+  }
   w.qi = (double*)take(2 * th), w.ki = (double*)take(2 * th);
-  w.kd = take(th), w.dots = take(4 * th);
-  w.pa = take(2 * sh), w.dd = take(sh);
+  w.kd = take(th), w.dd = take(sh);
   w.sums = take(3 * sh);
-  w.part = take(2 * sb_groups(slots, nheads) * T * 2 * kSqN);
+  w.part = take((sb_states(T) ? 2 : 1) * sb_groups(slots, nheads) * T * 2 * kSqN);
   w.bytes = (int64_t)((uintptr_t)f - (uintptr_t)p);
   return w;
 }
@@ -747,27 +755,27 @@ static hipError_t scan_bwd_go(const SeqIn& in, const uint16_t* u, const float* d
   const ScanBwdWs w = sb_ws(workspace, in.T, in.nseq, in.nheads);
   const int64_t slots = slot_count(in.T, in.nseq, kSbQ);
   const int groups = sb_groups(slots, in.nheads);
-  // up to 128 tokens a sequence is one chunk, and no state is read (four sequences
-  // of 64 heads in 128 tokens 56 us; in 129, with the four launches, 71)
-  if (in.T > kSbQ) {
+  const dim3 grid((unsigned)slots, (unsigned)groups);
+  float* inside = w.part;  // the partial sums of dB and dC from inside the chunks
+  int parts = groups;
+  if (sb_states(in.T)) {
     hipError_t e = launch_chunk_states(in, u, nullptr, false, dt_bias, A_log, w.S0, w.dec, stream);
     if (e != hipSuccess) return e;
     e = launch_chunk_states(in, u, dy, true, dt_bias, A_log, w.E, w.dec, stream);
     if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(scan_bwd_off_kernel<F32>, dim3((unsigned)((slots * groups + 7) / 8 * 32)),
+                       dim3(256), 0, stream, zx, u, dy, in.T, in.nheads, in.offsets, in.nseq,
+                       dt_bias, A_log, w.S0, w.E, w.part, w.dots, w.pa, (int)slots, groups);
+    inside += (int64_t)groups * in.T * 2 * kSqN;
+    parts += groups;
   }
-  const dim3 grid((unsigned)slots, (unsigned)groups);
-  float* part2 = w.part + (int64_t)groups * in.T * 2 * kSqN;
-  hipLaunchKernelGGL(scan_bwd_off_kernel<F32>, dim3((unsigned)((slots * groups + 7) / 8 * 32)),
-                     dim3(256), 0, stream, zx, u, dy, in.T, in.nheads, in.offsets, in.nseq,
-                     dt_bias, A_log, w.S0, w.E, w.part, w.dots, w.pa, (int)slots,
-                     groups);
   hipLaunchKernelGGL(scan_bwd_to_kernel<F32>, grid, dim3(kSbThreads), 0, stream, zx, u, dy, in.T,
-                     in.nheads, in.offsets, in.nseq, dt_bias, A_log, part2, w.qi);
+                     in.nheads, in.offsets, in.nseq, dt_bias, A_log, inside, w.qi);
   hipLaunchKernelGGL(scan_bwd_from_kernel<F32>, grid, dim3(kSbThreads), 0, stream, zx, u, dy, in.T,
-                     in.nheads, in.offsets, in.nseq, dt_bias, A_log, D, w.E, part2, w.ki, w.kd,
+                     in.nheads, in.offsets, in.nseq, dt_bias, A_log, D, w.E, inside, w.ki, w.kd,
                      w.dd, du);
   hipLaunchKernelGGL(scan_bwd_bc_kernel, dim3((unsigned)((in.T + 3) / 4)), dim3(256), 0, stream, w.part,
-                     2 * groups, in.T, in.nheads, in.offsets, in.nseq, du);
+                     parts, in.T, in.nheads, in.offsets, in.nseq, du);
   hipLaunchKernelGGL(scan_bwd_fin_kernel<F32>, dim3((unsigned)slots, (unsigned)((in.nheads + 3) / 4)),
                      dim3(256), 0, stream, zx, in.T, in.nheads, in.offsets, in.nseq, dt_bias,
                      A_log, w.qi, w.ki, w.kd, w.dots, w.pa, w.dd, (X*)dzx, w.sums);

@@ -202,6 +202,8 @@ def test_workspaces_of_many_sequences(L):
     one, many = L.tm_mixer_scan_bwd_workspace(T, 1, H), L.tm_mixer_scan_bwd_workspace(T, S, H)
     # per sequence and head: six float32 of a chunk's sums
     assert many <= one + 6 * 4 * S * H + 4096
+    # one chunk has none: the heads' sums of dB and dC, 1 KiB each, and little else
+    assert L.tm_mixer_scan_bwd_workspace(1, 1, H) < 2 ** 17
     assert L.tm_mixer_scan_bwd_workspace(16384, 1024, H) < 2 * 130 * H * 8192 * 4 + 2 ** 28
 
 
