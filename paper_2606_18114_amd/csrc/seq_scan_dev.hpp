@@ -96,9 +96,10 @@ constexpr double kScLeast = -4096.0;
 // A tile's token values in LDS.  The exponents c (base 2) are held as hi, a
 // multiple of 1/16 (at most 2^19 of them are 128 tokens': exact in float32), and
 // the rest lo: differences of two hi are exact, so that c_t - c_s keeps 2^-29 of
-// near tokens even where c itself is in the hundreds.
+// near tokens even where c itself is in the hundreds.  (Aligned: hi, lo and dt are read
+// four at a time.)
 template <int Q>
-struct Toks {
+struct alignas(16) Toks {
   float hi[Q], lo[Q];  // c_t log2(e)
   float dt[Q];         // dt'
   float ec[Q];         // e^{c_t}
