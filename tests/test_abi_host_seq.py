@@ -192,6 +192,15 @@ def test_workspace_sizes(L):
         assert f(*a) == -1, a
 
 
+def test_segments_of_many_heads(L):
+    """The heads fill the chip by themselves: no segments, so no workspace."""
+    if os.environ.get("TM_ABI_SEQ_LIB"):
+        pytest.skip("sizes of the kernels' own")
+    for T, H in ((1000, 512), (1000, 520), (16384, 300), (2 ** 23, 257), (2 ** 20, 4096)):
+        assert L.tm_mixer_scan_workspace(T, 1, H) == 0, (T, H)
+    assert L.tm_mixer_scan_workspace(16384, 1, 256) > 0
+
+
 def test_workspaces_of_many_sequences(L):
     """States lie between the segments of a sequence: tokens bound their number,
     not sequences (a state of 64 heads is 2 MiB)."""
