@@ -126,20 +126,19 @@ __global__ __launch_bounds__(64) void seq_conv_kernel(
 template <bool F32>
 __global__ __launch_bounds__(256) void seq_ring_kernel(
     const typename Zx<F32>::T* __restrict__ zx, int T, int nheads, const int* __restrict__ off,
-    const uint16_t* ring, const int* __restrict__ ring_pos, uint16_t* ring_out) {
+    const int* __restrict__ ring_pos, uint16_t* __restrict__ ring) {
   const int d = nheads * kSqP, cd = d + 2 * kSqN;
   const int64_t Z = (int64_t)2 * d + 2 * kSqN + nheads;
   const int c = (int)(blockIdx.x * 256 + threadIdx.x), i = (int)blockIdx.y;
   if (c >= cd) return;
   const int st = off ? off[i] : 0, en = off ? min(off[i + 1], T) : T;
   const int len = st >= 0 && en > st ? en - st : 0;
-  if (len == 0 && ring == ring_out) return;
+  if (len == 0) return;
   const int pos = ring_pos[0] & 3;
-  const int64_t at = ((int64_t)i * cd + c) * kSqTaps;
-  uint16_t old[kSqTaps] = {0, 0, 0, 0}, now[kSqTaps];
-  if (ring)
+  uint16_t* r = ring + ((int64_t)i * cd + c) * kSqTaps;
+  uint16_t old[kSqTaps], now[kSqTaps];
 #pragma unroll
-    for (int j = 0; j < kSqTaps; ++j) old[j] = ring[at + ((pos + j) & 3)];
+  for (int j = 0; j < kSqTaps; ++j) old[j] = r[(pos + j) & 3];
 #pragma unroll
   for (int j = 0; j < kSqTaps; ++j) {
     const int k = len + j - kSqTaps;  // the input's place in the sequence
@@ -153,7 +152,7 @@ __global__ __launch_bounds__(256) void seq_ring_kernel(
     }
   }
 #pragma unroll
-  for (int j = 0; j < kSqTaps; ++j) ring_out[at + ((pos + j) & 3)] = now[j];
+  for (int j = 0; j < kSqTaps; ++j) r[(pos + j) & 3] = now[j];
 }
 
 // Backward, a run of tokens (conv_bwd_run): da of the run's tokens and of the three
@@ -339,8 +338,8 @@ static hipError_t conv_go(const SeqIn& in, const float* conv_w, const float* con
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || ring_out == nullptr || ring_out != ring_in) return e;
   hipLaunchKernelGGL(seq_ring_kernel<F32>, dim3((unsigned)((cd + 255) / 256), (unsigned)in.nseq),
-                     dim3(256), 0, stream, (const E*)in.zx, in.T, in.nheads, in.offsets, ring_in,
-                     ring_pos, ring_out);
+                     dim3(256), 0, stream, (const E*)in.zx, in.T, in.nheads, in.offsets, ring_pos,
+                     ring_out);
   return hipGetLastError();
 }
 

@@ -54,7 +54,8 @@ hipError_t launch_embed_bwd(const void* ids, bool ids64, int64_t T, const float*
                             int64_t D, float scale, float* dW, bool accumulate, void* workspace,
                             hipStream_t stream);
 
-// out[c] = sum over r < rows of part[r * stride + c], c < cols, in 64 interleaved chains of rows
+// out[c] = sum over r < rows of part[r * stride + c], c < cols, in 16 or 64 interleaved
+// chains of rows, as there are more or fewer columns
 hipError_t launch_sum_rows(const float* part, int64_t rows, int64_t cols, int64_t stride,
                            float* out, hipStream_t stream);
 
