@@ -25,7 +25,9 @@ __device__ __forceinline__ float nm_sum(float v, float* lds) {
     __syncthreads();  // the previous sum has been read
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    float a = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    if constexpr (L == 512) a += (lds[4] + lds[5]) + (lds[6] + lds[7]);
+    return a;
   }
 }
 
@@ -42,7 +44,7 @@ __global__ __launch_bounds__(L) void seq_norm_kernel(
     const typename Zx<F32>::T* __restrict__ zx, int64_t Z, int d, const uint16_t* __restrict__ y,
     const float* __restrict__ w, float eps, const int* __restrict__ off, int nseq,
     uint16_t* __restrict__ out) {
-  __shared__ float lds[4];
+  __shared__ float lds[8];
   const int64_t t = blockIdx.x;
   if (nm_outside(off, nseq, t)) return;
   const typename Zx<F32>::T* zr = zx + t * Z;
@@ -109,7 +111,7 @@ __global__ __launch_bounds__(L) void seq_norm_bwd_kernel(
     const uint16_t* __restrict__ y, const float* __restrict__ w, float eps,
     const int* __restrict__ off, int nseq, const uint16_t* __restrict__ dout, typename Zx<F32>::T* __restrict__ dzx,
     uint16_t* __restrict__ dy, float* __restrict__ part) {
-  __shared__ float lds[4];
+  __shared__ float lds[8];
   constexpr int kV = NV > 0 ? NV : 1;
   float dw[kV][8], wv[kV][8];
   float* prow = part + (int64_t)blockIdx.x * d;
@@ -169,6 +171,10 @@ __global__ __launch_bounds__(L) void seq_norm_bwd_kernel(
         const int c = ((int)threadIdx.x + k * L) * 8;
         if (c >= d) continue;
         float q[8];
+        if constexpr (NV == 4) {  // the sums' SiLUs are made again: kept, they spill
+#pragma unroll
+          for (int i = 0; i < 8; ++i) asm("" : "+v"(z[k][i]));
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float g = yv[k][i] * z[k][i] * sq_sigmoid(z[k][i]);
@@ -225,16 +231,21 @@ __global__ __launch_bounds__(L) void seq_norm_bwd_kernel(
   }
 }
 
-// calls f with the row's thread count and vectors a thread
-template <typename Fn>
+// Calls f with the row's thread count and vectors a thread.  Backward a thread also
+// holds the weight, dout and the sums of dw: above 4096 channels 512 threads share a
+// row (8192 rows of 8192 channels 152 us, 201 with 256 threads, whose 276 registers
+// leave a wave a SIMD; of 16384 300, 574 with spills; in float32 202, 219; 387, 582).
+// From 16385 on the row is read twice.
+template <bool BWD, typename Fn>
 static void norm_form(int d, Fn&& f) {
   using std::integral_constant;
+  constexpr int kWide = BWD ? 512 : 256;
   if (d <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
   else if (d <= 1024) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
   else if (d <= 2048) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
   else if (d <= 4096) f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-  else if (d <= 8192) f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
-  else if (d <= 16384) f(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+  else if (d <= 8192) f(integral_constant<int, kWide>{}, integral_constant<int, 1024 / kWide>{});
+  else if (d <= 16384) f(integral_constant<int, kWide>{}, integral_constant<int, 2048 / kWide>{});
   else f(integral_constant<int, 256>{}, integral_constant<int, 0>{});
 }
 
@@ -242,7 +253,7 @@ hipError_t launch_seq_norm(const SeqIn& in, const uint16_t* y, const float* norm
                            uint16_t* out, hipStream_t stream) {
   const int d = in.nheads * kSqP;
   const int64_t Z = (int64_t)2 * d + 2 * kSqN + in.nheads;
-  norm_form(d, [&](auto l, auto nv) {
+  norm_form<false>(d, [&](auto l, auto nv) {
     if (in.f32)
       hipLaunchKernelGGL((seq_norm_kernel<true, l(), nv()>), dim3((unsigned)in.T), dim3(l()), 0,
                          stream, (const float*)in.zx, Z, d, y, norm_w, eps,
@@ -268,7 +279,7 @@ hipError_t launch_seq_norm_bwd(const SeqIn& in, const uint16_t* y, const float* 
   const int64_t Z = (int64_t)2 * d + 2 * kSqN + in.nheads;
   const int64_t groups = norm_groups(in.T);
   float* part = (float*)workspace;
-  norm_form(d, [&](auto l, auto nv) {
+  norm_form<true>(d, [&](auto l, auto nv) {
     if (in.f32)
       hipLaunchKernelGGL((seq_norm_bwd_kernel<true, l(), nv()>), dim3((unsigned)groups), dim3(l()),
                          0, stream, (const float*)in.zx, Z, d, in.T, y, norm_w, eps,

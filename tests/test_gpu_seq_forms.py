@@ -173,6 +173,29 @@ def test_conv_bwd_in_runs(T, H, dtype):
     assert bool((dzx[n:] == 3.0).all())
 
 
+# the backward's row forms at their borders, with more rows than it has groups of
+# them (the sums of dnorm_w go on from row to row)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H", [8, 9, 16, 17, 33, 64, 65, 97, 128, 129, 193, 256, 257])
+def test_norm_bwd_forms(H, dtype):
+    T = 1030
+    rng = np.random.default_rng(H)
+    prm, dev, zx, d, cd = _layer(rng, T, H, dtype)
+    y = _t(rng.standard_normal((T, d)), torch.bfloat16)
+    dout = _t(0.1 * rng.standard_normal((T, d)), torch.bfloat16)
+    dzx = torch.full_like(zx, 3.0)
+    dy, dw = ops.mixer_norm_bwd(y, zx, dev["norm_w"], dout, dzx, 1e-5)
+    a = (_np(y), _np(zx[:, :d]), prm["norm_w"], float(np.float32(1e-5)), _np(dout))
+    r, m = O.norm_bwd(*a), O.norm_bwd(*a, absolute=True)
+    near("dy", dy, r[0], m[0], 2.0 ** -19)
+    sig = 1.0 / (1.0 + np.exp(-a[1]))
+    flat = m[1] / np.maximum(np.abs(sig * (1 + a[1] * (1 - sig))), 1e-9)
+    near("dz", dzx[:, :d], r[1], flat, 2.0 ** -19)
+    # (two rows a group, 16 or 64 chains of up to 64: 2^-24 of 82 links and 2^-19)
+    near("dnorm_w", dw, r[2], m[2], 2.0 ** -17)
+    assert bool((dzx[:, d:] == 3.0).all())
+
+
 # rows of more columns than any workgroup takes in one step, and no multiple of 8
 @pytest.mark.parametrize("w_dtype", [torch.float32, torch.bfloat16, torch.float16])
 def test_embed_wide(w_dtype):

@@ -68,3 +68,10 @@ def scratch(tmp_path_factory):
 ])
 def test_scratch(scratch, kernel, most):
     assert scratch["tmk::" + kernel] <= most
+
+
+def test_the_norms_gradients_stay_in_registers(scratch):
+    """Rows of up to 16384 channels: the values of a row and the sums of the weight's
+    gradient are held from one row to the next."""
+    forms = {n: b for n, b in scratch.items() if n.startswith("tmk::seq_norm")}
+    assert sum("bwd" in n for n in forms) == 14 and not any(forms.values()), forms
