@@ -355,7 +355,7 @@ class Mamba2Decoder:
             raise RuntimeError("the decoder was made without an embedding")
         if ids.shape != (self.B,):
             raise ValueError(f"ids must be [{self.B}], got {tuple(ids.shape)}")
-        return ops.embed(ids, self.embedding, self.embed_scale, out=self.emb)
+        return ops.embed(ids.contiguous(), self.embedding, self.embed_scale, out=self.emb)
 
     def _proj_rows(self, lay, kind: str, x: torch.Tensor, out_dtype: torch.dtype) -> torch.Tensor:
         """A projection of many rows x bfloat16 [T, K] (tm_tgemm_fwd; the layers
@@ -394,14 +394,14 @@ class Mamba2Decoder:
         if prompts.dim() == 1:
             if self.embedding is None:
                 raise RuntimeError("the decoder was made without an embedding")
-            residual = ops.embed(prompts, self.embedding, self.embed_scale)
+            residual = ops.embed(prompts.contiguous(), self.embedding, self.embed_scale)
         else:
             if prompts.dim() != 2 or prompts.shape[1] != self.d_model:
                 raise ValueError(f"prompts must be ids [T] or float32 [T, {self.d_model}], got "
                                  f"{tuple(prompts.shape)}")
             if prompts.dtype != torch.float32:
                 raise TypeError(f"embedded prompts must be float32 (got {prompts.dtype})")
-            residual = prompts.clone()
+            residual = prompts.clone(memory_format=torch.contiguous_format)
         if offsets is None:
             if self.B != 1:
                 raise ValueError(f"a batch of {self.B} needs offsets")
