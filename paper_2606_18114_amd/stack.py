@@ -394,19 +394,24 @@ class Mamba2Decoder:
         if prompts.dim() == 1:
             if self.embedding is None:
                 raise RuntimeError("the decoder was made without an embedding")
-            residual = ops.embed(prompts.contiguous(), self.embedding, self.embed_scale)
-        else:
-            if prompts.dim() != 2 or prompts.shape[1] != self.d_model:
-                raise ValueError(f"prompts must be ids [T] or float32 [T, {self.d_model}], got "
-                                 f"{tuple(prompts.shape)}")
-            if prompts.dtype != torch.float32:
-                raise TypeError(f"embedded prompts must be float32 (got {prompts.dtype})")
-            residual = prompts.clone(memory_format=torch.contiguous_format)
+        elif prompts.dim() != 2 or prompts.shape[1] != self.d_model:
+            raise ValueError(f"prompts must be ids [T] or float32 [T, {self.d_model}], got "
+                             f"{tuple(prompts.shape)}")
+        elif prompts.dtype != torch.float32:
+            raise TypeError(f"embedded prompts must be float32 (got {prompts.dtype})")
         if offsets is None:
             if self.B != 1:
                 raise ValueError(f"a batch of {self.B} needs offsets")
         elif offsets.shape != (self.B + 1,):
             raise ValueError(f"offsets must be [{self.B + 1}], got {tuple(offsets.shape)}")
+        with torch.cuda.device(self.emb.device):  # (the projections run on the current one)
+            return self._prefill(prompts, offsets)
+
+    def _prefill(self, prompts: torch.Tensor, offsets: Optional[torch.Tensor]) -> torch.Tensor:
+        if prompts.dim() == 1:
+            residual = ops.embed(prompts.contiguous(), self.embedding, self.embed_scale)
+        else:
+            residual = prompts.clone(memory_format=torch.contiguous_format)
         T = residual.shape[0]
         if T == 0:
             return self.x_out

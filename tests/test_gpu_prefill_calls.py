@@ -1,5 +1,6 @@
 """Calls of ``Mamba2Decoder.prefill`` and ``set_ids`` that a program makes beside
-those of ``test_gpu_seq_model.py``: strided prompts and ids."""
+those of ``test_gpu_seq_model.py``: strided prompts and ids, a decoder on another
+device than the current one."""
 
 import numpy as np
 import pytest
@@ -30,3 +31,18 @@ def test_strided_prompts_and_ids():
     dec, _, _, _ = _decoder(B=2, embedding=table)
     turned = ids[:2].t().contiguous()  # [sequence, token]
     assert torch.equal(dec.set_ids(turned[:, 1]), table[ids[1]])
+
+
+def test_prefill_runs_on_the_decoders_device(monkeypatch):
+    """Its calls take the current device's stream, so that device is made current."""
+    dec, _, _, _ = _decoder()
+    seen = []
+
+    class Device(torch.cuda.device):
+        def __init__(self, device):
+            seen.append(torch.device(device))
+            super().__init__(device)
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    dec.prefill(torch.zeros((3, 128), device="cuda"))
+    assert dec.emb.device in seen
