@@ -375,8 +375,8 @@ class Mamba2Decoder:
                                  x=x[rows])
         return x
 
-    def prefill(self, prompts: torch.Tensor,
-                offsets: Optional[torch.Tensor] = None) -> torch.Tensor:
+    def prefill(self, prompts: torch.Tensor, offsets: Optional[torch.Tensor] = None, *,
+                zx_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
         """Prompts through every block: prompts float32 [T, d_model] (embedded)
         or ids [T], the batch rows' tokens packed one after another, row i's
         being offsets[i] .. offsets[i + 1] - 1 (int32 [B + 1] on the GPU; None
@@ -386,9 +386,11 @@ class Mamba2Decoder:
         d_model]) = the final norm behind each row's last token; a row without
         tokens keeps its own there too.
 
-        The projections write bfloat16, as a bfloat16 model stores them; the
-        states are float32 inside the call and rounded once at its end (a token
-        at a time rounds them at every token).  A multi-row normalization, a
+        in_proj's outputs are zx_dtype: bfloat16, as a bfloat16 model stores
+        them, or float32, as a token at a time keeps them (z, the convolution's
+        inputs and the steps unrounded, for twice their bytes); out_proj's are
+        float32.  The states are float32 inside the call and rounded once at its
+        end (a token at a time rounds them at every token).  A multi-row normalization, a
         product, the mixer's three calls (tm_mixer_conv, tm_mixer_scan,
         tm_mixer_norm) and a product per block."""
         if prompts.dim() == 1:
@@ -399,15 +401,18 @@ class Mamba2Decoder:
                              f"{tuple(prompts.shape)}")
         elif prompts.dtype != torch.float32:
             raise TypeError(f"embedded prompts must be float32 (got {prompts.dtype})")
+        if zx_dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError(f"zx_dtype must be bfloat16 or float32 (got {zx_dtype})")
         if offsets is None:
             if self.B != 1:
                 raise ValueError(f"a batch of {self.B} needs offsets")
         elif offsets.shape != (self.B + 1,):
             raise ValueError(f"offsets must be [{self.B + 1}], got {tuple(offsets.shape)}")
         with torch.cuda.device(self.emb.device):  # (the projections run on the current one)
-            return self._prefill(prompts, offsets)
+            return self._prefill(prompts, offsets, zx_dtype)
 
-    def _prefill(self, prompts: torch.Tensor, offsets: Optional[torch.Tensor]) -> torch.Tensor:
+    def _prefill(self, prompts: torch.Tensor, offsets: Optional[torch.Tensor],
+                 zx_dtype: torch.dtype) -> torch.Tensor:
         if prompts.dim() == 1:
             residual = ops.embed(prompts.contiguous(), self.embedding, self.embed_scale)
         else:
@@ -419,7 +424,7 @@ class Mamba2Decoder:
         for lay in self.layers:
             mp = lay["mixer"]
             x = self._norm_rows(residual, y, lay["pre"])
-            zx = self._proj_rows(lay, "in", x, torch.bfloat16)
+            zx = self._proj_rows(lay, "in", x, zx_dtype)
             u = ops.mixer_conv(zx, mp["conv_w"], mp["conv_b"], offsets, lay["conv"], lay["pos"],
                                conv_out=lay["conv"])
             s = ops.mixer_scan(u, zx, mp["dt_bias"], mp["A_log"], mp["D"], offsets, lay["ssm"],

@@ -1,13 +1,15 @@
 """Calls of ``Mamba2Decoder.prefill`` and ``set_ids`` that a program makes beside
 those of ``test_gpu_seq_model.py``: strided prompts and ids, a decoder on another
-device than the current one."""
+device than the current one, projections kept in float32."""
 
 import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 
-from test_gpu_seq_model import _decoder  # noqa: E402
+from oracle import mamba_seq as O  # noqa: E402
+from oracle import ternary as OT  # noqa: E402
+from test_gpu_seq_model import BF, N, P, _bf, _decoder, _np, _rel, _states  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +48,36 @@ def test_prefill_runs_on_the_decoders_device(monkeypatch):
     monkeypatch.setattr(torch.cuda, "device", Device)
     dec.prefill(torch.zeros((3, 128), device="cuda"))
     assert dec.emb.device in seen
+
+
+# the inputs of layer 0's states, rounded only where the calls do: x to bfloat16, u to
+# bfloat16 (2^-9 in the mean square, averaged over tokens in the state; the oracle's
+# alike but for values next to a border), the state to float16: 2^-12 in the mean
+# square at most; 2^-10 with bfloat16's rounding of B or x falling the other way for
+# one value in a hundred
+def test_float32_projections():
+    """zx_dtype float32: the states are those of unrounded projections."""
+    rng = np.random.default_rng(5)
+    emb = rng.standard_normal((140, 128)).astype(np.float32)
+    dec, mix, pre, w = _decoder()
+    dec.prefill(torch.from_numpy(emb).cuda(), zx_dtype=torch.float32)
+    H, d = dec.nheads, dec.d_inner
+    lay, p = dec.layers[0], {k: v.astype(np.float64) for k, v in mix[0].items()}
+    q = OT.unpack(lay["in"][1][0].cpu().numpy(), 128).astype(np.float64)
+    wi = q * np.repeat(_np(lay["in"][2][0]), dec.g, axis=1)
+    res = emb.astype(np.float64)
+    x = _bf(res / np.sqrt((res * res).mean(-1, keepdims=True) + dec.eps) * _np(pre[0]))
+    zx = x @ wi.T
+    xbc = zx[:, d:-H]
+    u = _bf(O.conv(xbc, p["conv_w"], p["conv_b"]))
+    _, state = O.scan(u[:, :d].reshape(-1, H, P), u[:, d:d + N], u[:, d + N:], zx[:, -H:],
+                      p["dt_bias"], p["A_log"], p["D"])
+    conv, ssm = _states(dec, 0, 0)
+    assert _rel(conv, xbc[-4:]) < 2.0 ** -11  # float16 alone
+    assert _rel(ssm, state) < 2.0 ** -10
+    with pytest.raises(TypeError, match="zx_dtype"):
+        dec.prefill(torch.from_numpy(emb).cuda(), zx_dtype=torch.float16)
+    dec, _, _, _ = _decoder()
+    a = dec.prefill(torch.from_numpy(emb).cuda()).clone()
+    dec, _, _, _ = _decoder()
+    assert torch.equal(a, dec.prefill(torch.from_numpy(emb).cuda(), zx_dtype=BF))
