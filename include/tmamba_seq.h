@@ -16,8 +16,9 @@
  * (behind the last offset) are read by nothing that is written, and their
  * outputs are left as they were.  Being device data, the offsets are not
  * checked; whatever they hold, no call accesses memory outside its arrays.
- * Inputs must be finite: an infinity or NaN may reach other tokens of its own
- * sequence, earlier ones among them (not other sequences).
+ * Infinities and NaN reach what depends on them, by their own token or a later
+ * one of the same sequence (where tm_mixer_step would give an infinity, it may be
+ * NaN).  In the gradients they may reach any token of their own sequence.
  *
  * u, y, their gradients and the outputs are bfloat16 (16-byte aligned),
  * parameters and their gradients float32 (4-byte aligned), zxbcdt and its

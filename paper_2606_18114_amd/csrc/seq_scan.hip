@@ -60,6 +60,48 @@ __device__ __forceinline__ void tile_store(const TileRegs& r, uint8_t* m, uint8_
   }
 }
 
+// Values of x in a tile that are not finite.  A token's x stands in the products of
+// all the tile's tokens, with zeros for those before it, and zero times infinity is
+// not zero: such a value goes into LDS as zero, its token is noted, and what depends
+// on it is made NaN after the products (one prompt of 16384 tokens: 241 us, 237
+// without).  Values of B, C and dt need none of it: the products of a token before
+// them are other rows, columns or masked ones.
+struct Spoilt {
+  int first[kSqP];  // a channel's first such token, kScQ: none
+  int any;
+};
+__device__ __forceinline__ void spoilt_clear(Spoilt& p, int i) {
+  if (i < kSqP) p.first[i] = kScQ;
+  if (i == 0) p.any = 0;
+}
+// zeros in their place in this thread's part of x (TileRegs::v)
+__device__ __forceinline__ void spoilt_take(TileRegs& r, Spoilt& p, int n) {
+  typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+  u16x2 m = {0, 0};
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, r.v[q][k] & 0x7FFF7FFFu));
+  if (m.x < 0x7F80 && m.y < 0x7F80) return;
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int row = q * 32 + (tid >> 3);
+    if (row >= n) continue;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t half = 0xFFFFu << (16 * i), most = 0x7F80u << (16 * i);
+        if ((r.v[q][k] & most) != most) continue;
+        r.v[q][k] &= ~half;
+        atomicMin(&p.first[(tid & 7) * 8 + 2 * k + i], row);
+        p.any = 1;
+      }
+  }
+}
+
 // The wave's state slice += sum_s coef_s vec_s mat_s^T over the tile: rows
 // (states) 32 w + 16 nb + 4 (lane / 16) + i, columns (channels) 16 pb + lane % 16.
 template <int NT>
@@ -261,6 +303,7 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
   __shared__ __attribute__((aligned(16))) uint8_t Sl[2][kSqP * kScRowS];  // the state's terms
   __shared__ Toks<kScQ> tks[2];
   __shared__ __attribute__((aligned(16))) float coefs[2][kScQ];
+  __shared__ __attribute__((aligned(16))) Spoilt spoilt[2];
   const int h = blockIdx.x, sl = blockIdx.y + blockIdx.z * gridDim.y;
   const Slot s = slot_find(off, nseq, T, segT, sl);
   const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
@@ -302,8 +345,10 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
     toks_make<kScQ>(tks[buf], rr, min(s.t1, t0 + kScQ) - t0, rate);
     coefs[buf][lane] = tks[buf].eq[lane] * tks[buf].dt[lane];
   };
+  spoilt_clear(spoilt[0], threadIdx.x);
   if (wave == 0) raw_load(s.t0);
   load(s.t0);
+  __syncthreads();
   // C of this lane's states and the last tile's first tokens, in case it is short
   u32x2 cv[kScShort][2];
   const int tail = s.t0 + (s.t1 - s.t0 - 1) / kScQ * kScQ;
@@ -363,6 +408,7 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
   int t0 = s.t0;
   for (; s.t1 - t0 > kScShort; t0 += kScQ, buf ^= 1) {
     const int t1 = min(s.t1, t0 + kScQ);
+    spoilt_take(r, spoilt[buf], t1 - t0);
     tile_store(r, Bt, xt, t1 - t0);
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
@@ -385,6 +431,9 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
     __syncthreads();
     const Toks<kScQ>& tk = tks[buf];
     const float* coef = coefs[buf];
+    const Spoilt& sp = spoilt[buf];
+    const int any = sp.any;
+    spoilt_clear(spoilt[buf ^ 1], threadIdx.x);
     if (t0 + kScQ < s.t1) {
       load(t0 + kScQ);
       if (wave == 0) {
@@ -454,6 +503,13 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
         acc[pb] = mfma16(xo, gt[0], acc[pb]);
       }
     }
+    const bool spoils = __builtin_amdgcn_readfirstlane(any) != 0;
+    if (spoils)
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (tt >= sp.first[16 * pb + 4 * g + i]) acc[pb][i] = __builtin_nanf("");
     if (t0 + tt < t1) {
       uint16_t* o = y + (int64_t)(t0 + tt) * d + h * kSqP + 4 * g;
 #pragma unroll
@@ -472,6 +528,12 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
 #pragma unroll
       for (int pb = 0; pb < 4; ++pb) S[nb][pb] *= last;
     state_add<2>(S, Bt, xt, coef);
+    if (spoils)
+#pragma unroll
+      for (int pb = 0; pb < 4; ++pb)
+        if (sp.first[16 * pb + col] < kScQ)
+#pragma unroll
+          for (int nb = 0; nb < 2; ++nb) S[nb][pb] = f32x4{1.f, 1.f, 1.f, 1.f} * __builtin_nanf("");
     __syncthreads();
   }
   if (t0 < s.t1) {
