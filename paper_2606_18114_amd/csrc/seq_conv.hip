@@ -10,7 +10,7 @@
 // Bound by memory: a thread owns 8 channels (16 bytes of bfloat16; 4 backward)
 // and walks a run of tokens with the last three inputs in registers, so an input
 // is read once but for the three before each run.  16384 tokens of 64 heads in
-// bfloat16: 61 us (4.7 TB/s, a copy reaches 5.1), the gradients 112 + 6 us (3.9).
+// bfloat16: 61 us (4.7 TB/s, a copy reaches 5.1), the gradients 114 + 6 us (3.8).
 #include "seq.hpp"
 #include "seq_launch.hpp"
 

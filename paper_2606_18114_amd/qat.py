@@ -305,7 +305,7 @@ class Mamba2Mixer(torch.nn.Module):
 
     forward(zxbcdt, offsets=None): in_proj's output, bfloat16 or float32,
     [L, Z] or [batch, L, Z] (a sequence a row), or with offsets (int32
-    [nseq + 1] on the GPU) packed sequences [T, Z]; returns out_proj's input,
+    [nseq + 1] on the GPU) packed sequences [T, Z] (65535 sequences at most); returns out_proj's input,
     bfloat16 [..., d_inner].  Sequences begin with zero states; rows outside
     the offsets come out zero and have no gradient."""
 
