@@ -345,10 +345,12 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
     toks_make<kScQ>(tks[buf], rr, min(s.t1, t0 + kScQ) - t0, rate);
     coefs[buf][lane] = tks[buf].eq[lane] * tks[buf].dt[lane];
   };
-  spoilt_clear(spoilt[0], threadIdx.x);
   if (wave == 0) raw_load(s.t0);
   load(s.t0);
-  __syncthreads();
+  if (s.t1 - s.t0 > kScShort) {  // (there are tiles)
+    spoilt_clear(spoilt[0], threadIdx.x);
+    __syncthreads();
+  }
   // C of this lane's states and the last tile's first tokens, in case it is short
   u32x2 cv[kScShort][2];
   const int tail = s.t0 + (s.t1 - s.t0 - 1) / kScQ * kScQ;
