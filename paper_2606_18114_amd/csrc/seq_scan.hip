@@ -600,9 +600,9 @@ __global__ __launch_bounds__(256, 2) void scan_y_kernel(
 
 // Tokens of a segment: as many segments of all heads as the chip takes
 // workgroups at once (512), whatever the sequences' lengths, which the host does
-// not know.  Two sequences of 8192 tokens and 64 heads: 245 us, 455 in one
-// segment each; one of 4096: 76 and 228; eight of 2048, where one segment each
-// would do: 177 and 161.  Above 256 heads two segments of all of them do not fit
+// not know.  Two sequences of 8192 tokens and 64 heads: 247 us, 437 in one
+// segment each; one of 4096: 79 and 215; eight of 2048, where one segment each
+// would do: 168 and 163.  Above 256 heads two segments of all of them do not fit
 // (16384 tokens of 400 heads 1181 us, 1541 in 1.3; 1000 of 520 121, 160 in 960 + 40).
 // Up to 512 tokens in one segment, whatever the heads: 300 tokens in three sequences
 // 13 us, 16 in segments of 128, in one 21 and 19; 512 in one 30 and 22; 150 15 and 18.
