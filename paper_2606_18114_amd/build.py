@@ -31,6 +31,7 @@ SOURCES = [
     "abi_parts.cpp",
     "abi_decode16.cpp",
     "abi_seq.cpp",
+    "abi_head.cpp",
     "ternarize_pack.hip",
     "tgemm_fwd.hip",
     "tgemm_bwd_dx.hip",
@@ -49,6 +50,9 @@ SOURCES = [
     "seq_scan.hip",
     "seq_scan_bwd.hip",
     "embed.hip",
+    "head_gemm.hip",
+    "head_loss.hip",
+    "block_norm.hip",
 ]
 
 ARCH = "gfx950"

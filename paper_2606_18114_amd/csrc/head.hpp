@@ -1,0 +1,95 @@
+// The head's loss and the block norm (tmamba_head.h): sizes, workspaces and what the kernels of
+// head_gemm.hip and head_loss.hip hand each other.  Arguments are checked by
+// the caller (abi_head.cpp).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace tmk {
+
+// rows of h with a loss, their labels and teacher, the weight
+struct HeadIn {
+  const uint16_t* h;  // [T, D]
+  const uint16_t* w;  // [V, D]
+  bool f16;           // else bfloat16
+  int64_t T, V;
+  int D;
+  const void* targets;  // [T], int32 or int64
+  const void* ids;      // [T, K] or NULL, int32 or int64
+  bool targets64, ids64;
+  int K;
+  float alpha, tau;  // (0, 1 without a teacher)
+};
+
+// A token's row of `stats`: log2 of its sum of exponentials, the same at the
+// temperature, which terms it has (1: cross entropy, 2: divergence), then the
+// logit gradient (of the loss over head_unit) at its label and at the teacher's words.
+constexpr int kHeadStatLse = 0, kHeadStatLseT = 1, kHeadStatTerms = 2, kHeadStatLabel = 3,
+              kHeadStatTop = 4;
+inline __host__ __device__ int64_t head_stats_cols(int64_t K) { return kHeadStatTop + K; }
+
+// |gradient of a logit| <= head_unit * |dloss|; the gradient over it is what
+// is held in 16 bits
+inline __host__ __device__ float head_unit(float alpha, float tau) {
+  return (1.0f - alpha) + alpha * tau;
+}
+
+// A row of the backward pass: the exponents' offsets and the factors of the
+// two softmaxes, 16 bytes
+struct HeadRow {
+  float lse, lse_t, c1, c2;
+};
+
+// dlogits in 16 bits are (gradient over head_unit and a power of two) times
+// 2^kHeadShift: float16 then holds probabilities down to 2^-27 with 11 bits;
+// bfloat16 has the exponents anyway
+template <bool F16>
+constexpr int kHeadShift = F16 ? 13 : 0;
+
+// Pieces of the vocabulary in the backward pass, and how products are cut
+struct HeadPlan {
+  int64_t piece = 0, pieces = 0;  // words (a multiple of 256) of a piece; their number
+  int parts_h = 1, per_h = 0;     // dh's contraction (words of a piece), stages of 32
+  int parts_w = 1, per_w = 0;     // dW's contraction (tokens)
+};
+HeadPlan head_plan(int64_t T, int64_t V, int64_t D);
+
+int64_t head_loss_bytes(int64_t T, int64_t V);
+hipError_t launch_head_loss(const HeadIn& in, const void* top, int top_type, float* loss,
+                            float* stats, void* workspace, hipStream_t stream);
+int64_t head_loss_bwd_bytes(int64_t T, int64_t V, int64_t D);
+// dw_type 0 float32, 1 h's type; accumulate only with float32
+hipError_t launch_head_loss_bwd(const HeadIn& in, const float* stats, const float* dloss,
+                                uint16_t* dh, void* dw, int dw_type, bool accumulate,
+                                void* workspace, hipStream_t stream);
+
+hipError_t launch_block_norm(const float* residual, const float* y, int64_t T, int d,
+                             const float* w, float eps, float* residual_out, uint16_t* x,
+                             hipStream_t stream);
+int64_t block_norm_bwd_bytes(int64_t T, int64_t d);
+hipError_t launch_block_norm_bwd(const float* r, int64_t T, int d, const float* w, float eps,
+                                 const uint16_t* dx, const float* dres, float* dr, float* dw,
+                                 void* workspace, hipStream_t stream);
+
+// ---- products (head_gemm.hip); `count` [1]: rows in use, on the device
+// partial softmax sums of the rows idx: part[(wg + tile)][half][token][pair], see head_loss.hip
+int64_t head_part_floats(int64_t T);
+int head_logits_grid(int64_t T, int64_t words);  // its workgroups
+hipError_t launch_head_logits(const HeadIn& in, const int* idx, const int* count, float* part,
+                              hipStream_t stream);
+// dlogits of words w0 .. w0 + n - 1 to G [rows, ld], ld >= n rounded up to 256
+hipError_t launch_head_dlogits(const HeadIn& in, const int* idx, const int* count,
+                               const HeadRow* rows, int64_t w0, int64_t n, uint16_t* G, int64_t ld,
+                               hipStream_t stream);
+// part_h[s][row][D] (+)= the s-th part of G . W[w0 ..]
+hipError_t launch_head_dh(const HeadIn& in, const int* count, const uint16_t* G, int64_t ld,
+                          int64_t w0, int64_t n, int parts, int per, bool add, float* part_h,
+                          hipStream_t stream);
+// dW[w0 ..] (+)= 2^(*exp) G^T . hs, whole, or into part_w[s][n][D] and from there
+hipError_t launch_head_dw(const HeadIn& in, const int* count, const uint16_t* G, int64_t ld,
+                          const uint16_t* hs, int64_t w0, int64_t n, int parts, int per,
+                          const int* exp, void* dw, int dw_type, bool accumulate, float* part_w,
+                          hipStream_t stream);
+
+}  // namespace tmk

@@ -1,0 +1,752 @@
+// The products of the head's loss (tmamba_head.h) on the gfx950 matrix cores,
+// 16-bit operands (bfloat16 or float16), float32 sums:
+//   logits   z[v, t]  = W[v, :] . h[t, :]        -> running softmax sums, or dlogits G
+//   dh       dh[t, :] = sum_v G[t, v] W[v, :]
+//   dW       dW[v, :] = sum_t G[t, v] h[t, :]
+// Logits are made in the registers of a tile and never stored: forward, a
+// lane keeps the maximum and the sum of exponentials of its tokens over all the
+// words that its workgroup walks; backward the tile becomes 16-bit dlogits of one
+// piece of the vocabulary, which dh and dW contract.
+//
+// One main loop for the three.  Operands lie along the contraction (h, W for
+// the logits, G for dh) or across it (W for dh; G and h for dW).  Tiles are
+// staged in LDS in their natural order by direct-to-LDS loads, 32 steps of the
+// contraction a stage, in a ring of four stages.  Along: rows of 64 bytes,
+// whose 16-byte pieces are XOR-permuted so that 16 rows read at one step lie in
+// different banks; one ds_read_b128 is an operand.  Across: rows of 512 bytes
+// in permuted 32-byte units, read with the transpose read ds_read_b64_tr_b16, two
+// an operand.
+//
+// Tile 256 x 256 of 4 waves, 128 x 128 each (4 x 4 blocks of 32 x 32,
+// accumulators in AGPRs, one wave a SIMD), every MFMA a slot of its own with the
+// reads of the next step and the loads of stage + 3 dealt over the slots.
+#include <type_traits>
+
+#include "common.hpp"
+#include "head.hpp"
+#include "launchers.hpp"
+
+namespace tmk {
+
+namespace {
+
+constexpr int kBK = 32, kRing = 4;
+constexpr int kTM = 256, kTN = 256;
+constexpr int kOpA = kTM * kBK * 2, kOpB = kTN * kBK * 2;
+constexpr int kSlot = kOpA + kOpB;
+constexpr int kLoads = 8;  // direct-to-LDS loads of a wave and stage
+constexpr float kLog2e = 1.4426950408889634f;
+
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+
+enum Mode { kStats, kDlogits, kDh, kDw };
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// lane i: 16 bytes at base + voff -> LDS lds_base + 16 i (lds_base wave-uniform)
+__device__ __forceinline__ void dma16(const void* base, uint32_t voff, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff),
+               "s"(base), "s"(lds_base)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void dma16(const void* addr, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr),
+               "s"(lds_base)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+template <int kVm>
+__device__ __forceinline__ void stage_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kVm) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+template <int I, int N, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    static_for<I + 1, N>(f);
+  }
+}
+
+template <bool F16>
+__device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (F16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return mfma32(as_bf16x8(a), as_bf16x8(b), c);
+}
+
+// two values rounded to nearest even
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  if constexpr (F16) {
+    typedef __attribute__((ext_vector_type(2))) _Float16 h2;
+    return __builtin_bit_cast(uint32_t, h2{(_Float16)a, (_Float16)b});
+  } else {
+    typedef __attribute__((ext_vector_type(2))) __bf16 b2;
+    return __builtin_bit_cast(uint32_t, b2{(__bf16)a, (__bf16)b});
+  }
+}
+
+__device__ __forceinline__ float acc_val(float v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// across: XOR applied to the 32-byte unit index of row r (the four rows of a
+// transpose read land in distinct bank groups)
+__device__ __forceinline__ int swz(int r) { return (r & 3) ^ ((r & 3) << 1); }
+// across: byte offset of (row r, column c) of a 256-column operand, c % 4 == 0
+__device__ __forceinline__ uint32_t off_across(int r, int c) {
+  return (uint32_t)(r * 512 + 32 * ((c >> 4) ^ swz(r)) + 2 * (c & 15));
+}
+// along: byte offset of 16-byte piece p of row r
+__device__ __forceinline__ uint32_t off_along(int r, int p) {
+  return (uint32_t)(r * 64 + 16 * (p ^ ((r >> 2) & 3)));
+}
+
+// An operand's loads: wave w's four of a stage, and the addresses they need.
+// Rows (columns) past the array re-read its last one, steps past the
+// contraction's end its last ones; what they bring is masked or not stored.
+template <bool ALONG>
+struct Loader {
+  const uint8_t* base;  // the array, at the tile's first row (along) or column (across)
+  uint32_t row[4];      // along: byte offsets of the lane's rows; across: of its rows in a stage
+  uint32_t col[4];      // along: of its piece in a stage; across: of its columns
+  int64_t pitch;        // bytes of a row
+  int64_t K;
+
+  // left: rows (along) or columns (across; a multiple of 8) of the array from the tile on
+  __device__ __forceinline__ void begin(const uint8_t* b, int64_t left, int64_t pitch_,
+                                        int64_t K_, int wave, int lane) {
+    base = b;
+    pitch = pitch_;
+    K = K_;
+    const int most = (int)(left < 256 ? left : 256);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (ALONG) {
+        const int r = 64 * wave + 16 * i + (lane >> 2);
+        row[i] = (uint32_t)(r < most ? r : most - 1) * (uint32_t)pitch;
+        col[i] = 16u * (uint32_t)((lane & 3) ^ ((r >> 2) & 3));
+      } else {
+        const int r = 2 * (wave * 4 + i) + (lane >> 5), p = lane & 31;
+        const int c = 8 * (2 * ((p >> 1) ^ swz(r)) + (p & 1));
+        row[i] = (uint32_t)r * (uint32_t)pitch;
+        col[i] = 2u * (uint32_t)(c < most ? c : most - 8);
+      }
+    }
+  }
+  struct At {
+    const uint8_t* b;
+    uint32_t last;
+  };
+  __device__ __forceinline__ At stage(int st) const {
+    const int64_t k0 = (int64_t)st * kBK, left = K - k0 < kBK ? K - k0 : kBK;
+    if constexpr (ALONG)  // (whole pieces: the rows go on to a multiple of 8)
+      return At{base + 2 * k0, 16u * (uint32_t)((left - 1) >> 3)};
+    else
+      return At{base + k0 * pitch, (uint32_t)(left - 1) * (uint32_t)pitch};
+  }
+  template <int I>
+  __device__ __forceinline__ void load(const At& a, uint32_t dst) const {
+    if constexpr (ALONG)
+      dma16(a.b, row[I] + (col[I] < a.last ? col[I] : a.last), dst + 1024 * I);
+    else
+      dma16(a.b, (row[I] < a.last ? row[I] : a.last) + col[I], dst + 1024 * I);
+  }
+};
+
+// rows of h given by an index, anywhere in memory: 64-bit addresses
+struct RowLoader {
+  const uint8_t* row[4];
+  uint32_t col[4];
+  int64_t K;
+  __device__ __forceinline__ void begin(const uint8_t* h, const int* idx, int n0, int n,
+                                        int64_t pitch, int64_t K_, int wave, int lane) {
+    K = K_;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 64 * wave + 16 * i + (lane >> 2);
+      const int t = idx[n0 + r < n ? n0 + r : n - 1];
+      row[i] = h + (int64_t)t * pitch;
+      col[i] = 16u * (uint32_t)((lane & 3) ^ ((r >> 2) & 3));
+    }
+  }
+  struct At {
+    uint32_t k, last;
+  };
+  __device__ __forceinline__ At stage(int st) const {
+    const int64_t k0 = (int64_t)st * kBK, left = K - k0 < kBK ? K - k0 : kBK;
+    return At{(uint32_t)(2 * k0), 16u * (uint32_t)((left - 1) >> 3)};
+  }
+  template <int I>
+  __device__ __forceinline__ void load(const At& a, uint32_t dst) const {
+    dma16(row[I] + (a.k + (col[I] < a.last ? col[I] : a.last)), dst + 1024 * I);
+  }
+};
+
+// The main loop: acc = the tile's sums over stages s_beg .. s_end - 1 of a
+// contraction of K steps (s_end > s_beg).  ALONG_A, ALONG_B: how the operands lie.
+template <bool F16, bool ALONG_A, bool ALONG_B, typename LA, typename LB>
+__device__ __forceinline__ void product(uint8_t* lds, const LA& la, const LB& lb, int64_t K,
+                                        int s_beg, int s_end, f32x16 (&acc)[4][4]) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wy = wave >> 1, wx = wave & 1;
+  const int l32 = lane & 31, half = lane >> 5;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+  const int nst = (int)((K + kBK - 1) / kBK);
+
+#pragma unroll
+  for (int a = 0; a < 4; ++a)
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
+
+  struct DmaStage {
+    typename LA::At a;
+    typename LB::At b;
+    uint32_t dst;
+  };
+  auto dma_begin = [&](int st, int slot) {
+    st = st < s_end ? st : s_end - 1;  // past the range: reload its last stage
+    return DmaStage{la.stage(st), lb.stage(st), lds0 + slot * kSlot + 4096u * wave};
+  };
+  auto dma_piece = [&](const DmaStage& d, auto j_tag) {
+    constexpr int J = decltype(j_tag)::value, i = J % 4;
+    if constexpr (J < 4)
+      la.template load<i>(d.a, d.dst);
+    else
+      lb.template load<i>(d.b, d.dst + kOpA);
+  };
+  auto dma = [&](int st, int slot) {
+    const DmaStage d = dma_begin(st, slot);
+    static_for<0, kLoads>([&](auto j_tag) { dma_piece(d, j_tag); });
+  };
+
+#pragma unroll
+  for (int p = 0; p < kRing - 1; ++p) dma(s_beg + p, p);
+  stage_barrier<kLoads>();
+
+  // per-lane byte offsets of the operand reads in a stage
+  const int trow = 8 * half + ((lane & 15) >> 2);
+  const int tcol = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  uint32_t aoff[4], boff[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    aoff[x] = ALONG_A ? off_along(wy * 128 + 32 * x + l32, half)
+                      : off_across(trow, wy * 128 + 32 * x + tcol);
+    boff[x] = kOpA + (ALONG_B ? off_along(wx * 128 + 32 * x + l32, half)
+                              : off_across(trow, wx * 128 + 32 * x + tcol));
+  }
+  auto frag = [&](auto along_tag, const uint8_t* sb, uint32_t off, int t) {
+    if constexpr (decltype(along_tag)::value) {
+      return *reinterpret_cast<const u32x4*>(sb + (off ^ (uint32_t)(32 * t)));
+    } else {
+      const s16x4 lo =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(sb + off + 16 * t * 512));
+      const s16x4 hi =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(sb + off + (16 * t + 4) * 512));
+      const u32x2 l = __builtin_bit_cast(u32x2, lo), u = __builtin_bit_cast(u32x2, hi);
+      return u32x4{l.x, l.y, u.x, u.y};
+    }
+  };
+  auto frag_a = [&](const uint8_t* sb, int x, int t) {
+    return frag(std::integral_constant<bool, ALONG_A>{}, sb, aoff[x], t);
+  };
+  auto frag_b = [&](const uint8_t* sb, int x, int t) {
+    return frag(std::integral_constant<bool, ALONG_B>{}, sb, boff[x], t);
+  };
+  u32x4 af[2][4], bf[2][4];
+  auto read_op = [&](const uint8_t* sb, auto t_tag, auto x_tag) {
+    constexpr int T = decltype(t_tag)::value, X = decltype(x_tag)::value;
+    if constexpr (X == 0)
+      af[T][0] = frag_a(sb, 0, T);
+    else if constexpr (X < 5)
+      bf[T][X - 1] = frag_b(sb, X - 1, T);
+    else
+      af[T][X - 4] = frag_a(sb, X - 4, T);
+  };
+
+  // One full stage in ring slot SLOT.  Its first 16 MFMAs cover the reads of
+  // its second step (even slots) and the loads of stage st + 3 (odd slots), the
+  // second 16 the first reads of stage st + 1.
+  auto stage = [&](auto slot_tag, int st) {
+    constexpr int SLOT = decltype(slot_tag)::value;
+    const uint8_t* sb = lds + SLOT * kSlot;
+    const uint8_t* nb = lds + ((SLOT + 1) & (kRing - 1)) * kSlot;
+    const DmaStage d = dma_begin(st + kRing - 1, (SLOT + kRing - 1) & (kRing - 1));
+    static_for<0, 32>([&](auto k_tag) {
+      constexpr int k = decltype(k_tag)::value;
+      constexpr int t = k / 16, a = (k % 16) / 4, b = k % 4;
+      acc[a][b] = mfma<F16>(af[t][a], bf[t][b], acc[a][b]);
+      if constexpr (k % 2 == 0)
+        read_op(t == 0 ? sb : nb, std::integral_constant<int, 1 - t>{},
+                std::integral_constant<int, (k % 16) / 2>{});
+      else if constexpr (k < 16)
+        dma_piece(d, std::integral_constant<int, k / 2>{});
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  // the same without the overlap, for the last stages: steps past the end are
+  // zeros in both operands (what lies there may be an infinity)
+  auto stage_tail = [&](auto slot_tag, int st) {
+    constexpr int SLOT = decltype(slot_tag)::value;
+    const uint8_t* sb = lds + SLOT * kSlot;
+    const int64_t valid = K - (int64_t)st * kBK;
+#pragma unroll
+    for (int t = 0; t < kBK / 16; ++t) {
+      u32x4 ta[4], tb[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) ta[x] = frag_a(sb, x, t);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) tb[x] = frag_b(sb, x, t);
+      if (valid < kBK) {
+        const int first = 16 * t + 8 * half;  // this lane's eight steps
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int lo = first + 2 * e;
+          const uint32_t keep =
+              (lo < valid ? 0x0000FFFFu : 0u) | (lo + 1 < valid ? 0xFFFF0000u : 0u);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            ta[x][e] &= keep;
+            tb[x][e] &= keep;
+          }
+        }
+      }
+#pragma unroll
+      for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) acc[a][b] = mfma<F16>(ta[a], tb[b], acc[a][b]);
+    }
+  };
+
+  const int s_full = s_end < nst || K % kBK == 0 ? s_end : s_end - 1;
+  int st0 = s_beg;
+  if (st0 + kRing <= s_full)
+    static_for<0, 8>([&](auto x_tag) { read_op(lds, std::integral_constant<int, 0>{}, x_tag); });
+  for (; st0 + kRing <= s_full; st0 += kRing) {
+    static_for<0, kRing>([&](auto i_tag) {
+      stage(i_tag, st0 + decltype(i_tag)::value);
+      stage_barrier<kLoads>();
+    });
+  }
+  for (; st0 < s_end; st0 += kRing) {  // (the stages past s_end only load and wait)
+    static_for<0, kRing>([&](auto i_tag) {
+      constexpr int i = decltype(i_tag)::value;
+      const int st = st0 + i;
+      dma(st + kRing - 1, (i + kRing - 1) & (kRing - 1));
+      if (st < s_end) stage_tail(i_tag, st);
+      stage_barrier<kLoads>();
+    });
+  }
+  // every load has landed before the ring is used again
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+}
+
+// The items (token tile, word tile), words fastest, that workgroup w of P has:
+// a run floor(w N / P) .. floor((w + 1) N / P) - 1 of all N
+__device__ __forceinline__ int64_t run_begin(int64_t w, int64_t N, int64_t P) { return w * N / P; }
+
+}  // namespace
+
+// Logits: A = W (words), B = rows idx of h (tokens), so that a lane has one
+// token a block and 64 of its logits.  Lane: token 32 b + l32, words 32 a +
+// 8 (i / 4) + 4 half + i % 4.
+//
+// kStats: part[(workgroup + token tile)][wave row][256][2 or 4] = maximum and sum
+// of 2^(log2e (z - maximum)) over the run's words, and the same at the temperature
+// where TEMP.  A workgroup walks many word tiles of one token tile, so
+// a step of the softmax costs no memory.
+// kDlogits: G[row][word - w0] in 16 bits.
+template <bool F16, Mode MODE, bool TEMP>
+__global__ __launch_bounds__(256) void head_logits_kernel(
+    const uint16_t* __restrict__ h, const uint16_t* __restrict__ w, int D,
+    const int* __restrict__ idx, const int* __restrict__ count, int64_t words, float inv_tau,
+    float* __restrict__ part, const HeadRow* __restrict__ rows, uint16_t* __restrict__ G,
+    int64_t ld) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing * kSlot];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wy = wave >> 1, wx = wave & 1, l32 = lane & 31, half = lane >> 5;
+  const int n = __builtin_amdgcn_readfirstlane(*count);
+  const int nt = (n + kTN - 1) / kTN, nv = (int)((words + kTM - 1) / kTM);
+  const int64_t N = (int64_t)nt * nv, P = N < gridDim.x ? N : gridDim.x;  // (no empty runs)
+  const int64_t wg = xcd_remap(blockIdx.x, gridDim.x);
+  if (wg >= P) return;
+  const int64_t i0 = run_begin(wg, N, P), i1 = run_begin(wg + 1, N, P);
+  const int nst = (D + kBK - 1) / kBK;
+  const float k1 = kLog2e, k2 = kLog2e * inv_tau;
+
+  float mx[4], sm[4], st[4];  // the running maximum, its sum, the sum at the temperature
+  auto reset = [&]() {
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      mx[b] = -__builtin_inff();
+      sm[b] = st[b] = 0.f;
+    }
+  };
+  auto flush = [&](int tile) {  // the two halves of a token's words, then one entry a wave
+    constexpr int E = TEMP ? 3 : 2;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const float om = __shfl_xor(mx[b], 32, 64), os = __shfl_xor(sm[b], 32, 64);
+      const float m = fmaxf(mx[b], om);
+      const float ref = m == -__builtin_inff() ? 0.f : m;
+      const float s = sm[b] * __builtin_amdgcn_exp2f((mx[b] - ref) * k1) +
+                      os * __builtin_amdgcn_exp2f((om - ref) * k1);
+      float* p = part + ((((wg + tile) * 2 + wy) * 256) + wx * 128 + 32 * b + l32) * E;
+      float sT = 0.f;
+      if constexpr (TEMP) {
+        const float ot = __shfl_xor(st[b], 32, 64);
+        sT = st[b] * __builtin_amdgcn_exp2f((mx[b] - ref) * k2) +
+             ot * __builtin_amdgcn_exp2f((om - ref) * k2);
+      }
+      if (half == 0) {
+        p[0] = m;
+        p[1] = s;
+        if constexpr (TEMP) p[2] = sT;
+      }
+    }
+  };
+
+  int tile = -1;
+  HeadRow hr[4];
+  for (int64_t item = i0; item < i1; ++item) {
+    const int nt_i = (int)(item / nv), nv_i = (int)(item % nv);
+    if (nt_i != tile) {
+      if constexpr (MODE == kStats) {
+        if (tile >= 0) flush(tile);
+        reset();
+      } else {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const int r = nt_i * kTN + wx * 128 + 32 * b + l32;
+          hr[b] = rows[r < n ? r : n - 1];
+        }
+      }
+      tile = nt_i;
+    }
+    f32x16 acc[4][4];
+    {
+      Loader<true> la;
+      la.begin(reinterpret_cast<const uint8_t*>(w) + (int64_t)nv_i * kTM * D * 2,
+               words - (int64_t)nv_i * kTM, 2 * (int64_t)D, D, wave, lane);
+      RowLoader lb;
+      lb.begin(reinterpret_cast<const uint8_t*>(h), idx, nt_i * kTN, n, 2 * (int64_t)D, D, wave,
+               lane);
+      product<F16, true, true>(lds, la, lb, D, 0, nst, acc);
+    }
+    const int v0 = nv_i * kTM + wy * 128;  // the wave's first word
+    if constexpr (MODE == kStats) {
+      const int left = (int)(words - v0 < 128 ? words - v0 : 128) - 4 * half;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        float m = mx[b];
+        if (left + 4 * half < 128) {  // past the last word: no logit
+#pragma unroll
+          for (int a = 0; a < 4; ++a)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (32 * a + 8 * (i / 4) + i % 4 >= left) acc[a][b][i] = -__builtin_inff();
+        }
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) m = fmaxf(m, acc_val(acc[a][b][i]));
+        const float ref = m == -__builtin_inff() ? 0.f : m;
+        const float c1 = -ref * k1, c2 = -ref * k2;
+        float s = sm[b] * __builtin_amdgcn_exp2f((mx[b] - ref) * k1), s2 = 0.f;
+        if constexpr (TEMP) s2 = st[b] * __builtin_amdgcn_exp2f((mx[b] - ref) * k2);
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float z = acc_val(acc[a][b][i]);
+            s += __builtin_amdgcn_exp2f(__builtin_fmaf(z, k1, c1));
+            if constexpr (TEMP) s2 += __builtin_amdgcn_exp2f(__builtin_fmaf(z, k2, c2));
+          }
+        mx[b] = m;
+        sm[b] = s;
+        st[b] = s2;
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int r = nt_i * kTN + wx * 128 + 32 * b + l32;
+        uint16_t* g = G + (int64_t)r * ld + v0 + 8 * half;
+        auto dz = [&](float z) {
+          float p = hr[b].c1 * __builtin_amdgcn_exp2f(__builtin_fmaf(z, k1, -hr[b].lse));
+          if constexpr (TEMP)
+            p += hr[b].c2 * __builtin_amdgcn_exp2f(__builtin_fmaf(z, k2, -hr[b].lse_t));
+          return p;
+        };
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {  // 16 words: a lane's eight, exchanged to follow each other
+            uint32_t x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              x[i] = pack2<F16>(dz(acc_val(acc[a][b][8 * q + 2 * i])),
+                                dz(acc_val(acc[a][b][8 * q + 2 * i + 1])));
+            // lanes 32 .. 63 of x[0], x[1] change with lanes 0 .. 31 of x[2], x[3]
+            const auto e0 = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
+            const auto e1 = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
+            if (r < n) st16(g + 32 * a + 16 * q, u32x4{e0[0], e1[0], e0[1], e1[1]});
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+  }
+  if constexpr (MODE == kStats)
+    if (tile >= 0) flush(tile);
+}
+
+// op(pointer, value) for every element of the wave's 128 x 128 that is inside;
+// row by row through a pitch that the compiler cannot take apart (precomputed
+// offsets would need the accumulators' registers)
+template <typename T, typename Op>
+__device__ __forceinline__ void each_out(T* base, int64_t pitch, int64_t rows_left,
+                                         int64_t cols_left, const f32x16 (&acc)[4][4], Op op) {
+  const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+  int64_t pv = pitch;
+  asm volatile("" : "+v"(pv));
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      if (32 * b + l32 < cols_left) {
+        T* p = base + (int64_t)(32 * a) * pitch + 32 * b + (4 * half * pv + l32);
+        const int64_t left = rows_left - 32 * a - 4 * half;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          if (8 * (i / 4) + i % 4 < left) op(p, acc_val(acc[a][b][i]));
+          if (i < 15) p += i % 4 == 3 ? 5 * pv : pv;
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
+// dh: A = G (tokens; along the words), B = W (across).  The parts of the
+// contraction and the pieces of the vocabulary meet in part[s][row][D].
+template <bool F16>
+__global__ __launch_bounds__(256) void head_dh_kernel(
+    const uint16_t* __restrict__ G, int64_t ld, const uint16_t* __restrict__ w, int D,
+    const int* __restrict__ count, int64_t T, int64_t words, int parts, int per, int add,
+    float* __restrict__ part) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing * kSlot];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wy = wave >> 1, wx = wave & 1;
+  const int n = __builtin_amdgcn_readfirstlane(*count);
+  const int nt = (n + kTM - 1) / kTM, nd = (D + kTN - 1) / kTN;
+  const int64_t tiles = (int64_t)nt * nd, P = gridDim.x;
+  const int64_t wg = xcd_remap(blockIdx.x, gridDim.x);
+  const int nst = (int)((words + kBK - 1) / kBK);
+  for (int64_t item = wg; item < tiles * parts; item += P) {
+    const int s = (int)(item / tiles), tile = (int)(item % tiles);
+    const int64_t m0 = (int64_t)(tile / nd) * kTM;
+    const int d0 = tile % nd * kTN;
+    const int s_end = s * per + per < nst ? s * per + per : nst;
+    if (s * per >= s_end) continue;  // a last piece of fewer words: its part adds nothing
+    f32x16 acc[4][4];
+    {
+      Loader<true> la;
+      la.begin(reinterpret_cast<const uint8_t*>(G + m0 * ld), n - m0, 2 * ld, words, wave, lane);
+      Loader<false> lb;
+      lb.begin(reinterpret_cast<const uint8_t*>(w + d0), D - d0, 2 * (int64_t)D, words, wave,
+               lane);
+      product<F16, true, false>(lds, la, lb, words, s * per, s_end, acc);
+    }
+    const int64_t r0 = m0 + wy * 128;
+    const int c0 = d0 + wx * 128;
+    float* out = part + ((int64_t)s * T + r0) * D + c0;
+    if (add)
+      each_out(out, D, n - r0, D - c0, acc, [](float* p, float v) { *p += v; });
+    else
+      each_out(out, D, n - r0, D - c0, acc, [](float* p, float v) { *p = v; });
+  }
+}
+
+// dW: A = G (words), B = hs (columns), both across the tokens.  PARTS: to
+// part[s][word][D], unscaled; else to dW's rows, times 2^(*exp).
+template <bool F16, bool PARTS, typename O, bool ACC>
+__global__ __launch_bounds__(256) void head_dw_kernel(
+    const uint16_t* __restrict__ G, int64_t ld, const uint16_t* __restrict__ hs, int D,
+    const int* __restrict__ count, int64_t words, int parts, int per, const int* __restrict__ exp,
+    O* __restrict__ dw) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing * kSlot];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wy = wave >> 1, wx = wave & 1;
+  const int n = __builtin_amdgcn_readfirstlane(*count);
+  const int nv = (int)((words + kTM - 1) / kTM), nd = (D + kTN - 1) / kTN;
+  const int64_t tiles = (int64_t)nv * nd, P = gridDim.x;
+  const int64_t wg = xcd_remap(blockIdx.x, gridDim.x);
+  const int nst = (n + kBK - 1) / kBK;
+  const int e = PARTS ? 0 : __builtin_amdgcn_readfirstlane(*exp);
+  for (int64_t item = wg; item < tiles * parts; item += P) {
+    const int s = (int)(item / tiles), tile = (int)(item % tiles);
+    const int64_t m0 = (int64_t)(tile / nd) * kTM;
+    const int d0 = tile % nd * kTN;
+    const int s_end = s * per + per < nst ? s * per + per : nst;
+    f32x16 acc[4][4];
+    if (s * per < s_end) {
+      Loader<false> la, lb;
+      la.begin(reinterpret_cast<const uint8_t*>(G + m0), ld - m0, 2 * ld, n, wave, lane);
+      lb.begin(reinterpret_cast<const uint8_t*>(hs + d0), D - d0, 2 * (int64_t)D, n, wave, lane);
+      product<F16, false, false>(lds, la, lb, n, s * per, s_end, acc);
+    } else {  // fewer rows than the parts were made for
+#pragma unroll
+      for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
+    }
+    const int64_t r0 = m0 + wy * 128;
+    const int c0 = d0 + wx * 128;
+    O* out = dw + ((int64_t)s * words + r0) * D + c0;
+    each_out(out, D, words - r0, D - c0, acc, [&](O* p, float v) {
+      if constexpr (PARTS)
+        *p = v;
+      else if constexpr (ACC)
+        *p += ldexpf(v, e);
+      else
+        *p = (O)ldexpf(v, e);
+    });
+  }
+}
+
+// dW (+)= 2^(*exp) times the sum of the parts, in their order; n elements, a multiple of 8
+template <typename O, bool ACC>
+__global__ __launch_bounds__(256) void head_dw_sum_kernel(const float* __restrict__ part,
+                                                          int64_t n, int parts,
+                                                          const int* __restrict__ exp,
+                                                          O* __restrict__ dw) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  f32x4 v = *reinterpret_cast<const f32x4*>(part + i);
+  for (int s = 1; s < parts; ++s) v += *reinterpret_cast<const f32x4*>(part + s * n + i);
+  const int e = *exp;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float x = ldexpf(v[j], e);
+    if constexpr (ACC)
+      dw[i + j] += x;
+    else
+      dw[i + j] = (O)x;
+  }
+}
+
+int64_t head_part_floats(int64_t T) {
+  return (current_cu_count() + (T + kTN - 1) / kTN + 1) * 2 * 256 * 3;
+}
+
+#define TM_HEAD_GRID(GRID) dim3((unsigned)(GRID)), dim3(256), 0, stream
+
+static int64_t grid_of(int64_t items) {
+  const int64_t cus = current_cu_count();
+  return items < cus ? items : cus;
+}
+
+int head_logits_grid(int64_t T, int64_t words) {
+  return (int)grid_of(((T + kTN - 1) / kTN) * ((words + kTM - 1) / kTM));
+}
+
+template <bool F16, Mode MODE>
+static hipError_t run_logits(const HeadIn& in, const int* idx, const int* count, int64_t w0,
+                             int64_t n, float* part, const HeadRow* rows, uint16_t* G, int64_t ld,
+                             hipStream_t stream) {
+  const int grid = head_logits_grid(in.T, n);
+  const uint16_t* w = in.w + w0 * in.D;
+  if (in.K > 0 && in.tau != 1.0f)
+    hipLaunchKernelGGL((head_logits_kernel<F16, MODE, true>), TM_HEAD_GRID(grid), in.h,
+                       w, in.D, idx, count, n, 1.0f / in.tau, part, rows, G, ld);
+  else
+    hipLaunchKernelGGL((head_logits_kernel<F16, MODE, false>), TM_HEAD_GRID(grid), in.h,
+                       w, in.D, idx, count, n, 1.0f, part, rows, G, ld);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_logits(const HeadIn& in, const int* idx, const int* count, float* part,
+                              hipStream_t stream) {
+  return in.f16 ? run_logits<true, kStats>(in, idx, count, 0, in.V, part, nullptr, nullptr, 0, stream)
+                : run_logits<false, kStats>(in, idx, count, 0, in.V, part, nullptr, nullptr, 0,
+                                            stream);
+}
+
+hipError_t launch_head_dlogits(const HeadIn& in, const int* idx, const int* count,
+                               const HeadRow* rows, int64_t w0, int64_t n, uint16_t* G, int64_t ld,
+                               hipStream_t stream) {
+  return in.f16 ? run_logits<true, kDlogits>(in, idx, count, w0, n, nullptr, rows, G, ld, stream)
+                : run_logits<false, kDlogits>(in, idx, count, w0, n, nullptr, rows, G, ld, stream);
+}
+
+hipError_t launch_head_dh(const HeadIn& in, const int* count, const uint16_t* G, int64_t ld,
+                          int64_t w0, int64_t n, int parts, int per, bool add, float* part_h,
+                          hipStream_t stream) {
+  const int64_t items = ((in.T + kTM - 1) / kTM) * ((in.D + kTN - 1) / kTN) * parts;
+  const uint16_t* w = in.w + w0 * in.D;
+#define TM_HEAD_DH(F16)                                                                         \
+  hipLaunchKernelGGL(head_dh_kernel<F16>, TM_HEAD_GRID(grid_of(items)), G, ld, w, in.D, count, \
+                     in.T, n, parts, per, (int)add, part_h)
+  if (in.f16)
+    TM_HEAD_DH(true);
+  else
+    TM_HEAD_DH(false);
+#undef TM_HEAD_DH
+  return hipGetLastError();
+}
+
+template <bool F16, typename O, bool ACC>
+static hipError_t run_dw(const HeadIn& in, const int* count, const uint16_t* G, int64_t ld,
+                         const uint16_t* hs, int64_t n, int parts, int per, const int* exp, O* dw,
+                         float* part_w, hipStream_t stream) {
+  const int64_t items = ((n + kTM - 1) / kTM) * ((in.D + kTN - 1) / kTN) * parts;
+  if (parts == 1) {
+    hipLaunchKernelGGL((head_dw_kernel<F16, false, O, ACC>), TM_HEAD_GRID(grid_of(items)), G, ld,
+                       hs, in.D, count, n, 1, per, exp, dw);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((head_dw_kernel<F16, true, float, false>), TM_HEAD_GRID(grid_of(items)), G, ld,
+                     hs, in.D, count, n, parts, per, exp, part_w);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t all = n * in.D;
+  hipLaunchKernelGGL((head_dw_sum_kernel<O, ACC>), TM_HEAD_GRID((all / 4 + 255) / 256), part_w, all,
+                     parts, exp, dw);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_dw(const HeadIn& in, const int* count, const uint16_t* G, int64_t ld,
+                          const uint16_t* hs, int64_t w0, int64_t n, int parts, int per,
+                          const int* exp, void* dw, int dw_type, bool accumulate, float* part_w,
+                          hipStream_t stream) {
+#define TM_HEAD_DW(F16, O, ACC)                                                                 \
+  run_dw<F16, O, ACC>(in, count, G, ld, hs, n, parts, per, exp, static_cast<O*>(dw) + w0 * in.D, \
+                      part_w, stream)
+  if (dw_type == 0) {
+    if (accumulate) return in.f16 ? TM_HEAD_DW(true, float, true) : TM_HEAD_DW(false, float, true);
+    return in.f16 ? TM_HEAD_DW(true, float, false) : TM_HEAD_DW(false, float, false);
+  }
+  return in.f16 ? TM_HEAD_DW(true, _Float16, false) : TM_HEAD_DW(false, __bf16, false);
+#undef TM_HEAD_DW
+}
+
+}  // namespace tmk

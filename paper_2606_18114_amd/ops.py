@@ -128,6 +128,22 @@ SIGNATURES_SEQ = {
 }
 
 
+# the calls of include/tmamba_head.h
+SIGNATURES_HEAD = {
+    "tm_head_loss": (ctypes.c_int, [_P, _P, _I32, _I64, _I64, _I64, _P, _I32, _P, _I32, _P, _I32,
+                                    _I32, ctypes.c_float, ctypes.c_float, _P, _P, _P, _I64, _P]),
+    "tm_head_loss_workspace": (ctypes.c_int64, [_I64, _I64, _I64]),
+    "tm_head_loss_bwd": (ctypes.c_int, [_P, _P, _I32, _I64, _I64, _I64, _P, _I32, _P, _I32, _I32,
+                                        ctypes.c_float, ctypes.c_float, _P, _P, _P, _P, _I32, _I32,
+                                        _P, _I64, _P]),
+    "tm_head_loss_bwd_workspace": (ctypes.c_int64, [_I64, _I64, _I64]),
+    "tm_block_norm": (ctypes.c_int, [_P, _P, _I64, _I64, _P, ctypes.c_float, _P, _P, _P]),
+    "tm_block_norm_bwd": (ctypes.c_int, [_P, _I64, _I64, _P, ctypes.c_float, _P, _P, _P, _P, _P,
+                                         _I64, _P]),
+    "tm_block_norm_bwd_workspace": (ctypes.c_int64, [_I64, _I64]),
+}
+
+
 class TernaryError(RuntimeError):
     def __init__(self, fn: str, status: int):
         self.status = status
@@ -149,7 +165,8 @@ def lib() -> ctypes.CDLL:
                 "(or __graft_entry__.build()); there is no fallback implementation")
         L = ctypes.CDLL(_LIB_PATH)
         for name, (res, args) in (*SIGNATURES.items(), *SIGNATURES_PARTS.items(),
-                                  *SIGNATURES_DECODE16.items(), *SIGNATURES_SEQ.items()):
+                                  *SIGNATURES_DECODE16.items(), *SIGNATURES_SEQ.items(),
+                                  *SIGNATURES_HEAD.items()):
             f = getattr(L, name)
             f.restype = res
             f.argtypes = args
@@ -1187,3 +1204,159 @@ def embed_bwd(ids: torch.Tensor, dout: torch.Tensor, vocab: int, scale: float = 
     _call("tm_embed_bwd", dev, _ptr(ids), int(ids.dtype == torch.int64), T, _ptr(dout), vocab, D,
           scale, _ptr(dW), int(bool(accumulate)), wp, wb)
     return dW
+
+
+# ---- the ends of a training step: the head's loss, the block norm (include/tmamba_head.h) ----
+
+_HEAD_TYPE = {torch.bfloat16: 1, torch.float16: 2}
+HEAD_STATS = 4  # columns of head_loss's stats beside the teacher's words
+
+
+def _head_args(h, weight, targets, teacher_ids, alpha, temperature):
+    """Checks what both calls take; (device, T, V, D, K, the ABI's teacher arguments)."""
+    for t, name in ((h, "h"), (weight, "weight")):
+        if not isinstance(t, torch.Tensor) or t.dim() != 2:
+            _need(t, name, tuple(_HEAD_TYPE), 2)
+    dev = h.device
+    (T, D), V = h.shape, weight.shape[0]
+    _of(h, "h", _HEAD_TYPE, (T, D), dev)
+    _of(weight, "weight", (h.dtype,), (V, D), dev)
+    _of(targets, "targets", _IDS, (T,), dev)
+    K = 0
+    if teacher_ids is not None:
+        if not isinstance(teacher_ids, torch.Tensor) or teacher_ids.dim() != 2:
+            _need(teacher_ids, "teacher_ids", _IDS, 2)
+        K = teacher_ids.shape[1]
+        _of(teacher_ids, "teacher_ids", _IDS, (T, K), dev)
+        if K < 1:
+            raise ValueError("teacher_ids must hold at least one word a token")
+        if not 0.0 <= alpha <= 1.0:
+            raise ValueError(f"alpha must lie in 0 .. 1 (got {alpha})")
+        if not 0.0 < temperature < float("inf"):
+            raise ValueError(f"temperature must be positive and finite (got {temperature})")
+    return dev, T, V, D, K
+
+
+def head_loss(h: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
+              teacher_ids: Optional[torch.Tensor] = None,
+              teacher_logits: Optional[torch.Tensor] = None, *, alpha: float = 0.5,
+              temperature: float = 1.0, loss: Optional[torch.Tensor] = None):
+    """The losses of tokens from the head's input, without keeping the logits
+    h weight^T (tm_head_loss): h [T, D] and weight [V, D] bfloat16 or float16,
+    targets int32 or int64 [T] -> (loss float32 [T], stats for head_loss_bwd).
+    Cross entropy; with a teacher's top words and logits (teacher_ids [T, K]
+    int32 or int64, teacher_logits [T, K] float32, bfloat16 or float16)
+    (1 - alpha) CE + alpha temperature^2 KL(teacher's softmax over them ||
+    softmax), both at the temperature.  A target outside the vocabulary has no
+    CE, a token whose teacher holds no word of it (ids outside, logits
+    -infinity) no KL."""
+    dev, T, V, D, K = _head_args(h, weight, targets, teacher_ids, alpha, temperature)
+    if (teacher_logits is None) != (teacher_ids is None):
+        raise ValueError("teacher_ids and teacher_logits go together")
+    if teacher_logits is not None:
+        _of(teacher_logits, "teacher_logits", _EMBED_TYPE, (T, K), dev)
+    if loss is None:
+        loss = torch.empty((T,), dtype=torch.float32, device=dev)
+    else:
+        _of(loss, "loss", _F32, (T,), dev)
+    stats = torch.empty((T, HEAD_STATS + K), dtype=torch.float32, device=dev)
+    if T == 0:
+        return loss, stats
+    ws, wp, wb = _seq_ws("tm_head_loss_workspace", dev, T, V, D)
+    _call("tm_head_loss", dev, _ptr(h), _ptr(weight), _HEAD_TYPE[h.dtype], T, V, D, _ptr(targets),
+          int(targets.dtype == torch.int64), _ptr(teacher_ids),
+          int(K > 0 and teacher_ids.dtype == torch.int64), _ptr(teacher_logits),
+          _EMBED_TYPE[teacher_logits.dtype] if K > 0 else 0, K, alpha, temperature, _ptr(loss),
+          _ptr(stats), wp, wb)
+    return loss, stats
+
+
+def head_loss_bwd(h: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
+                  stats: torch.Tensor, dloss: torch.Tensor,
+                  teacher_ids: Optional[torch.Tensor] = None, *, alpha: float = 0.5,
+                  temperature: float = 1.0, dh: Optional[torch.Tensor] = None,
+                  dW: Optional[torch.Tensor] = None, accumulate: bool = False):
+    """Gradients of head_loss (tm_head_loss_bwd): dloss float32 [T] -> (dh
+    [T, D], dW [V, D]), both in h's type; dW float32 where a float32 one is
+    given, then also added to (accumulate).  The other arguments are the
+    forward call's."""
+    dev, T, V, D, K = _head_args(h, weight, targets, teacher_ids, alpha, temperature)
+    _of(stats, "stats", _F32, (T, HEAD_STATS + K), dev)
+    _of(dloss, "dloss", _F32, (T,), dev)
+    if dh is None:
+        dh = torch.empty_like(h)
+    else:
+        _of(dh, "dh", (h.dtype,), (T, D), dev)
+    if dW is None:
+        if accumulate:
+            raise ValueError("accumulate=True needs an existing dW")
+        dW = torch.empty_like(weight)
+    else:
+        _of(dW, "dW", (torch.float32,) if accumulate else (torch.float32, h.dtype), (V, D), dev)
+    if T == 0:
+        return dh, dW if accumulate else dW.zero_()
+    ws, wp, wb = _seq_ws("tm_head_loss_bwd_workspace", dev, T, V, D)
+    _call("tm_head_loss_bwd", dev, _ptr(h), _ptr(weight), _HEAD_TYPE[h.dtype], T, V, D,
+          _ptr(targets), int(targets.dtype == torch.int64), _ptr(teacher_ids),
+          int(K > 0 and teacher_ids.dtype == torch.int64), K, alpha, temperature, _ptr(stats),
+          _ptr(dloss), _ptr(dh), _ptr(dW), 0 if dW.dtype == torch.float32 else _HEAD_TYPE[h.dtype],
+          int(bool(accumulate)), wp, wb)
+    return dh, dW
+
+
+def block_norm(residual: torch.Tensor, y: Optional[torch.Tensor], w: torch.Tensor,
+               eps: float = 1e-5, *, residual_out: Optional[torch.Tensor] = None,
+               x: Optional[torch.Tensor] = None):
+    """The pre-norm of a block over rows (tm_block_norm): residual, y float32
+    [T, D] (y None: nothing is added), w float32 [D] -> (x bfloat16 [T, D] =
+    the RMS norm of residual + y, that sum).  residual_out may be residual;
+    without y the sum is residual itself unless residual_out is given."""
+    if not isinstance(residual, torch.Tensor) or residual.dim() != 2:
+        _need(residual, "residual", _F32, 2)
+    T, D = residual.shape
+    dev = residual.device
+    _of(residual, "residual", _F32, (T, D), dev)
+    _of(w, "w", _F32, (D,), dev)
+    if y is not None:
+        _of(y, "y", _F32, (T, D), dev)
+    if residual_out is not None:
+        _of(residual_out, "residual_out", _F32, (T, D), dev)
+    elif y is not None:
+        residual_out = torch.empty_like(residual)
+    if x is None:
+        x = torch.empty((T, D), dtype=torch.bfloat16, device=dev)
+    else:
+        _of(x, "x", _BF16, (T, D), dev)
+    if T > 0:
+        _call("tm_block_norm", dev, _ptr(residual), _ptr(y), T, D, _ptr(w), eps,
+              _ptr(residual_out), _ptr(x))
+    return x, residual if residual_out is None else residual_out
+
+
+def block_norm_bwd(residual: torch.Tensor, w: torch.Tensor, dx: torch.Tensor,
+                   dresidual: Optional[torch.Tensor] = None, eps: float = 1e-5, *,
+                   dr: Optional[torch.Tensor] = None):
+    """Gradients of block_norm (tm_block_norm_bwd): residual is the sum that it
+    returned, dx bfloat16 [T, D], dresidual float32 [T, D] that sum's gradient
+    (None: zeros) -> (dr float32 [T, D], the gradient of residual and of y;
+    dw float32 [D]).  dr may be dresidual."""
+    if not isinstance(residual, torch.Tensor) or residual.dim() != 2:
+        _need(residual, "residual", _F32, 2)
+    T, D = residual.shape
+    dev = residual.device
+    _of(residual, "residual", _F32, (T, D), dev)
+    _of(w, "w", _F32, (D,), dev)
+    _of(dx, "dx", _BF16, (T, D), dev)
+    if dresidual is not None:
+        _of(dresidual, "dresidual", _F32, (T, D), dev)
+    if dr is None:
+        dr = torch.empty_like(residual)
+    else:
+        _of(dr, "dr", _F32, (T, D), dev)
+    dw = torch.empty((D,), dtype=torch.float32, device=dev)
+    if T == 0:
+        return dr, dw.zero_()
+    ws, wp, wb = _seq_ws("tm_block_norm_bwd_workspace", dev, T, D)
+    _call("tm_block_norm_bwd", dev, _ptr(residual), T, D, _ptr(w), eps, _ptr(dx), _ptr(dresidual),
+          _ptr(dr), _ptr(dw), wp, wb)
+    return dr, dw
