@@ -32,7 +32,7 @@ extern "C" {
  *              (top_type 0), bfloat16 (1) or float16 (2); both NULL with K = 0: no teacher
  *   alpha      0 .. 1, tau > 0, finite (both ignored without a teacher)
  *   loss       float32 [T]
- *   stats      float32 [T, 4 + K]: what tm_head_loss_bwd needs of this call
+ *   stats      float32 [T (4 + K)]: what tm_head_loss_bwd needs of this call
  *   T 1 .. 2^23, V 1 .. 2^23, D 8 .. 2^16, K 0 .. 1024, T (K + 1) < 2^31
  * Products are exact, sums and softmax statistics float32.
  */

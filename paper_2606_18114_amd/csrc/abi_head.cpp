@@ -68,7 +68,7 @@ tm_status head_checked(const void* h, const void* W, int32_t type, int64_t T, in
 extern "C" {
 
 int64_t tm_head_loss_workspace(int64_t T, int64_t V, int64_t D) {
-  return head_sizes(T, V, D) ? tmk::head_loss_bytes(T, V) : -1;
+  return head_sizes(T, V, D) ? tmk::head_loss_bytes(T, D) : -1;
 }
 
 tm_status tm_head_loss(const void* h, const void* W, int32_t type, int64_t T, int64_t V, int64_t D,
@@ -82,12 +82,12 @@ tm_status tm_head_loss(const void* h, const void* W, int32_t type, int64_t T, in
                                   alpha, tau, &in))
     return st;
   if ((K > 0) != (top != nullptr)) return TM_EINVAL;
-  const int64_t need = tmk::head_loss_bytes(T, V), te = top_type == 0 ? 4 : 2;
+  const int64_t need = tmk::head_loss_bytes(T, D), te = top_type == 0 ? 4 : 2;
   if (tm_status st = ws_checked(workspace, workspace_bytes, need)) return st;
   if (!aligned(top, (uintptr_t)te) || !aligned(loss, 4) || !aligned(stats, 4)) return TM_EALIGN;
   if (!apart({span(h, T * D * 2), span(W, V * D * 2), span(labels, T * (labels_i64 ? 8 : 4)),
               opt(top_ids, T * K * (ids_i64 ? 8 : 4)), opt(top, T * K * te)},
-             {span(loss, T * 4), span(stats, T * tmk::head_stats_cols(K) * 4),
+             {span(loss, T * 4), span(stats, tmk::head_stats_floats(T, K) * 4),
               span(workspace, need)}))
     return TM_EINVAL;
   return hip_status(tmk::launch_head_loss(in, top, top_type, loss, stats, workspace,
@@ -116,7 +116,7 @@ tm_status tm_head_loss_bwd(const void* h, const void* W, int32_t type, int64_t T
     return TM_EALIGN;
   if (!apart({span(h, T * D * 2), span(W, V * D * 2), span(labels, T * (labels_i64 ? 8 : 4)),
               opt(top_ids, T * K * (ids_i64 ? 8 : 4)),
-              span(stats, T * tmk::head_stats_cols(K) * 4), span(dloss, T * 4)},
+              span(stats, tmk::head_stats_floats(T, K) * 4), span(dloss, T * 4)},
              {span(dh, T * D * 2), span(dW, V * D * (dW_type == 0 ? 4 : 2)),
               span(workspace, need)}))
     return TM_EINVAL;

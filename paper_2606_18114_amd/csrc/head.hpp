@@ -22,12 +22,13 @@ struct HeadIn {
   float alpha, tau;  // (0, 1 without a teacher)
 };
 
-// A token's row of `stats`: log2 of its sum of exponentials, the same at the
-// temperature, which terms it has (1: cross entropy, 2: divergence), then the
-// logit gradient (of the loss over head_unit) at its label and at the teacher's words.
-constexpr int kHeadStatLse = 0, kHeadStatLseT = 1, kHeadStatTerms = 2, kHeadStatLabel = 3,
-              kHeadStatTop = 4;
-inline __host__ __device__ int64_t head_stats_cols(int64_t K) { return kHeadStatTop + K; }
+// `stats`: four planes [T], log2 of the sum of exponentials, the same at the temperature,
+// which terms a token has (1: cross entropy, 2: divergence), the logit gradient (of
+// the loss over head_unit) at its label; then [T, K], that gradient at the teacher's words.
+enum HeadStat { kStatLse, kStatLseT, kStatTerms, kStatLabel, kStatPlanes };
+inline __host__ __device__ int64_t head_stats_floats(int64_t T, int64_t K) {
+  return (kStatPlanes + K) * T;
+}
 
 // |gradient of a logit| <= head_unit * |dloss|; the gradient over it is what
 // is held in 16 bits
@@ -52,10 +53,11 @@ struct HeadPlan {
   int64_t piece = 0, pieces = 0;  // words (a multiple of 256) of a piece; their number
   int parts_h = 1, per_h = 0;     // dh's contraction (words of a piece), stages of 32
   int parts_w = 1, per_w = 0;     // dW's contraction (tokens)
+  int last_w = 1, last_per = 0;   // the same of the last piece
 };
 HeadPlan head_plan(int64_t T, int64_t V, int64_t D);
 
-int64_t head_loss_bytes(int64_t T, int64_t V);
+int64_t head_loss_bytes(int64_t T, int64_t D);
 hipError_t launch_head_loss(const HeadIn& in, const void* top, int top_type, float* loss,
                             float* stats, void* workspace, hipStream_t stream);
 int64_t head_loss_bwd_bytes(int64_t T, int64_t V, int64_t D);
@@ -73,13 +75,15 @@ hipError_t launch_block_norm_bwd(const float* r, int64_t T, int d, const float* 
                                  void* workspace, hipStream_t stream);
 
 // ---- products (head_gemm.hip); `count` [1]: rows in use, on the device
-// partial softmax sums of the rows idx: part[(wg + tile)][half][token][pair], see head_loss.hip
+// ht [D, head_padded(T)]: the transposed rows in use.
+inline int64_t head_padded(int64_t T) { return (T + 255) / 256 * 256; }
+// partial softmax sums of the rows: part[(wg + tile)][half][token][pair], see head_loss.hip
 int64_t head_part_floats(int64_t T);
 int head_logits_grid(int64_t T, int64_t words);  // its workgroups
-hipError_t launch_head_logits(const HeadIn& in, const int* idx, const int* count, float* part,
+hipError_t launch_head_logits(const HeadIn& in, const uint16_t* ht, const int* count, float* part,
                               hipStream_t stream);
 // dlogits of words w0 .. w0 + n - 1 to G [rows, ld], ld >= n rounded up to 256
-hipError_t launch_head_dlogits(const HeadIn& in, const int* idx, const int* count,
+hipError_t launch_head_dlogits(const HeadIn& in, const uint16_t* ht, const int* count,
                                const HeadRow* rows, int64_t w0, int64_t n, uint16_t* G, int64_t ld,
                                hipStream_t stream);
 // part_h[s][row][D] (+)= the s-th part of G . W[w0 ..]

@@ -8,14 +8,16 @@
 // words that its workgroup walks; backward the tile becomes 16-bit dlogits of one
 // piece of the vocabulary, which dh and dW contract.
 //
-// One main loop for the three.  Operands lie along the contraction (h, W for
-// the logits, G for dh) or across it (W for dh; G and h for dW).  Tiles are
-// staged in LDS in their natural order by direct-to-LDS loads, 32 steps of the
-// contraction a stage, in a ring of four stages.  Along: rows of 64 bytes,
-// whose 16-byte pieces are XOR-permuted so that 16 rows read at one step lie in
-// different banks; one ds_read_b128 is an operand.  Across: rows of 512 bytes
-// in permuted 32-byte units, read with the transpose read ds_read_b64_tr_b16, two
-// an operand.
+// One main loop for the three.  The first operand lies along the contraction (W
+// for the logits, G for dh) or across it (G for dW), the second across it (h^T for
+// the logits, W for dh, h for dW).  Tiles are staged in LDS in their natural order
+// by direct-to-LDS loads, 32 steps of the contraction a stage.  Across: rows of 512
+// bytes, in 32-byte units that are XOR-permuted against bank conflicts, read with
+// the transpose read ds_read_b64_tr_b16, two an operand; a ring of four stages, loaded
+// three ahead.  Along: 128-byte rows, the lines of the caches, hold two stages (with
+// 64-byte rows, one stage, the requests to the L2 double, and a stage took 1.05 us, not
+// XXX); their 16-byte pieces are XOR-permuted, one ds_read_b128 is an operand;
+// three pairs of stages, loaded two pairs ahead.
 //
 // Tile 256 x 256 of 4 waves, 128 x 128 each (4 x 4 blocks of 32 x 32,
 // accumulators in AGPRs, one wave a SIMD), every MFMA a slot of its own with the
@@ -32,8 +34,11 @@ namespace {
 
 constexpr int kBK = 32, kRing = 4;
 constexpr int kTM = 256, kTN = 256;
-constexpr int kOpA = kTM * kBK * 2, kOpB = kTN * kBK * 2;
-constexpr int kSlot = kOpA + kOpB;
+constexpr int kOp = kTM * kBK * 2;  // an operand's bytes of a stage
+// LDS: the ring of the second operand, then the first's: a ring, or three pairs
+constexpr int kLdsB = kRing * kOp;
+template <bool ALONG>
+constexpr int kLds = kLdsB + (ALONG ? 6 : kRing) * kOp;
 constexpr int kLoads = 8;  // direct-to-LDS loads of a wave and stage
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -49,11 +54,6 @@ enum Mode { kStats, kDlogits, kDh, kDw };
 __device__ __forceinline__ void dma16(const void* base, uint32_t voff, uint32_t lds_base) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff),
                "s"(base), "s"(lds_base)
-               : "memory", "m0");
-}
-__device__ __forceinline__ void dma16(const void* addr, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr),
-               "s"(lds_base)
                : "memory", "m0");
 }
 #pragma clang diagnostic pop
@@ -108,34 +108,41 @@ __device__ __forceinline__ uint32_t off_across(int r, int c) {
 }
 // along: byte offset of 16-byte piece p of row r
 __device__ __forceinline__ uint32_t off_along(int r, int p) {
-  return (uint32_t)(r * 64 + 16 * (p ^ ((r >> 2) & 3)));
+  return (uint32_t)(r * 128 + 16 * (p ^ ((r >> 1) & 7)));
 }
 
-// An operand's loads: wave w's four of a stage, and the addresses they need.
-// Rows (columns) past the array re-read its last one, steps past the
-// contraction's end its last ones; what they bring is masked or not stored.
+// An operand's loads and the addresses they need: four of a wave and stage.  Along,
+// the two stages of a pair load half of the rows each.  Rows (columns) past the
+// array re-read its last one, steps past the contraction's end its last ones;
+// what they bring is masked or not stored.
 template <bool ALONG>
 struct Loader {
   const uint8_t* base;  // the array, at the tile's first row (along) or column (across)
-  uint32_t row[4];      // along: byte offsets of the lane's rows; across: of its rows in a stage
-  uint32_t col[4];      // along: of its piece in a stage; across: of its columns
-  int64_t pitch;        // bytes of a row
+  // along: byte offsets of the lane's rows in the array, of its piece in a row (the same
+  // for all); across: of its rows in a stage, of its columns
+  uint32_t row[ALONG ? 8 : 4];
+  uint32_t col[ALONG ? 1 : 4];
+  int64_t pitch;  // bytes of a row
   int64_t K;
 
   // left: rows (along) or columns (across; a multiple of 8) of the array from the tile on
-  __device__ __forceinline__ void begin(const uint8_t* b, int64_t left, int64_t pitch_,
+  __device__ __forceinline__ void begin(const uint16_t* b, int64_t left, int64_t pitch_,
                                         int64_t K_, int wave, int lane) {
-    base = b;
-    pitch = pitch_;
+    base = reinterpret_cast<const uint8_t*>(b);
+    pitch = 2 * pitch_;
     K = K_;
     const int most = (int)(left < 256 ? left : 256);
+    if constexpr (ALONG) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (ALONG) {
-        const int r = 64 * wave + 16 * i + (lane >> 2);
+      for (int i = 0; i < 8; ++i) {  // 8 rows a load; wave w's are 64 w ..
+        const int r = 64 * wave + 8 * i + (lane >> 3);
         row[i] = (uint32_t)(r < most ? r : most - 1) * (uint32_t)pitch;
-        col[i] = 16u * (uint32_t)((lane & 3) ^ ((r >> 2) & 3));
-      } else {
+      }
+      // (r >> 1) & 7 = (4 i + (lane >> 4)) & 7: the upper bit is i's parity
+      col[0] = 16u * (uint32_t)((lane & 7) ^ (lane >> 4));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
         const int r = 2 * (wave * 4 + i) + (lane >> 5), p = lane & 31;
         const int c = 8 * (2 * ((p >> 1) ^ swz(r)) + (p & 1));
         row[i] = (uint32_t)r * (uint32_t)pitch;
@@ -147,8 +154,10 @@ struct Loader {
     const uint8_t* b;
     uint32_t last;
   };
+  // st: a stage (across), or a pair (along)
   __device__ __forceinline__ At stage(int st) const {
-    const int64_t k0 = (int64_t)st * kBK, left = K - k0 < kBK ? K - k0 : kBK;
+    constexpr int kSteps = ALONG ? 2 * kBK : kBK;
+    const int64_t k0 = (int64_t)st * kSteps, left = K - k0 < kSteps ? K - k0 : kSteps;
     if constexpr (ALONG)  // (whole pieces: the rows go on to a multiple of 8)
       return At{base + 2 * k0, 16u * (uint32_t)((left - 1) >> 3)};
     else
@@ -156,47 +165,21 @@ struct Loader {
   }
   template <int I>
   __device__ __forceinline__ void load(const At& a, uint32_t dst) const {
-    if constexpr (ALONG)
-      dma16(a.b, row[I] + (col[I] < a.last ? col[I] : a.last), dst + 1024 * I);
-    else
+    if constexpr (ALONG) {
+      const uint32_t c = I & 1 ? col[0] ^ 64u : col[0];
+      dma16(a.b, row[I] + (c < a.last ? c : a.last), dst + 1024 * I);
+    } else {
       dma16(a.b, (row[I] < a.last ? row[I] : a.last) + col[I], dst + 1024 * I);
-  }
-};
-
-// rows of h given by an index, anywhere in memory: 64-bit addresses
-struct RowLoader {
-  const uint8_t* row[4];
-  uint32_t col[4];
-  int64_t K;
-  __device__ __forceinline__ void begin(const uint8_t* h, const int* idx, int n0, int n,
-                                        int64_t pitch, int64_t K_, int wave, int lane) {
-    K = K_;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = 64 * wave + 16 * i + (lane >> 2);
-      const int t = idx[n0 + r < n ? n0 + r : n - 1];
-      row[i] = h + (int64_t)t * pitch;
-      col[i] = 16u * (uint32_t)((lane & 3) ^ ((r >> 2) & 3));
     }
   }
-  struct At {
-    uint32_t k, last;
-  };
-  __device__ __forceinline__ At stage(int st) const {
-    const int64_t k0 = (int64_t)st * kBK, left = K - k0 < kBK ? K - k0 : kBK;
-    return At{(uint32_t)(2 * k0), 16u * (uint32_t)((left - 1) >> 3)};
-  }
-  template <int I>
-  __device__ __forceinline__ void load(const At& a, uint32_t dst) const {
-    dma16(row[I] + (a.k + (col[I] < a.last ? col[I] : a.last)), dst + 1024 * I);
-  }
 };
 
-// The main loop: acc = the tile's sums over stages s_beg .. s_end - 1 of a
-// contraction of K steps (s_end > s_beg).  ALONG_A, ALONG_B: how the operands lie.
-template <bool F16, bool ALONG_A, bool ALONG_B, typename LA, typename LB>
-__device__ __forceinline__ void product(uint8_t* lds, const LA& la, const LB& lb, int64_t K,
-                                        int s_beg, int s_end, f32x16 (&acc)[4][4]) {
+// The main loop: acc = the tile's sums over stages s_beg .. s_end - 1 (s_end > s_beg;
+// along, s_beg is even) of a contraction of K steps.
+template <bool F16, bool ALONG>
+__device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
+                                        const Loader<false>& lb, int64_t K, int s_beg, int s_end,
+                                        f32x16 (&acc)[4][4]) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wy = wave >> 1, wx = wave & 1;
@@ -211,104 +194,130 @@ __device__ __forceinline__ void product(uint8_t* lds, const LA& la, const LB& lb
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
 
+  // Stages and slots are counted from s_beg.  Past the range the last stage is loaded again.
   struct DmaStage {
-    typename LA::At a;
-    typename LB::At b;
-    uint32_t dst;
+    typename Loader<ALONG>::At a;
+    typename Loader<false>::At b;
+    uint32_t adst, bdst;
   };
-  auto dma_begin = [&](int st, int slot) {
-    st = st < s_end ? st : s_end - 1;  // past the range: reload its last stage
-    return DmaStage{la.stage(st), lb.stage(st), lds0 + slot * kSlot + 4096u * wave};
+  // the loads that go with stage i: the second operand's stage i + 3 and the first's, or
+  // half of its pair i / 2 + 2, to slot aslot
+  auto dma_begin = [&](int i, uint32_t aslot) {
+    const int st = s_beg + i + 3 < s_end ? s_beg + i + 3 : s_end - 1;
+    DmaStage d;
+    d.b = lb.stage(st);
+    d.bdst = lds0 + (uint32_t)((i + 3) & 3) * kOp + 4096u * wave;
+    if constexpr (ALONG) {
+      const int pair = s_beg / 2 + (i >> 1) + 2, end = (s_end - 1) / 2;
+      d.a = la.stage(pair < end ? pair : end);
+      d.adst = lds0 + kLdsB + aslot * (2 * kOp) + 8192u * wave;
+    } else {
+      d.a = la.stage(st);
+      d.adst = lds0 + kLdsB + (uint32_t)((i + 3) & 3) * kOp + 4096u * wave;
+    }
+    return d;
   };
-  auto dma_piece = [&](const DmaStage& d, auto j_tag) {
-    constexpr int J = decltype(j_tag)::value, i = J % 4;
+  // load J of the eight of stage i (par = i % 2)
+  auto dma_piece = [&](const DmaStage& d, auto j_tag, auto par_tag) {
+    constexpr int J = decltype(j_tag)::value, I = J % 4, kPar = decltype(par_tag)::value;
     if constexpr (J < 4)
-      la.template load<i>(d.a, d.dst);
+      la.template load<ALONG ? 4 * kPar + I : I>(d.a, d.adst);
     else
-      lb.template load<i>(d.b, d.dst + kOpA);
-  };
-  auto dma = [&](int st, int slot) {
-    const DmaStage d = dma_begin(st, slot);
-    static_for<0, kLoads>([&](auto j_tag) { dma_piece(d, j_tag); });
+      lb.template load<I>(d.b, d.bdst);
   };
 
-#pragma unroll
-  for (int p = 0; p < kRing - 1; ++p) dma(s_beg + p, p);
+  {  // the first three stages of the second operand, three stages or two pairs of the first
+    static_for<0, 4>([&](auto p_tag) {
+      constexpr int p = decltype(p_tag)::value;
+      if constexpr (!ALONG && p == 0) return;
+      const DmaStage d = dma_begin(p - 4, ALONG ? (uint32_t)(p / 2) : 0u);
+      // (stage p - 4: the second operand's p - 1, the first's p - 1 or pair p / 2)
+      static_for<0, kLoads>([&](auto j_tag) {
+        if constexpr (p > 0 || decltype(j_tag)::value < 4)
+          dma_piece(d, j_tag, std::integral_constant<int, p % 2>{});
+      });
+    });
+  }
   stage_barrier<kLoads>();
 
-  // per-lane byte offsets of the operand reads in a stage
+  // per-lane byte offsets of the operand reads: across, of the four blocks in a stage;
+  // along, of the four steps of a pair
   const int trow = 8 * half + ((lane & 15) >> 2);
   const int tcol = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
   uint32_t aoff[4], boff[4];
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
-    aoff[x] = ALONG_A ? off_along(wy * 128 + 32 * x + l32, half)
-                      : off_across(trow, wy * 128 + 32 * x + tcol);
-    boff[x] = kOpA + (ALONG_B ? off_along(wx * 128 + 32 * x + l32, half)
-                              : off_across(trow, wx * 128 + 32 * x + tcol));
+    aoff[x] = kLdsB + (ALONG ? off_along(wy * 128 + l32, 2 * x + half)
+                             : off_across(trow, wy * 128 + 32 * x + tcol));
+    boff[x] = off_across(trow, wx * 128 + 32 * x + tcol);
   }
-  auto frag = [&](auto along_tag, const uint8_t* sb, uint32_t off, int t) {
-    if constexpr (decltype(along_tag)::value) {
-      return *reinterpret_cast<const u32x4*>(sb + (off ^ (uint32_t)(32 * t)));
-    } else {
-      const s16x4 lo =
-          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(sb + off + 16 * t * 512));
-      const s16x4 hi =
-          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(sb + off + (16 * t + 4) * 512));
-      const u32x2 l = __builtin_bit_cast(u32x2, lo), u = __builtin_bit_cast(u32x2, hi);
-      return u32x4{l.x, l.y, u.x, u.y};
-    }
+  auto across = [&](uint32_t off, int t) {
+    const s16x4 lo =
+        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + off + 16 * t * 512));
+    const s16x4 hi =
+        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + off + (16 * t + 4) * 512));
+    const u32x2 l = __builtin_bit_cast(u32x2, lo), u = __builtin_bit_cast(u32x2, hi);
+    return u32x4{l.x, l.y, u.x, u.y};
   };
-  auto frag_a = [&](const uint8_t* sb, int x, int t) {
-    return frag(std::integral_constant<bool, ALONG_A>{}, sb, aoff[x], t);
+  // operands of block x, step t of the stage in slot S (along: of the pair whose slot's
+  // offset is apair)
+  auto frag_a = [&](uint32_t apair, auto s_tag, int x, int t) {
+    constexpr int S = decltype(s_tag)::value;
+    if constexpr (ALONG)
+      return *reinterpret_cast<const u32x4*>(lds + (aoff[2 * (S & 1) + t] + apair) + 4096 * x);
+    else
+      return across(aoff[x] + S * kOp, t);
   };
-  auto frag_b = [&](const uint8_t* sb, int x, int t) {
-    return frag(std::integral_constant<bool, ALONG_B>{}, sb, boff[x], t);
+  auto frag_b = [&](auto s_tag, int x, int t) {
+    return across(boff[x] + decltype(s_tag)::value * kOp, t);
   };
   u32x4 af[2][4], bf[2][4];
-  auto read_op = [&](const uint8_t* sb, auto t_tag, auto x_tag) {
+  auto read_op = [&](uint32_t apair, auto s_tag, auto t_tag, auto x_tag) {
     constexpr int T = decltype(t_tag)::value, X = decltype(x_tag)::value;
     if constexpr (X == 0)
-      af[T][0] = frag_a(sb, 0, T);
+      af[T][0] = frag_a(apair, s_tag, 0, T);
     else if constexpr (X < 5)
-      bf[T][X - 1] = frag_b(sb, X - 1, T);
+      bf[T][X - 1] = frag_b(s_tag, X - 1, T);
     else
-      af[T][X - 4] = frag_a(sb, X - 4, T);
+      af[T][X - 4] = frag_a(apair, s_tag, X - 4, T);
   };
 
-  // One full stage in ring slot SLOT.  Its first 16 MFMAs cover the reads of
-  // its second step (even slots) and the loads of stage st + 3 (odd slots), the
-  // second 16 the first reads of stage st + 1.
-  auto stage = [&](auto slot_tag, int st) {
-    constexpr int SLOT = decltype(slot_tag)::value;
-    const uint8_t* sb = lds + SLOT * kSlot;
-    const uint8_t* nb = lds + ((SLOT + 1) & (kRing - 1)) * kSlot;
-    const DmaStage d = dma_begin(st + kRing - 1, (SLOT + kRing - 1) & (kRing - 1));
+  // One full stage, i % 4 = S.  Its first 16 MFMAs cover the reads of its second
+  // step (even slots) and the loads (odd slots), the second 16 the first reads of the
+  // next stage.  a0, a1: slots (0 .. 2) of the pairs of this stage and the next one, a2 of
+  // the pair that is loaded.
+  auto stage = [&](auto s_tag, int i, uint32_t a0, uint32_t a1, uint32_t a2) {
+    constexpr int S = decltype(s_tag)::value;
+    typedef std::integral_constant<int, (S + 1) & 3> Next;
+    const DmaStage d = dma_begin(i, a2);
+    const uint32_t p0 = a0 * (2 * kOp), p1 = (S & 1 ? a1 : a0) * (2 * kOp);
     static_for<0, 32>([&](auto k_tag) {
       constexpr int k = decltype(k_tag)::value;
       constexpr int t = k / 16, a = (k % 16) / 4, b = k % 4;
       acc[a][b] = mfma<F16>(af[t][a], bf[t][b], acc[a][b]);
-      if constexpr (k % 2 == 0)
-        read_op(t == 0 ? sb : nb, std::integral_constant<int, 1 - t>{},
-                std::integral_constant<int, (k % 16) / 2>{});
-      else if constexpr (k < 16)
-        dma_piece(d, std::integral_constant<int, k / 2>{});
+      typedef std::integral_constant<int, (k % 16) / 2> X;
+      if constexpr (k % 2 == 0) {
+        if constexpr (t == 0)
+          read_op(p0, s_tag, std::integral_constant<int, 1>{}, X{});
+        else
+          read_op(p1, Next{}, std::integral_constant<int, 0>{}, X{});
+      } else if constexpr (k < 16) {
+        dma_piece(d, std::integral_constant<int, k / 2>{}, std::integral_constant<int, S & 1>{});
+      }
       __builtin_amdgcn_sched_barrier(0);
     });
   };
   // the same without the overlap, for the last stages: steps past the end are
   // zeros in both operands (what lies there may be an infinity)
-  auto stage_tail = [&](auto slot_tag, int st) {
-    constexpr int SLOT = decltype(slot_tag)::value;
-    const uint8_t* sb = lds + SLOT * kSlot;
-    const int64_t valid = K - (int64_t)st * kBK;
+  auto stage_tail = [&](auto s_tag, int i, uint32_t a0) {
+    const int64_t valid = K - (int64_t)(s_beg + i) * kBK;
 #pragma unroll
     for (int t = 0; t < kBK / 16; ++t) {
       u32x4 ta[4], tb[4];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) ta[x] = frag_a(sb, x, t);
+      for (int x = 0; x < 4; ++x) ta[x] = frag_a(a0 * (2 * kOp), s_tag, x, t);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) tb[x] = frag_b(sb, x, t);
+      for (int x = 0; x < 4; ++x) tb[x] = frag_b(s_tag, x, t);
       if (valid < kBK) {
         const int first = 16 * t + 8 * half;  // this lane's eight steps
 #pragma unroll
@@ -330,22 +339,37 @@ __device__ __forceinline__ void product(uint8_t* lds, const LA& la, const LB& lb
     }
   };
 
-  const int s_full = s_end < nst || K % kBK == 0 ? s_end : s_end - 1;
-  int st0 = s_beg;
-  if (st0 + kRing <= s_full)
-    static_for<0, 8>([&](auto x_tag) { read_op(lds, std::integral_constant<int, 0>{}, x_tag); });
-  for (; st0 + kRing <= s_full; st0 += kRing) {
-    static_for<0, kRing>([&](auto i_tag) {
-      stage(i_tag, st0 + decltype(i_tag)::value);
+  const int total = s_end - s_beg;
+  const int full = s_end < nst || K % kBK == 0 ? total : total - 1;
+  uint32_t a0 = 0, a1 = 1, a2 = 2;  // slots of this pair, the next one and the one to load
+  auto turn = [&]() {
+    const uint32_t t = a0;
+    a0 = a1;
+    a1 = a2;
+    a2 = t;
+  };
+  int i0 = 0;
+  if (kRing <= full)
+    static_for<0, 8>([&](auto x_tag) {
+      read_op(0, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{}, x_tag);
+    });
+  for (; i0 + kRing <= full; i0 += kRing) {
+    static_for<0, kRing>([&](auto s_tag) {
+      constexpr int S = decltype(s_tag)::value;
+      stage(s_tag, i0 + S, a0, a1, a2);
+      if constexpr (S & 1) turn();
       stage_barrier<kLoads>();
     });
   }
-  for (; st0 < s_end; st0 += kRing) {  // (the stages past s_end only load and wait)
-    static_for<0, kRing>([&](auto i_tag) {
-      constexpr int i = decltype(i_tag)::value;
-      const int st = st0 + i;
-      dma(st + kRing - 1, (i + kRing - 1) & (kRing - 1));
-      if (st < s_end) stage_tail(i_tag, st);
+  for (; i0 < total; i0 += kRing) {  // (the stages past the end only load and wait)
+    static_for<0, kRing>([&](auto s_tag) {
+      constexpr int S = decltype(s_tag)::value;
+      const DmaStage d = dma_begin(i0 + S, a2);
+      static_for<0, kLoads>([&](auto j_tag) {
+        dma_piece(d, j_tag, std::integral_constant<int, S & 1>{});
+      });
+      if (i0 + S < total) stage_tail(s_tag, i0 + S, a0);
+      if constexpr (S & 1) turn();
       stage_barrier<kLoads>();
     });
   }
@@ -360,7 +384,7 @@ __device__ __forceinline__ int64_t run_begin(int64_t w, int64_t N, int64_t P) { 
 
 }  // namespace
 
-// Logits: A = W (words), B = rows idx of h (tokens), so that a lane has one
+// Logits: A = W (words), B = h^T (tokens), so that a lane has one
 // token a block and 64 of its logits.  Lane: token 32 b + l32, words 32 a +
 // 8 (i / 4) + 4 half + i % 4.
 //
@@ -371,11 +395,11 @@ __device__ __forceinline__ int64_t run_begin(int64_t w, int64_t N, int64_t P) { 
 // kDlogits: G[row][word - w0] in 16 bits.
 template <bool F16, Mode MODE, bool TEMP>
 __global__ __launch_bounds__(256) void head_logits_kernel(
-    const uint16_t* __restrict__ h, const uint16_t* __restrict__ w, int D,
-    const int* __restrict__ idx, const int* __restrict__ count, int64_t words, float inv_tau,
+    const uint16_t* __restrict__ ht, int64_t tp, const uint16_t* __restrict__ w, int D,
+    const int* __restrict__ count, int64_t words, float inv_tau,
     float* __restrict__ part, const HeadRow* __restrict__ rows, uint16_t* __restrict__ G,
     int64_t ld) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing * kSlot];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds<true>];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wy = wave >> 1, wx = wave & 1, l32 = lane & 31, half = lane >> 5;
@@ -440,12 +464,10 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
     f32x16 acc[4][4];
     {
       Loader<true> la;
-      la.begin(reinterpret_cast<const uint8_t*>(w) + (int64_t)nv_i * kTM * D * 2,
-               words - (int64_t)nv_i * kTM, 2 * (int64_t)D, D, wave, lane);
-      RowLoader lb;
-      lb.begin(reinterpret_cast<const uint8_t*>(h), idx, nt_i * kTN, n, 2 * (int64_t)D, D, wave,
-               lane);
-      product<F16, true, true>(lds, la, lb, D, 0, nst, acc);
+      la.begin(w + (int64_t)nv_i * kTM * D, words - (int64_t)nv_i * kTM, D, D, wave, lane);
+      Loader<false> lb;
+      lb.begin(ht + nt_i * kTN, tp - nt_i * kTN, tp, D, wave, lane);
+      product<F16, true>(lds, la, lb, D, 0, nst, acc);
     }
     const int v0 = nv_i * kTM + wy * 128;  // the wave's first word
     if constexpr (MODE == kStats) {
@@ -549,7 +571,7 @@ __global__ __launch_bounds__(256) void head_dh_kernel(
     const uint16_t* __restrict__ G, int64_t ld, const uint16_t* __restrict__ w, int D,
     const int* __restrict__ count, int64_t T, int64_t words, int parts, int per, int add,
     float* __restrict__ part) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing * kSlot];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds<true>];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wy = wave >> 1, wx = wave & 1;
@@ -567,11 +589,10 @@ __global__ __launch_bounds__(256) void head_dh_kernel(
     f32x16 acc[4][4];
     {
       Loader<true> la;
-      la.begin(reinterpret_cast<const uint8_t*>(G + m0 * ld), n - m0, 2 * ld, words, wave, lane);
+      la.begin(G + m0 * ld, n - m0, ld, words, wave, lane);
       Loader<false> lb;
-      lb.begin(reinterpret_cast<const uint8_t*>(w + d0), D - d0, 2 * (int64_t)D, words, wave,
-               lane);
-      product<F16, true, false>(lds, la, lb, words, s * per, s_end, acc);
+      lb.begin(w + d0, D - d0, D, words, wave, lane);
+      product<F16, true>(lds, la, lb, words, s * per, s_end, acc);
     }
     const int64_t r0 = m0 + wy * 128;
     const int c0 = d0 + wx * 128;
@@ -590,7 +611,7 @@ __global__ __launch_bounds__(256) void head_dw_kernel(
     const uint16_t* __restrict__ G, int64_t ld, const uint16_t* __restrict__ hs, int D,
     const int* __restrict__ count, int64_t words, int parts, int per, const int* __restrict__ exp,
     O* __restrict__ dw) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing * kSlot];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds<false>];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wy = wave >> 1, wx = wave & 1;
@@ -608,9 +629,9 @@ __global__ __launch_bounds__(256) void head_dw_kernel(
     f32x16 acc[4][4];
     if (s * per < s_end) {
       Loader<false> la, lb;
-      la.begin(reinterpret_cast<const uint8_t*>(G + m0), ld - m0, 2 * ld, n, wave, lane);
-      lb.begin(reinterpret_cast<const uint8_t*>(hs + d0), D - d0, 2 * (int64_t)D, n, wave, lane);
-      product<F16, false, false>(lds, la, lb, n, s * per, s_end, acc);
+      la.begin(G + m0, ld - m0, ld, n, wave, lane);
+      lb.begin(hs + d0, D - d0, D, n, wave, lane);
+      product<F16, false>(lds, la, lb, n, s * per, s_end, acc);
     } else {  // fewer rows than the parts were made for
 #pragma unroll
       for (int a = 0; a < 4; ++a)
@@ -670,32 +691,32 @@ int head_logits_grid(int64_t T, int64_t words) {
 }
 
 template <bool F16, Mode MODE>
-static hipError_t run_logits(const HeadIn& in, const int* idx, const int* count, int64_t w0,
+static hipError_t run_logits(const HeadIn& in, const uint16_t* ht, const int* count, int64_t w0,
                              int64_t n, float* part, const HeadRow* rows, uint16_t* G, int64_t ld,
                              hipStream_t stream) {
   const int grid = head_logits_grid(in.T, n);
   const uint16_t* w = in.w + w0 * in.D;
   if (in.K > 0 && in.tau != 1.0f)
-    hipLaunchKernelGGL((head_logits_kernel<F16, MODE, true>), TM_HEAD_GRID(grid), in.h,
-                       w, in.D, idx, count, n, 1.0f / in.tau, part, rows, G, ld);
+    hipLaunchKernelGGL((head_logits_kernel<F16, MODE, true>), TM_HEAD_GRID(grid), ht,
+                       head_padded(in.T), w, in.D, count, n, 1.0f / in.tau, part, rows, G, ld);
   else
-    hipLaunchKernelGGL((head_logits_kernel<F16, MODE, false>), TM_HEAD_GRID(grid), in.h,
-                       w, in.D, idx, count, n, 1.0f, part, rows, G, ld);
+    hipLaunchKernelGGL((head_logits_kernel<F16, MODE, false>), TM_HEAD_GRID(grid), ht,
+                       head_padded(in.T), w, in.D, count, n, 1.0f, part, rows, G, ld);
   return hipGetLastError();
 }
 
-hipError_t launch_head_logits(const HeadIn& in, const int* idx, const int* count, float* part,
+hipError_t launch_head_logits(const HeadIn& in, const uint16_t* ht, const int* count, float* part,
                               hipStream_t stream) {
-  return in.f16 ? run_logits<true, kStats>(in, idx, count, 0, in.V, part, nullptr, nullptr, 0, stream)
-                : run_logits<false, kStats>(in, idx, count, 0, in.V, part, nullptr, nullptr, 0,
+  return in.f16 ? run_logits<true, kStats>(in, ht, count, 0, in.V, part, nullptr, nullptr, 0, stream)
+                : run_logits<false, kStats>(in, ht, count, 0, in.V, part, nullptr, nullptr, 0,
                                             stream);
 }
 
-hipError_t launch_head_dlogits(const HeadIn& in, const int* idx, const int* count,
+hipError_t launch_head_dlogits(const HeadIn& in, const uint16_t* ht, const int* count,
                                const HeadRow* rows, int64_t w0, int64_t n, uint16_t* G, int64_t ld,
                                hipStream_t stream) {
-  return in.f16 ? run_logits<true, kDlogits>(in, idx, count, w0, n, nullptr, rows, G, ld, stream)
-                : run_logits<false, kDlogits>(in, idx, count, w0, n, nullptr, rows, G, ld, stream);
+  return in.f16 ? run_logits<true, kDlogits>(in, ht, count, w0, n, nullptr, rows, G, ld, stream)
+                : run_logits<false, kDlogits>(in, ht, count, w0, n, nullptr, rows, G, ld, stream);
 }
 
 hipError_t launch_head_dh(const HeadIn& in, const int* count, const uint16_t* G, int64_t ld,

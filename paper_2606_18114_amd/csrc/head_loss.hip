@@ -104,22 +104,21 @@ __global__ __launch_bounds__(256) void terms_kernel(HeadIn in, const void* __res
   if (lane == 0) terms[t] = (uint8_t)((y >= 0 && y < in.V ? 1 : 0) | (kl ? 2 : 0));
 }
 
-// One workgroup lists the rows in the tokens' order: every thread counts a run
-// of tokens, the counts are summed along the threads, then it writes its run.
+// Lists the rows in the tokens' order.  A workgroup has `per` tokens (a multiple of
+// 1024); it counts the rows before them by itself, then lists its own, 1024 at a time.
+// At most 64 workgroups, so that counting again costs 32 reads a token at most.
 // BWD: rows whose loss has a gradient, with their factors.
 template <bool BWD>
 __global__ __launch_bounds__(1024) void rows_kernel(HeadIn in, const float* __restrict__ stats,
-                                                    int64_t cols, const float* __restrict__ dloss,
-                                                    int shift, Rows out) {
+                                                    const float* __restrict__ dloss, int shift,
+                                                    int64_t per, Rows out) {
   __shared__ int sums[16];
   __shared__ int maxs[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t per = (in.T + 1023) / 1024;
-  const int64_t t0 = tid * per < in.T ? tid * per : in.T;
-  const int64_t t1 = t0 + per < in.T ? t0 + per : in.T;
+  const int64_t T = in.T, t0 = blockIdx.x * per, t1 = t0 + per < T ? t0 + per : T;
   auto has = [&](int64_t t) {
     if constexpr (BWD) {
-      return stats[t * cols + kHeadStatTerms] != 0.f && !(dloss[t] == 0.f);
+      return stats[kStatTerms * T + t] != 0.f && !(dloss[t] == 0.f);
     } else {
       if (in.K > 0) return out.terms[t] != 0;
       const int64_t y = id_at(in.targets, in.targets64, t);
@@ -128,59 +127,69 @@ __global__ __launch_bounds__(1024) void rows_kernel(HeadIn in, const float* __re
   };
   const float unit = head_unit(in.alpha, in.tau);
   int n = 0, e = -1000;
-  for (int64_t t = t0; t < t1; ++t) {
-    if (!has(t)) continue;
-    ++n;
+  // the first workgroup looks at all gradients for the largest
+#pragma unroll 4
+  for (int64_t t = tid; t < (BWD && blockIdx.x == 0 ? T : t0); t += 1024) {
+    const bool yes = has(t);
+    if (t < t0) n += yes;
     if constexpr (BWD) {
       const float g = dloss[t] * unit;
-      if (fabsf(g) < __builtin_inff() && g != 0.f) e = max(e, ilogbf(g));
+      if (yes && fabsf(g) < __builtin_inff() && g != 0.f) e = max(e, ilogbf(g));
     }
   }
-  int before = n;  // inclusive sums along the wave's lanes
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(before, o, 64);
-    if (lane >= o) before += v;
+  for (int o = 32; o > 0; o >>= 1) {
+    n += __shfl_xor(n, o, 64);
+    e = max(e, __shfl_xor(e, o, 64));
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) e = max(e, __shfl_xor(e, o, 64));
-  if (lane == 63) sums[wave] = before;
-  if (lane == 0) maxs[wave] = e;
+  if (lane == 0) {
+    sums[wave] = n;
+    maxs[wave] = e;
+  }
   __syncthreads();
-  int base = 0, all = 0, top = -1000;
+  int base = 0;
+#pragma unroll
   for (int w = 0; w < 16; ++w) {
-    if (w < wave) base += sums[w];
-    all += sums[w];
-    top = max(top, maxs[w]);
+    base += sums[w];
+    e = max(e, maxs[w]);
   }
-  if (tid == 0) {
-    *out.count = all;
-    if constexpr (BWD) {
-      out.exps[0] = top == -1000 ? 0 : top;
-      out.exps[1] = out.exps[0] - shift;
+  if (BWD && blockIdx.x == 0 && tid == 0) {
+    out.exps[0] = e == -1000 ? 0 : e;
+    out.exps[1] = out.exps[0] - shift;
+  }
+  for (int64_t c = t0; c < t1; c += 1024) {
+    const int64_t t = c + tid;
+    const bool yes = t < t1 && has(t);
+    const uint64_t mask = __ballot(yes);
+    __syncthreads();  // the previous sums have been read
+    if (lane == 0) sums[wave] = __popcll(mask);
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      before += w < wave ? sums[w] : 0;
+      all += sums[w];
     }
-  }
-  int r = base + before - n;
-  for (int64_t t = t0; t < t1; ++t) {
-    const bool yes = has(t);
-    out.pos[t] = yes ? r : -1;
-    if constexpr (BWD) {
-      if (yes) {
-        const float* s = stats + t * cols;
+    const int r = base + before + __popcll(mask & ((uint64_t(1) << lane) - 1));
+    base += all;
+    if (t < t1) out.pos[t] = yes ? r : -1;
+    if (yes) {
+      out.idx[r] = (int)t;
+      if constexpr (BWD) {
         const float g = dloss[t] * unit;
         const float m = ldexpf(g, shift - exp_of(g));
-        const int terms = (int)s[kHeadStatTerms];
+        const int terms = (int)stats[kStatTerms * T + t];
         float c1 = terms & 1 ? (1.0f - in.alpha) / unit * m : 0.f;
         float c2 = terms & 2 ? in.alpha * in.tau / unit * m : 0.f;
         if (in.tau == 1.0f) {  // one softmax
           c1 += c2;
           c2 = 0.f;
         }
-        out.row[r] = HeadRow{s[kHeadStatLse], s[kHeadStatLseT], c1, c2};
+        out.row[r] = HeadRow{stats[kStatLse * T + t], stats[kStatLseT * T + t], c1, c2};
       }
     }
-    if (yes) out.idx[r++] = (int)t;
   }
+  if (t1 == T && tid == 0) *out.count = base;
 }
 
 // The loss and the row of stats of a token, a wave (K = 0) or a workgroup of
@@ -246,14 +255,15 @@ __global__ __launch_bounds__(256) void finish_kernel(Finish f) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t t = TEACH ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   if (t >= in.T) return;
-  const int64_t cols = head_stats_cols(in.K);
-  float* st = f.stats + t * cols;
+  float* st = f.stats + t;  // the token's place in each plane
+  float* st_top = f.stats + kStatPlanes * in.T + t * in.K;
   const int64_t y = id_at(in.targets, in.targets64, t);
   const bool ce = y >= 0 && y < in.V;
   const int terms = TEACH ? f.rows.terms[t] : (ce ? 1 : 0);
   const int first = TEACH ? threadIdx.x : lane;
   if (terms == 0) {  // no loss
-    for (int64_t i = first; i < cols; i += TEACH ? 256 : 64) st[i] = 0.f;
+    if (first < kStatPlanes) st[first * in.T] = 0.f;
+    for (int i = first; i < in.K; i += 256) st_top[i] = 0.f;
     if (first == 0) f.loss[t] = 0.f;
     return;
   }
@@ -278,10 +288,10 @@ __global__ __launch_bounds__(256) void finish_kernel(Finish f) {
   if constexpr (!TEACH) {
     if (lane == 0) {
       f.loss[t] = ce_loss;
-      st[kHeadStatLse] = lse2;
-      st[kHeadStatLseT] = lse2;
-      st[kHeadStatTerms] = 1.f;
-      st[kHeadStatLabel] = grad(zy, 1.0f);
+      st[kStatLse * in.T] = lse2;
+      st[kStatLseT * in.T] = lse2;
+      st[kStatTerms * in.T] = 1.f;
+      st[kStatLabel * in.T] = grad(zy, 1.0f);
     }
     return;
   }
@@ -353,14 +363,41 @@ __global__ __launch_bounds__(256) void finish_kernel(Finish f) {
     return c2 * x + (v == y ? c1 : 0.f);
   };
   for (int k = threadIdx.x; k < K; k += 256)
-    st[kHeadStatTop + k] = id[k] >= 0 ? grad(id[k] == y ? zy : z[k], hits(id[k])) : 0.f;
+    st_top[k] = id[k] >= 0 ? grad(id[k] == y ? zy : z[k], hits(id[k])) : 0.f;
   if (threadIdx.x == 0) {
     f.loss[t] = (terms & 1 ? (1.0f - in.alpha) * ce_loss : 0.f) +
                 (terms & 2 ? in.alpha * in.tau * in.tau * kl : 0.f);
-    st[kHeadStatLse] = lse2;
-    st[kHeadStatLseT] = lseT2;
-    st[kHeadStatTerms] = (float)terms;
-    st[kHeadStatLabel] = ce ? grad(zy, hits(y)) : 0.f;
+    st[kStatLse * in.T] = lse2;
+    st[kStatLseT * in.T] = lseT2;
+    st[kStatTerms * in.T] = (float)terms;
+    st[kStatLabel * in.T] = ce ? grad(zy, hits(y)) : 0.f;
+  }
+}
+
+// ht[d][r] = h[idx[r]][d]: the logits' second operand.  64 x 64 a workgroup, through LDS.
+__global__ __launch_bounds__(256) void rows_transpose_kernel(HeadIn in, Rows rows, int64_t tp,
+                                                             uint16_t* __restrict__ ht) {
+  __shared__ uint16_t s[64][72];
+  const int n = *rows.count;
+  const int64_t r0 = (int64_t)blockIdx.x * 64;
+  const int d0 = blockIdx.y * 64, q = threadIdx.x >> 3, c = 8 * (threadIdx.x & 7);
+  if (r0 >= n) return;
+#pragma unroll
+  for (int i = 0; i < 64; i += 32) {
+    u32x4 v = {0, 0, 0, 0};
+    if (r0 + q + i < n && d0 + c < in.D)
+      v = ld16(in.h + (int64_t)rows.idx[r0 + q + i] * in.D + d0 + c);
+    st16(&s[q + i][c], v);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 64; i += 32) {
+    if (d0 + q + i >= in.D) continue;
+    u32x4 v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      v[j] = (uint32_t)s[c + 2 * j][q + i] | (uint32_t)s[c + 2 * j + 1][q + i] << 16;
+    st16(ht + (int64_t)(d0 + q + i) * tp + r0 + c, v);
   }
 }
 
@@ -400,15 +437,15 @@ __global__ __launch_bounds__(256) void sparse_kernel(HeadIn in, const float* __r
   const int e = (int)(i % (in.K + 1));
   if (r >= *rows.count) return;
   const int64_t t = rows.idx[r];
-  const float* st = stats + t * head_stats_cols(in.K);
-  const int terms = (int)st[kHeadStatTerms];
+  const int terms = (int)stats[kStatTerms * in.T + t];
   if (!(terms & (e == 0 ? 1 : 2))) return;
   const int64_t v =
       (e == 0 ? id_at(in.targets, in.targets64, t) : id_at(in.ids, in.ids64, t * in.K + e - 1)) -
       w0;
   if (v < 0 || v >= n) return;
   const float g = dloss[t] * head_unit(in.alpha, in.tau);
-  G[r * ld + v] = narrow<F16>(st[kHeadStatLabel + e] * ldexpf(g, kHeadShift<F16> - exp_of(g)));
+  const float x = stats[e == 0 ? kStatLabel * in.T + t : kStatPlanes * in.T + t * in.K + e - 1];
+  G[r * ld + v] = narrow<F16>(x * ldexpf(g, kHeadShift<F16> - exp_of(g)));
 }
 
 // dh[t] = 2^(e - shift) times the sum of the row's parts; zeros for a token without a row
@@ -445,11 +482,12 @@ constexpr int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
 // Parts of a contraction of nst stages of `tiles` tiles on P workgroups: the
 // fewest rounds times stages, against 0.5 us for writing and reading a tile's
-// part (256 KiB each way).  A stage takes 0.8 us a workgroup.
-void cut(int64_t tiles, int64_t nst, int64_t P, int* parts, int* per) {
+// part (256 KiB each way).  A stage takes 0.8 us a workgroup; parts are a multiple of
+// `unit` stages, the ring's.
+void cut(int64_t tiles, int64_t nst, int64_t P, int unit, int* parts, int* per) {
   double best = 0;
   for (int64_t k = 1; k <= nst && k <= 64 && (k == 1 || tiles * k <= 4 * P); ++k) {
-    const int64_t len = (nst + k - 1) / k;
+    const int64_t len = ((nst + k - 1) / k + unit - 1) / unit * unit;
     if ((nst + len - 1) / len != k) continue;  // an empty part
     const int64_t rounds = (tiles * k + P - 1) / P;
     const double us = (double)rounds * ((double)len * 0.8 + 3.0) +
@@ -466,7 +504,8 @@ void cut(int64_t tiles, int64_t nst, int64_t P, int* parts, int* per) {
 
 // A piece holds at most 2^28 dlogits (512 MiB: with dh's float32 sums read
 // and written once a piece, a quarter of it adds a tenth to the time of dh),
-// or 4096 words where tokens are many.
+// or 4096 words where tokens are many.  Where there are several pieces, dW's tiles of all but
+// the last one fill whole rounds of the workgroups.
 HeadPlan head_plan(int64_t T, int64_t V, int64_t D) {
   HeadPlan p;
   const int64_t P = current_cu_count();
@@ -474,11 +513,17 @@ HeadPlan head_plan(int64_t T, int64_t V, int64_t D) {
   if (most < 4096) most = 4096;
   p.pieces = (up256(V) + most - 1) / most;
   p.piece = up256((V + p.pieces - 1) / p.pieces);
+  if (p.pieces > 1) {
+    const int64_t round = P / ((D + 255) / 256) * 256;  // words of a round
+    if (round > 0 && round <= most) p.piece = most / round * round;
+  }
   p.pieces = (V + p.piece - 1) / p.piece;
   const int64_t nd = (D + 255) / 256, nt = (T + 255) / 256, nv = p.piece / 256;
   const int64_t words = p.pieces == 1 ? V : p.piece;
-  cut(nt * nd, (words + 31) / 32, P, &p.parts_h, &p.per_h);
-  cut(nv * nd, (T + 31) / 32, P, &p.parts_w, &p.per_w);
+  cut(nt * nd, (words + 31) / 32, P, 4, &p.parts_h, &p.per_h);
+  cut(nv * nd, (T + 31) / 32, P, 4, &p.parts_w, &p.per_w);
+  const int64_t rest = V - (p.pieces - 1) * p.piece;
+  cut((rest + 255) / 256 * nd, (T + 31) / 32, P, 4, &p.last_w, &p.last_per);
   return p;
 }
 
@@ -487,7 +532,7 @@ namespace {
 struct Layout {
   Rows rows;
   float* part;
-  uint16_t *hs, *G;
+  uint16_t *ht, *hs, *G;
   float *part_h, *part_w;
   int64_t bytes;
 };
@@ -498,18 +543,19 @@ void take(T** p, uint8_t* base, int64_t* at, int64_t bytes) {
   *at += up256(bytes);
 }
 
-Layout forward_layout(int64_t T, void* ws) {
+Layout forward_layout(int64_t T, int64_t D, void* ws) {
   Layout l{};
   uint8_t* b = static_cast<uint8_t*>(ws);
   take(&l.rows.count, b, &l.bytes, 4);
   take(&l.rows.idx, b, &l.bytes, 4 * T);
   take(&l.rows.pos, b, &l.bytes, 4 * T);
   take(&l.rows.terms, b, &l.bytes, T);
+  take(&l.ht, b, &l.bytes, 2 * head_padded(T) * D);
   take(&l.part, b, &l.bytes, 4 * head_part_floats(T));
   return l;
 }
 
-Layout backward_layout(int64_t T, int64_t D, const HeadPlan& p, void* ws) {
+Layout backward_layout(int64_t T, int64_t V, int64_t D, const HeadPlan& p, void* ws) {
   Layout l{};
   uint8_t* b = static_cast<uint8_t*>(ws);
   take(&l.rows.count, b, &l.bytes, 4);
@@ -517,19 +563,23 @@ Layout backward_layout(int64_t T, int64_t D, const HeadPlan& p, void* ws) {
   take(&l.rows.idx, b, &l.bytes, 4 * T);
   take(&l.rows.pos, b, &l.bytes, 4 * T);
   take(&l.rows.row, b, &l.bytes, (int64_t)sizeof(HeadRow) * T);
+  take(&l.ht, b, &l.bytes, 2 * head_padded(T) * D);
   take(&l.hs, b, &l.bytes, 2 * T * D);
   take(&l.G, b, &l.bytes, 2 * T * p.piece);
   take(&l.part_h, b, &l.bytes, 4 * p.parts_h * T * D);
-  if (p.parts_w > 1) take(&l.part_w, b, &l.bytes, 4 * p.parts_w * p.piece * D);
+  const int64_t rest = V - (p.pieces - 1) * p.piece;
+  const int64_t full = p.pieces > 1 && p.parts_w > 1 ? p.parts_w * p.piece : 0;
+  const int64_t end = p.last_w > 1 ? p.last_w * rest : 0;
+  take(&l.part_w, b, &l.bytes, 4 * D * (full > end ? full : end));
   return l;
 }
 
 }  // namespace
 
-int64_t head_loss_bytes(int64_t T, int64_t) { return forward_layout(T, nullptr).bytes; }
+int64_t head_loss_bytes(int64_t T, int64_t D) { return forward_layout(T, D, nullptr).bytes; }
 
 int64_t head_loss_bwd_bytes(int64_t T, int64_t V, int64_t D) {
-  return backward_layout(T, D, head_plan(T, V, D), nullptr).bytes;
+  return backward_layout(T, V, D, head_plan(T, V, D), nullptr).bytes;
 }
 
 #define TM_RET(expr)                     \
@@ -537,6 +587,18 @@ int64_t head_loss_bwd_bytes(int64_t T, int64_t V, int64_t D) {
     const hipError_t e_ = (expr);        \
     if (e_ != hipSuccess) return e_;     \
   } while (0)
+
+static int64_t rows_per_group(int64_t T) {
+  const int64_t per = (T + 63) / 64;
+  return (per + 1023) / 1024 * 1024;
+}
+
+static hipError_t transpose(const HeadIn& in, const Layout& l, hipStream_t stream) {
+  hipLaunchKernelGGL(rows_transpose_kernel,
+                     dim3((unsigned)((in.T + 63) / 64), (unsigned)((in.D + 63) / 64)), dim3(256), 0,
+                     stream, in, l.rows, head_padded(in.T), l.ht);
+  return hipGetLastError();
+}
 
 template <bool F16>
 static hipError_t run_finish(const Finish& f, hipStream_t stream) {
@@ -555,16 +617,18 @@ static hipError_t run_finish(const Finish& f, hipStream_t stream) {
 
 hipError_t launch_head_loss(const HeadIn& in, const void* top, int top_type, float* loss,
                             float* stats, void* workspace, hipStream_t stream) {
-  const Layout l = forward_layout(in.T, workspace);
+  const Layout l = forward_layout(in.T, in.D, workspace);
   if (in.K > 0) {
     hipLaunchKernelGGL(terms_kernel, dim3((unsigned)((in.T + 3) / 4)), dim3(256), 0, stream, in,
                        top, top_type, l.rows.terms);
     TM_RET(hipGetLastError());
   }
-  hipLaunchKernelGGL(rows_kernel<false>, dim3(1), dim3(1024), 0, stream, in, nullptr, 0, nullptr, 0,
-                     l.rows);
+  const int64_t per = rows_per_group(in.T);
+  hipLaunchKernelGGL(rows_kernel<false>, dim3((unsigned)((in.T + per - 1) / per)), dim3(1024), 0,
+                     stream, in, nullptr, nullptr, 0, per, l.rows);
   TM_RET(hipGetLastError());
-  TM_RET(launch_head_logits(in, l.rows.idx, l.rows.count, l.part, stream));
+  TM_RET(transpose(in, l, stream));
+  TM_RET(launch_head_logits(in, l.ht, l.rows.count, l.part, stream));
   const Finish f{in, top, top_type, l.part, head_logits_grid(in.T, in.V), l.rows, loss, stats};
   return in.f16 ? run_finish<true>(f, stream) : run_finish<false>(f, stream);
 }
@@ -574,25 +638,27 @@ static hipError_t run_bwd(const HeadIn& in, const float* stats, const float* dlo
                           void* dw, int dw_type, bool accumulate, void* workspace,
                           hipStream_t stream) {
   const HeadPlan p = head_plan(in.T, in.V, in.D);
-  const Layout l = backward_layout(in.T, in.D, p, workspace);
-  const int64_t cols = head_stats_cols(in.K);
-  hipLaunchKernelGGL(rows_kernel<true>, dim3(1), dim3(1024), 0, stream, in, stats, cols, dloss,
-                     kHeadShift<F16>, l.rows);
+  const Layout l = backward_layout(in.T, in.V, in.D, p, workspace);
+  const int64_t per = rows_per_group(in.T);
+  hipLaunchKernelGGL(rows_kernel<true>, dim3((unsigned)((in.T + per - 1) / per)), dim3(1024), 0,
+                     stream, in, stats, dloss, kHeadShift<F16>, per, l.rows);
   TM_RET(hipGetLastError());
   hipLaunchKernelGGL(rows_copy_kernel<F16>, dim3((unsigned)in.T), dim3(256), 0, stream, in, dloss,
                      l.rows, l.hs);
   TM_RET(hipGetLastError());
+  TM_RET(transpose(in, l, stream));
   for (int64_t i = 0; i < p.pieces; ++i) {
     const int64_t w0 = i * p.piece, n = in.V - w0 < p.piece ? in.V - w0 : p.piece;
-    TM_RET(launch_head_dlogits(in, l.rows.idx, l.rows.count, l.rows.row, w0, n, l.G, p.piece,
+    TM_RET(launch_head_dlogits(in, l.ht, l.rows.count, l.rows.row, w0, n, l.G, p.piece,
                                stream));
     hipLaunchKernelGGL(sparse_kernel<F16>, dim3((unsigned)((in.T * (in.K + 1) + 255) / 256)),
                        dim3(256), 0, stream, in, stats, dloss, l.rows, w0, n, l.G, p.piece);
     TM_RET(hipGetLastError());
     TM_RET(launch_head_dh(in, l.rows.count, l.G, p.piece, w0, n, p.parts_h, p.per_h, i > 0,
                           l.part_h, stream));
-    TM_RET(launch_head_dw(in, l.rows.count, l.G, p.piece, l.hs, w0, n, p.parts_w, p.per_w,
-                          l.rows.exps + 1, dw, dw_type, accumulate, l.part_w, stream));
+    const bool last = i == p.pieces - 1;
+    TM_RET(launch_head_dw(in, l.rows.count, l.G, p.piece, l.hs, w0, n, last ? p.last_w : p.parts_w,
+                          last ? p.last_per : p.per_w, l.rows.exps + 1, dw, dw_type, accumulate, l.part_w, stream));
   }
   hipLaunchKernelGGL(dh_out_kernel<F16>, dim3((unsigned)in.T), dim3(256), 0, stream, in, dloss,
                      l.rows, l.part_h, p.parts_h, dh);

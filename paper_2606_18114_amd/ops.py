@@ -1209,7 +1209,7 @@ def embed_bwd(ids: torch.Tensor, dout: torch.Tensor, vocab: int, scale: float = 
 # ---- the ends of a training step: the head's loss, the block norm (include/tmamba_head.h) ----
 
 _HEAD_TYPE = {torch.bfloat16: 1, torch.float16: 2}
-HEAD_STATS = 4  # columns of head_loss's stats beside the teacher's words
+HEAD_STATS = 4  # values a token in head_loss's stats beside the teacher's words
 
 
 def _head_args(h, weight, targets, teacher_ids, alpha, temperature):
@@ -1259,7 +1259,7 @@ def head_loss(h: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
         loss = torch.empty((T,), dtype=torch.float32, device=dev)
     else:
         _of(loss, "loss", _F32, (T,), dev)
-    stats = torch.empty((T, HEAD_STATS + K), dtype=torch.float32, device=dev)
+    stats = torch.empty((T * (HEAD_STATS + K),), dtype=torch.float32, device=dev)
     if T == 0:
         return loss, stats
     ws, wp, wb = _seq_ws("tm_head_loss_workspace", dev, T, V, D)
@@ -1281,7 +1281,7 @@ def head_loss_bwd(h: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
     given, then also added to (accumulate).  The other arguments are the
     forward call's."""
     dev, T, V, D, K = _head_args(h, weight, targets, teacher_ids, alpha, temperature)
-    _of(stats, "stats", _F32, (T, HEAD_STATS + K), dev)
+    _of(stats, "stats", _F32, (T * (HEAD_STATS + K),), dev)
     _of(dloss, "dloss", _F32, (T,), dev)
     if dh is None:
         dh = torch.empty_like(h)
