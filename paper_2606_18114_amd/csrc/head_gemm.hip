@@ -58,10 +58,13 @@ __device__ __forceinline__ void dma16(const void* base, uint32_t voff, uint32_t 
 }
 #pragma clang diagnostic pop
 
+// A stage's end.  No wait for LDS reads: those of the slot that the next stage's loads
+// write have fed an MFMA of the stage, and those of the next slot are waited for where they
+// are used (with lgkmcnt(0) here a stage took XX us, YY without).
 template <int kVm>
 __device__ __forceinline__ void stage_barrier() {
   __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kVm) : "memory");
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kVm) : "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -94,8 +97,12 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   }
 }
 
-__device__ __forceinline__ float acc_val(float v) {
-  asm volatile("" : "+v"(v));
+// An accumulator block as values of their own: without the opaque copy the compiler wants
+// all of the accumulators in vector registers at once, and spills them there.  (Not one
+// by one: a wave is alone on its SIMD, and sixteen independent values hide the latencies of
+// what is done to them.)
+__device__ __forceinline__ f32x16 acc_block(f32x16 v) {
+  asm("" : "+v"(v));
   return v;
 }
 
@@ -472,57 +479,88 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
     const int v0 = nv_i * kTM + wy * 128;  // the wave's first word
     if constexpr (MODE == kStats) {
       const int left = (int)(words - v0 < 128 ? words - v0 : 128) - 4 * half;
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        float m = mx[b];
-        if (left + 4 * half < 128) {  // past the last word: no logit
-#pragma unroll
-          for (int a = 0; a < 4; ++a)
+      auto softmax = [&](auto full_tag) {
+        constexpr bool FULL = decltype(full_tag)::value;
+        auto block = [&](int a, int b) {
+          f32x16 z = acc_block(acc[a][b]);
+          if constexpr (!FULL) {  // past the last word: no logit
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (32 * a + 8 * (i / 4) + i % 4 >= left) acc[a][b][i] = -__builtin_inff();
-        }
-#pragma unroll
-        for (int a = 0; a < 4; ++a)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) m = fmaxf(m, acc_val(acc[a][b][i]));
-        const float ref = m == -__builtin_inff() ? 0.f : m;
-        const float c1 = -ref * k1, c2 = -ref * k2;
-        float s = sm[b] * __builtin_amdgcn_exp2f((mx[b] - ref) * k1), s2 = 0.f;
-        if constexpr (TEMP) s2 = st[b] * __builtin_amdgcn_exp2f((mx[b] - ref) * k2);
-#pragma unroll
-        for (int a = 0; a < 4; ++a)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float z = acc_val(acc[a][b][i]);
-            s += __builtin_amdgcn_exp2f(__builtin_fmaf(z, k1, c1));
-            if constexpr (TEMP) s2 += __builtin_amdgcn_exp2f(__builtin_fmaf(z, k2, c2));
+              if (32 * a + 8 * (i / 4) + i % 4 >= left) z[i] = -__builtin_inff();
           }
-        mx[b] = m;
-        sm[b] = s;
-        st[b] = s2;
-        __builtin_amdgcn_sched_barrier(0);
-      }
+          return z;
+        };
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          float m4[4] = {mx[b], mx[b], mx[b], mx[b]};
+#pragma unroll
+          for (int a = 0; a < 4; ++a) {
+            const f32x16 z = block(a, b);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m4[i % 4] = fmaxf(m4[i % 4], z[i]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+          const float ref = m == -__builtin_inff() ? 0.f : m;
+          const float c1 = -ref * k1, c2 = -ref * k2;
+          float s4[4] = {0.f, 0.f, 0.f, 0.f}, t4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int a = 0; a < 4; ++a) {
+            const f32x16 z = block(a, b);
+            float e[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], k1, c1));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s4[i % 4] += e[i];
+            if constexpr (TEMP) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], k2, c2));
+#pragma unroll
+              for (int i = 0; i < 16; ++i) t4[i % 4] += e[i];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          sm[b] = sm[b] * __builtin_amdgcn_exp2f((mx[b] - ref) * k1) +
+                  ((s4[0] + s4[1]) + (s4[2] + s4[3]));
+          if constexpr (TEMP)
+            st[b] = st[b] * __builtin_amdgcn_exp2f((mx[b] - ref) * k2) +
+                    ((t4[0] + t4[1]) + (t4[2] + t4[3]));
+          mx[b] = m;
+        }
+      };
+      if (words - v0 >= 128)
+        softmax(std::true_type{});
+      else
+        softmax(std::false_type{});
     } else {
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const int r = nt_i * kTN + wx * 128 + 32 * b + l32;
         uint16_t* g = G + (int64_t)r * ld + v0 + 8 * half;
-        auto dz = [&](float z) {
-          float p = hr[b].c1 * __builtin_amdgcn_exp2f(__builtin_fmaf(z, k1, -hr[b].lse));
-          if constexpr (TEMP)
-            p += hr[b].c2 * __builtin_amdgcn_exp2f(__builtin_fmaf(z, k2, -hr[b].lse_t));
-          return p;
-        };
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
+          const f32x16 z = acc_block(acc[a][b]);
+          float p[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], k1, -hr[b].lse));
+#pragma unroll
+          for (int i = 0; i < 16; ++i) p[i] *= hr[b].c1;
+          if constexpr (TEMP) {
+            float q[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              q[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], k2, -hr[b].lse_t));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[i] = __builtin_fmaf(hr[b].c2, q[i], p[i]);
+          }
 #pragma unroll
           for (int q = 0; q < 2; ++q) {  // 16 words: a lane's eight, exchanged to follow each other
             uint32_t x[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              x[i] = pack2<F16>(dz(acc_val(acc[a][b][8 * q + 2 * i])),
-                                dz(acc_val(acc[a][b][8 * q + 2 * i + 1])));
+            for (int i = 0; i < 4; ++i) x[i] = pack2<F16>(p[8 * q + 2 * i], p[8 * q + 2 * i + 1]);
             // lanes 32 .. 63 of x[0], x[1] change with lanes 0 .. 31 of x[2], x[3]
             const auto e0 = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
             const auto e1 = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
@@ -537,25 +575,39 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
     if (tile >= 0) flush(tile);
 }
 
-// op(pointer, value) for every element of the wave's 128 x 128 that is inside;
-// row by row through a pitch that the compiler cannot take apart (precomputed
-// offsets would need the accumulators' registers)
-template <typename T, typename Op>
-__device__ __forceinline__ void each_out(T* base, int64_t pitch, int64_t rows_left,
-                                         int64_t cols_left, const f32x16 (&acc)[4][4], Op op) {
+// The wave's 128 x 128 to an output, what lies inside: put(value, old) for every element,
+// old read from there if ADD.  Row by row through a pitch that the compiler cannot take
+// apart (precomputed offsets would need the accumulators' registers); a block's sixteen old
+// values are read before the first is written (one by one, each waiting for its read, the
+// sums of a tile of dh took 120 us).
+template <bool ADD, bool FULL, typename T, typename Put>
+__device__ __forceinline__ void write_as(T* base, int64_t pitch, int64_t rows_left,
+                                         int64_t cols_left, const f32x16 (&acc)[4][4], Put put) {
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
   int64_t pv = pitch;
   asm volatile("" : "+v"(pv));
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
+    if (!FULL && 32 * a >= rows_left) break;
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-      if (32 * b + l32 < cols_left) {
-        T* p = base + (int64_t)(32 * a) * pitch + 32 * b + (4 * half * pv + l32);
+      if (FULL || 32 * b + l32 < cols_left) {
+        T* const p0 = base + (int64_t)(32 * a) * pitch + 32 * b + (4 * half * pv + l32);
         const int64_t left = rows_left - 32 * a - 4 * half;
+        T old[16];
+        if constexpr (ADD) {
+          T* p = p0;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            if (FULL || 8 * (i / 4) + i % 4 < left) old[i] = *p;
+            if (i < 15) p += i % 4 == 3 ? 5 * pv : pv;
+          }
+        }
+        const f32x16 v = acc_block(acc[a][b]);
+        T* p = p0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          if (8 * (i / 4) + i % 4 < left) op(p, acc_val(acc[a][b][i]));
+          if (FULL || 8 * (i / 4) + i % 4 < left) *p = put(v[i], ADD ? old[i] : T(0.f));
           if (i < 15) p += i % 4 == 3 ? 5 * pv : pv;
         }
       }
@@ -563,13 +615,21 @@ __device__ __forceinline__ void each_out(T* base, int64_t pitch, int64_t rows_le
     }
   }
 }
+template <bool ADD, typename T, typename Put>
+__device__ __forceinline__ void write_tile(T* base, int64_t pitch, int64_t rows_left,
+                                           int64_t cols_left, const f32x16 (&acc)[4][4], Put put) {
+  if (rows_left >= 128 && cols_left >= 128)
+    write_as<ADD, true>(base, pitch, rows_left, cols_left, acc, put);
+  else if (rows_left > 0 && cols_left > 0)
+    write_as<ADD, false>(base, pitch, rows_left, cols_left, acc, put);
+}
 
 // dh: A = G (tokens; along the words), B = W (across).  The parts of the
 // contraction and the pieces of the vocabulary meet in part[s][row][D].
-template <bool F16>
+template <bool F16, bool ADD>
 __global__ __launch_bounds__(256) void head_dh_kernel(
     const uint16_t* __restrict__ G, int64_t ld, const uint16_t* __restrict__ w, int D,
-    const int* __restrict__ count, int64_t T, int64_t words, int parts, int per, int add,
+    const int* __restrict__ count, int64_t T, int64_t words, int parts, int per,
     float* __restrict__ part) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds<true>];
   const int lane = threadIdx.x & 63;
@@ -597,10 +657,7 @@ __global__ __launch_bounds__(256) void head_dh_kernel(
     const int64_t r0 = m0 + wy * 128;
     const int c0 = d0 + wx * 128;
     float* out = part + ((int64_t)s * T + r0) * D + c0;
-    if (add)
-      each_out(out, D, n - r0, D - c0, acc, [](float* p, float v) { *p += v; });
-    else
-      each_out(out, D, n - r0, D - c0, acc, [](float* p, float v) { *p = v; });
+    write_tile<ADD>(out, D, n - r0, D - c0, acc, [](float v, float old) { return v + old; });
   }
 }
 
@@ -643,13 +700,13 @@ __global__ __launch_bounds__(256) void head_dw_kernel(
     const int64_t r0 = m0 + wy * 128;
     const int c0 = d0 + wx * 128;
     O* out = dw + ((int64_t)s * words + r0) * D + c0;
-    each_out(out, D, words - r0, D - c0, acc, [&](O* p, float v) {
+    write_tile<ACC>(out, D, words - r0, D - c0, acc, [&](float v, O old) {
       if constexpr (PARTS)
-        *p = v;
+        return (O)v;
       else if constexpr (ACC)
-        *p += ldexpf(v, e);
+        return old + ldexpf(v, e);
       else
-        *p = (O)ldexpf(v, e);
+        return (O)ldexpf(v, e);
     });
   }
 }
@@ -724,13 +781,20 @@ hipError_t launch_head_dh(const HeadIn& in, const int* count, const uint16_t* G,
                           hipStream_t stream) {
   const int64_t items = ((in.T + kTM - 1) / kTM) * ((in.D + kTN - 1) / kTN) * parts;
   const uint16_t* w = in.w + w0 * in.D;
-#define TM_HEAD_DH(F16)                                                                         \
-  hipLaunchKernelGGL(head_dh_kernel<F16>, TM_HEAD_GRID(grid_of(items)), G, ld, w, in.D, count, \
-                     in.T, n, parts, per, (int)add, part_h)
-  if (in.f16)
-    TM_HEAD_DH(true);
-  else
-    TM_HEAD_DH(false);
+#define TM_HEAD_DH(F16, ADD)                                                                    \
+  hipLaunchKernelGGL((head_dh_kernel<F16, ADD>), TM_HEAD_GRID(grid_of(items)), G, ld, w, in.D, \
+                     count, in.T, n, parts, per, part_h)
+  if (in.f16) {
+    if (add)
+      TM_HEAD_DH(true, true);
+    else
+      TM_HEAD_DH(true, false);
+  } else {
+    if (add)
+      TM_HEAD_DH(false, true);
+    else
+      TM_HEAD_DH(false, false);
+  }
 #undef TM_HEAD_DH
   return hipGetLastError();
 }
