@@ -82,7 +82,8 @@ int64_t head_part_floats(int64_t T);
 int head_logits_grid(int64_t T, int64_t words);  // its workgroups
 hipError_t launch_head_logits(const HeadIn& in, const uint16_t* ht, const int* count, float* part,
                               hipStream_t stream);
-// dlogits of words w0 .. w0 + n - 1 to G [rows, ld], ld >= n rounded up to 256
+// dlogits of words w0 .. w0 + n - 1 to G [rows rounded up to 256, ld], ld >= n rounded up to
+// 256; what lies past the rows and words is written, but nobody's
 hipError_t launch_head_dlogits(const HeadIn& in, const uint16_t* ht, const int* count,
                                const HeadRow* rows, int64_t w0, int64_t n, uint16_t* G, int64_t ld,
                                hipStream_t stream);

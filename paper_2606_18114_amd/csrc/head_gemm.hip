@@ -452,19 +452,12 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
   };
 
   int tile = -1;
-  HeadRow hr[4];
   for (int64_t item = i0; item < i1; ++item) {
     const int nt_i = (int)(item / nv), nv_i = (int)(item % nv);
     if (nt_i != tile) {
       if constexpr (MODE == kStats) {
         if (tile >= 0) flush(tile);
         reset();
-      } else {
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const int r = nt_i * kTN + wx * 128 + 32 * b + l32;
-          hr[b] = rows[r < n ? r : n - 1];
-        }
       }
       tile = nt_i;
     }
@@ -538,6 +531,7 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const int r = nt_i * kTN + wx * 128 + 32 * b + l32;
+        const HeadRow hr = rows[r < n ? r : n - 1];
         uint16_t* g = G + (int64_t)r * ld + v0 + 8 * half;
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
@@ -545,16 +539,16 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
           float p[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], k1, -hr[b].lse));
+            p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], k1, -hr.lse));
 #pragma unroll
-          for (int i = 0; i < 16; ++i) p[i] *= hr[b].c1;
+          for (int i = 0; i < 16; ++i) p[i] *= hr.c1;
           if constexpr (TEMP) {
             float q[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              q[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], k2, -hr[b].lse_t));
+              q[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], k2, -hr.lse_t));
 #pragma unroll
-            for (int i = 0; i < 16; ++i) p[i] = __builtin_fmaf(hr[b].c2, q[i], p[i]);
+            for (int i = 0; i < 16; ++i) p[i] = __builtin_fmaf(hr.c2, q[i], p[i]);
           }
 #pragma unroll
           for (int q = 0; q < 2; ++q) {  // 16 words: a lane's eight, exchanged to follow each other
@@ -564,7 +558,7 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
             // lanes 32 .. 63 of x[0], x[1] change with lanes 0 .. 31 of x[2], x[3]
             const auto e0 = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
             const auto e1 = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
-            if (r < n) st16(g + 32 * a + 16 * q, u32x4{e0[0], e1[0], e0[1], e1[1]});
+            st16(g + 32 * a + 16 * q, u32x4{e0[0], e1[0], e0[1], e1[1]});
           }
           __builtin_amdgcn_sched_barrier(0);
         }

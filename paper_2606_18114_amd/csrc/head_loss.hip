@@ -565,7 +565,7 @@ Layout backward_layout(int64_t T, int64_t V, int64_t D, const HeadPlan& p, void*
   take(&l.rows.row, b, &l.bytes, (int64_t)sizeof(HeadRow) * T);
   take(&l.ht, b, &l.bytes, 2 * head_padded(T) * D);
   take(&l.hs, b, &l.bytes, 2 * T * D);
-  take(&l.G, b, &l.bytes, 2 * T * p.piece);
+  take(&l.G, b, &l.bytes, 2 * up256(T) * p.piece);  // (tiles are written whole)
   take(&l.part_h, b, &l.bytes, 4 * p.parts_h * T * D);
   const int64_t rest = V - (p.pieces - 1) * p.piece;
   const int64_t full = p.pieces > 1 && p.parts_w > 1 ? p.parts_w * p.piece : 0;
