@@ -40,6 +40,8 @@ constexpr int kLdsB = kRing * kOp;
 template <bool ALONG>
 constexpr int kLds = kLdsB + (ALONG ? 6 : kRing) * kOp;
 constexpr int kLoads = 8;  // direct-to-LDS loads of a wave and stage
+constexpr int kRowB = 128 * 2 + 16;  // bytes of a row of a wave's dlogits in LDS
+static_assert(4 * 128 * kRowB <= kLds<true>, "the dlogits' rows");
 constexpr float kLog2e = 1.4426950408889634f;
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -528,11 +530,14 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
       else
         softmax(std::false_type{});
     } else {
+      // a token's words pass through LDS, so that whole lines are stored (from the
+      // registers, 32 bytes of 32 rows a store, a tile took 11 us more)
+      uint8_t* mine = lds + wave * (128 * kRowB);
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const int r = nt_i * kTN + wx * 128 + 32 * b + l32;
         const HeadRow hr = rows[r < n ? r : n - 1];
-        uint16_t* g = G + (int64_t)r * ld + v0 + 8 * half;
+        uint8_t* row = mine + (32 * b + l32) * kRowB + 8 * half;
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
           const f32x16 z = acc_block(acc[a][b]);
@@ -551,18 +556,22 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
             for (int i = 0; i < 16; ++i) p[i] = __builtin_fmaf(hr.c2, q[i], p[i]);
           }
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {  // 16 words: a lane's eight, exchanged to follow each other
-            uint32_t x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = pack2<F16>(p[8 * q + 2 * i], p[8 * q + 2 * i + 1]);
-            // lanes 32 .. 63 of x[0], x[1] change with lanes 0 .. 31 of x[2], x[3]
-            const auto e0 = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
-            const auto e1 = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
-            st16(g + 32 * a + 16 * q, u32x4{e0[0], e1[0], e0[1], e1[1]});
-          }
+          for (int q = 0; q < 4; ++q)  // words 32 a + 8 q + 4 half ..
+            *reinterpret_cast<u32x2*>(row + 64 * a + 16 * q) =
+                u32x2{pack2<F16>(p[4 * q], p[4 * q + 1]), pack2<F16>(p[4 * q + 2], p[4 * q + 3])};
           __builtin_amdgcn_sched_barrier(0);
         }
       }
+      __builtin_amdgcn_wave_barrier();  // (a wave reads only what it wrote)
+      uint16_t* g = G + (int64_t)(nt_i * kTN + wx * 128 + (lane >> 4)) * ld + v0 + 8 * (lane & 15);
+      const uint8_t* from = mine + (lane >> 4) * kRowB + 16 * (lane & 15);
+#pragma unroll 4
+      for (int i = 0; i < 32; ++i) {
+        st16(g, *reinterpret_cast<const u32x4*>(from));
+        g += 4 * ld;
+        from += 4 * kRowB;
+      }
+      __syncthreads();  // the next tile's loads write where other waves read
     }
   }
   if constexpr (MODE == kStats)
