@@ -75,7 +75,7 @@ hipError_t launch_block_norm_bwd(const float* r, int64_t T, int d, const float* 
                                  void* workspace, hipStream_t stream);
 
 // ---- products (head_gemm.hip); `count` [1]: rows in use, on the device
-// ht [D, head_padded(T)]: the transposed rows in use.
+// ht [D rounded up to 128, head_padded(T)]: the transposed rows in use, zeros around them.
 inline int64_t head_padded(int64_t T) { return (T + 255) / 256 * 256; }
 // partial softmax sums of the rows: part[(wg + tile)][half][token][pair], see head_loss.hip
 int64_t head_part_floats(int64_t T);
@@ -83,7 +83,7 @@ int head_logits_grid(int64_t T, int64_t words);  // its workgroups
 hipError_t launch_head_logits(const HeadIn& in, const uint16_t* ht, const int* count, float* part,
                               hipStream_t stream);
 // dlogits of words w0 .. w0 + n - 1 to G [rows rounded up to 256, ld], ld >= n rounded up to
-// 256; what lies past the rows and words is written, but nobody's
+// 256, with zeros past the rows and words
 hipError_t launch_head_dlogits(const HeadIn& in, const uint16_t* ht, const int* count,
                                const HeadRow* rows, int64_t w0, int64_t n, uint16_t* G, int64_t ld,
                                hipStream_t stream);

@@ -122,8 +122,8 @@ __device__ __forceinline__ uint32_t off_along(int r, int p) {
 
 // An operand's loads and the addresses they need: four of a wave and stage.  Along,
 // the two stages of a pair load half of the rows each.  Rows (columns) past the
-// array re-read its last one, steps past the contraction's end its last ones;
-// what they bring is masked or not stored.
+// array re-read its last one, and what they bring is not stored; steps past the
+// contraction's end re-read its last ones, against zeros in the other operand.
 template <bool ALONG>
 struct Loader {
   const uint8_t* base;  // the array, at the tile's first row (along) or column (across)
@@ -132,14 +132,16 @@ struct Loader {
   uint32_t row[ALONG ? 8 : 4];
   uint32_t col[ALONG ? 1 : 4];
   int64_t pitch;  // bytes of a row
-  int64_t K;
+  int end, rest;  // the contraction's last stage (along: pair), and its steps
 
   // left: rows (along) or columns (across; a multiple of 8) of the array from the tile on
   __device__ __forceinline__ void begin(const uint16_t* b, int64_t left, int64_t pitch_,
-                                        int64_t K_, int wave, int lane) {
+                                        int K, int wave, int lane) {
     base = reinterpret_cast<const uint8_t*>(b);
     pitch = 2 * pitch_;
-    K = K_;
+    constexpr int kSteps = ALONG ? 2 * kBK : kBK;
+    end = __builtin_amdgcn_readfirstlane((K - 1) / kSteps);
+    rest = __builtin_amdgcn_readfirstlane(K - end * kSteps);
     const int most = (int)(left < 256 ? left : 256);
     if constexpr (ALONG) {
 #pragma unroll
@@ -166,7 +168,9 @@ struct Loader {
   // st: a stage (across), or a pair (along)
   __device__ __forceinline__ At stage(int st) const {
     constexpr int kSteps = ALONG ? 2 * kBK : kBK;
-    const int64_t k0 = (int64_t)st * kSteps, left = K - k0 < kSteps ? K - k0 : kSteps;
+    st = st < end ? st : end;
+    const int64_t k0 = (int64_t)st * kSteps;
+    const int left = st < end ? kSteps : rest;
     if constexpr (ALONG)  // (whole pieces: the rows go on to a multiple of 8)
       return At{base + 2 * k0, 16u * (uint32_t)((left - 1) >> 3)};
     else
@@ -183,18 +187,18 @@ struct Loader {
   }
 };
 
-// The main loop: acc = the tile's sums over stages s_beg .. s_end - 1 (s_end > s_beg;
-// along, s_beg is even) of a contraction of K steps.
+// The main loop: acc = the tile's sums over stages s_beg .. s_end - 1, both
+// multiples of the ring (4 stages, 128 steps), s_end > s_beg.  One of the operands holds
+// zeros up to a multiple of 128 steps, so that there is no other end.
 template <bool F16, bool ALONG>
 __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
-                                        const Loader<false>& lb, int64_t K, int s_beg, int s_end,
+                                        const Loader<false>& lb, int s_beg, int s_end,
                                         f32x16 (&acc)[4][4]) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wy = wave >> 1, wx = wave & 1;
   const int l32 = lane & 31, half = lane >> 5;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
-  const int nst = (int)((K + kBK - 1) / kBK);
 
 #pragma unroll
   for (int a = 0; a < 4; ++a)
@@ -316,40 +320,6 @@ __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
       __builtin_amdgcn_sched_barrier(0);
     });
   };
-  // the same without the overlap, for the last stages: steps past the end are
-  // zeros in both operands (what lies there may be an infinity)
-  auto stage_tail = [&](auto s_tag, int i, uint32_t a0) {
-    const int64_t valid = K - (int64_t)(s_beg + i) * kBK;
-#pragma unroll
-    for (int t = 0; t < kBK / 16; ++t) {
-      u32x4 ta[4], tb[4];
-#pragma unroll
-      for (int x = 0; x < 4; ++x) ta[x] = frag_a(a0 * (2 * kOp), s_tag, x, t);
-#pragma unroll
-      for (int x = 0; x < 4; ++x) tb[x] = frag_b(s_tag, x, t);
-      if (valid < kBK) {
-        const int first = 16 * t + 8 * half;  // this lane's eight steps
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int lo = first + 2 * e;
-          const uint32_t keep =
-              (lo < valid ? 0x0000FFFFu : 0u) | (lo + 1 < valid ? 0xFFFF0000u : 0u);
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            ta[x][e] &= keep;
-            tb[x][e] &= keep;
-          }
-        }
-      }
-#pragma unroll
-      for (int a = 0; a < 4; ++a)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) acc[a][b] = mfma<F16>(ta[a], tb[b], acc[a][b]);
-    }
-  };
-
-  const int total = s_end - s_beg;
-  const int full = s_end < nst || K % kBK == 0 ? total : total - 1;
   uint32_t a0 = 0, a1 = 1, a2 = 2;  // slots of this pair, the next one and the one to load
   auto turn = [&]() {
     const uint32_t t = a0;
@@ -357,12 +327,10 @@ __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
     a1 = a2;
     a2 = t;
   };
-  int i0 = 0;
-  if (kRing <= full)
-    static_for<0, 8>([&](auto x_tag) {
-      read_op(0, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{}, x_tag);
-    });
-  for (; i0 + kRing <= full; i0 += kRing) {
+  static_for<0, 8>([&](auto x_tag) {
+    read_op(0, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{}, x_tag);
+  });
+  for (int i0 = 0; i0 < s_end - s_beg; i0 += kRing) {
     static_for<0, kRing>([&](auto s_tag) {
       constexpr int S = decltype(s_tag)::value;
       stage(s_tag, i0 + S, a0, a1, a2);
@@ -370,21 +338,19 @@ __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
       stage_barrier<kLoads>();
     });
   }
-  for (; i0 < total; i0 += kRing) {  // (the stages past the end only load and wait)
-    static_for<0, kRing>([&](auto s_tag) {
-      constexpr int S = decltype(s_tag)::value;
-      const DmaStage d = dma_begin(i0 + S, a2);
-      static_for<0, kLoads>([&](auto j_tag) {
-        dma_piece(d, j_tag, std::integral_constant<int, S & 1>{});
-      });
-      if (i0 + S < total) stage_tail(s_tag, i0 + S, a0);
-      if constexpr (S & 1) turn();
-      stage_barrier<kLoads>();
-    });
-  }
   // every load has landed before the ring is used again
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
+  // (they stay in the accumulator registers until the epilogue takes them block by block)
+#pragma unroll
+  for (int a = 0; a < 4; ++a)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) asm volatile("" : "+a"(acc[a][b]));
+}
+
+// stages of a contraction of k steps
+__device__ __forceinline__ int stages(int64_t k) {
+  return (int)((k + kRing * kBK - 1) / (kRing * kBK)) * kRing;
 }
 
 // The items (token tile, word tile), words fastest, that workgroup w of P has:
@@ -418,7 +384,7 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
   const int64_t wg = xcd_remap(blockIdx.x, gridDim.x);
   if (wg >= P) return;
   const int64_t i0 = run_begin(wg, N, P), i1 = run_begin(wg + 1, N, P);
-  const int nst = (D + kBK - 1) / kBK;
+  const int nst = stages(D);
   const float k1 = kLog2e, k2 = kLog2e * inv_tau;
 
   float mx[4], sm[4], st[4];  // the running maximum, its sum, the sum at the temperature
@@ -468,8 +434,8 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
       Loader<true> la;
       la.begin(w + (int64_t)nv_i * kTM * D, words - (int64_t)nv_i * kTM, D, D, wave, lane);
       Loader<false> lb;
-      lb.begin(ht + nt_i * kTN, tp - nt_i * kTN, tp, D, wave, lane);
-      product<F16, true>(lds, la, lb, D, 0, nst, acc);
+      lb.begin(ht + nt_i * kTN, kTN, tp, nst * kBK, wave, lane);
+      product<F16, true>(lds, la, lb, 0, nst, acc);
     }
     const int v0 = nv_i * kTM + wy * 128;  // the wave's first word
     if constexpr (MODE == kStats) {
@@ -536,7 +502,9 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const int r = nt_i * kTN + wx * 128 + 32 * b + l32;
-        const HeadRow hr = rows[r < n ? r : n - 1];
+        // rows and words past the last are zeros, for dW's and dh's contractions
+        const HeadRow hr = r < n ? rows[r] : HeadRow{0.f, 0.f, 0.f, 0.f};
+        const int left = (int)(words - v0 < 128 ? words - v0 : 128) - 4 * half;
         uint8_t* row = mine + (32 * b + l32) * kRowB + 8 * half;
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
@@ -554,6 +522,11 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
               q[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], k2, -hr.lse_t));
 #pragma unroll
             for (int i = 0; i < 16; ++i) p[i] = __builtin_fmaf(hr.c2, q[i], p[i]);
+          }
+          if (words - v0 < 128) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (32 * a + 8 * (i / 4) + i % 4 >= left) p[i] = 0.f;
           }
 #pragma unroll
           for (int q = 0; q < 4; ++q)  // words 32 a + 8 q + 4 half ..
@@ -642,7 +615,7 @@ __global__ __launch_bounds__(256) void head_dh_kernel(
   const int nt = (n + kTM - 1) / kTM, nd = (D + kTN - 1) / kTN;
   const int64_t tiles = (int64_t)nt * nd, P = gridDim.x;
   const int64_t wg = xcd_remap(blockIdx.x, gridDim.x);
-  const int nst = (int)((words + kBK - 1) / kBK);
+  const int nst = stages(words);
   for (int64_t item = wg; item < tiles * parts; item += P) {
     const int s = (int)(item / tiles), tile = (int)(item % tiles);
     const int64_t m0 = (int64_t)(tile / nd) * kTM;
@@ -652,10 +625,10 @@ __global__ __launch_bounds__(256) void head_dh_kernel(
     f32x16 acc[4][4];
     {
       Loader<true> la;
-      la.begin(G + m0 * ld, n - m0, ld, words, wave, lane);
+      la.begin(G + m0 * ld, n - m0, ld, nst * kBK, wave, lane);
       Loader<false> lb;
-      lb.begin(w + d0, D - d0, D, words, wave, lane);
-      product<F16, true>(lds, la, lb, words, s * per, s_end, acc);
+      lb.begin(w + d0, D - d0, D, (int)words, wave, lane);
+      product<F16, true>(lds, la, lb, s * per, s_end, acc);
     }
     const int64_t r0 = m0 + wy * 128;
     const int c0 = d0 + wx * 128;
@@ -679,30 +652,29 @@ __global__ __launch_bounds__(256) void head_dw_kernel(
   const int nv = (int)((words + kTM - 1) / kTM), nd = (D + kTN - 1) / kTN;
   const int64_t tiles = (int64_t)nv * nd, P = gridDim.x;
   const int64_t wg = xcd_remap(blockIdx.x, gridDim.x);
-  const int nst = (n + kBK - 1) / kBK;
+  const int nst = stages(n);
   const int e = PARTS ? 0 : __builtin_amdgcn_readfirstlane(*exp);
   for (int64_t item = wg; item < tiles * parts; item += P) {
     const int s = (int)(item / tiles), tile = (int)(item % tiles);
     const int64_t m0 = (int64_t)(tile / nd) * kTM;
     const int d0 = tile % nd * kTN;
     const int s_end = s * per + per < nst ? s * per + per : nst;
-    f32x16 acc[4][4];
-    if (s * per < s_end) {
-      Loader<false> la, lb;
-      la.begin(G + m0, ld - m0, ld, n, wave, lane);
-      lb.begin(hs + d0, D - d0, D, n, wave, lane);
-      product<F16, false>(lds, la, lb, n, s * per, s_end, acc);
-    } else {  // fewer rows than the parts were made for
-#pragma unroll
-      for (int a = 0; a < 4; ++a)
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
-    }
     const int64_t r0 = m0 + wy * 128;
     const int c0 = d0 + wx * 128;
     O* out = dw + ((int64_t)s * words + r0) * D + c0;
+    if (s * per >= s_end) {  // fewer rows than the parts were made for
+      if constexpr (!ACC)
+        for (int64_t r = 0; r < 128 && r0 + r < words; ++r)
+          for (int c = lane; c < 128 && c0 + c < D; c += 64) out[r * D + c] = O(0.f);
+      continue;
+    }
+    f32x16 acc[4][4];
+    {
+      Loader<false> la, lb;
+      la.begin(G + m0, ld - m0, ld, nst * kBK, wave, lane);
+      lb.begin(hs + d0, D - d0, D, n, wave, lane);
+      product<F16, false>(lds, la, lb, s * per, s_end, acc);
+    }
     write_tile<ACC>(out, D, words - r0, D - c0, acc, [&](float v, O old) {
       if constexpr (PARTS)
         return (O)v;

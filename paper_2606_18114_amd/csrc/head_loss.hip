@@ -29,6 +29,9 @@ namespace {
 
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
+inline __host__ __device__ int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
+inline __host__ __device__ int64_t up128(int64_t v) { return (v + 127) / 128 * 128; }
+
 __device__ __forceinline__ int64_t id_at(const void* p, bool i64, int64_t i) {
   return i64 ? static_cast<const int64_t*>(p)[i] : (int64_t)static_cast<const int*>(p)[i];
 }
@@ -374,14 +377,15 @@ __global__ __launch_bounds__(256) void finish_kernel(Finish f) {
   }
 }
 
-// ht[d][r] = h[idx[r]][d]: the logits' second operand.  64 x 64 a workgroup, through LDS.
+// ht[d][r] = h[idx[r]][d]: the logits' second operand, with zeros up to a multiple of 128
+// columns d and of 256 rows r.  64 x 64 a workgroup, through LDS.
 __global__ __launch_bounds__(256) void rows_transpose_kernel(HeadIn in, Rows rows, int64_t tp,
                                                              uint16_t* __restrict__ ht) {
   __shared__ uint16_t s[64][72];
   const int n = *rows.count;
   const int64_t r0 = (int64_t)blockIdx.x * 64;
   const int d0 = blockIdx.y * 64, q = threadIdx.x >> 3, c = 8 * (threadIdx.x & 7);
-  if (r0 >= n) return;
+  if (r0 >= up256(n)) return;
 #pragma unroll
   for (int i = 0; i < 64; i += 32) {
     u32x4 v = {0, 0, 0, 0};
@@ -392,7 +396,6 @@ __global__ __launch_bounds__(256) void rows_transpose_kernel(HeadIn in, Rows row
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 64; i += 32) {
-    if (d0 + q + i >= in.D) continue;
     u32x4 v;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -478,8 +481,6 @@ __global__ __launch_bounds__(256) void dh_out_kernel(HeadIn in, const float* __r
   }
 }
 
-constexpr int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
-
 // Parts of a contraction of nst stages of `tiles` tiles on P workgroups: the
 // fewest rounds times stages, against 0.5 us for writing and reading a tile's
 // part (256 KiB each way).  A stage takes 0.8 us a workgroup; parts are a multiple of
@@ -550,7 +551,7 @@ Layout forward_layout(int64_t T, int64_t D, void* ws) {
   take(&l.rows.idx, b, &l.bytes, 4 * T);
   take(&l.rows.pos, b, &l.bytes, 4 * T);
   take(&l.rows.terms, b, &l.bytes, T);
-  take(&l.ht, b, &l.bytes, 2 * head_padded(T) * D);
+  take(&l.ht, b, &l.bytes, 2 * head_padded(T) * up128(D));
   take(&l.part, b, &l.bytes, 4 * head_part_floats(T));
   return l;
 }
@@ -563,7 +564,7 @@ Layout backward_layout(int64_t T, int64_t V, int64_t D, const HeadPlan& p, void*
   take(&l.rows.idx, b, &l.bytes, 4 * T);
   take(&l.rows.pos, b, &l.bytes, 4 * T);
   take(&l.rows.row, b, &l.bytes, (int64_t)sizeof(HeadRow) * T);
-  take(&l.ht, b, &l.bytes, 2 * head_padded(T) * D);
+  take(&l.ht, b, &l.bytes, 2 * head_padded(T) * up128(D));
   take(&l.hs, b, &l.bytes, 2 * T * D);
   take(&l.G, b, &l.bytes, 2 * up256(T) * p.piece);  // (tiles are written whole)
   take(&l.part_h, b, &l.bytes, 4 * p.parts_h * T * D);
@@ -595,7 +596,7 @@ static int64_t rows_per_group(int64_t T) {
 
 static hipError_t transpose(const HeadIn& in, const Layout& l, hipStream_t stream) {
   hipLaunchKernelGGL(rows_transpose_kernel,
-                     dim3((unsigned)((in.T + 63) / 64), (unsigned)((in.D + 63) / 64)), dim3(256), 0,
+                     dim3((unsigned)(head_padded(in.T) / 64), (unsigned)(up128(in.D) / 64)), dim3(256), 0,
                      stream, in, l.rows, head_padded(in.T), l.ht);
   return hipGetLastError();
 }
