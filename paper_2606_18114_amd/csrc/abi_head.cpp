@@ -68,7 +68,7 @@ tm_status head_checked(const void* h, const void* W, int32_t type, int64_t T, in
 extern "C" {
 
 int64_t tm_head_loss_workspace(int64_t T, int64_t V, int64_t D) {
-  return head_sizes(T, V, D) ? tmk::head_loss_bytes(T, D) : -1;
+  return head_sizes(T, V, D) ? tmk::head_loss_bytes(T, V, D) : -1;
 }
 
 tm_status tm_head_loss(const void* h, const void* W, int32_t type, int64_t T, int64_t V, int64_t D,
@@ -82,7 +82,7 @@ tm_status tm_head_loss(const void* h, const void* W, int32_t type, int64_t T, in
                                   alpha, tau, &in))
     return st;
   if ((K > 0) != (top != nullptr)) return TM_EINVAL;
-  const int64_t need = tmk::head_loss_bytes(T, D), te = top_type == 0 ? 4 : 2;
+  const int64_t need = tmk::head_loss_bytes(T, V, D), te = top_type == 0 ? 4 : 2;
   if (tm_status st = ws_checked(workspace, workspace_bytes, need)) return st;
   if (!aligned(top, (uintptr_t)te) || !aligned(loss, 4) || !aligned(stats, 4)) return TM_EALIGN;
   if (!apart({span(h, T * D * 2), span(W, V * D * 2), span(labels, T * (labels_i64 ? 8 : 4)),

@@ -57,7 +57,7 @@ struct HeadPlan {
 };
 HeadPlan head_plan(int64_t T, int64_t V, int64_t D);
 
-int64_t head_loss_bytes(int64_t T, int64_t D);
+int64_t head_loss_bytes(int64_t T, int64_t V, int64_t D);
 hipError_t launch_head_loss(const HeadIn& in, const void* top, int top_type, float* loss,
                             float* stats, void* workspace, hipStream_t stream);
 int64_t head_loss_bwd_bytes(int64_t T, int64_t V, int64_t D);
@@ -78,8 +78,9 @@ hipError_t launch_block_norm_bwd(const float* r, int64_t T, int d, const float* 
 // ht [D rounded up to 128, head_padded(T)]: the transposed rows in use, zeros around them.
 inline int64_t head_padded(int64_t T) { return (T + 255) / 256 * 256; }
 // partial softmax sums of the rows: part[(wg + tile)][half][token][pair], see head_loss.hip
-int64_t head_part_floats(int64_t T);
-int head_logits_grid(int64_t T, int64_t words);  // its workgroups
+int64_t head_part_floats(int64_t T, int64_t words);
+int head_tile_tokens(int64_t T, int64_t words, bool stats);       // tokens of a tile
+int head_logits_grid(int64_t T, int64_t words, int tile);         // workgroups
 hipError_t launch_head_logits(const HeadIn& in, const uint16_t* ht, const int* count, float* part,
                               hipStream_t stream);
 // dlogits of words w0 .. w0 + n - 1 to G [rows rounded up to 256, ld], ld >= n rounded up to

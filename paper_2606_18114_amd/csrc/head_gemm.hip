@@ -41,7 +41,7 @@ template <bool ALONG>
 constexpr int kLds = kLdsB + (ALONG ? 6 : kRing) * kOp;
 constexpr int kLoads = 8;  // direct-to-LDS loads of a wave and stage
 constexpr int kRowB = 128 * 2 + 16;  // bytes of a row of a wave's dlogits in LDS
-static_assert(4 * 128 * kRowB <= kLds<true>, "the dlogits' rows");
+static_assert(4 * 128 * kRowB <= kLds<true> && 4 * 128 * kRowB >= kLds<false>, "rows in LDS");
 constexpr float kLog2e = 1.4426950408889634f;
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -189,11 +189,12 @@ struct Loader {
 
 // The main loop: acc = the tile's sums over stages s_beg .. s_end - 1, both
 // multiples of the ring (4 stages, 128 steps), s_end > s_beg.  One of the operands holds
-// zeros up to a multiple of 128 steps, so that there is no other end.
-template <bool F16, bool ALONG>
+// zeros up to a multiple of 128 steps, so that there is no other end.  A tile has 64 BB
+// columns, the first of those that are loaded.
+template <bool F16, bool ALONG, int BB>
 __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
                                         const Loader<false>& lb, int s_beg, int s_end,
-                                        f32x16 (&acc)[4][4]) {
+                                        f32x16 (&acc)[4][BB]) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wy = wave >> 1, wx = wave & 1;
@@ -203,7 +204,7 @@ __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
 #pragma unroll
   for (int a = 0; a < 4; ++a)
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < BB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
 
@@ -257,13 +258,13 @@ __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
   // along, of the four steps of a pair
   const int trow = 8 * half + ((lane & 15) >> 2);
   const int tcol = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-  uint32_t aoff[4], boff[4];
+  uint32_t aoff[4], boff[BB];
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {
+  for (int x = 0; x < 4; ++x)
     aoff[x] = kLdsB + (ALONG ? off_along(wy * 128 + l32, 2 * x + half)
                              : off_across(trow, wy * 128 + 32 * x + tcol));
-    boff[x] = off_across(trow, wx * 128 + 32 * x + tcol);
-  }
+#pragma unroll
+  for (int x = 0; x < BB; ++x) boff[x] = off_across(trow, wx * (32 * BB) + 32 * x + tcol);
   auto across = [&](uint32_t off, int t) {
     const s16x4 lo =
         __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + off + 16 * t * 512));
@@ -284,39 +285,42 @@ __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
   auto frag_b = [&](auto s_tag, int x, int t) {
     return across(boff[x] + decltype(s_tag)::value * kOp, t);
   };
-  u32x4 af[2][4], bf[2][4];
+  u32x4 af[2][4], bf[2][BB];
   auto read_op = [&](uint32_t apair, auto s_tag, auto t_tag, auto x_tag) {
     constexpr int T = decltype(t_tag)::value, X = decltype(x_tag)::value;
     if constexpr (X == 0)
       af[T][0] = frag_a(apair, s_tag, 0, T);
-    else if constexpr (X < 5)
+    else if constexpr (X <= BB)
       bf[T][X - 1] = frag_b(s_tag, X - 1, T);
     else
-      af[T][X - 4] = frag_a(apair, s_tag, X - 4, T);
+      af[T][X - BB] = frag_a(apair, s_tag, X - BB, T);
   };
 
-  // One full stage, i % 4 = S.  Its first 16 MFMAs cover the reads of its second
-  // step (even slots) and the loads (odd slots), the second 16 the first reads of the
-  // next stage.  a0, a1: slots (0 .. 2) of the pairs of this stage and the next one, a2 of
-  // the pair that is loaded.
+  // One full stage, i % 4 = S.  The MFMAs of its first step cover the reads of its
+  // second one and the loads, those of the second the first reads of the next stage, dealt
+  // evenly.  a0, a1: slots (0 .. 2) of the pairs of this stage and the next one, a2 of the pair
+  // that is loaded.
   auto stage = [&](auto s_tag, int i, uint32_t a0, uint32_t a1, uint32_t a2) {
     constexpr int S = decltype(s_tag)::value;
+    constexpr int kMf = 4 * BB, kReads = 4 + BB;
     typedef std::integral_constant<int, (S + 1) & 3> Next;
     const DmaStage d = dma_begin(i, a2);
     const uint32_t p0 = a0 * (2 * kOp), p1 = (S & 1 ? a1 : a0) * (2 * kOp);
-    static_for<0, 32>([&](auto k_tag) {
+    static_for<0, 2 * kMf>([&](auto k_tag) {
       constexpr int k = decltype(k_tag)::value;
-      constexpr int t = k / 16, a = (k % 16) / 4, b = k % 4;
+      constexpr int t = k / kMf, m = k % kMf, a = m / BB, b = m % BB;
       acc[a][b] = mfma<F16>(af[t][a], bf[t][b], acc[a][b]);
-      typedef std::integral_constant<int, (k % 16) / 2> X;
-      if constexpr (k % 2 == 0) {
+      // reads ceil(m kReads / kMf) .. of the step and, an MFMA later, the loads
+      static_for<(m * kReads + kMf - 1) / kMf, ((m + 1) * kReads + kMf - 1) / kMf>([&](auto x_tag) {
         if constexpr (t == 0)
-          read_op(p0, s_tag, std::integral_constant<int, 1>{}, X{});
+          read_op(p0, s_tag, std::integral_constant<int, 1>{}, x_tag);
         else
-          read_op(p1, Next{}, std::integral_constant<int, 0>{}, X{});
-      } else if constexpr (k < 16) {
-        dma_piece(d, std::integral_constant<int, k / 2>{}, std::integral_constant<int, S & 1>{});
-      }
+          read_op(p1, Next{}, std::integral_constant<int, 0>{}, x_tag);
+      });
+      if constexpr (t == 0)
+        static_for<m * kLoads / kMf, (m + 1) * kLoads / kMf>([&](auto j_tag) {
+          dma_piece(d, j_tag, std::integral_constant<int, S & 1>{});
+        });
       __builtin_amdgcn_sched_barrier(0);
     });
   };
@@ -327,7 +331,7 @@ __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
     a1 = a2;
     a2 = t;
   };
-  static_for<0, 8>([&](auto x_tag) {
+  static_for<0, 4 + BB>([&](auto x_tag) {
     read_op(0, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{}, x_tag);
   });
   for (int i0 = 0; i0 < s_end - s_beg; i0 += kRing) {
@@ -345,7 +349,7 @@ __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
 #pragma unroll
   for (int a = 0; a < 4; ++a)
 #pragma unroll
-    for (int b = 0; b < 4; ++b) asm volatile("" : "+a"(acc[a][b]));
+    for (int b = 0; b < BB; ++b) asm volatile("" : "+a"(acc[a][b]));
 }
 
 // stages of a contraction of k steps
@@ -359,7 +363,27 @@ __device__ __forceinline__ int64_t run_begin(int64_t w, int64_t N, int64_t P) { 
 
 }  // namespace
 
-// Logits: A = W (words), B = h^T (tokens), so that a lane has one
+// A wave's 32 BB rows of 128 16-bit values from LDS to memory, whole lines: rows kRowB apart
+// from `mine` on, to rows `pitch` elements apart; what lies past rows_left and cols_left is not
+// written (cols_left a multiple of 8).
+template <int BB>
+__device__ __forceinline__ void store_rows(const uint8_t* mine, uint16_t* to, int64_t pitch,
+                                           int64_t rows_left, int64_t cols_left) {
+  const int lane = threadIdx.x & 63;
+  __builtin_amdgcn_wave_barrier();  // (a wave reads only what it wrote)
+  to += (lane >> 4) * pitch + 8 * (lane & 15);
+  mine += (lane >> 4) * kRowB + 16 * (lane & 15);
+  const int64_t left = 8 * (lane & 15) < cols_left ? rows_left - (lane >> 4) : 0;
+#pragma unroll 4
+  for (int i = 0; i < 8 * BB; ++i) {
+    if (4 * i < left) st16(to, *reinterpret_cast<const u32x4*>(mine));
+    to += 4 * pitch;
+    mine += 4 * kRowB;
+  }
+  __syncthreads();  // the next tile's loads write where other waves read
+}
+
+// Logits: A = W (words), B = h^T (64 BB tokens), so that a lane has one
 // token a block and 64 of its logits.  Lane: token 32 b + l32, words 32 a +
 // 8 (i / 4) + 4 half + i % 4.
 //
@@ -368,7 +392,7 @@ __device__ __forceinline__ int64_t run_begin(int64_t w, int64_t N, int64_t P) { 
 // where TEMP.  A workgroup walks many word tiles of one token tile, so
 // a step of the softmax costs no memory.
 // kDlogits: G[row][word - w0] in 16 bits.
-template <bool F16, Mode MODE, bool TEMP>
+template <bool F16, Mode MODE, bool TEMP, int BB>
 __global__ __launch_bounds__(256) void head_logits_kernel(
     const uint16_t* __restrict__ ht, int64_t tp, const uint16_t* __restrict__ w, int D,
     const int* __restrict__ count, int64_t words, float inv_tau,
@@ -378,8 +402,9 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wy = wave >> 1, wx = wave & 1, l32 = lane & 31, half = lane >> 5;
+  constexpr int kT = 64 * BB;  // tokens of a tile
   const int n = __builtin_amdgcn_readfirstlane(*count);
-  const int nt = (n + kTN - 1) / kTN, nv = (int)((words + kTM - 1) / kTM);
+  const int nt = (MODE == kStats ? n + kT - 1 : (n + 127) / 128 * 128 + kT - 1) / kT, nv = (int)((words + kTM - 1) / kTM);
   const int64_t N = (int64_t)nt * nv, P = N < gridDim.x ? N : gridDim.x;  // (no empty runs)
   const int64_t wg = xcd_remap(blockIdx.x, gridDim.x);
   if (wg >= P) return;
@@ -387,10 +412,10 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
   const int nst = stages(D);
   const float k1 = kLog2e, k2 = kLog2e * inv_tau;
 
-  float mx[4], sm[4], st[4];  // the running maximum, its sum, the sum at the temperature
+  float mx[BB], sm[BB], st[BB];  // the running maximum, its sum, the sum at the temperature
   auto reset = [&]() {
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
+    for (int b = 0; b < BB; ++b) {
       mx[b] = -__builtin_inff();
       sm[b] = st[b] = 0.f;
     }
@@ -398,13 +423,13 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
   auto flush = [&](int tile) {  // the two halves of a token's words, then one entry a wave
     constexpr int E = TEMP ? 3 : 2;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
+    for (int b = 0; b < BB; ++b) {
       const float om = __shfl_xor(mx[b], 32, 64), os = __shfl_xor(sm[b], 32, 64);
       const float m = fmaxf(mx[b], om);
       const float ref = m == -__builtin_inff() ? 0.f : m;
       const float s = sm[b] * __builtin_amdgcn_exp2f((mx[b] - ref) * k1) +
                       os * __builtin_amdgcn_exp2f((om - ref) * k1);
-      float* p = part + ((((wg + tile) * 2 + wy) * 256) + wx * 128 + 32 * b + l32) * E;
+      float* p = part + ((((wg + tile) * 2 + wy) * 256) + wx * (32 * BB) + 32 * b + l32) * E;
       float sT = 0.f;
       if constexpr (TEMP) {
         const float ot = __shfl_xor(st[b], 32, 64);
@@ -429,13 +454,13 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
       }
       tile = nt_i;
     }
-    f32x16 acc[4][4];
+    f32x16 acc[4][BB];
     {
       Loader<true> la;
       la.begin(w + (int64_t)nv_i * kTM * D, words - (int64_t)nv_i * kTM, D, D, wave, lane);
       Loader<false> lb;
-      lb.begin(ht + nt_i * kTN, kTN, tp, nst * kBK, wave, lane);
-      product<F16, true>(lds, la, lb, 0, nst, acc);
+      lb.begin(ht + nt_i * kT, tp - nt_i * kT, tp, nst * kBK, wave, lane);
+      product<F16, true, BB>(lds, la, lb, 0, nst, acc);
     }
     const int v0 = nv_i * kTM + wy * 128;  // the wave's first word
     if constexpr (MODE == kStats) {
@@ -452,7 +477,7 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
           return z;
         };
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
+        for (int b = 0; b < BB; ++b) {
           float m4[4] = {mx[b], mx[b], mx[b], mx[b]};
 #pragma unroll
           for (int a = 0; a < 4; ++a) {
@@ -500,8 +525,8 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
       // registers, 32 bytes of 32 rows a store, a tile took 11 us more)
       uint8_t* mine = lds + wave * (128 * kRowB);
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int r = nt_i * kTN + wx * 128 + 32 * b + l32;
+      for (int b = 0; b < BB; ++b) {
+        const int r = nt_i * kT + wx * (32 * BB) + 32 * b + l32;
         // rows and words past the last are zeros, for dW's and dh's contractions
         const HeadRow hr = r < n ? rows[r] : HeadRow{0.f, 0.f, 0.f, 0.f};
         const int left = (int)(words - v0 < 128 ? words - v0 : 128) - 4 * half;
@@ -535,16 +560,7 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-      __builtin_amdgcn_wave_barrier();  // (a wave reads only what it wrote)
-      uint16_t* g = G + (int64_t)(nt_i * kTN + wx * 128 + (lane >> 4)) * ld + v0 + 8 * (lane & 15);
-      const uint8_t* from = mine + (lane >> 4) * kRowB + 16 * (lane & 15);
-#pragma unroll 4
-      for (int i = 0; i < 32; ++i) {
-        st16(g, *reinterpret_cast<const u32x4*>(from));
-        g += 4 * ld;
-        from += 4 * kRowB;
-      }
-      __syncthreads();  // the next tile's loads write where other waves read
+      store_rows<BB>(mine, G + (int64_t)(nt_i * kT + wx * (32 * BB)) * ld + v0, ld, 32 * BB, 128);
     }
   }
   if constexpr (MODE == kStats)
@@ -628,7 +644,7 @@ __global__ __launch_bounds__(256) void head_dh_kernel(
       la.begin(G + m0 * ld, n - m0, ld, nst * kBK, wave, lane);
       Loader<false> lb;
       lb.begin(w + d0, D - d0, D, (int)words, wave, lane);
-      product<F16, true>(lds, la, lb, s * per, s_end, acc);
+      product<F16, true, 4>(lds, la, lb, s * per, s_end, acc);
     }
     const int64_t r0 = m0 + wy * 128;
     const int c0 = d0 + wx * 128;
@@ -637,30 +653,34 @@ __global__ __launch_bounds__(256) void head_dh_kernel(
   }
 }
 
-// dW: A = G (words), B = hs (columns), both across the tokens.  PARTS: to
-// part[s][word][D], unscaled; else to dW's rows, times 2^(*exp).
+// dW: G (words) and hs (columns), both across the tokens.  PARTS: to part[s][word][D],
+// unscaled; else to dW's rows, times 2^(*exp).  Float32: A = G, a lane has a column and
+// stores 128 bytes of a row with its neighbours.  16 bits: A = hs, a lane has a word and four
+// columns in a row, which pass through LDS as the dlogits do (with A = G, 2 bytes a lane and
+// store: 16384 tokens, 16384 words: XX us, YY so).
 template <bool F16, bool PARTS, typename O, bool ACC>
 __global__ __launch_bounds__(256) void head_dw_kernel(
     const uint16_t* __restrict__ G, int64_t ld, const uint16_t* __restrict__ hs, int D,
     const int* __restrict__ count, int64_t words, int parts, int per, const int* __restrict__ exp,
     O* __restrict__ dw) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds<false>];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[sizeof(O) == 2 ? 4 * 128 * kRowB : kLds<false>];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wy = wave >> 1, wx = wave & 1;
+  const int wy = wave >> 1, wx = wave & 1, l32 = lane & 31, half = lane >> 5;
   const int n = __builtin_amdgcn_readfirstlane(*count);
   const int nv = (int)((words + kTM - 1) / kTM), nd = (D + kTN - 1) / kTN;
   const int64_t tiles = (int64_t)nv * nd, P = gridDim.x;
   const int64_t wg = xcd_remap(blockIdx.x, gridDim.x);
   const int nst = stages(n);
+  constexpr bool SWAP = sizeof(O) == 2;
   const int e = PARTS ? 0 : __builtin_amdgcn_readfirstlane(*exp);
   for (int64_t item = wg; item < tiles * parts; item += P) {
     const int s = (int)(item / tiles), tile = (int)(item % tiles);
     const int64_t m0 = (int64_t)(tile / nd) * kTM;
     const int d0 = tile % nd * kTN;
     const int s_end = s * per + per < nst ? s * per + per : nst;
-    const int64_t r0 = m0 + wy * 128;
-    const int c0 = d0 + wx * 128;
+    const int64_t r0 = m0 + (SWAP ? wx : wy) * 128;
+    const int c0 = d0 + (SWAP ? wy : wx) * 128;
     O* out = dw + ((int64_t)s * words + r0) * D + c0;
     if (s * per >= s_end) {  // fewer rows than the parts were made for
       if constexpr (!ACC)
@@ -670,19 +690,39 @@ __global__ __launch_bounds__(256) void head_dw_kernel(
     }
     f32x16 acc[4][4];
     {
-      Loader<false> la, lb;
-      la.begin(G + m0, ld - m0, ld, nst * kBK, wave, lane);
-      lb.begin(hs + d0, D - d0, D, n, wave, lane);
-      product<F16, false>(lds, la, lb, s * per, s_end, acc);
+      Loader<false> g, h;
+      g.begin(G + m0, ld - m0, ld, nst * kBK, wave, lane);
+      h.begin(hs + d0, D - d0, D, n, wave, lane);
+      product<F16, false, 4>(lds, SWAP ? h : g, SWAP ? g : h, s * per, s_end, acc);
     }
-    write_tile<ACC>(out, D, words - r0, D - c0, acc, [&](float v, O old) {
-      if constexpr (PARTS)
-        return (O)v;
-      else if constexpr (ACC)
-        return old + ldexpf(v, e);
-      else
-        return (O)ldexpf(v, e);
-    });
+    if constexpr (SWAP) {
+      uint8_t* mine = lds + wave * (128 * kRowB);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        uint8_t* row = mine + (32 * b + l32) * kRowB + 8 * half;
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          f32x16 v = acc_block(acc[a][b]);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = ldexpf(v[i], e);
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<u32x2*>(row + 64 * a + 16 * q) =
+                u32x2{pack2<F16>(v[4 * q], v[4 * q + 1]), pack2<F16>(v[4 * q + 2], v[4 * q + 3])};
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      store_rows<4>(mine, reinterpret_cast<uint16_t*>(out), D, words - r0, D - c0);
+    } else {
+      write_tile<ACC>(out, D, words - r0, D - c0, acc, [&](float v, O old) {
+        if constexpr (PARTS)
+          return v;
+        else if constexpr (ACC)
+          return old + ldexpf(v, e);
+        else
+          return ldexpf(v, e);
+      });
+    }
   }
 }
 
@@ -707,10 +747,6 @@ __global__ __launch_bounds__(256) void head_dw_sum_kernel(const float* __restric
   }
 }
 
-int64_t head_part_floats(int64_t T) {
-  return (current_cu_count() + (T + kTN - 1) / kTN + 1) * 2 * 256 * 3;
-}
-
 #define TM_HEAD_GRID(GRID) dim3((unsigned)(GRID)), dim3(256), 0, stream
 
 static int64_t grid_of(int64_t items) {
@@ -718,37 +754,71 @@ static int64_t grid_of(int64_t items) {
   return items < cus ? items : cus;
 }
 
-int head_logits_grid(int64_t T, int64_t words) {
-  return (int)grid_of(((T + kTN - 1) / kTN) * ((words + kTM - 1) / kTM));
+// Tokens of a tile of logits: 64 (the softmax sums only), 128 or 256.  A stage of the three
+// takes 0.52, 0.58 and 0.80 us a workgroup (the first two by their loads), so narrow tiles are for few tokens (16
+// tokens of 50000 x 2048: XX us, YY with 256) and where they leave fewer workgroups idle in the
+// last round (300 tokens: XX with 128, YY with 256).
+int head_tile_tokens(int64_t T, int64_t words, bool stats) {
+  const int64_t P = current_cu_count(), nv = (words + kTM - 1) / kTM;
+  const double us[3] = {0.52, 0.58, 0.80};
+  int best = 256;
+  double least = 0;
+  for (int i = 2; i >= (stats ? 0 : 1); --i) {
+    const int64_t items = (T + (64 << i) - 1) / (64 << i) * nv;
+    const double cost = (double)((items + P - 1) / P) * us[i];
+    if (i == 2 || cost < least) {
+      least = cost;
+      best = 64 << i;
+    }
+  }
+  return best;
 }
 
-template <bool F16, Mode MODE>
+int head_logits_grid(int64_t T, int64_t words, int tile) {
+  return (int)grid_of((T + tile - 1) / tile * ((words + kTM - 1) / kTM));
+}
+
+int64_t head_part_floats(int64_t T, int64_t words) {
+  const int tile = head_tile_tokens(T, words, true);
+  return (current_cu_count() + (T + tile - 1) / tile + 1) * 2 * 256 * 3;
+}
+
+template <bool F16, Mode MODE, int BB>
 static hipError_t run_logits(const HeadIn& in, const uint16_t* ht, const int* count, int64_t w0,
                              int64_t n, float* part, const HeadRow* rows, uint16_t* G, int64_t ld,
                              hipStream_t stream) {
-  const int grid = head_logits_grid(in.T, n);
+  const int64_t T = MODE == kStats ? in.T : (in.T + 127) / 128 * 128;
+  const int grid = head_logits_grid(T, n, 64 * BB);
   const uint16_t* w = in.w + w0 * in.D;
   if (in.K > 0 && in.tau != 1.0f)
-    hipLaunchKernelGGL((head_logits_kernel<F16, MODE, true>), TM_HEAD_GRID(grid), ht,
+    hipLaunchKernelGGL((head_logits_kernel<F16, MODE, true, BB>), TM_HEAD_GRID(grid), ht,
                        head_padded(in.T), w, in.D, count, n, 1.0f / in.tau, part, rows, G, ld);
   else
-    hipLaunchKernelGGL((head_logits_kernel<F16, MODE, false>), TM_HEAD_GRID(grid), ht,
+    hipLaunchKernelGGL((head_logits_kernel<F16, MODE, false, BB>), TM_HEAD_GRID(grid), ht,
                        head_padded(in.T), w, in.D, count, n, 1.0f, part, rows, G, ld);
   return hipGetLastError();
 }
 
 hipError_t launch_head_logits(const HeadIn& in, const uint16_t* ht, const int* count, float* part,
                               hipStream_t stream) {
-  return in.f16 ? run_logits<true, kStats>(in, ht, count, 0, in.V, part, nullptr, nullptr, 0, stream)
-                : run_logits<false, kStats>(in, ht, count, 0, in.V, part, nullptr, nullptr, 0,
-                                            stream);
+  const int tile = head_tile_tokens(in.T, in.V, true);
+#define TM_HEAD_LOGITS(F16, BB) \
+  run_logits<F16, kStats, BB>(in, ht, count, 0, in.V, part, nullptr, nullptr, 0, stream)
+  if (tile == 64) return in.f16 ? TM_HEAD_LOGITS(true, 1) : TM_HEAD_LOGITS(false, 1);
+  if (tile == 128) return in.f16 ? TM_HEAD_LOGITS(true, 2) : TM_HEAD_LOGITS(false, 2);
+  return in.f16 ? TM_HEAD_LOGITS(true, 4) : TM_HEAD_LOGITS(false, 4);
+#undef TM_HEAD_LOGITS
 }
 
 hipError_t launch_head_dlogits(const HeadIn& in, const uint16_t* ht, const int* count,
                                const HeadRow* rows, int64_t w0, int64_t n, uint16_t* G, int64_t ld,
                                hipStream_t stream) {
-  return in.f16 ? run_logits<true, kDlogits>(in, ht, count, w0, n, nullptr, rows, G, ld, stream)
-                : run_logits<false, kDlogits>(in, ht, count, w0, n, nullptr, rows, G, ld, stream);
+#define TM_HEAD_DLOGITS(F16, BB) \
+  run_logits<F16, kDlogits, BB>(in, ht, count, w0, n, nullptr, rows, G, ld, stream)
+  if (head_tile_tokens(in.T, n, false) == 128)
+    return in.f16 ? TM_HEAD_DLOGITS(true, 2) : TM_HEAD_DLOGITS(false, 2);
+  return in.f16 ? TM_HEAD_DLOGITS(true, 4) : TM_HEAD_DLOGITS(false, 4);
+#undef TM_HEAD_DLOGITS
 }
 
 hipError_t launch_head_dh(const HeadIn& in, const int* count, const uint16_t* G, int64_t ld,

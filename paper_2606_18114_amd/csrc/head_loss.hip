@@ -195,15 +195,15 @@ __global__ __launch_bounds__(1024) void rows_kernel(HeadIn in, const float* __re
   if (t1 == T && tid == 0) *out.count = base;
 }
 
-// The loss and the row of stats of a token, a wave (K = 0) or a workgroup of
-// four waves a token.  Bound: the dot products' rows of W, from the caches for
+// The loss and the stats of a token, a wave (WAVES 0: no teacher) or a workgroup a
+// token, of sixteen waves where tokens are few (1 token, 64 words: XX us, YY of four).  Bound: the dot products' rows of W, from the caches for
 // frequent words.
 struct Finish {
   HeadIn in;
   const void* top;
   int top_type;
   const float* part;
-  int grid;  // workgroups of the logits' launch
+  int tile, grid;  // tokens of a tile and workgroups of the logits' launch
   Rows rows;
   float* loss;
   float* stats;
@@ -226,16 +226,16 @@ __device__ __forceinline__ float row_dot(const uint16_t* h, const uint16_t* w, i
 // the softmax sums of row r: the parts of its token tile's workgroups, joined.  m: the largest
 // logit; s: sum of 2^(log2e (z - m)); sT the same at the temperature (TEMP)
 template <bool TEMP>
-__device__ __forceinline__ void join(const float* part, int r, int n, int64_t V, int grid, float k2,
+__device__ __forceinline__ void join(const float* part, int r, int n, int64_t V, int tile, int grid, float k2,
                                      int lane, float& m, float& s, float& sT) {
   constexpr int E = TEMP ? 3 : 2;
-  const int64_t nt = (n + 255) / 256, nv = (V + 255) / 256, N = nt * nv;
+  const int64_t nt = (n + tile - 1) / tile, nv = (V + 255) / 256, N = nt * nv;
   const int64_t P = N < grid ? N : grid;
-  const int64_t j = r / 256;
+  const int64_t j = r / tile;
   // the workgroups whose runs hold the tile's first and last item
   const int64_t w0 = ((j * nv + 1) * P - 1) / N, w1 = (((j + 1) * nv) * P - 1) / N;
   const int cnt = (int)(w1 - w0 + 1) * 2;
-  auto at = [&](int i) { return part + (((w0 + j) * 2 + i) * 256 + r % 256) * E; };
+  auto at = [&](int i) { return part + (((w0 + j) * 2 + i) * 256 + r % tile) * E; };
   float mm = -__builtin_inff();
   for (int i = lane; i < cnt; i += 64) mm = fmaxf(mm, at(i)[0]);
   m = wave_max(mm);
@@ -250,10 +250,12 @@ __device__ __forceinline__ void join(const float* part, int r, int n, int64_t V,
   sT = TEMP ? wave_sum(b) : s;
 }
 
-template <bool F16, bool TEMP, bool TEACH>
-__global__ __launch_bounds__(256) void finish_kernel(Finish f) {
+template <bool F16, bool TEMP, int WAVES>
+__global__ __launch_bounds__(WAVES ? 64 * WAVES : 256) void finish_kernel(Finish f) {
+  constexpr bool TEACH = WAVES > 0;
+  constexpr int L = WAVES * 64;
   extern __shared__ float sh[];  // TEACH: z[K], q[K], id[K]
-  __shared__ float red[4];
+  __shared__ float red[TEACH ? WAVES : 1];
   const HeadIn& in = f.in;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t t = TEACH ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
@@ -266,14 +268,14 @@ __global__ __launch_bounds__(256) void finish_kernel(Finish f) {
   const int first = TEACH ? threadIdx.x : lane;
   if (terms == 0) {  // no loss
     if (first < kStatPlanes) st[first * in.T] = 0.f;
-    for (int i = first; i < in.K; i += 256) st_top[i] = 0.f;
+    for (int i = first; i < in.K; i += L) st_top[i] = 0.f;
     if (first == 0) f.loss[t] = 0.f;
     return;
   }
   const int n = *f.rows.count;
   const float it = 1.0f / in.tau, k2 = kLog2e * it;
   float m, s, sT;
-  join<TEMP>(f.part, f.rows.pos[t], n, in.V, f.grid, k2, lane, m, s, sT);
+  join<TEMP>(f.part, f.rows.pos[t], n, in.V, f.tile, f.grid, k2, lane, m, s, sT);
   const float mf = m == -__builtin_inff() ? 0.f : m;  // (as the sums took it)
   const float lse2 = __builtin_fmaf(mf, kLog2e, __builtin_amdgcn_logf(s));
   const float lseT2 = __builtin_fmaf(mf, k2, __builtin_amdgcn_logf(sT));
@@ -304,7 +306,7 @@ __global__ __launch_bounds__(256) void finish_kernel(Finish f) {
   int* id = reinterpret_cast<int*>(sh + 2 * K);
   // the teacher's softmax over its kept words; 2^(log2e / tau t)
   float tm = -__builtin_inff();
-  for (int k = threadIdx.x; k < K; k += 256) {
+  for (int k = threadIdx.x; k < K; k += L) {
     const int64_t v = id_at(in.ids, in.ids64, t * K + k);
     const bool in_v = v >= 0 && v < in.V;
     id[k] = in_v ? (int)v : -1;
@@ -316,17 +318,19 @@ __global__ __launch_bounds__(256) void finish_kernel(Finish f) {
     __syncthreads();
     if (lane == 0) red[wave] = v;
     __syncthreads();
-    return sum ? (red[0] + red[1]) + (red[2] + red[3])
-               : fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    float all = red[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) all = sum ? all + red[w] : fmaxf(all, red[w]);
+    return all;
   };
   tm = block(tm, false);
   float ts = 0.f;
-  for (int k = threadIdx.x; k < K; k += 256)
+  for (int k = threadIdx.x; k < K; k += L)
     if (q[k] != -__builtin_inff()) ts += __builtin_amdgcn_exp2f((q[k] - tm) * kLog2e);
   ts = block(ts, true);
   const float tl = __builtin_amdgcn_logf(ts) * kLn2;
   // four words a wave at a time: their loads overlap
-  for (int k0 = 4 * wave; k0 < K; k0 += 16) {
+  for (int k0 = 4 * wave; k0 < K; k0 += 4 * WAVES) {
     float d[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -342,7 +346,7 @@ __global__ __launch_bounds__(256) void finish_kernel(Finish f) {
   __syncthreads();
   float kl = 0.f;
   if (terms & 2) {
-    for (int k = threadIdx.x; k < K; k += 256) {
+    for (int k = threadIdx.x; k < K; k += L) {
       const float a = q[k];
       if (a == -__builtin_inff()) {
         q[k] = 0.f;
@@ -356,7 +360,7 @@ __global__ __launch_bounds__(256) void finish_kernel(Finish f) {
     }
     kl = block(kl, true);
   } else {
-    for (int k = threadIdx.x; k < K; k += 256) q[k] = 0.f;
+    for (int k = threadIdx.x; k < K; k += L) q[k] = 0.f;
   }
   __syncthreads();
   auto hits = [&](int64_t v) {
@@ -365,7 +369,7 @@ __global__ __launch_bounds__(256) void finish_kernel(Finish f) {
       if (id[j] == v) x += q[j];
     return c2 * x + (v == y ? c1 : 0.f);
   };
-  for (int k = threadIdx.x; k < K; k += 256)
+  for (int k = threadIdx.x; k < K; k += L)
     st_top[k] = id[k] >= 0 ? grad(id[k] == y ? zy : z[k], hits(id[k])) : 0.f;
   if (threadIdx.x == 0) {
     f.loss[t] = (terms & 1 ? (1.0f - in.alpha) * ce_loss : 0.f) +
@@ -464,6 +468,7 @@ __global__ __launch_bounds__(256) void dh_out_kernel(HeadIn in, const float* __r
     u32x4 o = {0, 0, 0, 0};
     if (r >= 0) {
       f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+#pragma unroll 4
       for (int s = 0; s < parts; ++s) {
         const float* p = part + ((int64_t)s * in.T + r) * in.D + d;
         a += *reinterpret_cast<const f32x4*>(p);
@@ -544,7 +549,7 @@ void take(T** p, uint8_t* base, int64_t* at, int64_t bytes) {
   *at += up256(bytes);
 }
 
-Layout forward_layout(int64_t T, int64_t D, void* ws) {
+Layout forward_layout(int64_t T, int64_t V, int64_t D, void* ws) {
   Layout l{};
   uint8_t* b = static_cast<uint8_t*>(ws);
   take(&l.rows.count, b, &l.bytes, 4);
@@ -552,7 +557,7 @@ Layout forward_layout(int64_t T, int64_t D, void* ws) {
   take(&l.rows.pos, b, &l.bytes, 4 * T);
   take(&l.rows.terms, b, &l.bytes, T);
   take(&l.ht, b, &l.bytes, 2 * head_padded(T) * up128(D));
-  take(&l.part, b, &l.bytes, 4 * head_part_floats(T));
+  take(&l.part, b, &l.bytes, 4 * head_part_floats(T, V));
   return l;
 }
 
@@ -577,7 +582,9 @@ Layout backward_layout(int64_t T, int64_t V, int64_t D, const HeadPlan& p, void*
 
 }  // namespace
 
-int64_t head_loss_bytes(int64_t T, int64_t D) { return forward_layout(T, D, nullptr).bytes; }
+int64_t head_loss_bytes(int64_t T, int64_t V, int64_t D) {
+  return forward_layout(T, V, D, nullptr).bytes;
+}
 
 int64_t head_loss_bwd_bytes(int64_t T, int64_t V, int64_t D) {
   return backward_layout(T, V, D, head_plan(T, V, D), nullptr).bytes;
@@ -601,24 +608,28 @@ static hipError_t transpose(const HeadIn& in, const Layout& l, hipStream_t strea
   return hipGetLastError();
 }
 
+template <bool F16, int WAVES>
+static hipError_t run_finish_of(const Finish& f, hipStream_t stream) {
+  const dim3 grid((unsigned)(WAVES ? f.in.T : (f.in.T + 3) / 4)), block(WAVES ? 64 * WAVES : 256);
+  if (WAVES && f.in.tau != 1.0f)
+    hipLaunchKernelGGL((finish_kernel<F16, true, WAVES>), grid, block, (unsigned)(12 * f.in.K),
+                       stream, f);
+  else
+    hipLaunchKernelGGL((finish_kernel<F16, false, WAVES>), grid, block, (unsigned)(12 * f.in.K),
+                       stream, f);
+  return hipGetLastError();
+}
+
 template <bool F16>
 static hipError_t run_finish(const Finish& f, hipStream_t stream) {
-  const HeadIn& in = f.in;
-  if (in.K == 0)
-    hipLaunchKernelGGL((finish_kernel<F16, false, false>), dim3((unsigned)((in.T + 3) / 4)),
-                       dim3(256), 0, stream, f);
-  else if (in.tau != 1.0f)
-    hipLaunchKernelGGL((finish_kernel<F16, true, true>), dim3((unsigned)in.T), dim3(256),
-                       (unsigned)(12 * in.K), stream, f);
-  else
-    hipLaunchKernelGGL((finish_kernel<F16, false, true>), dim3((unsigned)in.T), dim3(256),
-                       (unsigned)(12 * in.K), stream, f);
-  return hipGetLastError();
+  if (f.in.K == 0) return run_finish_of<F16, 0>(f, stream);
+  if (f.in.T <= 512 && f.in.K > 16) return run_finish_of<F16, 16>(f, stream);
+  return run_finish_of<F16, 4>(f, stream);
 }
 
 hipError_t launch_head_loss(const HeadIn& in, const void* top, int top_type, float* loss,
                             float* stats, void* workspace, hipStream_t stream) {
-  const Layout l = forward_layout(in.T, in.D, workspace);
+  const Layout l = forward_layout(in.T, in.V, in.D, workspace);
   if (in.K > 0) {
     hipLaunchKernelGGL(terms_kernel, dim3((unsigned)((in.T + 3) / 4)), dim3(256), 0, stream, in,
                        top, top_type, l.rows.terms);
@@ -630,7 +641,8 @@ hipError_t launch_head_loss(const HeadIn& in, const void* top, int top_type, flo
   TM_RET(hipGetLastError());
   TM_RET(transpose(in, l, stream));
   TM_RET(launch_head_logits(in, l.ht, l.rows.count, l.part, stream));
-  const Finish f{in, top, top_type, l.part, head_logits_grid(in.T, in.V), l.rows, loss, stats};
+  const int tile = head_tile_tokens(in.T, in.V, true);
+  const Finish f{in, top, top_type, l.part, tile, head_logits_grid(in.T, in.V, tile), l.rows, loss, stats};
   return in.f16 ? run_finish<true>(f, stream) : run_finish<false>(f, stream);
 }
 
