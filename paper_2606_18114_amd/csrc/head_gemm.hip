@@ -40,8 +40,6 @@ constexpr int kLdsB = kRing * kOp;
 template <bool ALONG>
 constexpr int kLds = kLdsB + (ALONG ? 6 : kRing) * kOp;
 constexpr int kLoads = 8;  // direct-to-LDS loads of a wave and stage
-constexpr int kRowB = 128 * 2 + 16;  // bytes of a row of a wave's dlogits in LDS
-static_assert(4 * 128 * kRowB <= kLds<true> && 4 * 128 * kRowB >= kLds<false>, "rows in LDS");
 constexpr float kLog2e = 1.4426950408889634f;
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -135,14 +133,14 @@ struct Loader {
   int end, rest;  // the contraction's last stage (along: pair), and its steps
 
   // left: rows (along) or columns (across; a multiple of 8) of the array from the tile on
-  __device__ __forceinline__ void begin(const uint16_t* b, int64_t left, int64_t pitch_,
-                                        int K, int wave, int lane) {
+  __device__ __forceinline__ void begin(const uint16_t* b, int left, int64_t pitch_, int K,
+                                        int wave, int lane) {
     base = reinterpret_cast<const uint8_t*>(b);
     pitch = 2 * pitch_;
     constexpr int kSteps = ALONG ? 2 * kBK : kBK;
     end = __builtin_amdgcn_readfirstlane((K - 1) / kSteps);
     rest = __builtin_amdgcn_readfirstlane(K - end * kSteps);
-    const int most = (int)(left < 256 ? left : 256);
+    const int most = left < 256 ? left : 256;
     if constexpr (ALONG) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {  // 8 rows a load; wave w's are 64 w ..
@@ -187,38 +185,25 @@ struct Loader {
   }
 };
 
-// The main loop: acc = the tile's sums over stages s_beg .. s_end - 1, both
-// multiples of the ring (4 stages, 128 steps), s_end > s_beg.  One of the operands holds
-// zeros up to a multiple of 128 steps, so that there is no other end.  A tile has 64 BB
-// columns, the first of those that are loaded.
-template <bool F16, bool ALONG, int BB>
-__device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
-                                        const Loader<false>& lb, int s_beg, int s_end,
-                                        f32x16 (&acc)[4][BB]) {
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wy = wave >> 1, wx = wave & 1;
-  const int l32 = lane & 31, half = lane >> 5;
-  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
-
-#pragma unroll
-  for (int a = 0; a < 4; ++a)
-#pragma unroll
-    for (int b = 0; b < BB; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
+// What a stage's loads need, and the loads
+template <bool ALONG>
+struct Loads {
+  const Loader<ALONG>& la;
+  const Loader<false>& lb;
+  uint32_t lds0;  // the wave's part of the ring
+  int s_beg, s_end;
 
   // Stages and slots are counted from s_beg.  Past the range the last stage is loaded again.
-  struct DmaStage {
+  struct Stage {
     typename Loader<ALONG>::At a;
     typename Loader<false>::At b;
     uint32_t adst, bdst;
   };
   // the loads that go with stage i: the second operand's stage i + 3 and the first's, or
   // half of its pair i / 2 + 2, to slot aslot
-  auto dma_begin = [&](int i, uint32_t aslot) {
+  __device__ __forceinline__ Stage begin(int i, uint32_t aslot, int wave) const {
     const int st = s_beg + i + 3 < s_end ? s_beg + i + 3 : s_end - 1;
-    DmaStage d;
+    Stage d;
     d.b = lb.stage(st);
     d.bdst = lds0 + (uint32_t)((i + 3) & 3) * kOp + 4096u * wave;
     if constexpr (ALONG) {
@@ -230,28 +215,56 @@ __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
       d.adst = lds0 + kLdsB + (uint32_t)((i + 3) & 3) * kOp + 4096u * wave;
     }
     return d;
-  };
-  // load J of the eight of stage i (par = i % 2)
-  auto dma_piece = [&](const DmaStage& d, auto j_tag, auto par_tag) {
-    constexpr int J = decltype(j_tag)::value, I = J % 4, kPar = decltype(par_tag)::value;
+  }
+  // load J of the eight of stage i (PAR = i % 2)
+  template <int J, int PAR>
+  __device__ __forceinline__ void piece(const Stage& d) const {
     if constexpr (J < 4)
-      la.template load<ALONG ? 4 * kPar + I : I>(d.a, d.adst);
+      la.template load<ALONG ? 4 * PAR + J : J>(d.a, d.adst);
     else
-      lb.template load<I>(d.b, d.bdst);
-  };
-
-  {  // the first three stages of the second operand, three stages or two pairs of the first
+      lb.template load<J - 4>(d.b, d.bdst);
+  }
+  // before the main loop: three stages of the second operand, three stages or two pairs of the
+  // first (along, the third pair's slot is not written)
+  __device__ __forceinline__ void first(int wave) const {
     static_for<0, 4>([&](auto p_tag) {
       constexpr int p = decltype(p_tag)::value;
       if constexpr (!ALONG && p == 0) return;
-      const DmaStage d = dma_begin(p - 4, ALONG ? (uint32_t)(p / 2) : 0u);
+      const Stage d = begin(p - 4, ALONG ? (uint32_t)(p / 2) : 0u, wave);
       // (stage p - 4: the second operand's p - 1, the first's p - 1 or pair p / 2)
       static_for<0, kLoads>([&](auto j_tag) {
         if constexpr (p > 0 || decltype(j_tag)::value < 4)
-          dma_piece(d, j_tag, std::integral_constant<int, p % 2>{});
+          piece<decltype(j_tag)::value, p % 2>(d);
       });
     });
   }
+};
+
+template <bool ALONG>
+__device__ __forceinline__ Loads<ALONG> loads_of(uint8_t* lds, const Loader<ALONG>& la,
+                                                 const Loader<false>& lb, int s_beg, int s_end) {
+  return Loads<ALONG>{la, lb, (uint32_t)(uintptr_t)lds, s_beg, s_end};
+}
+
+// The main loop: acc = the tile's sums over stages s_beg .. s_end - 1, both
+// multiples of the ring (4 stages, 128 steps), s_end > s_beg.  One of the operands holds
+// zeros up to a multiple of 128 steps, so that there is no other end.  A tile has 64 BB
+// columns, the first of those that are loaded.  Loads::first has been called.
+template <bool F16, bool ALONG, int BB>
+__device__ __forceinline__ void product(uint8_t* lds, const Loads<ALONG>& ld,
+                                        f32x16 (&acc)[4][BB]) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wy = wave >> 1, wx = wave & 1;
+  const int l32 = lane & 31, half = lane >> 5;
+
+#pragma unroll
+  for (int a = 0; a < 4; ++a)
+#pragma unroll
+    for (int b = 0; b < BB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
+
   stage_barrier<kLoads>();
 
   // per-lane byte offsets of the operand reads: across, of the four blocks in a stage;
@@ -304,7 +317,7 @@ __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
     constexpr int S = decltype(s_tag)::value;
     constexpr int kMf = 4 * BB, kReads = 4 + BB;
     typedef std::integral_constant<int, (S + 1) & 3> Next;
-    const DmaStage d = dma_begin(i, a2);
+    const typename Loads<ALONG>::Stage d = ld.begin(i, a2, wave);
     const uint32_t p0 = a0 * (2 * kOp), p1 = (S & 1 ? a1 : a0) * (2 * kOp);
     static_for<0, 2 * kMf>([&](auto k_tag) {
       constexpr int k = decltype(k_tag)::value;
@@ -319,7 +332,7 @@ __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
       });
       if constexpr (t == 0)
         static_for<m * kLoads / kMf, (m + 1) * kLoads / kMf>([&](auto j_tag) {
-          dma_piece(d, j_tag, std::integral_constant<int, S & 1>{});
+          ld.template piece<decltype(j_tag)::value, S & 1>(d);
         });
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -334,7 +347,7 @@ __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
   static_for<0, 4 + BB>([&](auto x_tag) {
     read_op(0, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{}, x_tag);
   });
-  for (int i0 = 0; i0 < s_end - s_beg; i0 += kRing) {
+  for (int i0 = 0; i0 < ld.s_end - ld.s_beg; i0 += kRing) {
     static_for<0, kRing>([&](auto s_tag) {
       constexpr int S = decltype(s_tag)::value;
       stage(s_tag, i0 + S, a0, a1, a2);
@@ -353,34 +366,36 @@ __device__ __forceinline__ void product(uint8_t* lds, const Loader<ALONG>& la,
 }
 
 // stages of a contraction of k steps
-__device__ __forceinline__ int stages(int64_t k) {
-  return (int)((k + kRing * kBK - 1) / (kRing * kBK)) * kRing;
+__device__ __forceinline__ int stages(int k) {
+  return (k + kRing * kBK - 1) / (kRing * kBK) * kRing;
 }
 
 // The items (token tile, word tile), words fastest, that workgroup w of P has:
 // a run floor(w N / P) .. floor((w + 1) N / P) - 1 of all N
 __device__ __forceinline__ int64_t run_begin(int64_t w, int64_t N, int64_t P) { return w * N / P; }
 
+// Sizes and what is left of them are int where they are compared: this compiler takes the
+// condition of a select from the wrong register when a branch goes by the same signed
+// 64-bit comparison (the words past the last were not masked).
+
 }  // namespace
 
-// A wave's 32 BB rows of 128 16-bit values from LDS to memory, whole lines: rows kRowB apart
-// from `mine` on, to rows `pitch` elements apart; what lies past rows_left and cols_left is not
-// written (cols_left a multiple of 8).
-template <int BB>
+// A wave's 32 rows of 128 16-bit values from LDS to memory, whole lines: rows of 256 bytes
+// from `mine` on, piece p of row r at p ^ (r & 15), to rows `pitch` elements apart; what lies
+// past rows_left and cols_left (a multiple of 8) is not written.
 __device__ __forceinline__ void store_rows(const uint8_t* mine, uint16_t* to, int64_t pitch,
-                                           int64_t rows_left, int64_t cols_left) {
-  const int lane = threadIdx.x & 63;
+                                           int rows_left, int cols_left) {
+  const int lane = threadIdx.x & 63, r0 = lane >> 4, p = lane & 15;
   __builtin_amdgcn_wave_barrier();  // (a wave reads only what it wrote)
-  to += (lane >> 4) * pitch + 8 * (lane & 15);
-  mine += (lane >> 4) * kRowB + 16 * (lane & 15);
-  const int64_t left = 8 * (lane & 15) < cols_left ? rows_left - (lane >> 4) : 0;
-#pragma unroll 4
-  for (int i = 0; i < 8 * BB; ++i) {
-    if (4 * i < left) st16(to, *reinterpret_cast<const u32x4*>(mine));
-    to += 4 * pitch;
-    mine += 4 * kRowB;
-  }
-  __syncthreads();  // the next tile's loads write where other waves read
+  to += r0 * pitch + 8 * p;
+  mine += r0 * 256;
+  const int left = 8 * p < cols_left ? rows_left - r0 : 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (4 * i < left)
+      st16(to + 4 * i * pitch,
+           *reinterpret_cast<const u32x4*>(mine + 1024 * i + 16 * (p ^ ((r0 + 4 * i) & 15))));
+  __builtin_amdgcn_wave_barrier();
 }
 
 // Logits: A = W (words), B = h^T (64 BB tokens), so that a lane has one
@@ -395,7 +410,7 @@ __device__ __forceinline__ void store_rows(const uint8_t* mine, uint16_t* to, in
 template <bool F16, Mode MODE, bool TEMP, int BB>
 __global__ __launch_bounds__(256) void head_logits_kernel(
     const uint16_t* __restrict__ ht, int64_t tp, const uint16_t* __restrict__ w, int D,
-    const int* __restrict__ count, int64_t words, float inv_tau,
+    const int* __restrict__ count, int words, float inv_tau,
     float* __restrict__ part, const HeadRow* __restrict__ rows, uint16_t* __restrict__ G,
     int64_t ld) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds<true>];
@@ -404,11 +419,12 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
   const int wy = wave >> 1, wx = wave & 1, l32 = lane & 31, half = lane >> 5;
   constexpr int kT = 64 * BB;  // tokens of a tile
   const int n = __builtin_amdgcn_readfirstlane(*count);
-  const int nt = (MODE == kStats ? n + kT - 1 : (n + 127) / 128 * 128 + kT - 1) / kT, nv = (int)((words + kTM - 1) / kTM);
+  const int nt = (MODE == kStats ? n + kT - 1 : (n + 127) / 128 * 128 + kT - 1) / kT, nv = (words + kTM - 1) / kTM;
   const int64_t N = (int64_t)nt * nv, P = N < gridDim.x ? N : gridDim.x;  // (no empty runs)
   const int64_t wg = xcd_remap(blockIdx.x, gridDim.x);
   if (wg >= P) return;
-  const int64_t i0 = run_begin(wg, N, P), i1 = run_begin(wg + 1, N, P);
+  const int64_t i0 = run_begin(wg, N, P);
+  const int items = (int)(run_begin(wg + 1, N, P) - i0);
   const int nst = stages(D);
   const float k1 = kLog2e, k2 = kLog2e * inv_tau;
 
@@ -445,8 +461,18 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
   };
 
   int tile = -1;
-  for (int64_t item = i0; item < i1; ++item) {
-    const int nt_i = (int)(item / nv), nv_i = (int)(item % nv);
+  Loader<true> la;
+  Loader<false> lb;
+  const Loads<true> loads = loads_of(lds, la, lb, 0, nst);
+  // an item's first loads are under way while the one before it is finished
+  auto first = [&](int nt_i, int nv_i) {
+    la.begin(w + (int64_t)nv_i * kTM * D, words - nv_i * kTM, D, D, wave, lane);
+    lb.begin(ht + nt_i * kT, (int)(tp - nt_i * kT), tp, nst * kBK, wave, lane);
+    loads.first(wave);
+  };
+  int nt_i = (int)(i0 / nv), nv_i = (int)(i0 % nv);
+  first(nt_i, nv_i);
+  for (int item = 0; item < items; ++item) {
     if (nt_i != tile) {
       if constexpr (MODE == kStats) {
         if (tile >= 0) flush(tile);
@@ -454,17 +480,17 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
       }
       tile = nt_i;
     }
+    const int v0 = nv_i * kTM + wy * 128, t0 = nt_i * kT + wx * (32 * BB);  // the wave's first ones
+    const int v_left = words - v0 < 128 ? words - v0 : 128;
     f32x16 acc[4][BB];
-    {
-      Loader<true> la;
-      la.begin(w + (int64_t)nv_i * kTM * D, words - (int64_t)nv_i * kTM, D, D, wave, lane);
-      Loader<false> lb;
-      lb.begin(ht + nt_i * kT, tp - nt_i * kT, tp, nst * kBK, wave, lane);
-      product<F16, true, BB>(lds, la, lb, 0, nst, acc);
+    product<F16, true, BB>(lds, loads, acc);
+    if (++nv_i == nv) {
+      nv_i = 0;
+      ++nt_i;
     }
-    const int v0 = nv_i * kTM + wy * 128;  // the wave's first word
+    if (item + 1 < items) first(nt_i, nv_i);
     if constexpr (MODE == kStats) {
-      const int left = (int)(words - v0 < 128 ? words - v0 : 128) - 4 * half;
+      const int left = v_left - 4 * half;
       auto softmax = [&](auto full_tag) {
         constexpr bool FULL = decltype(full_tag)::value;
         auto block = [&](int a, int b) {
@@ -516,21 +542,22 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
           mx[b] = m;
         }
       };
-      if (words - v0 >= 128)
+      if (v_left == 128)
         softmax(std::true_type{});
       else
         softmax(std::false_type{});
     } else {
       // a token's words pass through LDS, so that whole lines are stored (from the
-      // registers, 32 bytes of 32 rows a store, a tile took 11 us more)
-      uint8_t* mine = lds + wave * (128 * kRowB);
+      // registers, 32 bytes of 32 rows a store, a tile took 11 us more): 32 tokens of a wave at a
+      // time, in the third pair's slot, which the next item's first loads leave alone
+      uint8_t* mine = lds + kLdsB + 4 * kOp + wave * (32 * 256);
 #pragma unroll
       for (int b = 0; b < BB; ++b) {
-        const int r = nt_i * kT + wx * (32 * BB) + 32 * b + l32;
+        const int r = t0 + 32 * b + l32;
         // rows and words past the last are zeros, for dW's and dh's contractions
         const HeadRow hr = r < n ? rows[r] : HeadRow{0.f, 0.f, 0.f, 0.f};
-        const int left = (int)(words - v0 < 128 ? words - v0 : 128) - 4 * half;
-        uint8_t* row = mine + (32 * b + l32) * kRowB + 8 * half;
+        const int left = v_left - 4 * half;
+        uint8_t* row = mine + l32 * 256 + 8 * half;
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
           const f32x16 z = acc_block(acc[a][b]);
@@ -548,19 +575,19 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
 #pragma unroll
             for (int i = 0; i < 16; ++i) p[i] = __builtin_fmaf(hr.c2, q[i], p[i]);
           }
-          if (words - v0 < 128) {
+          if (v_left < 128) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
               if (32 * a + 8 * (i / 4) + i % 4 >= left) p[i] = 0.f;
           }
 #pragma unroll
           for (int q = 0; q < 4; ++q)  // words 32 a + 8 q + 4 half ..
-            *reinterpret_cast<u32x2*>(row + 64 * a + 16 * q) =
+            *reinterpret_cast<u32x2*>(row + 16 * ((4 * a + q) ^ (l32 & 15))) =
                 u32x2{pack2<F16>(p[4 * q], p[4 * q + 1]), pack2<F16>(p[4 * q + 2], p[4 * q + 3])};
           __builtin_amdgcn_sched_barrier(0);
         }
+        store_rows(mine, G + (int64_t)(t0 + 32 * b) * ld + v0, ld, 32, 128);
       }
-      store_rows<BB>(mine, G + (int64_t)(nt_i * kT + wx * (32 * BB)) * ld + v0, ld, 32 * BB, 128);
     }
   }
   if constexpr (MODE == kStats)
@@ -573,8 +600,8 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
 // values are read before the first is written (one by one, each waiting for its read, the
 // sums of a tile of dh took 120 us).
 template <bool ADD, bool FULL, typename T, typename Put>
-__device__ __forceinline__ void write_as(T* base, int64_t pitch, int64_t rows_left,
-                                         int64_t cols_left, const f32x16 (&acc)[4][4], Put put) {
+__device__ __forceinline__ void write_as(T* base, int64_t pitch, int rows_left, int cols_left,
+                                         const f32x16 (&acc)[4][4], Put put) {
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
   int64_t pv = pitch;
   asm volatile("" : "+v"(pv));
@@ -585,7 +612,7 @@ __device__ __forceinline__ void write_as(T* base, int64_t pitch, int64_t rows_le
     for (int b = 0; b < 4; ++b) {
       if (FULL || 32 * b + l32 < cols_left) {
         T* const p0 = base + (int64_t)(32 * a) * pitch + 32 * b + (4 * half * pv + l32);
-        const int64_t left = rows_left - 32 * a - 4 * half;
+        const int left = rows_left - 32 * a - 4 * half;
         T old[16];
         if constexpr (ADD) {
           T* p = p0;
@@ -608,8 +635,8 @@ __device__ __forceinline__ void write_as(T* base, int64_t pitch, int64_t rows_le
   }
 }
 template <bool ADD, typename T, typename Put>
-__device__ __forceinline__ void write_tile(T* base, int64_t pitch, int64_t rows_left,
-                                           int64_t cols_left, const f32x16 (&acc)[4][4], Put put) {
+__device__ __forceinline__ void write_tile(T* base, int64_t pitch, int rows_left, int cols_left,
+                                           const f32x16 (&acc)[4][4], Put put) {
   if (rows_left >= 128 && cols_left >= 128)
     write_as<ADD, true>(base, pitch, rows_left, cols_left, acc, put);
   else if (rows_left > 0 && cols_left > 0)
@@ -621,7 +648,7 @@ __device__ __forceinline__ void write_tile(T* base, int64_t pitch, int64_t rows_
 template <bool F16, bool ADD>
 __global__ __launch_bounds__(256) void head_dh_kernel(
     const uint16_t* __restrict__ G, int64_t ld, const uint16_t* __restrict__ w, int D,
-    const int* __restrict__ count, int64_t T, int64_t words, int parts, int per,
+    const int* __restrict__ count, int64_t T, int words, int parts, int per,
     float* __restrict__ part) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds<true>];
   const int lane = threadIdx.x & 63;
@@ -634,20 +661,20 @@ __global__ __launch_bounds__(256) void head_dh_kernel(
   const int nst = stages(words);
   for (int64_t item = wg; item < tiles * parts; item += P) {
     const int s = (int)(item / tiles), tile = (int)(item % tiles);
-    const int64_t m0 = (int64_t)(tile / nd) * kTM;
-    const int d0 = tile % nd * kTN;
+    const int m0 = tile / nd * kTM, d0 = tile % nd * kTN;
     const int s_end = s * per + per < nst ? s * per + per : nst;
     if (s * per >= s_end) continue;  // a last piece of fewer words: its part adds nothing
     f32x16 acc[4][4];
     {
       Loader<true> la;
-      la.begin(G + m0 * ld, n - m0, ld, nst * kBK, wave, lane);
+      la.begin(G + (int64_t)m0 * ld, n - m0, ld, nst * kBK, wave, lane);
       Loader<false> lb;
-      lb.begin(w + d0, D - d0, D, (int)words, wave, lane);
-      product<F16, true, 4>(lds, la, lb, s * per, s_end, acc);
+      lb.begin(w + d0, D - d0, D, words, wave, lane);
+      const Loads<true> l = loads_of(lds, la, lb, s * per, s_end);
+      l.first(wave);
+      product<F16, true, 4>(lds, l, acc);
     }
-    const int64_t r0 = m0 + wy * 128;
-    const int c0 = d0 + wx * 128;
+    const int r0 = m0 + wy * 128, c0 = d0 + wx * 128;
     float* out = part + ((int64_t)s * T + r0) * D + c0;
     write_tile<ADD>(out, D, n - r0, D - c0, acc, [](float v, float old) { return v + old; });
   }
@@ -661,14 +688,14 @@ __global__ __launch_bounds__(256) void head_dh_kernel(
 template <bool F16, bool PARTS, typename O, bool ACC>
 __global__ __launch_bounds__(256) void head_dw_kernel(
     const uint16_t* __restrict__ G, int64_t ld, const uint16_t* __restrict__ hs, int D,
-    const int* __restrict__ count, int64_t words, int parts, int per, const int* __restrict__ exp,
+    const int* __restrict__ count, int words, int parts, int per, const int* __restrict__ exp,
     O* __restrict__ dw) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[sizeof(O) == 2 ? 4 * 128 * kRowB : kLds<false>];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds<false> + (sizeof(O) == 2 ? 4 * 32 * 256 : 0)];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wy = wave >> 1, wx = wave & 1, l32 = lane & 31, half = lane >> 5;
   const int n = __builtin_amdgcn_readfirstlane(*count);
-  const int nv = (int)((words + kTM - 1) / kTM), nd = (D + kTN - 1) / kTN;
+  const int nv = (words + kTM - 1) / kTM, nd = (D + kTN - 1) / kTN;
   const int64_t tiles = (int64_t)nv * nd, P = gridDim.x;
   const int64_t wg = xcd_remap(blockIdx.x, gridDim.x);
   const int nst = stages(n);
@@ -676,30 +703,30 @@ __global__ __launch_bounds__(256) void head_dw_kernel(
   const int e = PARTS ? 0 : __builtin_amdgcn_readfirstlane(*exp);
   for (int64_t item = wg; item < tiles * parts; item += P) {
     const int s = (int)(item / tiles), tile = (int)(item % tiles);
-    const int64_t m0 = (int64_t)(tile / nd) * kTM;
-    const int d0 = tile % nd * kTN;
+    const int m0 = tile / nd * kTM, d0 = tile % nd * kTN;
     const int s_end = s * per + per < nst ? s * per + per : nst;
-    const int64_t r0 = m0 + (SWAP ? wx : wy) * 128;
-    const int c0 = d0 + (SWAP ? wy : wx) * 128;
+    const int r0 = m0 + (SWAP ? wx : wy) * 128, c0 = d0 + (SWAP ? wy : wx) * 128;
     O* out = dw + ((int64_t)s * words + r0) * D + c0;
     if (s * per >= s_end) {  // fewer rows than the parts were made for
       if constexpr (!ACC)
-        for (int64_t r = 0; r < 128 && r0 + r < words; ++r)
-          for (int c = lane; c < 128 && c0 + c < D; c += 64) out[r * D + c] = O(0.f);
+        for (int r = 0; r < 128 && r0 + r < words; ++r)
+          for (int c = lane; c < 128 && c0 + c < D; c += 64) out[(int64_t)r * D + c] = O(0.f);
       continue;
     }
     f32x16 acc[4][4];
     {
       Loader<false> g, h;
-      g.begin(G + m0, ld - m0, ld, nst * kBK, wave, lane);
+      g.begin(G + m0, (int)ld - m0, ld, nst * kBK, wave, lane);
       h.begin(hs + d0, D - d0, D, n, wave, lane);
-      product<F16, false, 4>(lds, SWAP ? h : g, SWAP ? g : h, s * per, s_end, acc);
+      const Loads<false> l = loads_of(lds, SWAP ? h : g, SWAP ? g : h, s * per, s_end);
+      l.first(wave);
+      product<F16, false, 4>(lds, l, acc);
     }
     if constexpr (SWAP) {
-      uint8_t* mine = lds + wave * (128 * kRowB);
+      uint8_t* mine = lds + kLds<false> + wave * (32 * 256);
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        uint8_t* row = mine + (32 * b + l32) * kRowB + 8 * half;
+        uint8_t* row = mine + l32 * 256 + 8 * half;
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
           f32x16 v = acc_block(acc[a][b]);
@@ -707,12 +734,13 @@ __global__ __launch_bounds__(256) void head_dw_kernel(
           for (int i = 0; i < 16; ++i) v[i] = ldexpf(v[i], e);
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<u32x2*>(row + 64 * a + 16 * q) =
+            *reinterpret_cast<u32x2*>(row + 16 * ((4 * a + q) ^ (l32 & 15))) =
                 u32x2{pack2<F16>(v[4 * q], v[4 * q + 1]), pack2<F16>(v[4 * q + 2], v[4 * q + 3])};
           __builtin_amdgcn_sched_barrier(0);
         }
+        store_rows(mine, reinterpret_cast<uint16_t*>(out) + (int64_t)(32 * b) * D, D,
+                   words - r0 - 32 * b, D - c0);
       }
-      store_rows<4>(mine, reinterpret_cast<uint16_t*>(out), D, words - r0, D - c0);
     } else {
       write_tile<ACC>(out, D, words - r0, D - c0, acc, [&](float v, O old) {
         if constexpr (PARTS)
@@ -792,10 +820,10 @@ static hipError_t run_logits(const HeadIn& in, const uint16_t* ht, const int* co
   const uint16_t* w = in.w + w0 * in.D;
   if (in.K > 0 && in.tau != 1.0f)
     hipLaunchKernelGGL((head_logits_kernel<F16, MODE, true, BB>), TM_HEAD_GRID(grid), ht,
-                       head_padded(in.T), w, in.D, count, n, 1.0f / in.tau, part, rows, G, ld);
+                       head_padded(in.T), w, in.D, count, (int)n, 1.0f / in.tau, part, rows, G, ld);
   else
     hipLaunchKernelGGL((head_logits_kernel<F16, MODE, false, BB>), TM_HEAD_GRID(grid), ht,
-                       head_padded(in.T), w, in.D, count, n, 1.0f, part, rows, G, ld);
+                       head_padded(in.T), w, in.D, count, (int)n, 1.0f, part, rows, G, ld);
   return hipGetLastError();
 }
 
@@ -828,7 +856,7 @@ hipError_t launch_head_dh(const HeadIn& in, const int* count, const uint16_t* G,
   const uint16_t* w = in.w + w0 * in.D;
 #define TM_HEAD_DH(F16, ADD)                                                                    \
   hipLaunchKernelGGL((head_dh_kernel<F16, ADD>), TM_HEAD_GRID(grid_of(items)), G, ld, w, in.D, \
-                     count, in.T, n, parts, per, part_h)
+                     count, in.T, (int)n, parts, per, part_h)
   if (in.f16) {
     if (add)
       TM_HEAD_DH(true, true);
@@ -851,11 +879,11 @@ static hipError_t run_dw(const HeadIn& in, const int* count, const uint16_t* G, 
   const int64_t items = ((n + kTM - 1) / kTM) * ((in.D + kTN - 1) / kTN) * parts;
   if (parts == 1) {
     hipLaunchKernelGGL((head_dw_kernel<F16, false, O, ACC>), TM_HEAD_GRID(grid_of(items)), G, ld,
-                       hs, in.D, count, n, 1, per, exp, dw);
+                       hs, in.D, count, (int)n, 1, per, exp, dw);
     return hipGetLastError();
   }
   hipLaunchKernelGGL((head_dw_kernel<F16, true, float, false>), TM_HEAD_GRID(grid_of(items)), G, ld,
-                     hs, in.D, count, n, parts, per, exp, part_w);
+                     hs, in.D, count, (int)n, parts, per, exp, part_w);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t all = n * in.D;
