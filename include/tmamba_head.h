@@ -54,7 +54,8 @@ int64_t tm_head_loss_workspace(int64_t T, int64_t V, int64_t D); /* -1: sizes ou
  * a loss, or whose dloss is 0, have rows of zeros in dh and no part in dW,
  * whatever their rows of h hold.
  *   dh         [T, D], h's type (16-byte aligned)
- *   dW         [V, D], dW_type 0 float32 or h's type; accumulate 1 (float32 only): dW += that
+ *              or NULL: not wanted
+ *   dW         [V, D] or NULL (not both), dW_type 0 float32 or h's type; accumulate 1 (float32 only): dW += that
  */
 tm_status tm_head_loss_bwd(const void* h, const void* W, int32_t type, int64_t T, int64_t V,
                            int64_t D, const void* labels, int32_t labels_i64, const void* top_ids,

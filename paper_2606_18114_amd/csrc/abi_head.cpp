@@ -105,7 +105,7 @@ tm_status tm_head_loss_bwd(const void* h, const void* W, int32_t type, int64_t T
                            int32_t accumulate, void* workspace, int64_t workspace_bytes,
                            tm_stream stream) {
   tmk::HeadIn in;
-  if (!stats || !dloss || !dh || !dW || (accumulate & ~1)) return TM_EINVAL;
+  if (!stats || !dloss || (!dh && !dW) || (accumulate & ~1)) return TM_EINVAL;
   if (tm_status st = head_checked(h, W, type, T, V, D, labels, labels_i64, top_ids, ids_i64, K,
                                   alpha, tau, &in))
     return st;
@@ -117,7 +117,7 @@ tm_status tm_head_loss_bwd(const void* h, const void* W, int32_t type, int64_t T
   if (!apart({span(h, T * D * 2), span(W, V * D * 2), span(labels, T * (labels_i64 ? 8 : 4)),
               opt(top_ids, T * K * (ids_i64 ? 8 : 4)),
               span(stats, tmk::head_stats_floats(T, K) * 4), span(dloss, T * 4)},
-             {span(dh, T * D * 2), span(dW, V * D * (dW_type == 0 ? 4 : 2)),
+             {opt(dh, T * D * 2), opt(dW, V * D * (dW_type == 0 ? 4 : 2)),
               span(workspace, need)}))
     return TM_EINVAL;
   return hip_status(tmk::launch_head_loss_bwd(in, stats, dloss, static_cast<uint16_t*>(dh), dW,

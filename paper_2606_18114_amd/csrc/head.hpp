@@ -61,7 +61,7 @@ int64_t head_loss_bytes(int64_t T, int64_t V, int64_t D);
 hipError_t launch_head_loss(const HeadIn& in, const void* top, int top_type, float* loss,
                             float* stats, void* workspace, hipStream_t stream);
 int64_t head_loss_bwd_bytes(int64_t T, int64_t V, int64_t D);
-// dw_type 0 float32, 1 h's type; accumulate only with float32
+// dh or dw may be NULL; dw_type 0 float32, 1 h's type; accumulate only with float32
 hipError_t launch_head_loss_bwd(const HeadIn& in, const float* stats, const float* dloss,
                                 uint16_t* dh, void* dw, int dw_type, bool accumulate,
                                 void* workspace, hipStream_t stream);

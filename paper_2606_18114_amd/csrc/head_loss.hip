@@ -656,9 +656,11 @@ static hipError_t run_bwd(const HeadIn& in, const float* stats, const float* dlo
   hipLaunchKernelGGL(rows_kernel<true>, dim3((unsigned)((in.T + per - 1) / per)), dim3(1024), 0,
                      stream, in, stats, dloss, kHeadShift<F16>, per, l.rows);
   TM_RET(hipGetLastError());
-  hipLaunchKernelGGL(rows_copy_kernel<F16>, dim3((unsigned)in.T), dim3(256), 0, stream, in, dloss,
-                     l.rows, l.hs);
-  TM_RET(hipGetLastError());
+  if (dw) {
+    hipLaunchKernelGGL(rows_copy_kernel<F16>, dim3((unsigned)in.T), dim3(256), 0, stream, in, dloss,
+                       l.rows, l.hs);
+    TM_RET(hipGetLastError());
+  }
   TM_RET(transpose(in, l, stream));
   for (int64_t i = 0; i < p.pieces; ++i) {
     const int64_t w0 = i * p.piece, n = in.V - w0 < p.piece ? in.V - w0 : p.piece;
@@ -667,14 +669,17 @@ static hipError_t run_bwd(const HeadIn& in, const float* stats, const float* dlo
     hipLaunchKernelGGL(sparse_kernel<F16>, dim3((unsigned)((in.T * (in.K + 1) + 255) / 256)),
                        dim3(256), 0, stream, in, stats, dloss, l.rows, w0, n, l.G, p.piece);
     TM_RET(hipGetLastError());
-    TM_RET(launch_head_dh(in, l.rows.count, l.G, p.piece, w0, n, p.parts_h, p.per_h, i > 0,
+    if (dh)
+      TM_RET(launch_head_dh(in, l.rows.count, l.G, p.piece, w0, n, p.parts_h, p.per_h, i > 0,
                           l.part_h, stream));
     const bool last = i == p.pieces - 1;
-    TM_RET(launch_head_dw(in, l.rows.count, l.G, p.piece, l.hs, w0, n, last ? p.last_w : p.parts_w,
+    if (dw)
+      TM_RET(launch_head_dw(in, l.rows.count, l.G, p.piece, l.hs, w0, n, last ? p.last_w : p.parts_w,
                           last ? p.last_per : p.per_w, l.rows.exps + 1, dw, dw_type, accumulate, l.part_w, stream));
   }
-  hipLaunchKernelGGL(dh_out_kernel<F16>, dim3((unsigned)in.T), dim3(256), 0, stream, in, dloss,
-                     l.rows, l.part_h, p.parts_h, dh);
+  if (dh)
+    hipLaunchKernelGGL(dh_out_kernel<F16>, dim3((unsigned)in.T), dim3(256), 0, stream, in, dloss,
+                       l.rows, l.part_h, p.parts_h, dh);
   return hipGetLastError();
 }
 

@@ -1275,31 +1275,40 @@ def head_loss_bwd(h: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
                   stats: torch.Tensor, dloss: torch.Tensor,
                   teacher_ids: Optional[torch.Tensor] = None, *, alpha: float = 0.5,
                   temperature: float = 1.0, dh: Optional[torch.Tensor] = None,
-                  dW: Optional[torch.Tensor] = None, accumulate: bool = False):
+                  dW: Optional[torch.Tensor] = None, accumulate: bool = False,
+                  want_dh: bool = True, want_dW: bool = True):
     """Gradients of head_loss (tm_head_loss_bwd): dloss float32 [T] -> (dh
     [T, D], dW [V, D]), both in h's type; dW float32 where a float32 one is
     given, then also added to (accumulate).  The other arguments are the
-    forward call's."""
+    forward call's.  want_dh, want_dW: without one of them it is None, and its
+    product is not computed."""
     dev, T, V, D, K = _head_args(h, weight, targets, teacher_ids, alpha, temperature)
     _of(stats, "stats", _F32, (T * (HEAD_STATS + K),), dev)
     _of(dloss, "dloss", _F32, (T,), dev)
-    if dh is None:
+    if not (want_dh or want_dW):
+        raise ValueError("one of dh and dW must be wanted")
+    if not want_dh:
+        dh = None
+    elif dh is None:
         dh = torch.empty_like(h)
     else:
         _of(dh, "dh", (h.dtype,), (T, D), dev)
-    if dW is None:
+    if not want_dW:
+        dW, accumulate = None, False
+    elif dW is None:
         if accumulate:
             raise ValueError("accumulate=True needs an existing dW")
         dW = torch.empty_like(weight)
     else:
         _of(dW, "dW", (torch.float32,) if accumulate else (torch.float32, h.dtype), (V, D), dev)
     if T == 0:
-        return dh, dW if accumulate else dW.zero_()
+        return dh, dW if accumulate or dW is None else dW.zero_()
     ws, wp, wb = _seq_ws("tm_head_loss_bwd_workspace", dev, T, V, D)
     _call("tm_head_loss_bwd", dev, _ptr(h), _ptr(weight), _HEAD_TYPE[h.dtype], T, V, D,
           _ptr(targets), int(targets.dtype == torch.int64), _ptr(teacher_ids),
           int(K > 0 and teacher_ids.dtype == torch.int64), K, alpha, temperature, _ptr(stats),
-          _ptr(dloss), _ptr(dh), _ptr(dW), 0 if dW.dtype == torch.float32 else _HEAD_TYPE[h.dtype],
+          _ptr(dloss), _ptr(dh), _ptr(dW),
+          _HEAD_TYPE[h.dtype] if dW is not None and dW.dtype == h.dtype else 0,
           int(bool(accumulate)), wp, wb)
     return dh, dW
 

@@ -30,7 +30,9 @@ operations on the data).  ``pack_for_decode`` returns the deployment format
 
 ``Mamba2Mixer`` is the unquantized part between the two projections over whole
 sequences, ``Embedding`` the residual stream's beginning; with ``TernaryLinear``
-they make up a block's training step on the library's kernels.
+they make up a block's training step on the library's kernels.  ``BlockNorm`` is the
+norm before a block and before the head, ``Head`` the loss at the end: cross entropy and
+distillation (paper Eq. 1) without keeping the logits.
 """
 
 from __future__ import annotations
@@ -391,6 +393,128 @@ class Embedding(torch.nn.Module):
         return f"{self.weight.shape[0]}, {self.weight.shape[1]}, scale={self.scale}"
 
 
+class BlockNormFn(torch.autograd.Function):
+    """The norm of residual + y and that sum (``tm_block_norm`` and its
+    gradients): residual, y float32 [T, D] -> (x bfloat16 [T, D], float32
+    [T, D]); y None: x alone."""
+
+    @staticmethod
+    def forward(ctx, residual, y, w, eps):
+        w = w.detach().contiguous()
+        x, r = ops.block_norm(residual.contiguous(), None if y is None else y.contiguous(), w, eps)
+        ctx.save_for_backward(r, w)
+        ctx.eps, ctx.sum = eps, y is not None
+        return (x, r) if ctx.sum else x
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dx, dresidual=None):
+        r, w = ctx.saved_tensors
+        dr, dw = ops.block_norm_bwd(r, w, dx.to(torch.bfloat16).contiguous(),
+                                    None if dresidual is None else dresidual.contiguous(),
+                                    ctx.eps)
+        return dr, dr if ctx.sum else None, dw, None
+
+
+class BlockNorm(torch.nn.Module):
+    """The pre-norm of a block, or the final norm: forward(residual, y=None) ->
+    (x, residual + y), with the float32 residual stream [..., width], the
+    previous block's output y (any floating type; None: nothing is added) and x
+    bfloat16, the RMS norm of the sum times the weight: ``TernaryLinear``'s and
+    ``Head``'s input."""
+
+    def __init__(self, width: int, eps: float = 1e-5, device: Optional[torch.device] = None):
+        super().__init__()
+        self.eps = eps
+        self.weight = torch.nn.Parameter(torch.ones(width, dtype=torch.float32, device=device))
+
+    def forward(self, residual: torch.Tensor, y: Optional[torch.Tensor] = None):
+        width = self.weight.shape[0]
+        r = residual.reshape(-1, width)
+        if y is None:
+            return BlockNormFn.apply(r, None, self.weight, self.eps).reshape(residual.shape), \
+                residual
+        if y.shape != residual.shape:
+            raise ValueError(f"y has shape {tuple(y.shape)}, the residual {tuple(residual.shape)}")
+        x, r = BlockNormFn.apply(r, y.reshape(-1, width).to(torch.float32), self.weight, self.eps)
+        return x.reshape(residual.shape), r.reshape(residual.shape)
+
+    def extra_repr(self) -> str:
+        return f"{self.weight.shape[0]}, eps={self.eps}"
+
+
+class HeadLossFn(torch.autograd.Function):
+    """Losses of tokens at the head (``tm_head_loss``, ``tm_head_loss_bwd``).
+    The weight is read in h's type; its gradient has the weight's own."""
+
+    @staticmethod
+    def forward(ctx, h, weight, targets, teacher_ids, teacher_logits, alpha, temperature):
+        h, w = h.contiguous(), weight.detach().to(h.dtype).contiguous()
+        loss, stats = ops.head_loss(h, w, targets, teacher_ids, teacher_logits, alpha=alpha,
+                                    temperature=temperature)
+        ctx.save_for_backward(h, w, targets, stats, teacher_ids)
+        ctx.alpha, ctx.temperature, ctx.dtype = alpha, temperature, weight.dtype
+        return loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss):
+        h, w, targets, stats, ids = ctx.saved_tensors
+        want_dh, want_dw = ctx.needs_input_grad[:2]
+        dw = None
+        if want_dw and ctx.dtype != h.dtype:
+            dw = torch.empty(w.shape, dtype=torch.float32, device=w.device)
+        dh, dw = ops.head_loss_bwd(h, w, targets, stats, dloss.to(torch.float32).contiguous(), ids,
+                                   alpha=ctx.alpha, temperature=ctx.temperature, dW=dw,
+                                   want_dh=want_dh, want_dW=want_dw)
+        return dh, None if dw is None else dw.to(ctx.dtype), None, None, None, None, None
+
+
+class Head(torch.nn.Module):
+    """The head in training: forward(h, targets, teacher_ids=None,
+    teacher_logits=None) -> the tokens' losses, float32 [...].  h bfloat16 or
+    float16 [..., width] (``BlockNorm``'s output); targets int32 or int64 [...],
+    a label outside the vocabulary counts nowhere.  With a teacher's top K words
+    and their logits [..., K] the loss is the paper's Eq. 1, (1 - alpha) CE +
+    alpha temperature^2 KL over the teacher's words; ids outside the vocabulary
+    are places without a word.  The logits are never kept; the head's weight
+    [vocab, width] (float32, bfloat16 or float16; ``weight`` shares one, as
+    ``Embedding.weight``) is read in h's type."""
+
+    def __init__(self, vocab: int, width: int, alpha: float = 0.5, temperature: float = 1.0,
+                 weight: Optional[torch.nn.Parameter] = None,
+                 device: Optional[torch.device] = None, dtype: torch.dtype = torch.float32):
+        super().__init__()
+        if weight is None:
+            weight = torch.nn.Parameter(torch.empty((vocab, width), device=device, dtype=dtype))
+            torch.nn.init.normal_(weight, 0.0, 0.02)
+        elif tuple(weight.shape) != (vocab, width):
+            raise ValueError(f"weight has shape {tuple(weight.shape)}, expected {(vocab, width)}")
+        self.alpha, self.temperature, self.weight = alpha, temperature, weight
+
+    def forward(self, h: torch.Tensor, targets: torch.Tensor,
+                teacher_ids: Optional[torch.Tensor] = None,
+                teacher_logits: Optional[torch.Tensor] = None) -> torch.Tensor:
+        if h.shape[:-1] != targets.shape:
+            raise ValueError(f"targets must be {tuple(h.shape[:-1])}, got {tuple(targets.shape)}")
+        if h.dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError(f"h must be bfloat16 or float16 (got {h.dtype})")
+        top = [t if t is None else t.reshape(-1, t.shape[-1]).contiguous()
+               for t in (teacher_ids, teacher_logits)]
+        for t, name in ((teacher_ids, "teacher_ids"), (teacher_logits, "teacher_logits")):
+            if t is not None and t.shape[:-1] != targets.shape:
+                raise ValueError(f"{name} must be [{', '.join(map(str, targets.shape))}, K], got "
+                                 f"{tuple(t.shape)}")
+        loss = HeadLossFn.apply(h.reshape(-1, h.shape[-1]), self.weight,
+                                targets.reshape(-1).contiguous(), *top, self.alpha,
+                                self.temperature)
+        return loss.reshape(targets.shape)
+
+    def extra_repr(self) -> str:
+        return (f"{self.weight.shape[0]}, {self.weight.shape[1]}, alpha={self.alpha}, "
+                f"temperature={self.temperature}")
+
+
 def flops_per_step(tokens: int, layer: TernaryLinear) -> float:
     """Algorithmic flops of one forward + straight-through backward (three
     dense products of 2 * tokens * in * out each; zeros not discounted)."""
@@ -398,4 +522,5 @@ def flops_per_step(tokens: int, layer: TernaryLinear) -> float:
 
 
 __all__ = ["SCALE_MODES", "TernaryLinear", "TernaryLinearFn", "Mamba2Mixer", "Mamba2MixerFn",
-           "Embedding", "EmbeddingFn", "flops_per_step"]
+           "Embedding", "EmbeddingFn", "BlockNorm", "BlockNormFn", "Head", "HeadLossFn",
+           "flops_per_step"]
