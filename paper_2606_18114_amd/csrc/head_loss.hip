@@ -90,55 +90,98 @@ struct Rows {
   uint8_t* terms;  // [T]: 1 label, 2 teacher (forward)
 };
 
-// terms[t]: a label in the vocabulary; a kept word of the teacher.  A wave a token.
-__global__ __launch_bounds__(256) void terms_kernel(HeadIn in, const void* __restrict__ top,
-                                                    int top_type, uint8_t* __restrict__ terms) {
-  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (t >= in.T) return;
-  bool some = false;
-  for (int k = lane; k < in.K; k += 64) {
-    const int64_t id = id_at(in.ids, in.ids64, t * in.K + k);
-    if (id >= 0 && id < in.V && top_at(top, top_type, t * in.K + k) != -__builtin_inff())
-      some = true;
-  }
-  const bool kl = __any(some);
-  const int64_t y = id_at(in.targets, in.targets64, t);
-  if (lane == 0) terms[t] = (uint8_t)((y >= 0 && y < in.V ? 1 : 0) | (kl ? 2 : 0));
+// What the list of rows is made from: forward the labels, or with a teacher `terms`; backward
+// the stats and the gradients of the losses.
+struct Of {
+  const void* top;  // forward, with a teacher
+  int top_type;
+  const float* stats;  // backward
+  const float* dloss;
+  int shift;
+};
+
+__device__ __forceinline__ bool in_vocabulary(const HeadIn& in, int64_t v) {
+  return v >= 0 && v < in.V;
 }
 
-// Lists the rows in the tokens' order.  A workgroup has `per` tokens (a multiple of
-// 1024); it counts the rows before them by itself, then lists its own, 1024 at a time.
-// At most 64 workgroups, so that counting again costs 32 reads a token at most.
-// BWD: rows whose loss has a gradient, with their factors.
+// which terms a token has, in every lane of a wave: 1 a label in the vocabulary, 2 a kept word of
+// the teacher
+__device__ __forceinline__ int terms_of(const HeadIn& in, const Of& of, int64_t t, int lane) {
+  bool some = false;
+  for (int k = lane; k < in.K; k += 64)
+    if (in_vocabulary(in, id_at(in.ids, in.ids64, t * in.K + k)) &&
+        top_at(of.top, of.top_type, t * in.K + k) != -__builtin_inff())
+      some = true;
+  return (in_vocabulary(in, id_at(in.targets, in.targets64, t)) ? 1 : 0) | (__any(some) ? 2 : 0);
+}
+
+// a wave a token
+__global__ __launch_bounds__(256) void terms_kernel(HeadIn in, Of of, uint8_t* __restrict__ terms) {
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= in.T) return;
+  const int v = terms_of(in, of, t, threadIdx.x & 63);
+  if ((threadIdx.x & 63) == 0) terms[t] = (uint8_t)v;
+}
+
+// whether token t has a row: a loss; backward, one whose gradient is not zero
 template <bool BWD>
-__global__ __launch_bounds__(1024) void rows_kernel(HeadIn in, const float* __restrict__ stats,
-                                                    const float* __restrict__ dloss, int shift,
-                                                    int64_t per, Rows out) {
+__device__ __forceinline__ bool has_row(const HeadIn& in, const Of& of, const uint8_t* terms,
+                                        int64_t t) {
+  if constexpr (BWD)
+    return of.stats[kStatTerms * in.T + t] != 0.f && !(of.dloss[t] == 0.f);
+  else
+    return in.K > 0 ? terms[t] != 0
+                    : in_vocabulary(in, id_at(in.targets, in.targets64, t));
+}
+
+// exponent of token t's gradient, -1000 where it has none
+__device__ __forceinline__ int row_exp(const HeadIn& in, const Of& of, int64_t t) {
+  const float g = of.dloss[t] * head_unit(in.alpha, in.tau);
+  return fabsf(g) < __builtin_inff() && g != 0.f ? ilogbf(g) : -1000;
+}
+
+// token t's row r
+template <bool BWD>
+__device__ __forceinline__ void put_row(const HeadIn& in, const Of& of, const Rows& out, int64_t t,
+                                        int r) {
+  out.idx[r] = (int)t;
+  if constexpr (BWD) {
+    const int64_t T = in.T;
+    const float unit = head_unit(in.alpha, in.tau), g = of.dloss[t] * unit;
+    const float m = ldexpf(g, of.shift - exp_of(g));
+    const int terms = (int)of.stats[kStatTerms * T + t];
+    float c1 = terms & 1 ? (1.0f - in.alpha) / unit * m : 0.f;
+    float c2 = terms & 2 ? in.alpha * in.tau / unit * m : 0.f;
+    if (in.tau == 1.0f) {  // one softmax
+      c1 += c2;
+      c2 = 0.f;
+    }
+    out.row[r] = HeadRow{of.stats[kStatLse * T + t], of.stats[kStatLseT * T + t], c1, c2};
+  }
+}
+
+__device__ __forceinline__ void put_exps(const Of& of, const Rows& out, int e) {
+  out.exps[0] = e == -1000 ? 0 : e;
+  out.exps[1] = out.exps[0] - of.shift;
+}
+
+// Lists the rows in the tokens' order, where tokens are many.  A workgroup has `per` tokens (a
+// multiple of 1024); it counts the rows before them by itself, then lists its own, 1024 at a time.
+// At most 64 workgroups, so that counting again costs 32 reads a token at most.
+template <bool BWD>
+__global__ __launch_bounds__(1024) void rows_kernel(HeadIn in, Of of, int64_t per, Rows out) {
   __shared__ int sums[16];
   __shared__ int maxs[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t T = in.T, t0 = blockIdx.x * per, t1 = t0 + per < T ? t0 + per : T;
-  auto has = [&](int64_t t) {
-    if constexpr (BWD) {
-      return stats[kStatTerms * T + t] != 0.f && !(dloss[t] == 0.f);
-    } else {
-      if (in.K > 0) return out.terms[t] != 0;
-      const int64_t y = id_at(in.targets, in.targets64, t);
-      return y >= 0 && y < in.V;
-    }
-  };
-  const float unit = head_unit(in.alpha, in.tau);
   int n = 0, e = -1000;
   // the first workgroup looks at all gradients for the largest
 #pragma unroll 4
   for (int64_t t = tid; t < (BWD && blockIdx.x == 0 ? T : t0); t += 1024) {
-    const bool yes = has(t);
+    const bool yes = has_row<BWD>(in, of, out.terms, t);
     if (t < t0) n += yes;
-    if constexpr (BWD) {
-      const float g = dloss[t] * unit;
-      if (yes && fabsf(g) < __builtin_inff() && g != 0.f) e = max(e, ilogbf(g));
-    }
+    if constexpr (BWD)
+      if (yes) e = max(e, row_exp(in, of, t));
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
@@ -156,13 +199,11 @@ __global__ __launch_bounds__(1024) void rows_kernel(HeadIn in, const float* __re
     base += sums[w];
     e = max(e, maxs[w]);
   }
-  if (BWD && blockIdx.x == 0 && tid == 0) {
-    out.exps[0] = e == -1000 ? 0 : e;
-    out.exps[1] = out.exps[0] - shift;
-  }
+  if constexpr (BWD)
+    if (blockIdx.x == 0 && tid == 0) put_exps(of, out, e);
   for (int64_t c = t0; c < t1; c += 1024) {
     const int64_t t = c + tid;
-    const bool yes = t < t1 && has(t);
+    const bool yes = t < t1 && has_row<BWD>(in, of, out.terms, t);
     const uint64_t mask = __ballot(yes);
     __syncthreads();  // the previous sums have been read
     if (lane == 0) sums[wave] = __popcll(mask);
@@ -176,225 +217,115 @@ __global__ __launch_bounds__(1024) void rows_kernel(HeadIn in, const float* __re
     const int r = base + before + __popcll(mask & ((uint64_t(1) << lane) - 1));
     base += all;
     if (t < t1) out.pos[t] = yes ? r : -1;
-    if (yes) {
-      out.idx[r] = (int)t;
-      if constexpr (BWD) {
-        const float g = dloss[t] * unit;
-        const float m = ldexpf(g, shift - exp_of(g));
-        const int terms = (int)stats[kStatTerms * T + t];
-        float c1 = terms & 1 ? (1.0f - in.alpha) / unit * m : 0.f;
-        float c2 = terms & 2 ? in.alpha * in.tau / unit * m : 0.f;
-        if (in.tau == 1.0f) {  // one softmax
-          c1 += c2;
-          c2 = 0.f;
-        }
-        out.row[r] = HeadRow{stats[kStatLse * T + t], stats[kStatLseT * T + t], c1, c2};
-      }
-    }
+    if (yes) put_row<BWD>(in, of, out, t, r);
   }
   if (t1 == T && tid == 0) *out.count = base;
 }
 
-// The loss and the stats of a token, a wave (WAVES 0: no teacher) or a workgroup a
-// token, of sixteen waves where tokens are few (1 token, 64 words: XX us, YY of four).  Bound: the dot products' rows of W, from the caches for
-// frequent words.
-struct Finish {
-  HeadIn in;
-  const void* top;
-  int top_type;
-  const float* part;
-  int tile, grid;  // tokens of a tile and workgroups of the logits' launch
-  Rows rows;
-  float* loss;
-  float* stats;
-};
+// The rows as the products read them, 64 rows x 64 columns a workgroup, through LDS:
+//   ht[d][r] = h[idx[r]][d], the logits' second operand, with zeros up to a multiple of 128
+//   columns d and of 256 rows r;
+//   backward, hs[r] = h[idx[r]] times 2^(e - largest e), what dW contracts (NULL: not wanted).
+// LIST (up to kListTokens tokens): every workgroup lists the rows by itself and the first one
+// writes the list, which saves a launch (16 tokens: XX us, YY with two); of up to kListTeach
+// tokens also what the teacher keeps.
+constexpr int kListTokens = 1024, kListTeach = 16;
 
-// h[t] . W[v] over the lanes of a wave, in every lane
-template <bool F16>
-__device__ __forceinline__ float row_dot(const uint16_t* h, const uint16_t* w, int D, int lane) {
-  float s = 0.f;
-  for (int d = lane * 8; d < D; d += 512) {
-    float x[8], y[8];
-    widen<F16>(ld16(h + d), x);
-    widen<F16>(ld16(w + d), y);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x[i], y[i], s);
-  }
-  return wave_sum(s);
-}
-
-// the softmax sums of row r: the parts of its token tile's workgroups, joined.  m: the largest
-// logit; s: sum of 2^(log2e (z - m)); sT the same at the temperature (TEMP)
-template <bool TEMP>
-__device__ __forceinline__ void join(const float* part, int r, int n, int64_t V, int tile, int grid, float k2,
-                                     int lane, float& m, float& s, float& sT) {
-  constexpr int E = TEMP ? 3 : 2;
-  const int64_t nt = (n + tile - 1) / tile, nv = (V + 255) / 256, N = nt * nv;
-  const int64_t P = N < grid ? N : grid;
-  const int64_t j = r / tile;
-  // the workgroups whose runs hold the tile's first and last item
-  const int64_t w0 = ((j * nv + 1) * P - 1) / N, w1 = (((j + 1) * nv) * P - 1) / N;
-  const int cnt = (int)(w1 - w0 + 1) * 2;
-  auto at = [&](int i) { return part + (((w0 + j) * 2 + i) * 256 + r % tile) * E; };
-  float mm = -__builtin_inff();
-  for (int i = lane; i < cnt; i += 64) mm = fmaxf(mm, at(i)[0]);
-  m = wave_max(mm);
-  const float ref = m == -__builtin_inff() ? 0.f : m;
-  float a = 0.f, b = 0.f;
-  for (int i = lane; i < cnt; i += 64) {
-    const float* p = at(i);
-    a += p[1] * __builtin_amdgcn_exp2f((p[0] - ref) * kLog2e);
-    if constexpr (TEMP) b += p[2] * __builtin_amdgcn_exp2f((p[0] - ref) * k2);
-  }
-  s = wave_sum(a);
-  sT = TEMP ? wave_sum(b) : s;
-}
-
-template <bool F16, bool TEMP, int WAVES>
-__global__ __launch_bounds__(WAVES ? 64 * WAVES : 256) void finish_kernel(Finish f) {
-  constexpr bool TEACH = WAVES > 0;
-  constexpr int L = WAVES * 64;
-  extern __shared__ float sh[];  // TEACH: z[K], q[K], id[K]
-  __shared__ float red[TEACH ? WAVES : 1];
-  const HeadIn& in = f.in;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t t = TEACH ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
-  if (t >= in.T) return;
-  float* st = f.stats + t;  // the token's place in each plane
-  float* st_top = f.stats + kStatPlanes * in.T + t * in.K;
-  const int64_t y = id_at(in.targets, in.targets64, t);
-  const bool ce = y >= 0 && y < in.V;
-  const int terms = TEACH ? f.rows.terms[t] : (ce ? 1 : 0);
-  const int first = TEACH ? threadIdx.x : lane;
-  if (terms == 0) {  // no loss
-    if (first < kStatPlanes) st[first * in.T] = 0.f;
-    for (int i = first; i < in.K; i += L) st_top[i] = 0.f;
-    if (first == 0) f.loss[t] = 0.f;
-    return;
-  }
-  const int n = *f.rows.count;
-  const float it = 1.0f / in.tau, k2 = kLog2e * it;
-  float m, s, sT;
-  join<TEMP>(f.part, f.rows.pos[t], n, in.V, f.tile, f.grid, k2, lane, m, s, sT);
-  const float mf = m == -__builtin_inff() ? 0.f : m;  // (as the sums took it)
-  const float lse2 = __builtin_fmaf(mf, kLog2e, __builtin_amdgcn_logf(s));
-  const float lseT2 = __builtin_fmaf(mf, k2, __builtin_amdgcn_logf(sT));
-  const uint16_t* h = in.h + t * in.D;
-  const float unit = head_unit(in.alpha, in.tau);
-  const float c1 = terms & 1 ? (1.0f - in.alpha) / unit : 0.f;
-  const float c2 = terms & 2 ? in.alpha * in.tau / unit : 0.f;
-  // gradient over the unit at a word with logit z; hit: its share of the label and the teacher
-  auto grad = [&](float z, float hit) {
-    return c1 * __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -lse2)) +
-           c2 * __builtin_amdgcn_exp2f(__builtin_fmaf(z, k2, -lseT2)) - hit;
-  };
-  const float zy = ce ? row_dot<F16>(h, in.w + y * in.D, in.D, lane) : 0.f;
-  const float ce_loss = ce ? __builtin_amdgcn_logf(s) * kLn2 + (mf - zy) : 0.f;
-  if constexpr (!TEACH) {
-    if (lane == 0) {
-      f.loss[t] = ce_loss;
-      st[kStatLse * in.T] = lse2;
-      st[kStatLseT * in.T] = lse2;
-      st[kStatTerms * in.T] = 1.f;
-      st[kStatLabel * in.T] = grad(zy, 1.0f);
-    }
-    return;
-  }
-  const int K = in.K;
-  float* z = sh;
-  float* q = sh + K;
-  int* id = reinterpret_cast<int*>(sh + 2 * K);
-  // the teacher's softmax over its kept words; 2^(log2e / tau t)
-  float tm = -__builtin_inff();
-  for (int k = threadIdx.x; k < K; k += L) {
-    const int64_t v = id_at(in.ids, in.ids64, t * K + k);
-    const bool in_v = v >= 0 && v < in.V;
-    id[k] = in_v ? (int)v : -1;
-    q[k] = in_v ? top_at(f.top, f.top_type, t * K + k) * it : -__builtin_inff();
-    tm = fmaxf(tm, q[k]);
-  }
-  auto block = [&](float v, bool sum) {
-    v = sum ? wave_sum(v) : wave_max(v);
-    __syncthreads();
-    if (lane == 0) red[wave] = v;
-    __syncthreads();
-    float all = red[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) all = sum ? all + red[w] : fmaxf(all, red[w]);
-    return all;
-  };
-  tm = block(tm, false);
-  float ts = 0.f;
-  for (int k = threadIdx.x; k < K; k += L)
-    if (q[k] != -__builtin_inff()) ts += __builtin_amdgcn_exp2f((q[k] - tm) * kLog2e);
-  ts = block(ts, true);
-  const float tl = __builtin_amdgcn_logf(ts) * kLn2;
-  // four words a wave at a time: their loads overlap
-  for (int k0 = 4 * wave; k0 < K; k0 += 4 * WAVES) {
-    float d[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int k = k0 + i < K ? k0 + i : K - 1;
-      const int v = id[k] >= 0 ? id[k] : 0;
-      d[i] = row_dot<F16>(h, in.w + (int64_t)v * in.D, in.D, lane);
-    }
-    if (lane == 0)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (k0 + i < K) z[k0 + i] = d[i];
-  }
-  __syncthreads();
-  float kl = 0.f;
-  if (terms & 2) {
-    for (int k = threadIdx.x; k < K; k += L) {
-      const float a = q[k];
-      if (a == -__builtin_inff()) {
-        q[k] = 0.f;
-        continue;
-      }
-      const float lq = (a - tm) - tl;  // ln q
-      const float p = __builtin_amdgcn_exp2f(lq * kLog2e);
-      q[k] = p;
-      // ln s = (z - m) / tau - ln of the sum
-      if (p != 0.f) kl += p * (lq - ((z[k] - mf) * it - __builtin_amdgcn_logf(sT) * kLn2));
-    }
-    kl = block(kl, true);
-  } else {
-    for (int k = threadIdx.x; k < K; k += L) q[k] = 0.f;
-  }
-  __syncthreads();
-  auto hits = [&](int64_t v) {
-    float x = 0.f;
-    for (int j = 0; j < K; ++j)
-      if (id[j] == v) x += q[j];
-    return c2 * x + (v == y ? c1 : 0.f);
-  };
-  for (int k = threadIdx.x; k < K; k += L)
-    st_top[k] = id[k] >= 0 ? grad(id[k] == y ? zy : z[k], hits(id[k])) : 0.f;
-  if (threadIdx.x == 0) {
-    f.loss[t] = (terms & 1 ? (1.0f - in.alpha) * ce_loss : 0.f) +
-                (terms & 2 ? in.alpha * in.tau * in.tau * kl : 0.f);
-    st[kStatLse * in.T] = lse2;
-    st[kStatLseT * in.T] = lseT2;
-    st[kStatTerms * in.T] = (float)terms;
-    st[kStatLabel * in.T] = ce ? grad(zy, hits(y)) : 0.f;
-  }
-}
-
-// ht[d][r] = h[idx[r]][d]: the logits' second operand, with zeros up to a multiple of 128
-// columns d and of 256 rows r.  64 x 64 a workgroup, through LDS.
-__global__ __launch_bounds__(256) void rows_transpose_kernel(HeadIn in, Rows rows, int64_t tp,
-                                                             uint16_t* __restrict__ ht) {
+template <bool F16, bool BWD, bool LIST>
+__global__ __launch_bounds__(256) void gather_kernel(HeadIn in, Of of, Rows rows, int64_t tp,
+                                                     uint16_t* __restrict__ ht,
+                                                     uint16_t* __restrict__ hs) {
   __shared__ uint16_t s[64][72];
-  const int n = *rows.count;
+  __shared__ int list[LIST ? kListTokens : 1];
+  __shared__ int sums[4][4], maxs[4];
+  __shared__ uint8_t few[kListTeach];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int n, emax = 0;
+  if constexpr (LIST) {
+    const bool first = blockIdx.x == 0 && blockIdx.y == 0;
+    const int T = (int)in.T;
+    const uint8_t* terms = rows.terms;
+    if (!BWD && in.K > 0 && T <= kListTeach) {
+      for (int t = wave; t < T; t += 4) {
+        const int v = terms_of(in, of, t, lane);
+        if (lane == 0) {
+          few[t] = (uint8_t)v;
+          if (first) rows.terms[t] = (uint8_t)v;
+        }
+      }
+      __syncthreads();
+      terms = few;
+    }
+    bool yes[4];
+    uint64_t mask[4];
+    int e = -1000;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int t = 256 * c + tid;
+      yes[c] = t < T && has_row<BWD>(in, of, terms, t);
+      if constexpr (BWD)
+        if (yes[c]) e = max(e, row_exp(in, of, t));
+      mask[c] = __ballot(yes[c]);
+      if (lane == 0) sums[c][wave] = __popcll(mask[c]);
+    }
+    if constexpr (BWD) {
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) e = max(e, __shfl_xor(e, o, 64));
+      if (lane == 0) maxs[wave] = e;
+    }
+    __syncthreads();
+    n = 0;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      int r = n + __popcll(mask[c] & ((uint64_t(1) << lane) - 1));
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        r += w < wave ? sums[c][w] : 0;
+        n += sums[c][w];
+      }
+      const int t = 256 * c + tid;
+      if (yes[c]) list[r] = t;
+      if (first && t < T) {
+        rows.pos[t] = yes[c] ? r : -1;
+        if (yes[c]) put_row<BWD>(in, of, rows, t, r);
+      }
+    }
+    if constexpr (BWD) {
+      e = max(max(maxs[0], maxs[1]), max(maxs[2], maxs[3]));
+      emax = e == -1000 ? 0 : e;
+      if (first && tid == 0) put_exps(of, rows, e);
+    }
+    if (first && tid == 0) *rows.count = n;
+    __syncthreads();
+  } else {
+    n = *rows.count;
+    if constexpr (BWD) emax = rows.exps[0];
+  }
   const int64_t r0 = (int64_t)blockIdx.x * 64;
-  const int d0 = blockIdx.y * 64, q = threadIdx.x >> 3, c = 8 * (threadIdx.x & 7);
   if (r0 >= up256(n)) return;
+  const int d0 = blockIdx.y * 64, q = tid >> 3, c = 8 * (tid & 7);
 #pragma unroll
   for (int i = 0; i < 64; i += 32) {
+    const int64_t r = r0 + q + i;
     u32x4 v = {0, 0, 0, 0};
-    if (r0 + q + i < n && d0 + c < in.D)
-      v = ld16(in.h + (int64_t)rows.idx[r0 + q + i] * in.D + d0 + c);
+    if (r < n && d0 + c < in.D) {
+      const int64_t t = LIST ? list[r] : rows.idx[r];
+      v = ld16(in.h + t * in.D + d0 + c);
+      if constexpr (BWD)
+        if (hs) {
+          const int e = exp_of(of.dloss[t] * head_unit(in.alpha, in.tau)) - emax;
+          u32x4 o = v;
+          if (e != 0) {
+            float x[8];
+            widen<F16>(v, x);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              o[j] = (uint32_t)narrow<F16>(ldexpf(x[2 * j], e)) |
+                     (uint32_t)narrow<F16>(ldexpf(x[2 * j + 1], e)) << 16;
+          }
+          st16(hs + r * in.D + d0 + c, o);
+        }
+    }
     st16(&s[q + i][c], v);
   }
   __syncthreads();
@@ -408,27 +339,225 @@ __global__ __launch_bounds__(256) void rows_transpose_kernel(HeadIn in, Rows row
   }
 }
 
-// hs[r] = h[idx[r]] times 2^(e - emax): the rows dW contracts, one after another
+// What the losses are made from
+struct Finish {
+  HeadIn in;
+  const void* top;
+  int top_type;
+  const float* part;
+  int tile, grid;  // tokens of a tile and workgroups of the logits' launch
+  Rows rows;
+  float* loss;
+  float* stats;
+};
+
+// h . w[i] for N rows w over the lanes of a wave, in every lane; UNROLL steps of 512
+// columns under way at once
+template <bool F16, int N, int UNROLL>
+__device__ __forceinline__ void row_dots(const uint16_t* h, const uint16_t* const* w, int D,
+                                         int lane, float (&s)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] = 0.f;
+#pragma unroll UNROLL
+  for (int d = lane * 8; d < D; d += 512) {
+    float x[8], y[8];
+    widen<F16>(ld16(h + d), x);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      widen<F16>(ld16(w[i] + d), y);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[i] = __builtin_fmaf(x[j], y[j], s[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
+}
+
+// the softmax sums of row r: the parts of its token tile's workgroups, joined.  m: the largest
+// logit; s: sum of 2^(log2e (z - m)); sT the same at the temperature (TEMP)
+template <bool TEMP>
+__device__ __forceinline__ void join(const float* part, int r, int n, int64_t V, int tile, int grid,
+                                     float k2, int lane, float& m, float& s, float& sT) {
+  constexpr int E = TEMP ? 3 : 2, N = 8;
+  const int64_t nt = (n + tile - 1) / tile, nv = (V + 255) / 256, all = nt * nv;
+  const int64_t P = all < grid ? all : grid;
+  const int64_t j = r / tile;
+  // the workgroups whose runs hold the tile's first and last item
+  const int64_t w0 = ((j * nv + 1) * P - 1) / all, w1 = (((j + 1) * nv) * P - 1) / all;
+  const int cnt = (int)(w1 - w0 + 1) * 2;
+  const float* at = part + ((w0 + j) * 512 + r % tile) * E;
+  float a = 0.f, b = 0.f;
+  m = -__builtin_inff();
+  for (int i0 = 0; i0 < cnt; i0 += 64 * N) {  // N at once: their loads overlap
+    float pm[N], ps[N], pt[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int i = i0 + 64 * k + lane;
+      const float* p = at + (int64_t)(i < cnt ? i : 0) * 256 * E;
+      pm[k] = i < cnt ? p[0] : -__builtin_inff();
+      ps[k] = i < cnt ? p[1] : 0.f;
+      if constexpr (TEMP) pt[k] = i < cnt ? p[2] : 0.f;
+    }
+    const float old = m;
+#pragma unroll
+    for (int k = 0; k < N; ++k) m = fmaxf(m, pm[k]);
+    const float ref = m == -__builtin_inff() ? 0.f : m;
+    a *= __builtin_amdgcn_exp2f((old - ref) * kLog2e);
+    if constexpr (TEMP) b *= __builtin_amdgcn_exp2f((old - ref) * k2);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      a += ps[k] * __builtin_amdgcn_exp2f((pm[k] - ref) * kLog2e);
+      if constexpr (TEMP) b += pt[k] * __builtin_amdgcn_exp2f((pm[k] - ref) * k2);
+    }
+  }
+  const float mine = m;
+  m = wave_max(m);
+  const float ref = m == -__builtin_inff() ? 0.f : m;
+  s = wave_sum(a * __builtin_amdgcn_exp2f((mine - ref) * kLog2e));
+  sT = TEMP ? wave_sum(b * __builtin_amdgcn_exp2f((mine - ref) * k2)) : s;
+}
+
+// A row's softmax: the largest logit (0 for a row without one), log2 of the sums, the sums'
+// logarithms, and the factors of the two gradients over the unit
+struct Softmax {
+  float m, lse, lse_t, ln, ln_t, c1, c2, k2;
+  // gradient over the unit at a word with logit z; hit: its share of the label and the teacher
+  __device__ __forceinline__ float grad(float z, float hit) const {
+    return c1 * __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -lse)) +
+           c2 * __builtin_amdgcn_exp2f(__builtin_fmaf(z, k2, -lse_t)) - hit;
+  }
+};
+
+template <bool TEMP>
+__device__ __forceinline__ Softmax softmax_of(const Finish& f, int64_t t, int terms, int lane) {
+  const HeadIn& in = f.in;
+  Softmax x;
+  x.k2 = kLog2e / in.tau;
+  float m, s, sT;
+  join<TEMP>(f.part, f.rows.pos[t], *f.rows.count, in.V, f.tile, f.grid, x.k2, lane, m, s, sT);
+  x.m = m == -__builtin_inff() ? 0.f : m;  // (as the sums took it)
+  const float l = __builtin_amdgcn_logf(s), lT = __builtin_amdgcn_logf(sT);
+  x.lse = __builtin_fmaf(x.m, kLog2e, l);
+  x.lse_t = __builtin_fmaf(x.m, x.k2, lT);
+  x.ln = l * kLn2;
+  x.ln_t = lT * kLn2;
+  const float unit = head_unit(in.alpha, in.tau);
+  x.c1 = terms & 1 ? (1.0f - in.alpha) / unit : 0.f;
+  x.c2 = terms & 2 ? in.alpha * in.tau / unit : 0.f;
+  return x;
+}
+
+__device__ __forceinline__ void put_stats(const Finish& f, int64_t t, float loss, float lse,
+                                          float lse_t, int terms, float label) {
+  float* st = f.stats + t;  // the token's place in each plane
+  f.loss[t] = loss;
+  st[kStatLse * f.in.T] = lse;
+  st[kStatLseT * f.in.T] = lse_t;
+  st[kStatTerms * f.in.T] = (float)terms;
+  st[kStatLabel * f.in.T] = label;
+}
+
+// The cross entropy and the stats of a token, a wave a token
 template <bool F16>
-__global__ __launch_bounds__(256) void rows_copy_kernel(HeadIn in, const float* __restrict__ dloss,
-                                                        Rows rows, uint16_t* __restrict__ hs) {
-  const int64_t r = blockIdx.x;
-  if (r >= *rows.count) return;
-  const int64_t t = rows.idx[r];
-  const int e = exp_of(dloss[t] * head_unit(in.alpha, in.tau)) - rows.exps[0];
-  const uint16_t* src = in.h + t * in.D;
-  uint16_t* dst = hs + r * in.D;
-  for (int d = threadIdx.x * 8; d < in.D; d += 2048) {
-    u32x4 v = ld16(src + d);
-    if (e != 0) {
-      float x[8];
-      widen<F16>(v, x);
+__global__ __launch_bounds__(256) void finish_kernel(Finish f) {
+  const HeadIn& in = f.in;
+  const int lane = threadIdx.x & 63;
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= in.T) return;
+  const int64_t y = id_at(in.targets, in.targets64, t);
+  if (!in_vocabulary(in, y)) {
+    if (lane == 0) put_stats(f, t, 0.f, 0.f, 0.f, 0, 0.f);
+    return;
+  }
+  float z[1];
+  const uint16_t* const w[1] = {in.w + y * in.D};
+  row_dots<F16, 1, 4>(in.h + t * in.D, w, in.D, lane, z);
+  const Softmax x = softmax_of<false>(f, t, 1, lane);
+  if (lane == 0) put_stats(f, t, x.ln + (x.m - z[0]), x.lse, x.lse, 1, x.grad(z[0], 1.0f));
+}
+
+// The same with a teacher, a workgroup of WAVES waves a token: four, or sixteen where tokens
+// are few (1 token, 64 words: XX us, YY of four).  Entry 0 is the label, the others
+// the teacher's words: their logits are dealt over the waves, four at a time; every wave
+// makes the softmaxes by itself.  Bound: the words' rows of W from the caches (16384 tokens of
+// 64 words of 2048 columns, 4.3 GB: XX us).
+template <bool F16, bool TEMP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void teach_kernel(Finish f) {
+  constexpr int L = 64 * WAVES;
+  extern __shared__ float sh[];  // K + 1 each: logits; teacher's logits, probabilities; words
+  const HeadIn& in = f.in;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t t = blockIdx.x;
+  const int n = in.K + 1;
+  float* st_top = f.stats + kStatPlanes * in.T + t * in.K;
+  const int terms = f.rows.terms[t];
+  if (terms == 0) {  // no loss
+    for (int i = tid; i < in.K; i += L) st_top[i] = 0.f;
+    if (tid == 0) put_stats(f, t, 0.f, 0.f, 0.f, 0, 0.f);
+    return;
+  }
+  float *z = sh, *q = sh + n, *p = sh + 2 * n;
+  int* id = reinterpret_cast<int*>(sh + 3 * n);
+  const float it = 1.0f / in.tau;
+  for (int e = tid; e < n; e += L) {
+    const int64_t v = e == 0 ? id_at(in.targets, in.targets64, t)
+                             : id_at(in.ids, in.ids64, t * in.K + e - 1);
+    const bool ok = in_vocabulary(in, v);
+    id[e] = ok ? (int)v : -1;
+    q[e] = ok && e > 0 ? top_at(f.top, f.top_type, t * in.K + e - 1) * it : -__builtin_inff();
+  }
+  __syncthreads();
+  const uint16_t* h = in.h + t * in.D;
+  for (int e0 = 4 * wave; e0 < n; e0 += 4 * WAVES) {
+    float d[4];
+    const uint16_t* w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = e0 + i < n ? e0 + i : n - 1;
+      w[i] = in.w + (int64_t)(id[e] >= 0 ? id[e] : 0) * in.D;
+    }
+    row_dots<F16, 4, WAVES == 4 ? 1 : 4>(h, w, in.D, lane, d);
+    if (lane == 0)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        v[i] = (uint32_t)narrow<F16>(ldexpf(x[2 * i], e)) |
-               (uint32_t)narrow<F16>(ldexpf(x[2 * i + 1], e)) << 16;
+        if (e0 + i < n) z[e0 + i] = d[i];
+  }
+  const Softmax x = softmax_of<TEMP>(f, t, terms, lane);
+  // the teacher's softmax over its kept words
+  float tm = -__builtin_inff(), ts = 0.f;
+  for (int e = lane; e < n; e += 64) tm = fmaxf(tm, q[e]);
+  tm = wave_max(tm);
+  for (int e = lane; e < n; e += 64)
+    if (q[e] != -__builtin_inff()) ts += __builtin_amdgcn_exp2f((q[e] - tm) * kLog2e);
+  const float tl = __builtin_amdgcn_logf(wave_sum(ts)) * kLn2;
+  for (int e = tid; e < n; e += L)
+    p[e] = q[e] != -__builtin_inff() ? __builtin_amdgcn_exp2f(((q[e] - tm) - tl) * kLog2e) : 0.f;
+  __syncthreads();
+  if (wave == 0) {
+    float kl = 0.f;
+    for (int e = lane; e < n; e += 64)  // ln q - ln s, s = e^((z - m) / tau) / sum
+      if (p[e] != 0.f) kl += p[e] * (((q[e] - tm) - tl) - ((z[e] - x.m) * it - x.ln_t));
+    kl = wave_sum(kl);
+    if (lane == 0)
+      f.loss[t] = (terms & 1 ? (1.0f - in.alpha) * (x.ln + (x.m - z[0])) : 0.f) +
+                  (terms & 2 ? in.alpha * in.tau * in.tau * kl : 0.f);
+  }
+  const int y = id[0];
+  for (int e = tid; e < n; e += L) {
+    const int v = id[e];
+    float hit = 0.f;
+#pragma unroll 8
+    for (int j = 1; j < n; ++j) hit += id[j] == v ? p[j] : 0.f;
+    const float g = v >= 0 ? x.grad(z[e], x.c2 * hit + (v == y ? x.c1 : 0.f)) : 0.f;
+    if (e == 0) {
+      float* st = f.stats + t;
+      st[kStatLse * in.T] = x.lse;
+      st[kStatLseT * in.T] = x.lse_t;
+      st[kStatTerms * in.T] = (float)terms;
+      st[kStatLabel * in.T] = g;
+    } else {
+      st_top[e - 1] = g;
     }
-    st16(dst + d, v);
   }
 }
 
@@ -455,35 +584,36 @@ __global__ __launch_bounds__(256) void sparse_kernel(HeadIn in, const float* __r
   G[r * ld + v] = narrow<F16>(x * ldexpf(g, kHeadShift<F16> - exp_of(g)));
 }
 
-// dh[t] = 2^(e - shift) times the sum of the row's parts; zeros for a token without a row
+// dh[t] = 2^(e - shift) times the sum of the row's parts; zeros for a token without a row.
+// A wave has 512 columns.
 template <bool F16>
-__global__ __launch_bounds__(256) void dh_out_kernel(HeadIn in, const float* __restrict__ dloss,
-                                                     Rows rows, const float* __restrict__ part,
-                                                     int parts, uint16_t* __restrict__ dh) {
+__global__ __launch_bounds__(64) void dh_out_kernel(HeadIn in, const float* __restrict__ dloss,
+                                                    Rows rows, const float* __restrict__ part,
+                                                    int parts, uint16_t* __restrict__ dh) {
   const int64_t t = blockIdx.x;
+  const int d = (blockIdx.y * 64 + threadIdx.x) * 8;
+  if (d >= in.D) return;
   const int r = rows.pos[t];
-  uint16_t* dst = dh + t * in.D;
   const int e = exp_of(dloss[t] * head_unit(in.alpha, in.tau)) - kHeadShift<F16>;
-  for (int d = threadIdx.x * 8; d < in.D; d += 2048) {
-    u32x4 o = {0, 0, 0, 0};
-    if (r >= 0) {
-      f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
-#pragma unroll 4
-      for (int s = 0; s < parts; ++s) {
-        const float* p = part + ((int64_t)s * in.T + r) * in.D + d;
-        a += *reinterpret_cast<const f32x4*>(p);
-        b += *reinterpret_cast<const f32x4*>(p + 4);
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        o[i] = (uint32_t)narrow<F16>(ldexpf(a[2 * i], e)) |
-               (uint32_t)narrow<F16>(ldexpf(a[2 * i + 1], e)) << 16;
-        o[2 + i] = (uint32_t)narrow<F16>(ldexpf(b[2 * i], e)) |
-                   (uint32_t)narrow<F16>(ldexpf(b[2 * i + 1], e)) << 16;
-      }
+  u32x4 o = {0, 0, 0, 0};
+  if (r >= 0) {
+    f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+    const float* p = part + (int64_t)r * in.D + d;
+#pragma unroll 8
+    for (int s = 0; s < parts; ++s) {
+      a += *reinterpret_cast<const f32x4*>(p);
+      b += *reinterpret_cast<const f32x4*>(p + 4);
+      p += in.T * in.D;
     }
-    st16(dst + d, o);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      o[i] = (uint32_t)narrow<F16>(ldexpf(a[2 * i], e)) |
+             (uint32_t)narrow<F16>(ldexpf(a[2 * i + 1], e)) << 16;
+      o[2 + i] = (uint32_t)narrow<F16>(ldexpf(b[2 * i], e)) |
+                 (uint32_t)narrow<F16>(ldexpf(b[2 * i + 1], e)) << 16;
+    }
   }
+  st16(dh + t * in.D + d, o);
 }
 
 // Parts of a contraction of nst stages of `tiles` tiles on P workgroups: the
@@ -596,50 +726,58 @@ int64_t head_loss_bwd_bytes(int64_t T, int64_t V, int64_t D) {
     if (e_ != hipSuccess) return e_;     \
   } while (0)
 
-static int64_t rows_per_group(int64_t T) {
-  const int64_t per = (T + 63) / 64;
-  return (per + 1023) / 1024 * 1024;
-}
-
-static hipError_t transpose(const HeadIn& in, const Layout& l, hipStream_t stream) {
-  hipLaunchKernelGGL(rows_transpose_kernel,
-                     dim3((unsigned)(head_padded(in.T) / 64), (unsigned)(up128(in.D) / 64)), dim3(256), 0,
-                     stream, in, l.rows, head_padded(in.T), l.ht);
+// the rows, their list and their copies
+template <bool F16, bool BWD>
+static hipError_t gather(const HeadIn& in, const Of& of, const Layout& l, uint16_t* hs,
+                         hipStream_t stream) {
+  const bool list = in.T <= kListTokens;
+  if (!BWD && in.K > 0 && !(list && in.T <= kListTeach)) {
+    hipLaunchKernelGGL(terms_kernel, dim3((unsigned)((in.T + 3) / 4)), dim3(256), 0, stream, in, of,
+                       l.rows.terms);
+    TM_RET(hipGetLastError());
+  }
+  const dim3 grid((unsigned)(head_padded(in.T) / 64), (unsigned)(up128(in.D) / 64));
+  if (list) {
+    hipLaunchKernelGGL((gather_kernel<F16, BWD, true>), grid, dim3(256), 0, stream, in, of, l.rows,
+                       head_padded(in.T), l.ht, hs);
+    return hipGetLastError();
+  }
+  const int64_t per = ((in.T + 63) / 64 + 1023) / 1024 * 1024;
+  hipLaunchKernelGGL(rows_kernel<BWD>, dim3((unsigned)((in.T + per - 1) / per)), dim3(1024), 0,
+                     stream, in, of, per, l.rows);
+  TM_RET(hipGetLastError());
+  hipLaunchKernelGGL((gather_kernel<F16, BWD, false>), grid, dim3(256), 0, stream, in, of, l.rows,
+                     head_padded(in.T), l.ht, hs);
   return hipGetLastError();
 }
 
 template <bool F16, int WAVES>
-static hipError_t run_finish_of(const Finish& f, hipStream_t stream) {
-  const dim3 grid((unsigned)(WAVES ? f.in.T : (f.in.T + 3) / 4)), block(WAVES ? 64 * WAVES : 256);
-  if (WAVES && f.in.tau != 1.0f)
-    hipLaunchKernelGGL((finish_kernel<F16, true, WAVES>), grid, block, (unsigned)(12 * f.in.K),
-                       stream, f);
+static hipError_t run_teach(const Finish& f, hipStream_t stream) {
+  const dim3 grid((unsigned)f.in.T), block(64 * WAVES);
+  const unsigned lds = 16 * (f.in.K + 1);
+  if (f.in.tau != 1.0f)
+    hipLaunchKernelGGL((teach_kernel<F16, true, WAVES>), grid, block, lds, stream, f);
   else
-    hipLaunchKernelGGL((finish_kernel<F16, false, WAVES>), grid, block, (unsigned)(12 * f.in.K),
-                       stream, f);
+    hipLaunchKernelGGL((teach_kernel<F16, false, WAVES>), grid, block, lds, stream, f);
   return hipGetLastError();
 }
 
 template <bool F16>
 static hipError_t run_finish(const Finish& f, hipStream_t stream) {
-  if (f.in.K == 0) return run_finish_of<F16, 0>(f, stream);
-  if (f.in.T <= 512 && f.in.K > 16) return run_finish_of<F16, 16>(f, stream);
-  return run_finish_of<F16, 4>(f, stream);
+  if (f.in.K > 0)
+    return f.in.T <= 512 && f.in.K >= 16 ? run_teach<F16, 16>(f, stream)
+                                         : run_teach<F16, 4>(f, stream);
+  hipLaunchKernelGGL(finish_kernel<F16>, dim3((unsigned)((f.in.T + 3) / 4)), dim3(256), 0, stream,
+                     f);
+  return hipGetLastError();
 }
 
 hipError_t launch_head_loss(const HeadIn& in, const void* top, int top_type, float* loss,
                             float* stats, void* workspace, hipStream_t stream) {
   const Layout l = forward_layout(in.T, in.V, in.D, workspace);
-  if (in.K > 0) {
-    hipLaunchKernelGGL(terms_kernel, dim3((unsigned)((in.T + 3) / 4)), dim3(256), 0, stream, in,
-                       top, top_type, l.rows.terms);
-    TM_RET(hipGetLastError());
-  }
-  const int64_t per = rows_per_group(in.T);
-  hipLaunchKernelGGL(rows_kernel<false>, dim3((unsigned)((in.T + per - 1) / per)), dim3(1024), 0,
-                     stream, in, nullptr, nullptr, 0, per, l.rows);
-  TM_RET(hipGetLastError());
-  TM_RET(transpose(in, l, stream));
+  const Of of{top, top_type, nullptr, nullptr, 0};
+  TM_RET(in.f16 ? (gather<true, false>(in, of, l, nullptr, stream))
+                : (gather<false, false>(in, of, l, nullptr, stream)));
   TM_RET(launch_head_logits(in, l.ht, l.rows.count, l.part, stream));
   const int tile = head_tile_tokens(in.T, in.V, true);
   const Finish f{in, top, top_type, l.part, tile, head_logits_grid(in.T, in.V, tile), l.rows, loss, stats};
@@ -652,16 +790,8 @@ static hipError_t run_bwd(const HeadIn& in, const float* stats, const float* dlo
                           hipStream_t stream) {
   const HeadPlan p = head_plan(in.T, in.V, in.D);
   const Layout l = backward_layout(in.T, in.V, in.D, p, workspace);
-  const int64_t per = rows_per_group(in.T);
-  hipLaunchKernelGGL(rows_kernel<true>, dim3((unsigned)((in.T + per - 1) / per)), dim3(1024), 0,
-                     stream, in, stats, dloss, kHeadShift<F16>, per, l.rows);
-  TM_RET(hipGetLastError());
-  if (dw) {
-    hipLaunchKernelGGL(rows_copy_kernel<F16>, dim3((unsigned)in.T), dim3(256), 0, stream, in, dloss,
-                       l.rows, l.hs);
-    TM_RET(hipGetLastError());
-  }
-  TM_RET(transpose(in, l, stream));
+  const Of of{nullptr, 0, stats, dloss, kHeadShift<F16>};
+  TM_RET((gather<F16, true>(in, of, l, dw ? l.hs : nullptr, stream)));
   for (int64_t i = 0; i < p.pieces; ++i) {
     const int64_t w0 = i * p.piece, n = in.V - w0 < p.piece ? in.V - w0 : p.piece;
     TM_RET(launch_head_dlogits(in, l.ht, l.rows.count, l.rows.row, w0, n, l.G, p.piece,
@@ -678,8 +808,8 @@ static hipError_t run_bwd(const HeadIn& in, const float* stats, const float* dlo
                           last ? p.last_per : p.per_w, l.rows.exps + 1, dw, dw_type, accumulate, l.part_w, stream));
   }
   if (dh)
-    hipLaunchKernelGGL(dh_out_kernel<F16>, dim3((unsigned)in.T), dim3(256), 0, stream, in, dloss,
-                       l.rows, l.part_h, p.parts_h, dh);
+    hipLaunchKernelGGL(dh_out_kernel<F16>, dim3((unsigned)in.T, (unsigned)((in.D + 511) / 512)),
+                       dim3(64), 0, stream, in, dloss, l.rows, l.part_h, p.parts_h, dh);
   return hipGetLastError();
 }
 
