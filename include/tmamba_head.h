@@ -30,7 +30,8 @@ extern "C" {
  *   labels     int32 (labels_i64 = 0) or int64 (1) [T]
  *   top_ids    int32 (ids_i64 = 0) or int64 (1) [T, K], top [T, K] float32
  *              (top_type 0), bfloat16 (1) or float16 (2); both NULL with K = 0: no teacher
- *   alpha      0 .. 1, tau > 0, finite (both ignored without a teacher)
+ *   alpha      0 .. 1, tau 2^-10 .. 2^10 (beyond, float32 holds too little of z / tau or of
+ *              tau^2 KL); both ignored without a teacher
  *   loss       float32 [T]
  *   stats      float32 [T (4 + K)]: what tm_head_loss_bwd needs of this call
  *   T 1 .. 2^23, V 1 .. 2^23, D 8 .. 2^16, K 0 .. 1024, T (K + 1) < 2^31
@@ -53,9 +54,9 @@ int64_t tm_head_loss_workspace(int64_t T, int64_t V, int64_t D); /* -1: sizes ou
  * own in every row) before the two products, whose sums are float32.  Tokens without
  * a loss, or whose dloss is 0, have rows of zeros in dh and no part in dW,
  * whatever their rows of h hold.
- *   dh         [T, D], h's type (16-byte aligned)
- *              or NULL: not wanted
- *   dW         [V, D] or NULL (not both), dW_type 0 float32 or h's type; accumulate 1 (float32 only): dW += that
+ *   dh         [T, D], h's type (16-byte aligned), or NULL: not wanted
+ *   dW         [V, D] (16-byte aligned) or NULL (not both); dW_type 0 float32 or h's
+ *              type; accumulate 1 (float32 only): dW += the gradient
  */
 tm_status tm_head_loss_bwd(const void* h, const void* W, int32_t type, int64_t T, int64_t V,
                            int64_t D, const void* labels, int32_t labels_i64, const void* top_ids,

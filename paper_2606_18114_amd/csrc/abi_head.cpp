@@ -51,8 +51,7 @@ tm_status head_checked(const void* h, const void* W, int32_t type, int64_t T, in
   if (K < 0 || K > 1024 || !head_sizes(T, V, D) || T * (K + 1) >= (int64_t(1) << 31))
     return TM_ESHAPE;
   if ((K > 0) != (top_ids != nullptr)) return TM_EINVAL;
-  if (K > 0 && (!(alpha >= 0.0f && alpha <= 1.0f) || !(tau > 0.0f) || !std::isfinite(tau) ||
-                !std::isfinite(1.0f / tau)))
+  if (K > 0 && (!(alpha >= 0.0f && alpha <= 1.0f) || !(tau >= 0x1p-10f && tau <= 0x1p10f)))
     return TM_EINVAL;
   if (!aligned(h, 16) || !aligned(W, 16) || !aligned(labels, labels_i64 ? 8 : 4) ||
       !aligned(top_ids, ids_i64 ? 8 : 4))

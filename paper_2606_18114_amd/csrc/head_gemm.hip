@@ -15,13 +15,20 @@
 // bytes, in 32-byte units that are XOR-permuted against bank conflicts, read with
 // the transpose read ds_read_b64_tr_b16, two an operand; a ring of four stages, loaded
 // three ahead.  Along: 128-byte rows, the lines of the caches, hold two stages (with
-// 64-byte rows, one stage, the requests to the L2 double, and a stage took 1.05 us, not
-// XXX); their 16-byte pieces are XOR-permuted, one ds_read_b128 is an operand;
-// three pairs of stages, loaded two pairs ahead.
+// 64-byte rows, one stage, the requests to the L2 double: 16384 tokens of 50000 x 2048
+// in 13.6 ms, 12.3 so); their 16-byte pieces are XOR-permuted, one ds_read_b128 is an
+// operand; three pairs of stages, loaded two pairs ahead.
 //
 // Tile 256 x 256 of 4 waves, 128 x 128 each (4 x 4 blocks of 32 x 32,
 // accumulators in AGPRs, one wave a SIMD), every MFMA a slot of its own with the
-// reads of the next step and the loads of stage + 3 dealt over the slots.
+// reads of the next step and the loads of stage + 3 dealt over the slots.  Nothing
+// spills: accumulators leave their registers a block at a time.
+//
+// Bound: the matrix cores under the power cap (a stage of a full tile takes 0.77 us, 1.36
+// PFLOP/s, at 1.7 to 1.85 GHz).  16384 tokens of 50000 x 2048: softmax sums 2.50 ms (1.34
+// PFLOP/s), dlogits 2.85, dh 2.53, dW 2.45; a tile's epilogue adds 3 us to the sums (its first
+// loads are then already under way) and 7 to the dlogits.  16 tokens: the sums 33 us, W at 6.2
+// TB/s.
 #include <type_traits>
 
 #include "common.hpp"
@@ -60,7 +67,7 @@ __device__ __forceinline__ void dma16(const void* base, uint32_t voff, uint32_t 
 
 // A stage's end.  No wait for LDS reads: those of the slot that the next stage's loads
 // write have fed an MFMA of the stage, and those of the next slot are waited for where they
-// are used (with lgkmcnt(0) here a stage took XX us, YY without).
+// are used (16384 tokens of 50000 x 2048: 12.29 ms with lgkmcnt(0) here, 12.19 without).
 template <int kVm>
 __device__ __forceinline__ void stage_barrier() {
   __builtin_amdgcn_sched_barrier(0);
@@ -684,7 +691,7 @@ __global__ __launch_bounds__(256) void head_dh_kernel(
 // unscaled; else to dW's rows, times 2^(*exp).  Float32: A = G, a lane has a column and
 // stores 128 bytes of a row with its neighbours.  16 bits: A = hs, a lane has a word and four
 // columns in a row, which pass through LDS as the dlogits do (with A = G, 2 bytes a lane and
-// store: 16384 tokens, 16384 words: XX us, YY so).
+// LDS write: 64 tokens, 50000 words 82 us, 65 so).
 template <bool F16, bool PARTS, typename O, bool ACC>
 __global__ __launch_bounds__(256) void head_dw_kernel(
     const uint16_t* __restrict__ G, int64_t ld, const uint16_t* __restrict__ hs, int D,
@@ -783,9 +790,10 @@ static int64_t grid_of(int64_t items) {
 }
 
 // Tokens of a tile of logits: 64 (the softmax sums only), 128 or 256.  A stage of the three
-// takes 0.52, 0.58 and 0.80 us a workgroup (the first two by their loads), so narrow tiles are for few tokens (16
-// tokens of 50000 x 2048: XX us, YY with 256) and where they leave fewer workgroups idle in the
-// last round (300 tokens: XX with 128, YY with 256).
+// takes 0.52, 0.58 and 0.80 us a workgroup (the first two by their loads), so narrow tiles
+// are for few tokens (loss of 16 tokens of 50000 x 2048: 44 us, 60 with 256) and for few
+// words, where 256 would leave workgroups idle (300 tokens of 5000 words: 36 us, 51 with
+// 256).  300 tokens of 50000 take 118 us either way: two rounds of tiles.
 int head_tile_tokens(int64_t T, int64_t words, bool stats) {
   const int64_t P = current_cu_count(), nv = (words + kTM - 1) / kTM;
   const double us[3] = {0.52, 0.58, 0.80};

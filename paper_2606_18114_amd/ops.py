@@ -1232,8 +1232,8 @@ def _head_args(h, weight, targets, teacher_ids, alpha, temperature):
             raise ValueError("teacher_ids must hold at least one word a token")
         if not 0.0 <= alpha <= 1.0:
             raise ValueError(f"alpha must lie in 0 .. 1 (got {alpha})")
-        if not 0.0 < temperature < float("inf"):
-            raise ValueError(f"temperature must be positive and finite (got {temperature})")
+        if not 2.0 ** -10 <= temperature <= 2.0 ** 10:
+            raise ValueError(f"temperature must lie in 2^-10 .. 2^10 (got {temperature})")
     return dev, T, V, D, K
 
 

@@ -32,7 +32,9 @@ operations on the data).  ``pack_for_decode`` returns the deployment format
 sequences, ``Embedding`` the residual stream's beginning; with ``TernaryLinear``
 they make up a block's training step on the library's kernels.  ``BlockNorm`` is the
 norm before a block and before the head, ``Head`` the loss at the end: cross entropy and
-distillation (paper Eq. 1) without keeping the logits.
+distillation (paper Eq. 1) without keeping the logits.  Their forward and backward may be
+captured as a HIP graph together, while no eager graph of the same parameters is alive
+(autograd would wait for its stream inside the capture).
 """
 
 from __future__ import annotations
@@ -430,6 +432,8 @@ class BlockNorm(torch.nn.Module):
 
     def forward(self, residual: torch.Tensor, y: Optional[torch.Tensor] = None):
         width = self.weight.shape[0]
+        if residual.shape[-1:] != (width,):
+            raise ValueError(f"the residual must be [..., {width}], got {tuple(residual.shape)}")
         r = residual.reshape(-1, width)
         if y is None:
             return BlockNormFn.apply(r, None, self.weight, self.eps).reshape(residual.shape), \

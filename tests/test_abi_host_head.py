@@ -119,7 +119,7 @@ def test_sizes_and_flags_of_the_loss(L):
         assert call(L, name, K=0) == EINVAL      # words without a number
         for k, bad in (("type", (0, 3)), ("l64", (2, -1)), ("i64", (2,)),
                        ("alpha", (-0.1, 1.1, float("nan"))),
-                       ("tau", (0.0, -1.0, float("nan"), float("inf"), 1e-45))):
+                       ("tau", (0.0, -1.0, float("nan"), float("inf"), 1e-45, 2.0 ** -11, 2.0 ** 11))):
             for v in bad:
                 assert call(L, name, **{k: v}) == EINVAL, (name, k, v)
         assert call(L, name, wsb=0) == ESHAPE

@@ -279,6 +279,28 @@ def test_teachers(top_dtype, ids_dtype):
         _check(c, *_run(c))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_gradients_that_vanish_beside_large_ones(dtype):
+    """A loss's gradient that is zero in float32 once it is taken over the logits' unit (alpha tau
+    = 1/4) adds nothing, whatever the others are."""
+    c = _inputs(5, 70, 24, dtype, K=3, seed=31)
+    c.update(alpha=1.0, tau=0.25)
+    c["dloss"] = torch.tensor([8.0, 1e-45, 100.0, -1e-45, 3.0], device="cuda")
+    loss, dh, dw = _run(c)
+    c["dloss"] = torch.tensor([8.0, 0.0, 100.0, 0.0, 3.0], device="cuda")
+    loss0, dh0, dw0 = _run(c)
+    assert bool(torch.isfinite(dw.float()).all()) and bool((dh[1::2] == 0).all())
+    assert torch.equal(loss, loss0) and torch.equal(dh, dh0) and torch.equal(dw, dw0)
+
+
+@pytest.mark.parametrize("tau", [2.0 ** -10, 2.0 ** 10])
+def test_temperatures_far_from_one(tau):
+    """Cold: the softmaxes are single words, the loss stays finite.  Hot: both are uniform."""
+    c = _inputs(5, 70, 24, K=3, seed=32)
+    c.update(alpha=0.5, tau=tau)
+    assert all(bool(torch.isfinite(t.float()).all()) for t in _run(c))
+
+
 def test_one_word_a_teacher_is_cross_entropy():
     """A teacher that knows one word: the divergence is the cross entropy of it."""
     c = _inputs(50, 200, 64, seed=12)
@@ -451,6 +473,8 @@ def test_block_norm_module():
     with torch.no_grad():
         x, s = norm(r)
         assert s is r
+    with pytest.raises(ValueError, match=r"\[..., 100\]"):
+        norm(torch.randn(100, 4, device="cuda"))  # 400 values, of another width
 
 
 def test_gradients_against_differences():
