@@ -59,6 +59,16 @@ __device__ __forceinline__ uint16_t narrow(float v) {
     return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
+template <bool F16>
+__device__ __forceinline__ f32x4 mfma_16(u32x4 a, u32x4 b, f32x4 c) {
+  typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+  if constexpr (F16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return mfma16(as_bf16x8(a), as_bf16x8(b), c);
+}
+
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -340,6 +350,224 @@ __global__ __launch_bounds__(256) void gather_kernel(HeadIn in, Of of, Rows rows
   }
 }
 
+// Softmax sums of up to 64 tokens, 16 NT: a read of W.  Every wave has a run of V / waves words to
+// itself, 64 at a time as four blocks of 16 x 16 x 32 matrix products with the tokens; W goes
+// from memory to registers (no other wave wants it), four steps of 64 columns ahead, 32 KiB a
+// wave, h from LDS, kCols columns at a time.  Every workgroup lists the rows by itself, the
+// first one writes the list.  part as the logits' kernel leaves it, one tile of tokens and a tile
+// of words a workgroup.
+// Bound: HBM.
+template <bool F16, bool TEMP, int NT>
+__global__ __launch_bounds__(256) void few_kernel(HeadIn in, Of of, Rows rows,
+                                                  float* __restrict__ part) {
+  constexpr int E = TEMP ? 3 : 2, NB = 4, R = 4;
+  constexpr int kCols = 4096 / NT, kPitch = 2 * kCols + 16;
+  __shared__ __attribute__((aligned(16))) uint8_t hl[16 * NT * kPitch];
+  __shared__ float sums[4][16 * NT][3];
+  __shared__ int list[64];
+  __shared__ int found;
+  __shared__ uint8_t few[kListTeach];
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int T = (int)in.T, D = in.D, V = (int)in.V;
+  const int waves = 4 * gridDim.x, wv = 4 * blockIdx.x + wave;
+  const int v_beg = (int)((int64_t)wv * V / waves), v_end = (int)((int64_t)(wv + 1) * V / waves);
+  const int blocks = ((V + waves - 1) / waves + 16 * NB - 1) / (16 * NB);  // of every wave's run
+  const int nit = (D + 63) / 64;
+  // A wave takes a chunk's columns from a place of its own on: rows are often a power of two
+  // apart, and waves in step would ask the same memory channels.
+  constexpr int C = kCols / 64;
+  const int last = (nit - 1) / C * C, c_last = nit - last;
+  const int rot = (wv * 5) % C, rot_last = (wv * 5) % c_last;
+  auto step = [&](int i) {  // the i-th step's columns, in 64s
+    const int base = i >= last ? last : i / C * C, c = i >= last ? c_last : C;
+    const int k = i - base + (i >= last ? rot_last : rot);
+    return base + (k >= c ? k - c : k);
+  };
+  int words = 0;  // of the block that the loads are for
+  const uint16_t* w[NB];
+  u32x4 a[R][NB][2];
+  auto load = [&](u32x4 (&to)[NB][2], int i) {
+    const int k = 64 * step(i < nit ? i : nit - 1) + 8 * g;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) to[b][x] = ld16(w[b] + (k + 32 * x < D ? k + 32 * x : D - 8));
+  };
+  auto begin = [&](int blk) {
+    const int v0 = v_beg + (int)((int64_t)(v_end - v_beg) * blk / blocks);
+    words = v_beg + (int)((int64_t)(v_end - v_beg) * (blk + 1) / blocks) - v0;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {  // (rows past the block's: its last one)
+      const int r = 16 * b + l16 < words ? 16 * b + l16 : words > 0 ? words - 1 : 0;
+      w[b] = in.w + (int64_t)(v0 + r < V ? v0 + r : V - 1) * D;
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j) load(a[j], j);
+  };
+  begin(0);  // W's first columns are under way while the rows are listed and h is copied
+  __builtin_amdgcn_sched_barrier(0);
+
+  const bool first = blockIdx.x == 0;
+  const uint8_t* terms = rows.terms;
+  if (in.K > 0 && T <= kListTeach) {
+    for (int t = wave; t < T; t += 4) {
+      const int v = terms_of(in, of, t, lane);
+      if (lane == 0) {
+        few[t] = (uint8_t)v;
+        if (first) rows.terms[t] = (uint8_t)v;
+      }
+    }
+    __syncthreads();
+    terms = few;
+  }
+  if (wave == 0) {
+    const bool yes = lane < T && has_row<false>(in, of, terms, lane);
+    const uint64_t mask = __ballot(yes);
+    const int r = __popcll(mask & ((uint64_t(1) << lane) - 1));
+    if (yes) list[r] = lane;
+    if (lane == 0) found = __popcll(mask);
+    if (first) {
+      if (lane < T) rows.pos[lane] = yes ? r : -1;
+      if (lane == 0) *rows.count = __popcll(mask);
+    }
+  }
+  __syncthreads();
+  const int n = __builtin_amdgcn_readfirstlane(found);
+  if (n == 0) return;
+
+  auto fill = [&](int base) {  // h's columns from 64 base on, 4096 pieces of 8 at once
+    const int per = 8 * (nit - base < C ? nit - base : C);  // pieces of a row
+    const int dr = 256 / per, dc = 256 - dr * per;
+    int r = tid / per, c = tid - r * per;
+    while (__any(r < n)) {
+      u32x4 v[16];
+      int at[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int col = 64 * base + 8 * c;
+        at[j] = r < n ? r * kPitch + 16 * c : -1;
+        v[j] = ld16(in.h + (int64_t)list[r < n ? r : 0] * D + (col < D ? col : 0));
+        if (col >= D) v[j] = u32x4{0, 0, 0, 0};
+        r += dr;
+        c += dc;
+        if (c >= per) {
+          c -= per;
+          ++r;
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (at[j] >= 0) st16(hl + at[j], v[j]);
+    }
+  };
+
+  const float k1 = kLog2e, k2 = kLog2e / in.tau;
+  float mx[NT], sm[NT], st[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    mx[t] = -__builtin_inff();
+    sm[t] = st[t] = 0.f;
+  }
+  for (int blk = 0; blk < blocks; ++blk) {
+    f32x4 acc[NB][NT];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[b][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < nit; i0 += R) {
+      if (i0 % C == 0 && (nit > C || blk == 0)) {
+        __syncthreads();  // the columns before have been read
+        fill(i0);
+        __syncthreads();
+      }
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        if (i0 + j < nit) {
+          const int at = step(i0 + j), k = 64 * at + 8 * g;
+          const uint8_t* hp = hl + l16 * kPitch + 128 * (at % C) + 16 * g;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const bool in_row = k + 32 * x < D;
+            u32x4 wf[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+              wf[b] = in_row ? a[j][b][x] : u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              const u32x4 hf = *reinterpret_cast<const u32x4*>(hp + 16 * t * kPitch + 64 * x);
+#pragma unroll
+              for (int b = 0; b < NB; ++b) acc[b][t] = mfma_16<F16>(wf[b], hf, acc[b][t]);
+            }
+          }
+        }
+        load(a[j], i0 + j + R);
+      }
+    }
+    // a lane: token 16 t + l16, words 16 b + 4 g + i
+    const int left = words;
+    if (blk + 1 < blocks) begin(blk + 1);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float m = mx[t];
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (16 * b + 4 * g + i >= left) acc[b][t][i] = -__builtin_inff();
+          m = fmaxf(m, acc[b][t][i]);
+        }
+      const float ref = m == -__builtin_inff() ? 0.f : m;
+      float s = sm[t] * __builtin_amdgcn_exp2f((mx[t] - ref) * k1);
+      float sT = TEMP ? st[t] * __builtin_amdgcn_exp2f((mx[t] - ref) * k2) : 0.f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s += __builtin_amdgcn_exp2f((acc[b][t][i] - ref) * k1);
+          if constexpr (TEMP) sT += __builtin_amdgcn_exp2f((acc[b][t][i] - ref) * k2);
+        }
+      mx[t] = m;
+      sm[t] = s;
+      st[t] = sT;
+    }
+  }
+  // (m, s, sT) of two runs of words
+  auto both = [&](float& m, float& s, float& sT, float om, float os, float oT) {
+    const float top = fmaxf(m, om), ref = top == -__builtin_inff() ? 0.f : top;
+    s = s * __builtin_amdgcn_exp2f((m - ref) * k1) + os * __builtin_amdgcn_exp2f((om - ref) * k1);
+    if constexpr (TEMP)
+      sT = sT * __builtin_amdgcn_exp2f((m - ref) * k2) +
+           oT * __builtin_amdgcn_exp2f((om - ref) * k2);
+    m = top;
+  };
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+#pragma unroll
+    for (int o = 16; o < 64; o <<= 1)
+      both(mx[t], sm[t], st[t], __shfl_xor(mx[t], o, 64), __shfl_xor(sm[t], o, 64),
+           TEMP ? __shfl_xor(st[t], o, 64) : 0.f);
+    if (g == 0) {
+      float* p = sums[wave][16 * t + l16];
+      p[0] = mx[t];
+      p[1] = sm[t];
+      p[2] = st[t];
+    }
+  }
+  __syncthreads();
+  const int e = tid >> 6;
+  if (e < 2 && lane < n) {
+    const float *x = sums[2 * e][lane], *y = sums[2 * e + 1][lane];
+    float m = x[0], s = x[1], sT = x[2];
+    both(m, s, sT, y[0], y[1], y[2]);
+    float* p = part + ((int64_t)(2 * blockIdx.x + e) * 256 + lane) * E;
+    p[0] = m;
+    p[1] = s;
+    if constexpr (TEMP) p[2] = sT;
+  }
+}
+
 // What the losses are made from
 struct Finish {
   HeadIn in;
@@ -347,6 +575,7 @@ struct Finish {
   int top_type;
   const float* part;
   int tile, grid;  // tokens of a tile and workgroups of the logits' launch
+  int64_t nv;      // its tiles of words
   Rows rows;
   float* loss;
   float* stats;
@@ -377,10 +606,10 @@ __device__ __forceinline__ void row_dots(const uint16_t* h, const uint16_t* cons
 // the softmax sums of row r: the parts of its token tile's workgroups, joined.  m: the largest
 // logit; s: sum of 2^(log2e (z - m)); sT the same at the temperature (TEMP)
 template <bool TEMP>
-__device__ __forceinline__ void join(const float* part, int r, int n, int64_t V, int tile, int grid,
-                                     float k2, int lane, float& m, float& s, float& sT) {
+__device__ __forceinline__ void join(const float* part, int r, int n, int64_t nv, int tile,
+                                     int grid, float k2, int lane, float& m, float& s, float& sT) {
   constexpr int E = TEMP ? 3 : 2, N = 8;
-  const int64_t nt = (n + tile - 1) / tile, nv = (V + 255) / 256, all = nt * nv;
+  const int64_t nt = (n + tile - 1) / tile, all = nt * nv;
   const int64_t P = all < grid ? all : grid;
   const int64_t j = r / tile;
   // the workgroups whose runs hold the tile's first and last item
@@ -435,7 +664,7 @@ __device__ __forceinline__ Softmax softmax_of(const Finish& f, int64_t t, int te
   Softmax x;
   x.k2 = kLog2e / in.tau;
   float m, s, sT;
-  join<TEMP>(f.part, f.rows.pos[t], *f.rows.count, in.V, f.tile, f.grid, x.k2, lane, m, s, sT);
+  join<TEMP>(f.part, f.rows.pos[t], *f.rows.count, f.nv, f.tile, f.grid, x.k2, lane, m, s, sT);
   x.m = m == -__builtin_inff() ? 0.f : m;  // (as the sums took it)
   const float l = __builtin_amdgcn_logf(s), lT = __builtin_amdgcn_logf(sT);
   x.lse = __builtin_fmaf(x.m, kLog2e, l);
@@ -479,13 +708,18 @@ __global__ __launch_bounds__(256) void finish_kernel(Finish f) {
 
 // The same with a teacher, a workgroup of WAVES waves a token: four, or sixteen where tokens
 // are few (1 token, 64 words: 22 us, 43 of four).  Entry 0 is the label, the others
-// the teacher's words: their logits are dealt over the waves, four at a time; every wave
-// makes the softmaxes by itself.  Bound: the words' rows of W from the caches (16384 tokens of
+// the teacher's words: their logits are dealt over the waves, four or five at a time; of four
+// waves each makes the softmaxes by itself.  Bound: the words' rows of W from the caches (16384 tokens of
 // 64 words of 2048 columns, 4.3 GB: 330 us).
 template <bool F16, bool TEMP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void teach_kernel(Finish f) {
   constexpr int L = 64 * WAVES;
+  // sixteen waves: the last one makes the softmaxes while the others make the logits
+  constexpr bool SPLIT = WAVES == 16;
+  constexpr int DOTS = SPLIT ? WAVES - 1 : WAVES, N = SPLIT ? 5 : 4;
   extern __shared__ float sh[];  // K + 1 each: logits; teacher's logits, probabilities; words
+  __shared__ Softmax shared_x;
+  __shared__ float shared_t[2];
   const HeadIn& in = f.in;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t t = blockIdx.x;
@@ -509,31 +743,46 @@ __global__ __launch_bounds__(64 * WAVES) void teach_kernel(Finish f) {
   }
   __syncthreads();
   const uint16_t* h = in.h + t * in.D;
-  for (int e0 = 4 * wave; e0 < n; e0 += 4 * WAVES) {
-    float d[4];
-    const uint16_t* w[4];
+  if (wave < DOTS)
+    for (int e0 = N * wave; e0 < n; e0 += N * DOTS) {
+      float d[N];
+      const uint16_t* w[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int e = e0 + i < n ? e0 + i : n - 1;
-      w[i] = in.w + (int64_t)(id[e] >= 0 ? id[e] : 0) * in.D;
+      for (int i = 0; i < N; ++i) {
+        const int e = e0 + i < n ? e0 + i : n - 1;
+        w[i] = in.w + (int64_t)(id[e] >= 0 ? id[e] : 0) * in.D;
+      }
+      row_dots<F16, N, SPLIT ? 4 : 1>(h, w, in.D, lane, d);
+      if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (e0 + i < n) z[e0 + i] = d[i];
     }
-    row_dots<F16, 4, WAVES == 4 ? 1 : 4>(h, w, in.D, lane, d);
-    if (lane == 0)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (e0 + i < n) z[e0 + i] = d[i];
+  Softmax x;
+  float tm = -__builtin_inff(), tl = 0.f;
+  if (!SPLIT || wave == DOTS) {
+    x = softmax_of<TEMP>(f, t, terms, lane);
+    // the teacher's softmax over its kept words
+    float ts = 0.f;
+    for (int e = lane; e < n; e += 64) tm = fmaxf(tm, q[e]);
+    tm = wave_max(tm);
+    for (int e = lane; e < n; e += 64)
+      if (q[e] != -__builtin_inff()) ts += __builtin_amdgcn_exp2f((q[e] - tm) * kLog2e);
+    tl = __builtin_amdgcn_logf(wave_sum(ts)) * kLn2;
+    for (int e = SPLIT ? lane : tid; e < n; e += SPLIT ? 64 : L)
+      p[e] = q[e] != -__builtin_inff() ? __builtin_amdgcn_exp2f(((q[e] - tm) - tl) * kLog2e) : 0.f;
+    if (SPLIT && lane == 0) {
+      shared_x = x;
+      shared_t[0] = tm;
+      shared_t[1] = tl;
+    }
   }
-  const Softmax x = softmax_of<TEMP>(f, t, terms, lane);
-  // the teacher's softmax over its kept words
-  float tm = -__builtin_inff(), ts = 0.f;
-  for (int e = lane; e < n; e += 64) tm = fmaxf(tm, q[e]);
-  tm = wave_max(tm);
-  for (int e = lane; e < n; e += 64)
-    if (q[e] != -__builtin_inff()) ts += __builtin_amdgcn_exp2f((q[e] - tm) * kLog2e);
-  const float tl = __builtin_amdgcn_logf(wave_sum(ts)) * kLn2;
-  for (int e = tid; e < n; e += L)
-    p[e] = q[e] != -__builtin_inff() ? __builtin_amdgcn_exp2f(((q[e] - tm) - tl) * kLog2e) : 0.f;
   __syncthreads();
+  if constexpr (SPLIT) {
+    x = shared_x;
+    tm = shared_t[0];
+    tl = shared_t[1];
+  }
   if (wave == 0) {
     float kl = 0.f;
     for (int e = lane; e < n; e += 64)  // ln q - ln s, s = e^((z - m) / tau) / sum
@@ -727,6 +976,32 @@ int64_t head_loss_bwd_bytes(int64_t T, int64_t V, int64_t D) {
     if (e_ != hipSuccess) return e_;     \
   } while (0)
 
+// Softmax sums of up to kFewTokens tokens, without gather's copies
+constexpr int kFewTokens = 64;
+
+static int few_grid(int64_t V) {
+  const int64_t cus = current_cu_count(), n = (V + 15) / 16;
+  return (int)(n < cus ? n : cus);
+}
+
+template <bool F16>
+static hipError_t run_few(const HeadIn& in, const Of& of, const Layout& l, hipStream_t stream) {
+  if (in.K > 0 && in.T > kListTeach) {
+    hipLaunchKernelGGL(terms_kernel, dim3((unsigned)((in.T + 3) / 4)), dim3(256), 0, stream, in, of,
+                       l.rows.terms);
+    TM_RET(hipGetLastError());
+  }
+  const dim3 grid((unsigned)few_grid(in.V));
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, in, of, l.rows, l.part);
+    return hipGetLastError();
+  };
+  const bool temp = in.K > 0 && in.tau != 1.0f;
+  if (in.T <= 16) return temp ? go(few_kernel<F16, true, 1>) : go(few_kernel<F16, false, 1>);
+  if (in.T <= 32) return temp ? go(few_kernel<F16, true, 2>) : go(few_kernel<F16, false, 2>);
+  return temp ? go(few_kernel<F16, true, 4>) : go(few_kernel<F16, false, 4>);
+}
+
 // the rows, their list and their copies
 template <bool F16, bool BWD>
 static hipError_t gather(const HeadIn& in, const Of& of, const Layout& l, uint16_t* hs,
@@ -777,11 +1052,18 @@ hipError_t launch_head_loss(const HeadIn& in, const void* top, int top_type, flo
                             float* stats, void* workspace, hipStream_t stream) {
   const Layout l = forward_layout(in.T, in.V, in.D, workspace);
   const Of of{top, top_type, nullptr, nullptr, 0};
-  TM_RET(in.f16 ? (gather<true, false>(in, of, l, nullptr, stream))
-                : (gather<false, false>(in, of, l, nullptr, stream)));
-  TM_RET(launch_head_logits(in, l.ht, l.rows.count, l.part, stream));
-  const int tile = head_tile_tokens(in.T, in.V, true);
-  const Finish f{in, top, top_type, l.part, tile, head_logits_grid(in.T, in.V, tile), l.rows, loss, stats};
+  Finish f{in, top, top_type, l.part, kFewTokens, 0, 0, l.rows, loss, stats};
+  if (in.T <= kFewTokens) {
+    f.nv = f.grid = few_grid(in.V);
+    TM_RET(in.f16 ? run_few<true>(in, of, l, stream) : run_few<false>(in, of, l, stream));
+  } else {
+    f.tile = head_tile_tokens(in.T, in.V, true);
+    f.grid = head_logits_grid(in.T, in.V, f.tile);
+    f.nv = (in.V + 255) / 256;
+    TM_RET(in.f16 ? (gather<true, false>(in, of, l, nullptr, stream))
+                  : (gather<false, false>(in, of, l, nullptr, stream)));
+    TM_RET(launch_head_logits(in, l.ht, l.rows.count, l.part, stream));
+  }
   return in.f16 ? run_finish<true>(f, stream) : run_finish<false>(f, stream);
 }
 

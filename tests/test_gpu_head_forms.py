@@ -156,6 +156,28 @@ def test_pieces_and_parts(T, V, D, K, why):
     _check(c, *out, tokens=some(T), words=words)
 
 
+@pytest.mark.parametrize("T,V,D,K,tau", [
+    (1, 3, 8, 0, 1.0), (1, 5000, 4104, 2, 1.0),     # fewer words than waves; h in two parts
+    (16, 70000, 72, 0, 1.0), (17, 70001, 1000, 9, 2.0),  # two blocks of words a wave
+    (5, 300, 8200, 0, 1.0), (20, 515, 4160, 40, 0.5),    # three parts of h
+    (32, 16383, 64, 0, 1.0), (33, 4097, 2056, 0, 1.0),
+    (64, 131073, 1096, 3, 1.5), (64, 2000, 40, 0, 1.0),
+    (3, 400, 128, 1024, 1.0), (16, 900, 264, 65, 3.0)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_few_tokens(T, V, D, K, tau, dtype):
+    c = _inputs(T, V, D, dtype, K=K, seed=T + V + K, masked=0.2 if T > 2 else 0.0)
+    if K:
+        c.update(tau=tau)
+    if T > 2:
+        c["h"][c["y"] == IGNORE] = math.nan if K == 0 else 1.0  # not read
+    loss = _run(c, grad=False)
+    ok = torch.arange(T, device="cuda") if K else torch.nonzero(c["y"] != IGNORE)[:, 0]
+    want, tol, _, _ = _reference(c, ok)
+    off = (loss[ok].double() - want).abs()
+    assert bool((off <= tol).all()), float((off - tol).max())
+    assert K or bool((loss[c["y"] == IGNORE] == 0).all())
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_float32_weight_gradient_and_its_sum(dtype):
     c = _inputs(300, 515, 136, dtype, K=4, seed=1, masked=0.2)
