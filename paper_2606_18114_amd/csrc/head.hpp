@@ -37,7 +37,9 @@ inline __host__ __device__ float head_unit(float alpha, float tau) {
 }
 
 // A row of the backward pass: the exponents' offsets and the factors of the
-// two softmaxes, 16 bytes
+// two softmaxes, 16 bytes.  Where there is one softmax, lse_t holds the bits of the label's
+// word and c2 its dlogit; word -1: a teacher's words and the label are stored by a
+// launch of their own.
 struct HeadRow {
   float lse, lse_t, c1, c2;
 };

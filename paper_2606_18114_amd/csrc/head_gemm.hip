@@ -53,6 +53,8 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 
+typedef uint16_t __attribute__((may_alias)) any16;
+
 enum Mode { kStats, kDlogits, kDh, kDw };
 
 #pragma clang diagnostic push
@@ -413,13 +415,13 @@ __device__ __forceinline__ void store_rows(const uint8_t* mine, uint16_t* to, in
 // of 2^(log2e (z - maximum)) over the run's words, and the same at the temperature
 // where TEMP.  A workgroup walks many word tiles of one token tile, so
 // a step of the softmax costs no memory.
-// kDlogits: G[row][word - w0] in 16 bits.
+// kDlogits: G[row][word - w0] in 16 bits; w and words are those from w0 on.
 template <bool F16, Mode MODE, bool TEMP, int BB>
 __global__ __launch_bounds__(256) void head_logits_kernel(
     const uint16_t* __restrict__ ht, int64_t tp, const uint16_t* __restrict__ w, int D,
     const int* __restrict__ count, int words, float inv_tau,
     float* __restrict__ part, const HeadRow* __restrict__ rows, uint16_t* __restrict__ G,
-    int64_t ld) {
+    int64_t ld, int w0) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds<true>];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -592,6 +594,14 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
             *reinterpret_cast<u32x2*>(row + 16 * ((4 * a + q) ^ (l32 & 15))) =
                 u32x2{pack2<F16>(p[4 * q], p[4 * q + 1]), pack2<F16>(p[4 * q + 2], p[4 * q + 3])};
           __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (!TEMP) {  // the label's word
+          asm volatile("" ::: "memory");
+          const int c = __float_as_int(hr.lse_t) - w0 - v0;
+          if (half == 0 && c >= 0 && c < 128)
+            *reinterpret_cast<any16*>(mine + l32 * 256 + 16 * ((c >> 3) ^ (l32 & 15)) +
+                                      2 * (c & 7)) = (uint16_t)pack2<F16>(hr.c2, 0.f);
+          asm volatile("" ::: "memory");
         }
         store_rows(mine, G + (int64_t)(t0 + 32 * b) * ld + v0, ld, 32, 128);
       }
@@ -789,22 +799,23 @@ static int64_t grid_of(int64_t items) {
   return items < cus ? items : cus;
 }
 
-// Tokens of a tile of logits: 64 (the softmax sums only), 128 or 256.  A stage of the three
-// takes 0.52, 0.58 and 0.80 us a workgroup (the first two by their loads), so narrow tiles
-// are for few tokens (loss of 16 tokens of 50000 x 2048: 44 us, 60 with 256) and for few
-// words, where 256 would leave workgroups idle (300 tokens of 5000 words: 36 us, 51 with
-// 256).  300 tokens of 50000 take 118 us either way: two rounds of tiles.
+// Tokens of a tile of logits: 64 and 192 (the softmax sums only), 128 or 256.  A stage takes
+// 0.52 us a workgroup of 64, 0.58 of 128 (both by their loads), 0.68 of 192, 0.80 of 256.  So
+// narrow tiles are for few words, where 256 would leave workgroups idle (300 tokens of 5000 x
+// 2048: 36 us, 51 with 256), and where they waste less of the last tile (300 of 50000: 93 us,
+// 113 with 256; 800 of 50000: 178, 208).
 int head_tile_tokens(int64_t T, int64_t words, bool stats) {
   const int64_t P = current_cu_count(), nv = (words + kTM - 1) / kTM;
-  const double us[3] = {0.52, 0.58, 0.80};
+  const double us[4] = {0.52, 0.58, 0.68, 0.80};
   int best = 256;
   double least = 0;
-  for (int i = 2; i >= (stats ? 0 : 1); --i) {
-    const int64_t items = (T + (64 << i) - 1) / (64 << i) * nv;
-    const double cost = (double)((items + P - 1) / P) * us[i];
-    if (i == 2 || cost < least) {
+  for (int tile = 256; tile >= 64; tile -= 64) {
+    if (!stats && tile != 256 && tile != 128) continue;
+    const int64_t items = (T + tile - 1) / tile * nv;
+    const double cost = (double)((items + P - 1) / P) * us[tile / 64 - 1];
+    if (tile == 256 || cost < least) {
       least = cost;
-      best = 64 << i;
+      best = tile;
     }
   }
   return best;
@@ -828,10 +839,10 @@ static hipError_t run_logits(const HeadIn& in, const uint16_t* ht, const int* co
   const uint16_t* w = in.w + w0 * in.D;
   if (in.K > 0 && in.tau != 1.0f)
     hipLaunchKernelGGL((head_logits_kernel<F16, MODE, true, BB>), TM_HEAD_GRID(grid), ht,
-                       head_padded(in.T), w, in.D, count, (int)n, 1.0f / in.tau, part, rows, G, ld);
+                       head_padded(in.T), w, in.D, count, (int)n, 1.0f / in.tau, part, rows, G, ld, (int)w0);
   else
     hipLaunchKernelGGL((head_logits_kernel<F16, MODE, false, BB>), TM_HEAD_GRID(grid), ht,
-                       head_padded(in.T), w, in.D, count, (int)n, 1.0f, part, rows, G, ld);
+                       head_padded(in.T), w, in.D, count, (int)n, 1.0f, part, rows, G, ld, (int)w0);
   return hipGetLastError();
 }
 
@@ -842,6 +853,7 @@ hipError_t launch_head_logits(const HeadIn& in, const uint16_t* ht, const int* c
   run_logits<F16, kStats, BB>(in, ht, count, 0, in.V, part, nullptr, nullptr, 0, stream)
   if (tile == 64) return in.f16 ? TM_HEAD_LOGITS(true, 1) : TM_HEAD_LOGITS(false, 1);
   if (tile == 128) return in.f16 ? TM_HEAD_LOGITS(true, 2) : TM_HEAD_LOGITS(false, 2);
+  if (tile == 192) return in.f16 ? TM_HEAD_LOGITS(true, 3) : TM_HEAD_LOGITS(false, 3);
   return in.f16 ? TM_HEAD_LOGITS(true, 4) : TM_HEAD_LOGITS(false, 4);
 #undef TM_HEAD_LOGITS
 }

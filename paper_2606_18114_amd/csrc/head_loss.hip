@@ -163,11 +163,13 @@ __device__ __forceinline__ void put_row(const HeadIn& in, const Of& of, const Ro
     const int terms = (int)of.stats[kStatTerms * T + t];
     float c1 = terms & 1 ? (1.0f - in.alpha) / unit * m : 0.f;
     float c2 = terms & 2 ? in.alpha * in.tau / unit * m : 0.f;
+    float lse_t = of.stats[kStatLseT * T + t];
     if (in.tau == 1.0f) {  // one softmax
       c1 += c2;
-      c2 = 0.f;
+      lse_t = __int_as_float(in.K > 0 ? -1 : (int)id_at(in.targets, in.targets64, t));
+      c2 = of.stats[kStatLabel * T + t] * m;
     }
-    out.row[r] = HeadRow{of.stats[kStatLse * T + t], of.stats[kStatLseT * T + t], c1, c2};
+    out.row[r] = HeadRow{of.stats[kStatLse * T + t], lse_t, c1, c2};
   }
 }
 
@@ -811,7 +813,8 @@ __global__ __launch_bounds__(64 * WAVES) void teach_kernel(Finish f) {
   }
 }
 
-// The label's and the teacher's words of the piece, over the dense dlogits.
+// With a teacher: the label's and its words of the piece, over the dense dlogits.  (A label
+// alone is stored with its tile: a launch less, 5 us.)
 // Words that coincide carry the same value, so their order does not matter.
 template <bool F16>
 __global__ __launch_bounds__(256) void sparse_kernel(HeadIn in, const float* __restrict__ stats,
@@ -1079,9 +1082,11 @@ static hipError_t run_bwd(const HeadIn& in, const float* stats, const float* dlo
     const int64_t w0 = i * p.piece, n = in.V - w0 < p.piece ? in.V - w0 : p.piece;
     TM_RET(launch_head_dlogits(in, l.ht, l.rows.count, l.rows.row, w0, n, l.G, p.piece,
                                stream));
-    hipLaunchKernelGGL(sparse_kernel<F16>, dim3((unsigned)((in.T * (in.K + 1) + 255) / 256)),
-                       dim3(256), 0, stream, in, stats, dloss, l.rows, w0, n, l.G, p.piece);
-    TM_RET(hipGetLastError());
+    if (in.K > 0) {
+      hipLaunchKernelGGL(sparse_kernel<F16>, dim3((unsigned)((in.T * (in.K + 1) + 255) / 256)),
+                         dim3(256), 0, stream, in, stats, dloss, l.rows, w0, n, l.G, p.piece);
+      TM_RET(hipGetLastError());
+    }
     if (dh)
       TM_RET(launch_head_dh(in, l.rows.count, l.G, p.piece, w0, n, p.parts_h, p.per_h, i > 0,
                           l.part_h, stream));
