@@ -792,6 +792,136 @@ __global__ __launch_bounds__(256) void head_dw_sum_kernel(const float* __restric
   }
 }
 
+// dW of up to 64 tokens: it is written, and little else.  A workgroup has 256 columns d, whose h it
+// keeps in registers as matrix operands, and a run of words, 128 of G at a time through LDS; a wave
+// has 64 of the columns.  Rows of the product are columns d, in an order in which a lane's sixteen
+// and its other block's are neighbours, columns are words; 32 words x 64 columns at a time
+// pass through LDS, so that whole lines are stored.  Two workgroups a CU.
+// Bound: HBM's writes.
+template <bool F16, typename O, bool ACC>
+__global__ __launch_bounds__(256, 2) void head_dw_few_kernel(
+    const uint16_t* __restrict__ G, int64_t ld, const uint16_t* __restrict__ hs, int D,
+    const int* __restrict__ count, int words, int runs, const int* __restrict__ exp,
+    O* __restrict__ dw) {
+  constexpr int kWords = 128, kPitch = 2 * kWords;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[64 * 512 + 64 * kPitch];
+  uint8_t* const gt = lds + 64 * 512;  // G's tile; before it h's, then the waves' results
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int nd = (D + 255) / 256, id = (int)xcd_remap(blockIdx.x, gridDim.x);
+  const int d0 = id % nd * 256, run = id / nd;
+  const int eights = (words + 7) / 8;
+  const int v_beg = 8 * (int)((int64_t)run * eights / runs);
+  int v_end = 8 * (int)((int64_t)(run + 1) * eights / runs);
+  v_end = v_end < words ? v_end : words;
+  const int n = __builtin_amdgcn_readfirstlane(*count), steps = (n + 15) / 16;
+  const int e = *exp;
+
+  u32x4 next[4];
+  auto load = [&](int v0) {  // 64 rows of 128 words
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = 256 * j + tid, r = i >> 4, c = v0 + 8 * (i & 15);
+      next[j] = ld16(G + r * ld + (c < ld ? c : ld - 8));
+    }
+  };
+  load(v_beg);
+  // h's 64 x 256: column 64 k + 32 half + 16 x + 4 a + b lies at 64 k + 32 x + 8 a + 4 half + b
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int i = 256 * j + tid, r = i >> 5, c = 8 * (i & 31);
+    u32x4 v = {0, 0, 0, 0};
+    if (r < n && d0 + c < D) v = ld16(hs + (int64_t)r * D + d0 + c);
+    const int at = (c & ~63) + 32 * ((c >> 4) & 1) + 2 * (c & 8) + 4 * ((c >> 5) & 1);
+    *reinterpret_cast<u32x2*>(lds + off_across(r, at)) = u32x2{v.x, v.y};
+    *reinterpret_cast<u32x2*>(lds + off_across(r, at + 8)) = u32x2{v.z, v.w};
+  }
+  __syncthreads();
+  const int trow = 8 * half + ((lane & 15) >> 2);
+  const int tcol = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  auto across = [&](const uint8_t* at, int pitch) {
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * pitch));
+    const u32x2 l = __builtin_bit_cast(u32x2, lo), u = __builtin_bit_cast(u32x2, hi);
+    return u32x4{l.x, l.y, u.x, u.y};
+  };
+  auto off_g = [&](int r, int c) { return r * kPitch + 32 * ((c >> 4) ^ swz(r)) + 2 * (c & 15); };
+  u32x4 hf[4][2];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      hf[t][x] = across(lds + off_across(trow, 64 * wave + 32 * x + tcol) + 16 * t * 512, 512);
+
+  constexpr int kEl = 16 / sizeof(O), kPieces = 64 / kEl, kRows = 64 / kPieces;  // of a store
+  uint8_t* const mine = lds + wave * 8192;
+  const int sr = lane / kPieces, sp = lane % kPieces, sc = d0 + 64 * wave + kEl * sp;
+  for (int v0 = v_beg; v0 < v_end; v0 += kWords) {
+    __syncthreads();  // h's operands, or the tile before, have been read
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = 256 * j + tid;
+      st16(gt + off_g(i >> 4, 8 * (i & 15)), next[j]);
+    }
+    __syncthreads();
+    if (v0 + kWords < v_end) load(v0 + kWords);
+#pragma unroll 1
+    for (int b = 0; b < kWords / 32; ++b) {
+      const int left = v_end - v0 - 32 * b;
+      if (left <= 0) break;
+      f32x16 acc[2] = {};
+      const uint8_t* gp = gt + off_g(trow, 32 * b + tcol);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (t < steps) {
+          const u32x4 gf = across(gp + 16 * t * kPitch, kPitch);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) acc[x] = mfma<F16>(hf[t][x], gf, acc[x]);
+        }
+      // a lane: word l32, columns 32 half + 16 x + i of the wave's 64
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+#pragma unroll
+        for (int i = 0; i < 16; i += kEl) {
+          u32x4 o;
+          if constexpr (sizeof(O) == 4) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[k] = __float_as_uint(ldexpf(acc[x][i + k], e));
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              o[k] = pack2<F16>(ldexpf(acc[x][i + 2 * k], e), ldexpf(acc[x][i + 2 * k + 1], e));
+          }
+          const int piece = (32 * half + 16 * x + i) / kEl;
+          st16(mine + l32 * (64 * sizeof(O)) + 16 * (piece ^ (l32 & (kPieces - 1))), o);
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+      O* to = dw + (int64_t)(v0 + 32 * b + sr) * D + sc;
+      const int rows = sc < D ? left - sr : 0;
+      u32x4 old[32 / kRows];
+      if constexpr (ACC) {
+#pragma unroll
+        for (int k = 0; k < 32 / kRows; ++k)
+          if (kRows * k < rows) old[k] = ld16(to + (int64_t)kRows * k * D);
+      }
+#pragma unroll
+      for (int k = 0; k < 32 / kRows; ++k) {
+        const int r = kRows * k + sr;
+        u32x4 o = *reinterpret_cast<const u32x4*>(mine + r * (64 * sizeof(O)) +
+                                                  16 * (sp ^ (r & (kPieces - 1))));
+        if constexpr (ACC) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            o[q] = __float_as_uint(__uint_as_float(o[q]) + __uint_as_float(old[k][q]));
+        }
+        if (kRows * k < rows) st16(to + (int64_t)kRows * k * D, o);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+}
+
 #define TM_HEAD_GRID(GRID) dim3((unsigned)(GRID)), dim3(256), 0, stream
 
 static int64_t grid_of(int64_t items) {
@@ -896,7 +1026,15 @@ template <bool F16, typename O, bool ACC>
 static hipError_t run_dw(const HeadIn& in, const int* count, const uint16_t* G, int64_t ld,
                          const uint16_t* hs, int64_t n, int parts, int per, const int* exp, O* dw,
                          float* part_w, hipStream_t stream) {
-  const int64_t items = ((n + kTM - 1) / kTM) * ((in.D + kTN - 1) / kTN) * parts;
+  const int64_t nd = (in.D + kTN - 1) / kTN, items = ((n + kTM - 1) / kTM) * nd * parts;
+  // few tokens: 64 of 50000 x 2048 in 45 us, 66 by the tiles of products
+  if (in.T <= 64) {
+    const int64_t most = (n + 63) / 64, all = 2 * current_cu_count() / nd;
+    const int64_t runs = all < 1 ? 1 : all < most ? all : most;
+    hipLaunchKernelGGL((head_dw_few_kernel<F16, O, ACC>), TM_HEAD_GRID(runs * nd), G, ld, hs, in.D,
+                       count, (int)n, (int)runs, exp, dw);
+    return hipGetLastError();
+  }
   if (parts == 1) {
     hipLaunchKernelGGL((head_dw_kernel<F16, false, O, ACC>), TM_HEAD_GRID(grid_of(items)), G, ld,
                        hs, in.D, count, (int)n, 1, per, exp, dw);

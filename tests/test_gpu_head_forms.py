@@ -125,7 +125,12 @@ def _check(c, loss, dh, dw, tokens=None, words=None, dw0=None):
         t = torch.arange(lo, min(T, lo + 4096), device="cuda")
         _, _, dz, edz = _reference(c, t, words)
         h = c["h"][t].double()
-        h = torch.where((dz != 0).any(1, keepdim=True), h, 0.0)
+        # a token without a loss has no part; one whose gradient is exactly zero (a vocabulary of
+        # one word) has a loss, and its logits' roundings edz count
+        some = (c["y"][t] >= 0) & (c["y"][t] < V)
+        if c["ids"] is not None:
+            some |= ((c["ids"][t] >= 0) & (c["ids"][t] < V) & (c["top"][t] > -math.inf)).any(1)
+        h = torch.where((some & (c["dloss"][t] != 0))[:, None], h, 0.0)
         want += dz.t() @ h
         tol += (edz + T * F * dz.abs()).t() @ h.abs()
         if c["h"].dtype == torch.float16:  # what falls under the smallest number in h's copy
@@ -176,6 +181,20 @@ def test_few_tokens(T, V, D, K, tau, dtype):
     off = (loss[ok].double() - want).abs()
     assert bool((off <= tol).all()), float((off - tol).max())
     assert K or bool((loss[c["y"] == IGNORE] == 0).all())
+
+
+@pytest.mark.parametrize("T,V,D,K", [(1, 1, 8, 0), (1, 70, 264, 3), (7, 129, 64, 0),
+                                     (16, 1001, 520, 0), (17, 1000, 248, 5), (40, 127, 2056, 0),
+                                     (64, 5003, 768, 0), (64, 33001, 72, 2), (33, 263, 4104, 0)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_gradients_of_few_tokens(T, V, D, K, dtype):
+    c = _inputs(T, V, D, dtype, K=K, seed=T + V + D, masked=0.3 if T > 6 else 0.0)
+    c["dloss"] *= 4.0 ** torch.randint(-3, 4, (T,), device="cuda")
+    _check(c, *_run(c))
+    dw0 = torch.randn(V, D, device="cuda")
+    for kw in ({"dW": torch.full_like(dw0, math.nan)}, {"dW": dw0.clone(), "accumulate": True}):
+        loss, dh, dw = _run(c, **kw)
+        _check(c, loss, None, dw, dw0=dw0 if "accumulate" in kw else None)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
