@@ -376,14 +376,22 @@ __global__ __launch_bounds__(256) void few_kernel(HeadIn in, Of of, Rows rows,
   const int v_beg = (int)((int64_t)wv * V / waves), v_end = (int)((int64_t)(wv + 1) * V / waves);
   const int blocks = ((V + waves - 1) / waves + 16 * NB - 1) / (16 * NB);  // of every wave's run
   const int nit = (D + 63) / 64;
-  // A wave takes a chunk's columns from a place of its own on: rows are often a power of two
-  // apart, and waves in step would ask the same memory channels.
+  // A wave takes a chunk's columns from a place of its own on, and a workgroup the chunks, where
+  // 64 tokens make them short and all are whole: rows are often a power of two apart, and waves
+  // in step would ask the same memory channels (50000 x 2048, 16 tokens: 50 us, 59 in step; 64
+  // tokens: 60, 66 with the chunks in step).
   constexpr int C = kCols / 64;
-  const int last = (nit - 1) / C * C, c_last = nit - last;
+  const int chunks = (nit + C - 1) / C, last = (chunks - 1) * C, c_last = nit - last;
+  const int turn = NT == 4 && c_last == C ? blockIdx.x % chunks : 0;
   const int rot = (wv * 5) % C, rot_last = (wv * 5) % c_last;
+  auto chunk = [&](int i) {  // the first step of the i-th step's chunk
+    if constexpr (NT < 4) return i >= last ? last : i / C * C;
+    const int p = i / C + turn;
+    return (p >= chunks ? p - chunks : p) * C;
+  };
   auto step = [&](int i) {  // the i-th step's columns, in 64s
-    const int base = i >= last ? last : i / C * C, c = i >= last ? c_last : C;
-    const int k = i - base + (i >= last ? rot_last : rot);
+    const int base = chunk(i), c = base == last ? c_last : C;
+    const int k = i % C + (base == last ? rot_last : rot);
     return base + (k >= c ? k - c : k);
   };
   int words = 0;  // of the block that the loads are for
@@ -481,7 +489,7 @@ __global__ __launch_bounds__(256) void few_kernel(HeadIn in, Of of, Rows rows,
     for (int i0 = 0; i0 < nit; i0 += R) {
       if (i0 % C == 0 && (nit > C || blk == 0)) {
         __syncthreads();  // the columns before have been read
-        fill(i0);
+        fill(chunk(i0));
         __syncthreads();
       }
 #pragma unroll
