@@ -240,9 +240,8 @@ __global__ __launch_bounds__(1024) void rows_kernel(HeadIn in, Of of, int64_t pe
 //   columns d and of 256 rows r;
 //   backward, hs[r] = h[idx[r]] times 2^(e - largest e), what dW contracts (NULL: not wanted).
 // LIST (up to kListTokens tokens): every workgroup lists the rows by itself and the first one
-// writes the list, which saves a launch (16 tokens of 50000 words: 47 us, 50 with two); of up to kListTeach
-// tokens also what the teacher keeps.
-constexpr int kListTokens = 1024, kListTeach = 16;
+// writes the list, which saves a launch (3 us).
+constexpr int kListTokens = 1024;
 
 template <bool F16, bool BWD, bool LIST>
 __global__ __launch_bounds__(256) void gather_kernel(HeadIn in, Of of, Rows rows, int64_t tp,
@@ -251,31 +250,18 @@ __global__ __launch_bounds__(256) void gather_kernel(HeadIn in, Of of, Rows rows
   __shared__ uint16_t s[64][72];
   __shared__ int list[LIST ? kListTokens : 1];
   __shared__ int sums[4][4], maxs[4];
-  __shared__ uint8_t few[kListTeach];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int n, emax = 0;
   if constexpr (LIST) {
     const bool first = blockIdx.x == 0 && blockIdx.y == 0;
     const int T = (int)in.T;
-    const uint8_t* terms = rows.terms;
-    if (!BWD && in.K > 0 && T <= kListTeach) {
-      for (int t = wave; t < T; t += 4) {
-        const int v = terms_of(in, of, t, lane);
-        if (lane == 0) {
-          few[t] = (uint8_t)v;
-          if (first) rows.terms[t] = (uint8_t)v;
-        }
-      }
-      __syncthreads();
-      terms = few;
-    }
     bool yes[4];
     uint64_t mask[4];
     int e = -1000;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const int t = 256 * c + tid;
-      yes[c] = t < T && has_row<BWD>(in, of, terms, t);
+      yes[c] = t < T && has_row<BWD>(in, of, rows.terms, t);
       if constexpr (BWD)
         if (yes[c]) e = max(e, row_exp(in, of, t));
       mask[c] = __ballot(yes[c]);
@@ -352,13 +338,18 @@ __global__ __launch_bounds__(256) void gather_kernel(HeadIn in, Of of, Rows rows
   }
 }
 
+// (few_kernel) tokens whose kept words every workgroup looks up by itself, for a launch less
+constexpr int kListTeach = 16;
+
 // Softmax sums of up to 64 tokens, 16 NT: a read of W.  Every wave has a run of V / waves words to
 // itself, 64 at a time as four blocks of 16 x 16 x 32 matrix products with the tokens; W goes
 // from memory to registers (no other wave wants it), four steps of 64 columns ahead, 32 KiB a
 // wave, h from LDS, kCols columns at a time.  Every workgroup lists the rows by itself, the
 // first one writes the list.  part as the logits' kernel leaves it, one tile of tokens and a tile
 // of words a workgroup.
-// Bound: HBM.
+// Bound: HBM (50000 x 2048, W in memory, the call: 1 token 46 us, 16 50, 64 60; by tiles of 64
+// tokens 62, 64 and 66; 5000 words: 28, 47 by tiles).  R = 8 and so twice the loads in flight:
+// 53 us; R = 2: 49, but 32 for 5000 words.
 template <bool F16, bool TEMP, int NT>
 __global__ __launch_bounds__(256) void few_kernel(HeadIn in, Of of, Rows rows,
                                                   float* __restrict__ part) {
@@ -1018,7 +1009,7 @@ template <bool F16, bool BWD>
 static hipError_t gather(const HeadIn& in, const Of& of, const Layout& l, uint16_t* hs,
                          hipStream_t stream) {
   const bool list = in.T <= kListTokens;
-  if (!BWD && in.K > 0 && !(list && in.T <= kListTeach)) {
+  if (!BWD && in.K > 0) {
     hipLaunchKernelGGL(terms_kernel, dim3((unsigned)((in.T + 3) / 4)), dim3(256), 0, stream, in, of,
                        l.rows.terms);
     TM_RET(hipGetLastError());
