@@ -151,14 +151,25 @@ def _check(c, loss, dh, dw, tokens=None, words=None, dw0=None):
     (70001, 9001, 64, 0, "pieces of 4096 words"),
     (256, 1100000, 64, 0, "two pieces, dh cut along the words, a last piece of fewer parts"),
     (5000, 130, 512, 2, "dW cut along the tokens"),
-    (65, 3000, 128, 0, "tiles of 128 tokens"), (129, 3000, 128, 5, "tiles of 256 tokens"),
-    (64, 70000, 136, 1, "tiles of 64 tokens")])
+    (65, 3000, 128, 0, "tiles of 64 tokens"), (129, 3000, 128, 5, "and one token more"),
+    (120, 70000, 136, 1, "tiles of 128 tokens"), (64, 70000, 136, 1, "few tokens")])
 def test_pieces_and_parts(T, V, D, K, why):
     c = _inputs(T, V, D, K=K, seed=T + V, masked=0.1)
     out = _run(c)
     some = lambda n: sorted({0, 1, n // 2, n - 2, n - 1, *range(0, n, max(1, n // 61))})  # noqa: E731
     words = some(V) + [v for v in (4095, 4096, 8191, 8192, 16383, 16384) if v < V]
     _check(c, *out, tokens=some(T), words=words)
+
+
+@pytest.mark.parametrize("T,V,K,tau", [(190, 33000, 2, 1.5), (300, 50000, 0, 1.0),
+                                       (384, 50000, 1, 1.0)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_tiles_of_192_tokens(T, V, K, tau, dtype):
+    c = _inputs(T, V, 72, dtype, K=K, seed=T, masked=0.1)
+    c["tau"] = tau
+    want, tol, _, _ = _reference(c, torch.arange(T, device="cuda"))
+    off = (_run(c, grad=False).double() - want).abs()
+    assert bool((off <= tol).all()), float((off - tol).max())
 
 
 @pytest.mark.parametrize("T,V,D,K,tau", [
