@@ -665,8 +665,8 @@ __device__ __forceinline__ void write_tile(T* base, int64_t pitch, int rows_left
 template <bool F16, bool ADD>
 __global__ __launch_bounds__(256) void head_dh_kernel(
     const uint16_t* __restrict__ G, int64_t ld, const uint16_t* __restrict__ w, int D,
-    const int* __restrict__ count, int64_t T, int words, int parts, int per,
-    float* __restrict__ part) {
+    const int* __restrict__ count, int64_t T, int words, HeadCut plan, int all,
+    float* __restrict__ part, int* __restrict__ used) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds<true>];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -675,6 +675,9 @@ __global__ __launch_bounds__(256) void head_dh_kernel(
   const int nt = (n + kTM - 1) / kTM, nd = (D + kTN - 1) / kTN;
   const int64_t tiles = (int64_t)nt * nd, P = gridDim.x;
   const int64_t wg = xcd_remap(blockIdx.x, gridDim.x);
+  const HeadCut cut = head_cut(plan, all, T, n, D, (int)P);
+  const int parts = cut.parts, per = cut.per;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *used = parts;
   const int nst = stages(words);
   for (int64_t item = wg; item < tiles * parts; item += P) {
     const int s = (int)(item / tiles), tile = (int)(item % tiles);
@@ -692,7 +695,7 @@ __global__ __launch_bounds__(256) void head_dh_kernel(
       product<F16, true, 4>(lds, l, acc);
     }
     const int r0 = m0 + wy * 128, c0 = d0 + wx * 128;
-    float* out = part + ((int64_t)s * T + r0) * D + c0;
+    float* out = part + ((int64_t)s * n + r0) * D + c0;
     write_tile<ADD>(out, D, n - r0, D - c0, acc, [](float v, float old) { return v + old; });
   }
 }
@@ -1000,13 +1003,12 @@ hipError_t launch_head_dlogits(const HeadIn& in, const uint16_t* ht, const int* 
 }
 
 hipError_t launch_head_dh(const HeadIn& in, const int* count, const uint16_t* G, int64_t ld,
-                          int64_t w0, int64_t n, int parts, int per, bool add, float* part_h,
-                          hipStream_t stream) {
-  const int64_t items = ((in.T + kTM - 1) / kTM) * ((in.D + kTN - 1) / kTN) * parts;
+                          int64_t w0, int64_t n, HeadCut plan, int nst, bool add, float* part_h,
+                          int* used, hipStream_t stream) {
   const uint16_t* w = in.w + w0 * in.D;
 #define TM_HEAD_DH(F16, ADD)                                                                    \
-  hipLaunchKernelGGL((head_dh_kernel<F16, ADD>), TM_HEAD_GRID(grid_of(items)), G, ld, w, in.D, \
-                     count, in.T, (int)n, parts, per, part_h)
+  hipLaunchKernelGGL((head_dh_kernel<F16, ADD>), TM_HEAD_GRID(current_cu_count()), G, ld, w, in.D, \
+                     count, in.T, (int)n, plan, nst, part_h, used)
   if (in.f16) {
     if (add)
       TM_HEAD_DH(true, true);

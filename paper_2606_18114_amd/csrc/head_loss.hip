@@ -96,7 +96,8 @@ struct Rows {
   int* count;  // [1]
   int* idx;    // [T]: the token of a row
   int* pos;    // [T]: the row of a token, or -1
-  int* exps;   // [2]: the largest exponent, and that without the dlogits' shift (backward)
+  // backward: the largest exponent, that without the dlogits' shift, the parts of dh
+  int* exps;
   HeadRow* row;  // [T] (backward)
   uint8_t* terms;  // [T]: 1 label, 2 teacher (forward)
 };
@@ -841,7 +842,7 @@ __global__ __launch_bounds__(256) void sparse_kernel(HeadIn in, const float* __r
 template <bool F16>
 __global__ __launch_bounds__(64) void dh_out_kernel(HeadIn in, const float* __restrict__ dloss,
                                                     Rows rows, const float* __restrict__ part,
-                                                    int parts, uint16_t* __restrict__ dh) {
+                                                    uint16_t* __restrict__ dh) {
   const int64_t t = blockIdx.x;
   const int d = (blockIdx.y * 64 + threadIdx.x) * 8;
   if (d >= in.D) return;
@@ -851,11 +852,12 @@ __global__ __launch_bounds__(64) void dh_out_kernel(HeadIn in, const float* __re
   if (r >= 0) {
     f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
     const float* p = part + (int64_t)r * in.D + d;
+    const int n = *rows.count, parts = rows.exps[2];
 #pragma unroll 8
     for (int s = 0; s < parts; ++s) {
       a += *reinterpret_cast<const f32x4*>(p);
       b += *reinterpret_cast<const f32x4*>(p + 4);
-      p += in.T * in.D;
+      p += (int64_t)n * in.D;
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -908,6 +910,7 @@ HeadPlan head_plan(int64_t T, int64_t V, int64_t D) {
   p.pieces = (V + p.piece - 1) / p.piece;
   const int64_t nd = (D + 255) / 256, nt = (T + 255) / 256, nv = p.piece / 256;
   const int64_t words = p.pieces == 1 ? V : p.piece;
+  p.nst_h = (int)((words + 127) / 128 * 4);
   cut(nt * nd, (words + 31) / 32, P, 4, &p.parts_h, &p.per_h);
   cut(nv * nd, (T + 31) / 32, P, 4, &p.parts_w, &p.per_w);
   const int64_t rest = V - (p.pieces - 1) * p.piece;
@@ -947,7 +950,7 @@ Layout backward_layout(int64_t T, int64_t V, int64_t D, const HeadPlan& p, void*
   Layout l{};
   uint8_t* b = static_cast<uint8_t*>(ws);
   take(&l.rows.count, b, &l.bytes, 4);
-  take(&l.rows.exps, b, &l.bytes, 8);
+  take(&l.rows.exps, b, &l.bytes, 12);
   take(&l.rows.idx, b, &l.bytes, 4 * T);
   take(&l.rows.pos, b, &l.bytes, 4 * T);
   take(&l.rows.row, b, &l.bytes, (int64_t)sizeof(HeadRow) * T);
@@ -1087,8 +1090,8 @@ static hipError_t run_bwd(const HeadIn& in, const float* stats, const float* dlo
       TM_RET(hipGetLastError());
     }
     if (dh)
-      TM_RET(launch_head_dh(in, l.rows.count, l.G, p.piece, w0, n, p.parts_h, p.per_h, i > 0,
-                          l.part_h, stream));
+      TM_RET(launch_head_dh(in, l.rows.count, l.G, p.piece, w0, n, HeadCut{p.parts_h, p.per_h},
+                            p.nst_h, i > 0, l.part_h, l.rows.exps + 2, stream));
     const bool last = i == p.pieces - 1;
     if (dw)
       TM_RET(launch_head_dw(in, l.rows.count, l.G, p.piece, l.hs, w0, n, last ? p.last_w : p.parts_w,
@@ -1096,7 +1099,7 @@ static hipError_t run_bwd(const HeadIn& in, const float* stats, const float* dlo
   }
   if (dh)
     hipLaunchKernelGGL(dh_out_kernel<F16>, dim3((unsigned)in.T, (unsigned)((in.D + 511) / 512)),
-                       dim3(64), 0, stream, in, dloss, l.rows, l.part_h, p.parts_h, dh);
+                       dim3(64), 0, stream, in, dloss, l.rows, l.part_h, dh);
   return hipGetLastError();
 }
 

@@ -161,6 +161,21 @@ def test_pieces_and_parts(T, V, D, K, why):
     _check(c, *out, tokens=some(T), words=words)
 
 
+@pytest.mark.parametrize("T,V,D,K,masked", [
+    (3001, 5003, 264, 0, 0.6), (1500, 9000, 768, 2, 0.9), (5000, 1000, 72, 0, 0.999),
+    (70001, 9001, 64, 0, 0.9), (17000, 17000, 520, 0, 0.97)])  # (the last two: several pieces)
+def test_many_tokens_without_a_loss(T, V, D, K, masked):
+    """dh's contraction is cut into more parts than for all tokens."""
+    c = _inputs(T, V, D, K=K, seed=T + D, masked=masked)
+    if K:
+        c["ids"][c["y"] == IGNORE] = -1
+    c["h"][c["y"] == IGNORE] = math.nan
+    out = _run(c)
+    some = torch.nonzero(c["y"] != IGNORE)[:, 0].tolist()
+    _check(c, *out[:2], None, tokens=some[::max(1, len(some) // 97)] + some[-1:])
+    assert bool((out[1][c["y"] == IGNORE] == 0).all())
+
+
 @pytest.mark.parametrize("T,V,K,tau", [(190, 33000, 2, 1.5), (300, 50000, 0, 1.0),
                                        (384, 50000, 1, 1.0)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
