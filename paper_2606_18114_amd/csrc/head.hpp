@@ -103,16 +103,17 @@ int head_tile_tokens(int64_t T, int64_t words, bool stats);       // tokens of a
 int head_logits_grid(int64_t T, int64_t words, int tile);         // workgroups
 hipError_t launch_head_logits(const HeadIn& in, const uint16_t* ht, const int* count, float* part,
                               hipStream_t stream);
-// dlogits of words w0 .. w0 + n - 1 to G [rows rounded up to 256, ld], ld >= n rounded up to
+// dlogits over *mantissa (a float's bits) of words w0 .. w0 + n - 1 to G [rows rounded up to 256, ld], ld >= n rounded up to
 // 256, with zeros past the rows and words
 hipError_t launch_head_dlogits(const HeadIn& in, const uint16_t* ht, const int* count,
-                               const HeadRow* rows, int64_t w0, int64_t n, uint16_t* G, int64_t ld,
+                               const HeadRow* rows, const int* mantissa, int64_t w0, int64_t n,
+                               uint16_t* G, int64_t ld,
                                hipStream_t stream);
 // part_h[s][row][D] (+)= the s-th part of G . W[w0 ..], cut by head_cut; *used: the parts
 hipError_t launch_head_dh(const HeadIn& in, const int* count, const uint16_t* G, int64_t ld,
                           int64_t w0, int64_t n, HeadCut plan, int nst, bool add, float* part_h,
                           int* used, hipStream_t stream);
-// dW[w0 ..] (+)= 2^(*exp) G^T . hs, whole, or into part_w[s][n][D] and from there
+// dW[w0 ..] (+)= 2^exp[0] (float at exp[2]) G^T . hs, whole, or into part_w[s][n][D] and from there
 hipError_t launch_head_dw(const HeadIn& in, const int* count, const uint16_t* G, int64_t ld,
                           const uint16_t* hs, int64_t w0, int64_t n, int parts, int per,
                           const int* exp, void* dw, int dw_type, bool accumulate, float* part_w,

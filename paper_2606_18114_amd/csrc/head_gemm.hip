@@ -421,7 +421,7 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
     const uint16_t* __restrict__ ht, int64_t tp, const uint16_t* __restrict__ w, int D,
     const int* __restrict__ count, int words, float inv_tau,
     float* __restrict__ part, const HeadRow* __restrict__ rows, uint16_t* __restrict__ G,
-    int64_t ld, int w0) {
+    int64_t ld, int w0, const int* __restrict__ mantissa) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds<true>];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -436,6 +436,7 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
   const int items = (int)(run_begin(wg + 1, N, P) - i0);
   const int nst = stages(D);
   const float k1 = kLog2e, k2 = kLog2e * inv_tau;
+  const float unit = MODE == kDlogits ? 1.0f / __int_as_float(*mantissa) : 0.f;
 
   float mx[BB], sm[BB], st[BB];  // the running maximum, its sum, the sum at the temperature
   auto reset = [&]() {
@@ -564,7 +565,9 @@ __global__ __launch_bounds__(256) void head_logits_kernel(
       for (int b = 0; b < BB; ++b) {
         const int r = t0 + 32 * b + l32;
         // rows and words past the last are zeros, for dW's and dh's contractions
-        const HeadRow hr = r < n ? rows[r] : HeadRow{0.f, 0.f, 0.f, 0.f};
+        HeadRow hr = r < n ? rows[r] : HeadRow{0.f, 0.f, 0.f, 0.f};
+        hr.c1 *= unit;
+        hr.c2 *= unit;
         const int left = v_left - 4 * half;
         uint8_t* row = mine + l32 * 256 + 8 * half;
 #pragma unroll
@@ -701,7 +704,7 @@ __global__ __launch_bounds__(256) void head_dh_kernel(
 }
 
 // dW: G (words) and hs (columns), both across the tokens.  PARTS: to part[s][word][D],
-// unscaled; else to dW's rows, times 2^(*exp).  Float32: A = G, a lane has a column and
+// unscaled; else to dW's rows, times 2^exp[0] (float at exp[2]).  Float32: A = G, a lane has a column and
 // stores 128 bytes of a row with its neighbours.  16 bits: A = hs, a lane has a word and four
 // columns in a row, which pass through LDS as the dlogits do (with A = G, 2 bytes a lane and
 // LDS write: 64 tokens, 50000 words 82 us, 65 so).
@@ -720,7 +723,8 @@ __global__ __launch_bounds__(256) void head_dw_kernel(
   const int64_t wg = xcd_remap(blockIdx.x, gridDim.x);
   const int nst = stages(n);
   constexpr bool SWAP = sizeof(O) == 2;
-  const int e = PARTS ? 0 : __builtin_amdgcn_readfirstlane(*exp);
+  const int e = PARTS ? 0 : __builtin_amdgcn_readfirstlane(exp[0]);
+  const float mant = PARTS ? 1.0f : __int_as_float(__builtin_amdgcn_readfirstlane(exp[2]));
   for (int64_t item = wg; item < tiles * parts; item += P) {
     const int s = (int)(item / tiles), tile = (int)(item % tiles);
     const int m0 = tile / nd * kTM, d0 = tile % nd * kTN;
@@ -751,7 +755,7 @@ __global__ __launch_bounds__(256) void head_dw_kernel(
         for (int a = 0; a < 4; ++a) {
           f32x16 v = acc_block(acc[a][b]);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = ldexpf(v[i], e);
+          for (int i = 0; i < 16; ++i) v[i] = ldexpf(mant * v[i], e);
 #pragma unroll
           for (int q = 0; q < 4; ++q)
             *reinterpret_cast<u32x2*>(row + 16 * ((4 * a + q) ^ (l32 & 15))) =
@@ -766,15 +770,15 @@ __global__ __launch_bounds__(256) void head_dw_kernel(
         if constexpr (PARTS)
           return v;
         else if constexpr (ACC)
-          return old + ldexpf(v, e);
+          return old + ldexpf(mant * v, e);
         else
-          return ldexpf(v, e);
+          return ldexpf(mant * v, e);
       });
     }
   }
 }
 
-// dW (+)= 2^(*exp) times the sum of the parts, in their order; n elements, a multiple of 8
+// dW (+)= 2^exp[0] (float at exp[2]) times the sum of the parts, in their order; n elements, a multiple of 8
 template <typename O, bool ACC>
 __global__ __launch_bounds__(256) void head_dw_sum_kernel(const float* __restrict__ part,
                                                           int64_t n, int parts,
@@ -784,10 +788,11 @@ __global__ __launch_bounds__(256) void head_dw_sum_kernel(const float* __restric
   if (i >= n) return;
   f32x4 v = *reinterpret_cast<const f32x4*>(part + i);
   for (int s = 1; s < parts; ++s) v += *reinterpret_cast<const f32x4*>(part + s * n + i);
-  const int e = *exp;
+  const int e = exp[0];
+  const float mant = __int_as_float(exp[2]);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float x = ldexpf(v[j], e);
+    const float x = ldexpf(mant * v[j], e);
     if constexpr (ACC)
       dw[i + j] += x;
     else
@@ -818,7 +823,8 @@ __global__ __launch_bounds__(256, 2) void head_dw_few_kernel(
   int v_end = 8 * (int)((int64_t)(run + 1) * eights / runs);
   v_end = v_end < words ? v_end : words;
   const int n = __builtin_amdgcn_readfirstlane(*count), steps = (n + 15) / 16;
-  const int e = *exp;
+  const int e = exp[0];
+  const float mant = __int_as_float(exp[2]);
 
   u32x4 next[4];
   auto load = [&](int v0) {  // 64 rows of 128 words
@@ -889,11 +895,12 @@ __global__ __launch_bounds__(256, 2) void head_dw_few_kernel(
           u32x4 o;
           if constexpr (sizeof(O) == 4) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) o[k] = __float_as_uint(ldexpf(acc[x][i + k], e));
+            for (int k = 0; k < 4; ++k) o[k] = __float_as_uint(ldexpf(mant * acc[x][i + k], e));
           } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              o[k] = pack2<F16>(ldexpf(acc[x][i + 2 * k], e), ldexpf(acc[x][i + 2 * k + 1], e));
+              o[k] = pack2<F16>(ldexpf(mant * acc[x][i + 2 * k], e),
+                                ldexpf(mant * acc[x][i + 2 * k + 1], e));
           }
           const int piece = (32 * half + 16 * x + i) / kEl;
           st16(mine + l32 * (64 * sizeof(O)) + 16 * (piece ^ (l32 & (kPieces - 1))), o);
@@ -965,17 +972,19 @@ int64_t head_part_floats(int64_t T, int64_t words) {
 
 template <bool F16, Mode MODE, int BB>
 static hipError_t run_logits(const HeadIn& in, const uint16_t* ht, const int* count, int64_t w0,
-                             int64_t n, float* part, const HeadRow* rows, uint16_t* G, int64_t ld,
-                             hipStream_t stream) {
+                             int64_t n, float* part, const HeadRow* rows, const int* mantissa,
+                             uint16_t* G, int64_t ld, hipStream_t stream) {
   const int64_t T = MODE == kStats ? in.T : (in.T + 127) / 128 * 128;
   const int grid = head_logits_grid(T, n, 64 * BB);
   const uint16_t* w = in.w + w0 * in.D;
   if (in.K > 0 && in.tau != 1.0f)
     hipLaunchKernelGGL((head_logits_kernel<F16, MODE, true, BB>), TM_HEAD_GRID(grid), ht,
-                       head_padded(in.T), w, in.D, count, (int)n, 1.0f / in.tau, part, rows, G, ld, (int)w0);
+                       head_padded(in.T), w, in.D, count, (int)n, 1.0f / in.tau, part, rows, G, ld,
+                       (int)w0, mantissa);
   else
     hipLaunchKernelGGL((head_logits_kernel<F16, MODE, false, BB>), TM_HEAD_GRID(grid), ht,
-                       head_padded(in.T), w, in.D, count, (int)n, 1.0f, part, rows, G, ld, (int)w0);
+                       head_padded(in.T), w, in.D, count, (int)n, 1.0f, part, rows, G, ld, (int)w0,
+                       mantissa);
   return hipGetLastError();
 }
 
@@ -983,7 +992,7 @@ hipError_t launch_head_logits(const HeadIn& in, const uint16_t* ht, const int* c
                               hipStream_t stream) {
   const int tile = head_tile_tokens(in.T, in.V, true);
 #define TM_HEAD_LOGITS(F16, BB) \
-  run_logits<F16, kStats, BB>(in, ht, count, 0, in.V, part, nullptr, nullptr, 0, stream)
+  run_logits<F16, kStats, BB>(in, ht, count, 0, in.V, part, nullptr, nullptr, nullptr, 0, stream)
   if (tile == 64) return in.f16 ? TM_HEAD_LOGITS(true, 1) : TM_HEAD_LOGITS(false, 1);
   if (tile == 128) return in.f16 ? TM_HEAD_LOGITS(true, 2) : TM_HEAD_LOGITS(false, 2);
   if (tile == 192) return in.f16 ? TM_HEAD_LOGITS(true, 3) : TM_HEAD_LOGITS(false, 3);
@@ -992,10 +1001,10 @@ hipError_t launch_head_logits(const HeadIn& in, const uint16_t* ht, const int* c
 }
 
 hipError_t launch_head_dlogits(const HeadIn& in, const uint16_t* ht, const int* count,
-                               const HeadRow* rows, int64_t w0, int64_t n, uint16_t* G, int64_t ld,
-                               hipStream_t stream) {
+                               const HeadRow* rows, const int* mantissa, int64_t w0, int64_t n,
+                               uint16_t* G, int64_t ld, hipStream_t stream) {
 #define TM_HEAD_DLOGITS(F16, BB) \
-  run_logits<F16, kDlogits, BB>(in, ht, count, w0, n, nullptr, rows, G, ld, stream)
+  run_logits<F16, kDlogits, BB>(in, ht, count, w0, n, nullptr, rows, mantissa, G, ld, stream)
   if (head_tile_tokens(in.T, n, false) == 128)
     return in.f16 ? TM_HEAD_DLOGITS(true, 2) : TM_HEAD_DLOGITS(false, 2);
   return in.f16 ? TM_HEAD_DLOGITS(true, 4) : TM_HEAD_DLOGITS(false, 4);

@@ -14,11 +14,12 @@
 // store over the dense part, whatever words coincide.
 //
 // Backward, per piece of the vocabulary: dlogits (dense), the sparse stores, dh and
-// dW.  A row's gradient is g = m 2^e, 1 <= m < 2; the dlogits hold m times the unit
-// gradient (16 bits, rounded once: by 2^-8 of each in bfloat16, 2^-11 in float16), h is
-// copied times 2^(e - largest e) (exact but for what falls under the type's
-// smallest number), and dh and dW are multiplied by powers of two at the end: the
-// roundings do not depend on how the loss is scaled.
+// dW.  A row's gradient is g = m 2^e, 1 <= m < 2, that of the largest M 2^E; the dlogits hold
+// m / M times the unit gradient (16 bits, rounded once: by 2^-8 of each in bfloat16, 2^-11 in
+// float16), h is copied times 2^(e - E) (exact but for what falls under the type's
+// smallest number), and dh and dW are multiplied by M and powers of two at the end: the
+// roundings do not depend on how the loss is scaled, and where all gradients are equal (a mean)
+// a label's dlogit, close to -1, is close to exact.
 #include "common.hpp"
 #include "head.hpp"
 #include "launchers.hpp"
@@ -96,7 +97,8 @@ struct Rows {
   int* count;  // [1]
   int* idx;    // [T]: the token of a row
   int* pos;    // [T]: the row of a token, or -1
-  // backward: the largest exponent, that without the dlogits' shift, the parts of dh
+  // backward: the largest gradient's exponent, that without the dlogits' shift, the parts of dh,
+  // the bits of the largest gradient's mantissa
   int* exps;
   HeadRow* row;  // [T] (backward)
   uint8_t* terms;  // [T]: 1 label, 2 teacher (forward)
@@ -146,10 +148,10 @@ __device__ __forceinline__ bool has_row(const HeadIn& in, const Of& of, const ui
                     : in_vocabulary(in, id_at(in.targets, in.targets64, t));
 }
 
-// exponent of token t's gradient, -1000 where it has none
-__device__ __forceinline__ int row_exp(const HeadIn& in, const Of& of, int64_t t) {
-  const float g = of.dloss[t] * head_unit(in.alpha, in.tau);
-  return fabsf(g) < __builtin_inff() && g != 0.f ? ilogbf(g) : -1000;
+// token t's gradient's size as bits (their order is the floats'), 0 where it has none
+__device__ __forceinline__ int row_size(const HeadIn& in, const Of& of, int64_t t) {
+  const float g = fabsf(of.dloss[t] * head_unit(in.alpha, in.tau));
+  return g < __builtin_inff() ? __float_as_int(g) : 0;
 }
 
 // token t's row r
@@ -174,9 +176,15 @@ __device__ __forceinline__ void put_row(const HeadIn& in, const Of& of, const Ro
   }
 }
 
-__device__ __forceinline__ void put_exps(const Of& of, const Rows& out, int e) {
-  out.exps[0] = e == -1000 ? 0 : e;
-  out.exps[1] = out.exps[0] - of.shift;
+// size: the largest of row_size
+__device__ __forceinline__ int exp_of_size(int size) {
+  return size == 0 ? 0 : ilogbf(__int_as_float(size));
+}
+__device__ __forceinline__ void put_exps(const Of& of, const Rows& out, int size) {
+  const int e = exp_of_size(size);
+  out.exps[0] = e;
+  out.exps[1] = e - of.shift;
+  out.exps[3] = __float_as_int(size == 0 ? 1.0f : ldexpf(__int_as_float(size), -e));
 }
 
 // Lists the rows in the tokens' order, where tokens are many.  A workgroup has `per` tokens (a
@@ -188,14 +196,14 @@ __global__ __launch_bounds__(1024) void rows_kernel(HeadIn in, Of of, int64_t pe
   __shared__ int maxs[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t T = in.T, t0 = blockIdx.x * per, t1 = t0 + per < T ? t0 + per : T;
-  int n = 0, e = -1000;
+  int n = 0, e = 0;
   // the first workgroup looks at all gradients for the largest
 #pragma unroll 4
   for (int64_t t = tid; t < (BWD && blockIdx.x == 0 ? T : t0); t += 1024) {
     const bool yes = has_row<BWD>(in, of, out.terms, t);
     if (t < t0) n += yes;
     if constexpr (BWD)
-      if (yes) e = max(e, row_exp(in, of, t));
+      if (yes) e = max(e, row_size(in, of, t));
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
@@ -258,13 +266,13 @@ __global__ __launch_bounds__(256) void gather_kernel(HeadIn in, Of of, Rows rows
     const int T = (int)in.T;
     bool yes[4];
     uint64_t mask[4];
-    int e = -1000;
+    int e = 0;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const int t = 256 * c + tid;
       yes[c] = t < T && has_row<BWD>(in, of, rows.terms, t);
       if constexpr (BWD)
-        if (yes[c]) e = max(e, row_exp(in, of, t));
+        if (yes[c]) e = max(e, row_size(in, of, t));
       mask[c] = __ballot(yes[c]);
       if (lane == 0) sums[c][wave] = __popcll(mask[c]);
     }
@@ -292,7 +300,7 @@ __global__ __launch_bounds__(256) void gather_kernel(HeadIn in, Of of, Rows rows
     }
     if constexpr (BWD) {
       e = max(max(maxs[0], maxs[1]), max(maxs[2], maxs[3]));
-      emax = e == -1000 ? 0 : e;
+      emax = exp_of_size(e);
       if (first && tid == 0) put_exps(of, rows, e);
     }
     if (first && tid == 0) *rows.count = n;
@@ -834,7 +842,8 @@ __global__ __launch_bounds__(256) void sparse_kernel(HeadIn in, const float* __r
   if (v < 0 || v >= n) return;
   const float g = dloss[t] * head_unit(in.alpha, in.tau);
   const float x = stats[e == 0 ? kStatLabel * in.T + t : kStatPlanes * in.T + t * in.K + e - 1];
-  G[r * ld + v] = narrow<F16>(x * ldexpf(g, kHeadShift<F16> - exp_of(g)));
+  const float m = ldexpf(g, kHeadShift<F16> - exp_of(g)) / __int_as_float(rows.exps[3]);
+  G[r * ld + v] = narrow<F16>(x * m);
 }
 
 // dh[t] = 2^(e - shift) times the sum of the row's parts; zeros for a token without a row.
@@ -852,6 +861,7 @@ __global__ __launch_bounds__(64) void dh_out_kernel(HeadIn in, const float* __re
   if (r >= 0) {
     f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
     const float* p = part + (int64_t)r * in.D + d;
+    const float m = __int_as_float(rows.exps[3]);
     const int n = *rows.count, parts = rows.exps[2];
 #pragma unroll 8
     for (int s = 0; s < parts; ++s) {
@@ -861,10 +871,10 @@ __global__ __launch_bounds__(64) void dh_out_kernel(HeadIn in, const float* __re
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      o[i] = (uint32_t)narrow<F16>(ldexpf(a[2 * i], e)) |
-             (uint32_t)narrow<F16>(ldexpf(a[2 * i + 1], e)) << 16;
-      o[2 + i] = (uint32_t)narrow<F16>(ldexpf(b[2 * i], e)) |
-                 (uint32_t)narrow<F16>(ldexpf(b[2 * i + 1], e)) << 16;
+      o[i] = (uint32_t)narrow<F16>(ldexpf(m * a[2 * i], e)) |
+             (uint32_t)narrow<F16>(ldexpf(m * a[2 * i + 1], e)) << 16;
+      o[2 + i] = (uint32_t)narrow<F16>(ldexpf(m * b[2 * i], e)) |
+                 (uint32_t)narrow<F16>(ldexpf(m * b[2 * i + 1], e)) << 16;
     }
   }
   st16(dh + t * in.D + d, o);
@@ -950,7 +960,7 @@ Layout backward_layout(int64_t T, int64_t V, int64_t D, const HeadPlan& p, void*
   Layout l{};
   uint8_t* b = static_cast<uint8_t*>(ws);
   take(&l.rows.count, b, &l.bytes, 4);
-  take(&l.rows.exps, b, &l.bytes, 12);
+  take(&l.rows.exps, b, &l.bytes, 16);
   take(&l.rows.idx, b, &l.bytes, 4 * T);
   take(&l.rows.pos, b, &l.bytes, 4 * T);
   take(&l.rows.row, b, &l.bytes, (int64_t)sizeof(HeadRow) * T);
@@ -1082,7 +1092,7 @@ static hipError_t run_bwd(const HeadIn& in, const float* stats, const float* dlo
   TM_RET((gather<F16, true>(in, of, l, dw ? l.hs : nullptr, stream)));
   for (int64_t i = 0; i < p.pieces; ++i) {
     const int64_t w0 = i * p.piece, n = in.V - w0 < p.piece ? in.V - w0 : p.piece;
-    TM_RET(launch_head_dlogits(in, l.ht, l.rows.count, l.rows.row, w0, n, l.G, p.piece,
+    TM_RET(launch_head_dlogits(in, l.ht, l.rows.count, l.rows.row, l.rows.exps + 3, w0, n, l.G, p.piece,
                                stream));
     if (in.K > 0) {
       hipLaunchKernelGGL(sparse_kernel<F16>, dim3((unsigned)((in.T * (in.K + 1) + 255) / 256)),
