@@ -452,13 +452,14 @@ def test_two_streams_at_once():
             assert all(torch.equal(a, b) for a, b in zip(w, out)) and torch.equal(x, y)
 
 
-def test_a_captured_step_and_its_replays():
+@pytest.mark.parametrize("T,K", [(333, 4), (9, 4), (40, 3), (64, 0), (1100, 0)])
+def test_a_captured_step_and_its_replays(T, K):
     """Forward and backward in a graph, replayed with other inputs, other tokens masked, and eager
     work between the replays."""
-    cases = [_inputs(333, 1500, 136, K=4, seed=s, masked=m) for s, m in ((19, 0.0), (20, 0.5),
-                                                                        (21, 0.9))]
+    cases = [_inputs(T, 1500, 136, K=K, seed=s, masked=m) for s, m in ((19, 0.0), (20, 0.5),
+                                                                       (21, 0.9))]
     c = {k: v.clone() if isinstance(v, torch.Tensor) else v for k, v in cases[0].items()}
-    r = torch.randn(333, 136, device="cuda")
+    r = torch.randn(T, 136, device="cuda")
     nw = torch.ones(136, device="cuda")
 
     def step():
