@@ -22,9 +22,10 @@ def _terms(V, labels, ids, top):
 def teacher(V, ids, top, tau):
     """The teacher's distribution over its places, zeros where no word is kept."""
     kept = (ids >= 0) & (ids < V) & ~(top == -np.inf)
-    t = np.where(kept, top / tau, -np.inf)
+    t = np.where(kept, top, -np.inf)
     some = kept.any(1, keepdims=True)
     t = np.where(some, t, 0.0)
+    t = (t - t.max(1, keepdims=True)) / tau
     return np.where(kept, np.exp(t - _lse(t)), 0.0), some[:, 0]
 
 

@@ -728,6 +728,8 @@ __global__ __launch_bounds__(64 * WAVES) void teach_kernel(Finish f) {
   constexpr bool SPLIT = WAVES == 16;
   constexpr int DOTS = SPLIT ? WAVES - 1 : WAVES, N = SPLIT ? 5 : 4;
   extern __shared__ float sh[];  // K + 1 each: logits; teacher's logits, probabilities; words
+  // (the teacher's logits as they are, -infinity: not kept; over tau only what is left of them once
+  // their largest is taken off, or float32's lowest value, a usual mask, would leave its range)
   __shared__ Softmax shared_x;
   __shared__ float shared_t[2];
   const HeadIn& in = f.in;
@@ -749,7 +751,7 @@ __global__ __launch_bounds__(64 * WAVES) void teach_kernel(Finish f) {
                              : id_at(in.ids, in.ids64, t * in.K + e - 1);
     const bool ok = in_vocabulary(in, v);
     id[e] = ok ? (int)v : -1;
-    q[e] = ok && e > 0 ? top_at(f.top, f.top_type, t * in.K + e - 1) * it : -__builtin_inff();
+    q[e] = ok && e > 0 ? top_at(f.top, f.top_type, t * in.K + e - 1) : -__builtin_inff();
   }
   __syncthreads();
   const uint16_t* h = in.h + t * in.D;
@@ -777,10 +779,12 @@ __global__ __launch_bounds__(64 * WAVES) void teach_kernel(Finish f) {
     for (int e = lane; e < n; e += 64) tm = fmaxf(tm, q[e]);
     tm = wave_max(tm);
     for (int e = lane; e < n; e += 64)
-      if (q[e] != -__builtin_inff()) ts += __builtin_amdgcn_exp2f((q[e] - tm) * kLog2e);
+      if (q[e] != -__builtin_inff()) ts += __builtin_amdgcn_exp2f((q[e] - tm) * it * kLog2e);
     tl = __builtin_amdgcn_logf(wave_sum(ts)) * kLn2;
     for (int e = SPLIT ? lane : tid; e < n; e += SPLIT ? 64 : L)
-      p[e] = q[e] != -__builtin_inff() ? __builtin_amdgcn_exp2f(((q[e] - tm) - tl) * kLog2e) : 0.f;
+      p[e] = q[e] != -__builtin_inff()
+                 ? __builtin_amdgcn_exp2f(((q[e] - tm) * it - tl) * kLog2e)
+                 : 0.f;
     if (SPLIT && lane == 0) {
       shared_x = x;
       shared_t[0] = tm;
@@ -796,7 +800,7 @@ __global__ __launch_bounds__(64 * WAVES) void teach_kernel(Finish f) {
   if (wave == 0) {
     float kl = 0.f;
     for (int e = lane; e < n; e += 64)  // ln q - ln s, s = e^((z - m) / tau) / sum
-      if (p[e] != 0.f) kl += p[e] * (((q[e] - tm) - tl) - ((z[e] - x.m) * it - x.ln_t));
+      if (p[e] != 0.f) kl += p[e] * (((q[e] - tm) * it - tl) - ((z[e] - x.m) * it - x.ln_t));
     kl = wave_sum(kl);
     if (lane == 0)
       f.loss[t] = (terms & 1 ? (1.0f - in.alpha) * (x.ln + (x.m - z[0])) : 0.f) +

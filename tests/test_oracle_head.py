@@ -71,3 +71,16 @@ def test_norm_gradients_against_differences():
             e = np.zeros_like(a)
             e[i] = 1e-5
             assert (f(a + e) - f(a - e)) / 2e-5 == pytest.approx(d[i], rel=1e-7, abs=1e-8)
+
+
+def test_teacher_of_the_lowest_values():
+    """A number added to all of a token's logits changes nothing, whatever its size."""
+    ids = np.array([[1, 2, 3, 4], [1, 2, 3, -1]])
+    for dtype in (np.float32, np.float16):
+        lo = float(np.finfo(dtype).min)
+        for tau in (0.5, 2.0 ** -10, 2.0):
+            q, some = O.teacher(5, ids, np.full((2, 4), lo), tau)
+            assert some.all()
+            assert np.allclose(q, [[0.25] * 4, [1 / 3, 1 / 3, 1 / 3, 0.0]], rtol=1e-15)
+            q, _ = O.teacher(5, ids, np.array([[2.0, lo, lo, lo], [2.0, 2.0, lo, 2.0]]), 0.5)
+            assert np.allclose(q, [[1, 0, 0, 0], [0.5, 0.5, 0, 0]], rtol=1e-15)
