@@ -51,7 +51,11 @@ int64_t tm_head_loss_workspace(int64_t T, int64_t V, int64_t D); /* -1: sizes ou
  * The other arguments as they were in the forward call that wrote stats.  The
  * logits are made again, a piece of the vocabulary at a time; a logit's gradient is
  * rounded once to h's type (by 2^-8 of it in bfloat16, 2^-11 in float16, at a scale of its
- * own in every row) before the two products, whose sums are float32.  Tokens without
+ * own in every row) before the two products, whose sums are float32.  dW's product takes h
+ * times its token's dloss, in h's type against the largest: exact in bfloat16 down to
+ * 2^-126 of it, in float16 where such a value is above 2^-28 of the largest one of the call, and
+ * off by at most 2^-39 of that below (one token's huge dloss hides others' small ones there).
+ * Tokens without
  * a loss, or whose dloss is 0, have rows of zeros in dh and no part in dW,
  * whatever their rows of h hold.
  *   dh         [T, D], h's type (16-byte aligned), or NULL: not wanted

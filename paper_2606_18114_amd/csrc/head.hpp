@@ -23,9 +23,16 @@ struct HeadIn {
 };
 
 // `stats`: four planes [T], log2 of the sum of exponentials, the same at the temperature,
-// which terms a token has (1: cross entropy, 2: divergence), the logit gradient (of
-// the loss over head_unit) at its label; then [T, K], that gradient at the teacher's words.
+// which terms a token has (1: cross entropy, 2: divergence) and, in float16, how large its row of h
+// is, the logit gradient (of the loss over head_unit) at its label; then [T, K], that gradient at
+// the teacher's words.
 enum HeadStat { kStatLse, kStatLseT, kStatTerms, kStatLabel, kStatPlanes };
+// the third plane: terms + 4 (25 + exponent of the row's largest value, -25 .. 15), 0 without terms
+inline __device__ float head_stat_terms(int terms, int exponent) {
+  return (float)(terms + 4 * (25 + exponent));
+}
+inline __device__ int head_terms(float stat) { return (int)stat & 3; }
+inline __device__ int head_exponent(float stat) { return ((int)stat >> 2) - 25; }
 inline __host__ __device__ int64_t head_stats_floats(int64_t T, int64_t K) {
   return (kStatPlanes + K) * T;
 }

@@ -16,10 +16,15 @@
 // Backward, per piece of the vocabulary: dlogits (dense), the sparse stores, dh and
 // dW.  A row's gradient is g = m 2^e, 1 <= m < 2, that of the largest M 2^E; the dlogits hold
 // m / M times the unit gradient (16 bits, rounded once: by 2^-8 of each in bfloat16, 2^-11 in
-// float16), h is copied times 2^(e - E) (exact but for what falls under the type's
-// smallest number), and dh and dW are multiplied by M and powers of two at the end: the
-// roundings do not depend on how the loss is scaled, and where all gradients are equal (a mean)
-// a label's dlogit, close to -1, is close to exact.
+// float16), h is copied times 2^e over a power of two that all rows share, and dh and dW are
+// multiplied by M and powers of two at the end: the roundings do not depend on how the loss is
+// scaled, and where all gradients are equal (a mean) a label's dlogit, close to -1, is close to
+// exact.  The copy of h is exact but for what falls under the type's smallest numbers.  In bfloat16
+// the power is 2^E: h times its gradient's share of the largest keeps its bits down to 2^-126.  In
+// float16 it is the one that brings the largest h 2^e to float16's own largest numbers (the forward
+// pass leaves each row's exponent in `stats`): a value keeps its 11 bits where it is, times its
+// gradient, above 2^-28 of the largest such product, and is off by at most 2^-39 of that product
+// below.
 #include "common.hpp"
 #include "head.hpp"
 #include "launchers.hpp"
@@ -87,9 +92,9 @@ __device__ __forceinline__ float top_at(const void* p, int type, int64_t i) {
 }
 
 // exponent of a row's gradient (0 where it is not finite; of a zero, which is left of a gradient
-// times a small unit, one below all others)
+// times a small unit, one so low that h times it is zero)
 __device__ __forceinline__ int exp_of(float g) {
-  if (g == 0.f) return -150;
+  if (g == 0.f) return -1000;
   return fabsf(g) < __builtin_inff() ? ilogbf(g) : 0;
 }
 
@@ -97,8 +102,8 @@ struct Rows {
   int* count;  // [1]
   int* idx;    // [T]: the token of a row
   int* pos;    // [T]: the row of a token, or -1
-  // backward: the largest gradient's exponent, that without the dlogits' shift, the parts of dh,
-  // the bits of the largest gradient's mantissa
+  // backward: the exponent that h's copy is over, that without the dlogits' shift, the parts of
+  // dh, the bits of the largest gradient's mantissa
   int* exps;
   HeadRow* row;  // [T] (backward)
   uint8_t* terms;  // [T]: 1 label, 2 teacher (forward)
@@ -142,7 +147,7 @@ template <bool BWD>
 __device__ __forceinline__ bool has_row(const HeadIn& in, const Of& of, const uint8_t* terms,
                                         int64_t t) {
   if constexpr (BWD)
-    return of.stats[kStatTerms * in.T + t] != 0.f && !(of.dloss[t] == 0.f);
+    return head_terms(of.stats[kStatTerms * in.T + t]) != 0 && !(of.dloss[t] == 0.f);
   else
     return in.K > 0 ? terms[t] != 0
                     : in_vocabulary(in, id_at(in.targets, in.targets64, t));
@@ -154,6 +159,16 @@ __device__ __forceinline__ int row_size(const HeadIn& in, const Of& of, int64_t 
   return g < __builtin_inff() ? __float_as_int(g) : 0;
 }
 
+// exponent of the largest value of token t's row of h times that of its gradient, kNowhere where
+// it has none
+constexpr int kNowhere = -100000;
+__device__ __forceinline__ int row_reach(const HeadIn& in, const Of& of, int64_t t) {
+  const float g = fabsf(of.dloss[t] * head_unit(in.alpha, in.tau));
+  return g > 0.f && g < __builtin_inff()
+             ? ilogbf(g) + head_exponent(of.stats[kStatTerms * in.T + t])
+             : kNowhere;
+}
+
 // token t's row r
 template <bool BWD>
 __device__ __forceinline__ void put_row(const HeadIn& in, const Of& of, const Rows& out, int64_t t,
@@ -163,7 +178,7 @@ __device__ __forceinline__ void put_row(const HeadIn& in, const Of& of, const Ro
     const int64_t T = in.T;
     const float unit = head_unit(in.alpha, in.tau), g = of.dloss[t] * unit;
     const float m = ldexpf(g, of.shift - exp_of(g));
-    const int terms = (int)of.stats[kStatTerms * T + t];
+    const int terms = head_terms(of.stats[kStatTerms * T + t]);
     float c1 = terms & 1 ? (1.0f - in.alpha) / unit * m : 0.f;
     float c2 = terms & 2 ? in.alpha * in.tau / unit * m : 0.f;
     float lse_t = of.stats[kStatLseT * T + t];
@@ -176,15 +191,23 @@ __device__ __forceinline__ void put_row(const HeadIn& in, const Of& of, const Ro
   }
 }
 
-// size: the largest of row_size
+// size: the largest of row_size; reach: of row_reach
 __device__ __forceinline__ int exp_of_size(int size) {
   return size == 0 ? 0 : ilogbf(__int_as_float(size));
 }
-__device__ __forceinline__ void put_exps(const Of& of, const Rows& out, int size) {
-  const int e = exp_of_size(size);
+// exponent that h's copy is over: the largest gradient's, or in float16 the one that leaves the
+// largest product with an exponent of 15, float16's largest
+__device__ __forceinline__ int copy_exp(bool f16, int size, int reach) {
+  if (!f16) return exp_of_size(size);
+  return reach == kNowhere ? 0 : reach - 15;
+}
+__device__ __forceinline__ void put_exps(const HeadIn& in, const Of& of, const Rows& out, int size,
+                                         int reach) {
+  const int e = copy_exp(in.f16, size, reach);
   out.exps[0] = e;
   out.exps[1] = e - of.shift;
-  out.exps[3] = __float_as_int(size == 0 ? 1.0f : ldexpf(__int_as_float(size), -e));
+  out.exps[3] = __float_as_int(
+      size == 0 ? 1.0f : ldexpf(__int_as_float(size), -exp_of_size(size)));
 }
 
 // Lists the rows in the tokens' order, where tokens are many.  A workgroup has `per` tokens (a
@@ -193,26 +216,33 @@ __device__ __forceinline__ void put_exps(const Of& of, const Rows& out, int size
 template <bool BWD>
 __global__ __launch_bounds__(1024) void rows_kernel(HeadIn in, Of of, int64_t per, Rows out) {
   __shared__ int sums[16];
-  __shared__ int maxs[16];
+  __shared__ int maxs[16], reaches[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t T = in.T, t0 = blockIdx.x * per, t1 = t0 + per < T ? t0 + per : T;
-  int n = 0, e = 0;
+  int n = 0, e = 0, reach = kNowhere;
   // the first workgroup looks at all gradients for the largest
 #pragma unroll 4
   for (int64_t t = tid; t < (BWD && blockIdx.x == 0 ? T : t0); t += 1024) {
     const bool yes = has_row<BWD>(in, of, out.terms, t);
     if (t < t0) n += yes;
     if constexpr (BWD)
-      if (yes) e = max(e, row_size(in, of, t));
+      if (yes) {
+        e = max(e, row_size(in, of, t));
+        reach = max(reach, row_reach(in, of, t));
+      }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     n += __shfl_xor(n, o, 64);
-    e = max(e, __shfl_xor(e, o, 64));
+    if constexpr (BWD) {
+      e = max(e, __shfl_xor(e, o, 64));
+      reach = max(reach, __shfl_xor(reach, o, 64));
+    }
   }
   if (lane == 0) {
     sums[wave] = n;
     maxs[wave] = e;
+    reaches[wave] = reach;
   }
   __syncthreads();
   int base = 0;
@@ -220,9 +250,10 @@ __global__ __launch_bounds__(1024) void rows_kernel(HeadIn in, Of of, int64_t pe
   for (int w = 0; w < 16; ++w) {
     base += sums[w];
     e = max(e, maxs[w]);
+    reach = max(reach, reaches[w]);
   }
   if constexpr (BWD)
-    if (blockIdx.x == 0 && tid == 0) put_exps(of, out, e);
+    if (blockIdx.x == 0 && tid == 0) put_exps(in, of, out, e, reach);
   for (int64_t c = t0; c < t1; c += 1024) {
     const int64_t t = c + tid;
     const bool yes = t < t1 && has_row<BWD>(in, of, out.terms, t);
@@ -247,7 +278,7 @@ __global__ __launch_bounds__(1024) void rows_kernel(HeadIn in, Of of, int64_t pe
 // The rows as the products read them, 64 rows x 64 columns a workgroup, through LDS:
 //   ht[d][r] = h[idx[r]][d], the logits' second operand, with zeros up to a multiple of 128
 //   columns d and of 256 rows r;
-//   backward, hs[r] = h[idx[r]] times 2^(e - largest e), what dW contracts (NULL: not wanted).
+//   backward, hs[r] = h[idx[r]] times 2^(e - exps[0]), what dW contracts (NULL: not wanted).
 // LIST (up to kListTokens tokens): every workgroup lists the rows by itself and the first one
 // writes the list, which saves a launch (3 us).
 constexpr int kListTokens = 1024;
@@ -258,28 +289,37 @@ __global__ __launch_bounds__(256) void gather_kernel(HeadIn in, Of of, Rows rows
                                                      uint16_t* __restrict__ hs) {
   __shared__ uint16_t s[64][72];
   __shared__ int list[LIST ? kListTokens : 1];
-  __shared__ int sums[4][4], maxs[4];
+  __shared__ int sums[4][4], maxs[4], reaches[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int n, emax = 0;
+  int n, over = 0;
   if constexpr (LIST) {
     const bool first = blockIdx.x == 0 && blockIdx.y == 0;
     const int T = (int)in.T;
     bool yes[4];
     uint64_t mask[4];
-    int e = 0;
+    int e = 0, reach = kNowhere;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const int t = 256 * c + tid;
       yes[c] = t < T && has_row<BWD>(in, of, rows.terms, t);
       if constexpr (BWD)
-        if (yes[c]) e = max(e, row_size(in, of, t));
+        if (yes[c]) {
+          e = max(e, row_size(in, of, t));
+          if constexpr (F16) reach = max(reach, row_reach(in, of, t));
+        }
       mask[c] = __ballot(yes[c]);
       if (lane == 0) sums[c][wave] = __popcll(mask[c]);
     }
     if constexpr (BWD) {
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) e = max(e, __shfl_xor(e, o, 64));
-      if (lane == 0) maxs[wave] = e;
+      for (int o = 32; o > 0; o >>= 1) {
+        e = max(e, __shfl_xor(e, o, 64));
+        if constexpr (F16) reach = max(reach, __shfl_xor(reach, o, 64));
+      }
+      if (lane == 0) {
+        maxs[wave] = e;
+        reaches[wave] = reach;
+      }
     }
     __syncthreads();
     n = 0;
@@ -300,14 +340,15 @@ __global__ __launch_bounds__(256) void gather_kernel(HeadIn in, Of of, Rows rows
     }
     if constexpr (BWD) {
       e = max(max(maxs[0], maxs[1]), max(maxs[2], maxs[3]));
-      emax = exp_of_size(e);
-      if (first && tid == 0) put_exps(of, rows, e);
+      reach = max(max(reaches[0], reaches[1]), max(reaches[2], reaches[3]));
+      over = copy_exp(F16, e, reach);
+      if (first && tid == 0) put_exps(in, of, rows, e, reach);
     }
     if (first && tid == 0) *rows.count = n;
     __syncthreads();
   } else {
     n = *rows.count;
-    if constexpr (BWD) emax = rows.exps[0];
+    if constexpr (BWD) over = rows.exps[0];
   }
   const int64_t r0 = (int64_t)blockIdx.x * 64;
   if (r0 >= up256(n)) return;
@@ -321,7 +362,7 @@ __global__ __launch_bounds__(256) void gather_kernel(HeadIn in, Of of, Rows rows
       v = ld16(in.h + t * in.D + d0 + c);
       if constexpr (BWD)
         if (hs) {
-          const int e = exp_of(of.dloss[t] * head_unit(in.alpha, in.tau)) - emax;
+          const int e = exp_of(of.dloss[t] * head_unit(in.alpha, in.tau)) - over;
           u32x4 o = v;
           if (e != 0) {
             float x[8];
@@ -592,16 +633,22 @@ struct Finish {
 };
 
 // h . w[i] for N rows w over the lanes of a wave, in every lane; UNROLL steps of 512
-// columns under way at once
+// columns under way at once.  Returns the size of the largest of the lane's values of h, where F16
+// (0 else).
 template <bool F16, int N, int UNROLL>
-__device__ __forceinline__ void row_dots(const uint16_t* h, const uint16_t* const* w, int D,
-                                         int lane, float (&s)[N]) {
+__device__ __forceinline__ float row_dots(const uint16_t* h, const uint16_t* const* w, int D,
+                                          int lane, float (&s)[N]) {
+  float most = 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) s[i] = 0.f;
 #pragma unroll UNROLL
   for (int d = lane * 8; d < D; d += 512) {
     float x[8], y[8];
     widen<F16>(ld16(h + d), x);
+    if constexpr (F16) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[j]));
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       widen<F16>(ld16(w[i] + d), y);
@@ -611,6 +658,15 @@ __device__ __forceinline__ void row_dots(const uint16_t* h, const uint16_t* cons
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
+  return most;
+}
+
+// the exponent of a row's largest value, from what row_dots left in the lanes (an infinity's: 15)
+template <bool F16>
+__device__ __forceinline__ int row_exponent(float most) {
+  if constexpr (!F16) return -25;
+  const float m = wave_max(most);
+  return m == 0.f ? -25 : m < 65536.f ? ilogbf(m) : 15;
 }
 
 // the softmax sums of row r: the parts of its token tile's workgroups, joined.  m: the largest
@@ -688,12 +744,12 @@ __device__ __forceinline__ Softmax softmax_of(const Finish& f, int64_t t, int te
 }
 
 __device__ __forceinline__ void put_stats(const Finish& f, int64_t t, float loss, float lse,
-                                          float lse_t, int terms, float label) {
+                                          float lse_t, float terms, float label) {
   float* st = f.stats + t;  // the token's place in each plane
   f.loss[t] = loss;
   st[kStatLse * f.in.T] = lse;
   st[kStatLseT * f.in.T] = lse_t;
-  st[kStatTerms * f.in.T] = (float)terms;
+  st[kStatTerms * f.in.T] = terms;
   st[kStatLabel * f.in.T] = label;
 }
 
@@ -706,14 +762,15 @@ __global__ __launch_bounds__(256) void finish_kernel(Finish f) {
   if (t >= in.T) return;
   const int64_t y = id_at(in.targets, in.targets64, t);
   if (!in_vocabulary(in, y)) {
-    if (lane == 0) put_stats(f, t, 0.f, 0.f, 0.f, 0, 0.f);
+    if (lane == 0) put_stats(f, t, 0.f, 0.f, 0.f, 0.f, 0.f);
     return;
   }
   float z[1];
   const uint16_t* const w[1] = {in.w + y * in.D};
-  row_dots<F16, 1, 4>(in.h + t * in.D, w, in.D, lane, z);
+  const float most = row_dots<F16, 1, 4>(in.h + t * in.D, w, in.D, lane, z);
+  const float terms = head_stat_terms(1, row_exponent<F16>(most));
   const Softmax x = softmax_of<false>(f, t, 1, lane);
-  if (lane == 0) put_stats(f, t, x.ln + (x.m - z[0]), x.lse, x.lse, 1, x.grad(z[0], 1.0f));
+  if (lane == 0) put_stats(f, t, x.ln + (x.m - z[0]), x.lse, x.lse, terms, x.grad(z[0], 1.0f));
 }
 
 // The same with a teacher, a workgroup of WAVES waves a token: four, or sixteen where tokens
@@ -740,7 +797,7 @@ __global__ __launch_bounds__(64 * WAVES) void teach_kernel(Finish f) {
   const int terms = f.rows.terms[t];
   if (terms == 0) {  // no loss
     for (int i = tid; i < in.K; i += L) st_top[i] = 0.f;
-    if (tid == 0) put_stats(f, t, 0.f, 0.f, 0.f, 0, 0.f);
+    if (tid == 0) put_stats(f, t, 0.f, 0.f, 0.f, 0.f, 0.f);
     return;
   }
   float *z = sh, *q = sh + n, *p = sh + 2 * n;
@@ -755,6 +812,7 @@ __global__ __launch_bounds__(64 * WAVES) void teach_kernel(Finish f) {
   }
   __syncthreads();
   const uint16_t* h = in.h + t * in.D;
+  float most = 0.f;
   if (wave < DOTS)
     for (int e0 = N * wave; e0 < n; e0 += N * DOTS) {
       float d[N];
@@ -764,7 +822,7 @@ __global__ __launch_bounds__(64 * WAVES) void teach_kernel(Finish f) {
         const int e = e0 + i < n ? e0 + i : n - 1;
         w[i] = in.w + (int64_t)(id[e] >= 0 ? id[e] : 0) * in.D;
       }
-      row_dots<F16, N, SPLIT ? 4 : 1>(h, w, in.D, lane, d);
+      most = row_dots<F16, N, SPLIT ? 4 : 1>(h, w, in.D, lane, d);
       if (lane == 0)
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -806,7 +864,7 @@ __global__ __launch_bounds__(64 * WAVES) void teach_kernel(Finish f) {
       f.loss[t] = (terms & 1 ? (1.0f - in.alpha) * (x.ln + (x.m - z[0])) : 0.f) +
                   (terms & 2 ? in.alpha * in.tau * in.tau * kl : 0.f);
   }
-  const int y = id[0];
+  const int y = id[0], exponent = row_exponent<F16>(most);  // (the first wave's counts)
   for (int e = tid; e < n; e += L) {
     const int v = id[e];
     float hit = 0.f;
@@ -817,7 +875,7 @@ __global__ __launch_bounds__(64 * WAVES) void teach_kernel(Finish f) {
       float* st = f.stats + t;
       st[kStatLse * in.T] = x.lse;
       st[kStatLseT * in.T] = x.lse_t;
-      st[kStatTerms * in.T] = (float)terms;
+      st[kStatTerms * in.T] = head_stat_terms(terms, exponent);
       st[kStatLabel * in.T] = g;
     } else {
       st_top[e - 1] = g;
@@ -838,7 +896,7 @@ __global__ __launch_bounds__(256) void sparse_kernel(HeadIn in, const float* __r
   const int e = (int)(i % (in.K + 1));
   if (r >= *rows.count) return;
   const int64_t t = rows.idx[r];
-  const int terms = (int)stats[kStatTerms * in.T + t];
+  const int terms = head_terms(stats[kStatTerms * in.T + t]);
   if (!(terms & (e == 0 ? 1 : 2))) return;
   const int64_t v =
       (e == 0 ? id_at(in.targets, in.targets64, t) : id_at(in.ids, in.ids64, t * in.K + e - 1)) -

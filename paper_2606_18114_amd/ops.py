@@ -1280,7 +1280,8 @@ def head_loss_bwd(h: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
     """Gradients of head_loss (tm_head_loss_bwd): dloss float32 [T] -> (dh
     [T, D], dW [V, D]), both in h's type; dW float32 where a float32 one is
     given, then also added to (accumulate).  The other arguments are the
-    forward call's.  want_dh, want_dW: without one of them it is None, and its
+    forward call's.  In float16 dW takes its parts h * dloss to 2^-11 of
+    themselves down to 2^-28 of the call's largest.  want_dh, want_dW: without one of them it is None, and its
     product is not computed."""
     dev, T, V, D, K = _head_args(h, weight, targets, teacher_ids, alpha, temperature)
     _of(stats, "stats", _F32, (T * (HEAD_STATS + K),), dev)

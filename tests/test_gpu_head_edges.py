@@ -7,7 +7,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from test_gpu_head_forms import IGNORE, _check, _inputs, _run  # noqa: E402
+from test_gpu_head_forms import F, _check, _inputs, _reference, _run  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -48,3 +48,100 @@ def test_teachers_of_the_types_ends(T, K, top_dtype, tau):
     got = _run(c)
     for a, b in zip(want, got):
         assert torch.equal(a, b)
+
+
+# ---------------------------------------------------------------- gradients of very different sizes
+
+def _check_dw(c, dw, dw0=None):
+    """dW float32, row by row within what its own tokens allow.  edz, sums and the output as in
+    test_gpu_head_forms.py, but a float16 dlogit that falls under the type's smallest number is off
+    by no more than itself.  The float16 copy of h: a value h 2^e of gradient g = m 2^e is off by
+    half of float16's smallest step, 2^-25, in units in which the largest has an exponent of 15,
+    so by 2^-40 max |g h|; times m < 2 and the unit gradient |dz / g|, which is at most 1."""
+    T, V = len(c["h"]), len(c["w"])
+    _, _, dz, edz = _reference(c, torch.arange(T, device="cuda"))
+    h = c["h"].double()
+    hs = torch.zeros_like(edz)
+    if c["h"].dtype == torch.float16:
+        g = c["dloss"].double().abs()[:, None] * ((1 - c["alpha"]) + c["alpha"] * c["tau"])
+        edz = edz - g * 2.0 ** -37 + torch.minimum(dz.abs(), g * 2.0 ** -37)
+        reach = (g[:, 0] * h.abs().amax(1)).max()
+        hs = torch.where(g > 0, dz.abs() / g, 0.0) * reach * 2.0 ** -39
+    want = dz.t() @ h
+    tol = (edz + T * F * dz.abs()).t() @ h.abs() + hs.sum(0)[:, None]
+    if dw0 is not None:
+        want = want + dw0.double()
+    tol = tol + want.abs() * 2 * F
+    off = (dw.double() - want).abs()
+    assert bool((off <= tol).all()), float((off / tol.clamp(min=1e-300)).max())
+
+
+def _spread(c, low, high, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    T = len(c["h"])
+    d = torch.randn(T, generator=g, device="cuda") * torch.exp2(
+        torch.randint(low, high + 1, (T,), generator=g, device="cuda").float())
+    d[torch.rand(T, generator=g, device="cuda") < 0.2] = 0.0
+    c["dloss"] = d
+
+
+@pytest.mark.parametrize("T,K,tau", [(40, 0, 1.0), (40, 3, 2.0), (200, 0, 1.0), (200, 20, 0.5),
+                                     (1500, 0, 1.0), (1500, 2, 1.0)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_small_gradients_beside_large_ones(T, K, tau, dtype):
+    """dloss over 2^-20 .. 2^8.  Some words have small tokens only: their logits at the others are
+    64 lower, and their rows of dW are as good as if the others were not there."""
+    V, D, rare = 300, 96, 40
+    c = _inputs(T, V, D, dtype, K=K, seed=T + K)
+    c["tau"] = tau
+    _spread(c, -20, 8)
+    small = torch.arange(T, device="cuda") % 3 == 0
+    c["dloss"][small] = c["dloss"][small].sign() * 2.0 ** -20
+    c["dloss"][1] = 2.0 ** 8
+    c["h"][:, 0] = torch.where(small, 0.0, 8.0).to(dtype)
+    c["w"][:, 0] = 0.0
+    c["w"][:rare, 0] = -8.0
+    n = int(small.sum())
+    c["y"] = torch.where(small, torch.arange(T, device="cuda") % rare, c["y"] % (V - rare) + rare)
+    if K:
+        c["ids"] = torch.where(small[:, None], c["ids"] % rare, c["ids"] % (V - rare) + rare)
+    dw = torch.full((V, D), math.nan, device="cuda")
+    _run(c, dW=dw)
+    _check_dw(c, dw)
+    # the same tokens alone
+    if n > 1 and dtype == torch.float16:
+        _check_dw(c, _run(c, dW=torch.zeros(V, D, device="cuda"), accumulate=True)[2])
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -24, 2.0 ** -10, 1.0, 2.0 ** 15])
+def test_float16_rows_of_any_size(scale):
+    """h from float16's smallest numbers to its largest, rows of zeros among them."""
+    T, V, D = 70, 200, 64
+    for rows in (T, 1100):
+        c = _inputs(rows, V, D, torch.float16, seed=rows)
+        c["h"] = (c["h"].float().clamp(-1.9, 1.9) * scale).to(torch.float16)
+        c["h"][::9] = 0.0
+        c["w"] = (c["w"].float() * 2.0 ** -16 if scale > 1 else c["w"].float()).to(torch.float16)
+        _spread(c, -6, 6)
+        _check_dw(c, _run(c, dW=torch.zeros(V, D, device="cuda"))[2])
+        c["h"][:] = 0.0
+        assert not _run(c)[2].any()
+
+
+@pytest.mark.parametrize("T", [5, 1300])
+def test_vanishing_and_infinite_gradients_of_float16_rows(T):
+    """Gradients of float32's smallest numbers, and of zero once they are taken over the logits'
+    unit (alpha tau = 1/4): a gradient of nothing adds nothing."""
+    c = _inputs(T, 70, 24, torch.float16, K=3, seed=T)
+    c.update(alpha=1.0, tau=0.25)
+    c["h"] = (c["h"].float() * 2.0 ** -20).to(torch.float16)
+    c["dloss"] = torch.full((T,), 1e-45, device="cuda")
+    c["dloss"][0] = 1e-44
+    _, dh, dw = _run(c)
+    assert bool(torch.isfinite(dh.float()).all()) and bool(torch.isfinite(dw.float()).all())
+    c = _inputs(T, 70, 24, torch.float16, seed=T)
+    c["dloss"][3] = math.inf
+    _, dh, dw = _run(c)
+    rest = torch.arange(T, device="cuda") != 3
+    assert bool(torch.isfinite(dh[rest].float()).all())
+    assert not torch.isfinite(dh[3]).all() and not torch.isfinite(dw).any()
