@@ -397,13 +397,27 @@ class Embedding(torch.nn.Module):
 
 class BlockNormFn(torch.autograd.Function):
     """The norm of residual + y and that sum (``tm_block_norm`` and its
-    gradients): residual, y float32 [T, D] -> (x bfloat16 [T, D], float32
-    [T, D]); y None: x alone."""
+    gradients): residual, y float32 [..., D] -> (x bfloat16 [..., D], float32
+    [..., D]); y None: x alone."""
+
+    # The arrays' shapes change in here: the residual and y have one gradient, which autograd
+    # copies where both want it for themselves, but not when it comes through a view of each.
 
     @staticmethod
     def forward(ctx, residual, y, w, eps):
         w = w.detach().contiguous()
-        x, r = ops.block_norm(residual.contiguous(), None if y is None else y.contiguous(), w, eps)
+
+        def rows(t):
+            return t.contiguous().view(-1, t.shape[-1])
+
+        r = rows(residual)
+        x = torch.empty(residual.shape, dtype=torch.bfloat16, device=residual.device)
+        if y is None:
+            ops.block_norm(r, None, w, eps, x=rows(x))
+        else:
+            total = torch.empty(residual.shape, dtype=torch.float32, device=residual.device)
+            ops.block_norm(r, rows(y), w, eps, residual_out=rows(total), x=rows(x))
+            r = total
         ctx.save_for_backward(r, w)
         ctx.eps, ctx.sum = eps, y is not None
         return (x, r) if ctx.sum else x
@@ -412,9 +426,11 @@ class BlockNormFn(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dx, dresidual=None):
         r, w = ctx.saved_tensors
-        dr, dw = ops.block_norm_bwd(r, w, dx.to(torch.bfloat16).contiguous(),
-                                    None if dresidual is None else dresidual.contiguous(),
-                                    ctx.eps)
+        shape, rows = dx.shape, (-1, w.shape[0])
+        dr, dw = ops.block_norm_bwd(
+            r.view(rows), w, dx.to(torch.bfloat16).contiguous().view(rows),
+            None if dresidual is None else dresidual.contiguous().view(rows), ctx.eps)
+        dr = dr.view(shape)
         return dr, dr if ctx.sum else None, dw, None
 
 
@@ -434,14 +450,11 @@ class BlockNorm(torch.nn.Module):
         width = self.weight.shape[0]
         if residual.shape[-1:] != (width,):
             raise ValueError(f"the residual must be [..., {width}], got {tuple(residual.shape)}")
-        r = residual.reshape(-1, width)
         if y is None:
-            return BlockNormFn.apply(r, None, self.weight, self.eps).reshape(residual.shape), \
-                residual
+            return BlockNormFn.apply(residual, None, self.weight, self.eps), residual
         if y.shape != residual.shape:
             raise ValueError(f"y has shape {tuple(y.shape)}, the residual {tuple(residual.shape)}")
-        x, r = BlockNormFn.apply(r, y.reshape(-1, width).to(torch.float32), self.weight, self.eps)
-        return x.reshape(residual.shape), r.reshape(residual.shape)
+        return BlockNormFn.apply(residual, y.to(torch.float32), self.weight, self.eps)
 
     def extra_repr(self) -> str:
         return f"{self.weight.shape[0]}, eps={self.eps}"
