@@ -10,7 +10,8 @@ using namespace tmk_abi;
 
 namespace {
 
-// a workgroup of 256 threads a token stays within a launch's 2^32 threads
+// a workgroup of 256 threads a token stays under a launch's 2^32 threads (the block norm's, of up to
+// 512, are dealt over two dimensions)
 constexpr int64_t kMaxTokens = int64_t(1) << 23;
 
 // outs: no overlap with an input or with each other

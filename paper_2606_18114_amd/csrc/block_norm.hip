@@ -2,8 +2,8 @@
 //   r = residual + y;  rho = 1 / sqrt(mean(r^2) + eps);  x = bf16(r rho w);
 //   a = w dx;  dr = dresidual + rho (a - r rho^2 mean(a r));  dw = sum_t dx r rho.
 //
-// Bound by memory: 14 bytes an element forward (10 without a sum of r and y: 6) and
-// backward.  A workgroup (a wave up to 512 columns) takes a row and keeps it in
+// Bound by memory: 14 bytes an element forward (6 without y) and backward (10 without
+// dresidual).  A workgroup (a wave up to 512 columns) takes a row and keeps it in
 // registers between the sum and the output, up to 8192 columns; wider rows are
 // read twice.  Columns are taken four at a time, whatever a row's alignment: the
 // hardware takes vectors at any multiple of their element.
@@ -18,6 +18,7 @@ namespace tmk {
 namespace {
 
 constexpr int kBnGroups = 1024;  // row groups of the backward's partial sums of dw
+constexpr int64_t kBnRows = int64_t(1) << 22;  // of a launch's first dimension, forward
 
 struct __attribute__((packed, aligned(4))) F4 {
   float v[4];
@@ -90,14 +91,17 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
   }
 }
 
-// grid (T), L threads; NV vectors a thread in registers (0: the row is read again)
+// grid (x, y) of at least T, L threads; NV vectors a thread in registers (0: the row is read again)
 template <int L, int NV>
 __global__ __launch_bounds__(L) void block_norm_kernel(const float* residual, const float* y,
-                                                       int d, const float* __restrict__ w,
-                                                       float eps, float* residual_out,
+                                                       int64_t T, int d,
+                                                       const float* __restrict__ w, float eps,
+                                                       float* residual_out,
                                                        uint16_t* __restrict__ x) {
   __shared__ float lds[8];
-  const int64_t at = (int64_t)blockIdx.x * d;
+  const int64_t t = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  if (t >= T) return;
+  const int64_t at = t * d;
   auto load = [&](int c, float (&r)[4]) {
     ld4(residual + at, c, d, r);
     if (y) {
@@ -260,9 +264,11 @@ int64_t bn_groups(int64_t T) { return T < kBnGroups ? T : kBnGroups; }
 hipError_t launch_block_norm(const float* residual, const float* y, int64_t T, int d,
                              const float* w, float eps, float* residual_out, uint16_t* x,
                              hipStream_t stream) {
+  // a dimension of a launch has less than 2^32 threads, here 512 a row at most
+  const int64_t ny = (T + kBnRows - 1) / kBnRows, nx = (T + ny - 1) / ny;
   bn_form(d, [&](auto l, auto nv) {
-    hipLaunchKernelGGL((block_norm_kernel<l(), nv()>), dim3((unsigned)T), dim3(l()), 0, stream,
-                       residual, y, d, w, eps, residual_out, x);
+    hipLaunchKernelGGL((block_norm_kernel<l(), nv()>), dim3((unsigned)nx, (unsigned)ny), dim3(l()),
+                       0, stream, residual, y, T, d, w, eps, residual_out, x);
   });
   return hipGetLastError();
 }
