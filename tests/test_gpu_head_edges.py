@@ -7,7 +7,8 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from test_gpu_head_forms import F, _check, _inputs, _reference, _run  # noqa: E402
+from test_gpu_head_forms import (F, IGNORE, _check, _inputs, _reference,  # noqa: E402
+                                 _run)
 
 pytestmark = pytest.mark.gpu
 
@@ -145,3 +146,75 @@ def test_vanishing_and_infinite_gradients_of_float16_rows(T):
     rest = torch.arange(T, device="cuda") != 3
     assert bool(torch.isfinite(dh[rest].float()).all())
     assert not torch.isfinite(dh[3]).all() and not torch.isfinite(dw).any()
+
+
+# ---------------------------------------------------------------- forms
+
+def _some(n):
+    return sorted({0, 1, n // 2, n - 2, n - 1, *range(0, n, max(1, n // 61))} & set(range(n)))
+
+
+@pytest.mark.parametrize("T,V,D,K", [(3, 300, 65536, 0), (33, 70, 16392, 2), (70, 515, 32768, 3),
+                                     (300, 260, 65536, 0), (1100, 130, 8200, 1)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_wide_heads(T, V, D, K, dtype):
+    c = _inputs(T, V, D, dtype, K=K, seed=T + D, masked=0.1 if T > 3 else 0.0)
+    _check(c, *_run(c))
+
+
+@pytest.mark.parametrize("T,V,D,K,tau", [(16384, 20001, 264, 3, 2.0), (70001, 9001, 64, 1, 0.7),
+                                         (256, 1100000, 64, 2, 1.5)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_several_pieces_at_a_temperature(T, V, D, K, tau, dtype):
+    c = _inputs(T, V, D, dtype, K=K, seed=T + K, masked=0.1)
+    c["tau"] = tau
+    words = _some(V) + [v for v in (4095, 4096, 8191, 8192, 16383, 16384) if v < V]
+    _check(c, *_run(c), tokens=_some(T), words=words)
+
+
+@pytest.mark.parametrize("T,V,D,K,tau", [(1, 50000, 264, 64, 2.0), (16, 20001, 1000, 5, 0.5),
+                                         (33, 33001, 72, 2, 1.5), (64, 9000, 2056, 17, 3.0)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_gradients_of_few_tokens_at_a_temperature(T, V, D, K, tau, dtype):
+    c = _inputs(T, V, D, dtype, K=K, seed=T + V, masked=0.2 if T > 6 else 0.0)
+    c["tau"] = tau
+    _check(c, *_run(c))
+    dw0 = torch.randn(V, D, device="cuda")
+    loss, dh, dw = _run(c, dW=dw0.clone(), accumulate=True)
+    _check(c, loss, dh, dw, dw0=dw0)
+
+
+@pytest.mark.parametrize("T,V,D,K,tau", [(600, 900, 136, 100, 1.0), (513, 2000, 72, 1024, 2.0),
+                                         (2000, 300, 64, 257, 0.5), (512, 400, 64, 15, 1.0),
+                                         (512, 400, 64, 16, 1.0), (513, 400, 64, 16, 1.0)])
+def test_long_teachers(T, V, D, K, tau):
+    c = _inputs(T, V, D, K=K, seed=T + K, masked=0.1)
+    c["tau"] = tau
+    c["ids"][::7, K // 2:] = -1
+    _check(c, *_run(c))
+
+
+@pytest.mark.parametrize("T,V,D,K,masked", [(3001, 5003, 264, 0, 0.6), (1500, 9000, 768, 2, 0.9),
+                                            (5000, 1000, 72, 0, 0.999), (5000, 130, 512, 2, 0.9),
+                                            (17000, 17000, 520, 0, 0.97)])
+def test_weight_gradients_of_many_tokens_without_a_loss(T, V, D, K, masked):
+    """dW's contraction is cut for all tokens: parts that are left without a row."""
+    c = _inputs(T, V, D, K=K, seed=T + D, masked=masked)
+    if K:
+        c["ids"][c["y"] == IGNORE] = -1
+    words = _some(V) + [v for v in (4095, 4096, 8191, 8192, 16383, 16384) if v < V]
+    c["y"][5] = V - 1
+    for kw in ({}, {"dW": torch.full((V, D), math.nan, device="cuda")},
+               {"dW": torch.ones(V, D, device="cuda"), "accumulate": True}):
+        ones = torch.ones(V, D, device="cuda") if "accumulate" in kw else None
+        loss, _, dw = _run(c, want_dh=False, **kw)
+        _check(c, loss, None, dw, words=words, dw0=ones)
+
+
+@pytest.mark.parametrize("T,V,D,K", [(5, 70, 24, 3), (40, 1500, 72, 5), (300, 600, 136, 20)])
+@pytest.mark.parametrize("tau", [2.0 ** -10, 2.0 ** -5, 2.0 ** 5, 2.0 ** 10])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_values_at_temperatures_far_from_one(T, V, D, K, tau, dtype):
+    c = _inputs(T, V, D, dtype, K=K, seed=T)
+    c["tau"] = tau
+    _check(c, *_run(c))
