@@ -2,7 +2,8 @@
  * tmamba_head.h — the ends of a training step around the blocks: the loss of the
  * head over a large vocabulary, with a teacher's top logits, and the block's norm,
  * with their gradients.  Conventions, status codes and stream semantics are those
- * of tmamba.h; workspaces as in tmamba_seq.h.  Results are deterministic.
+ * of tmamba.h; workspaces as in tmamba_seq.h, the head's of the size that is asked for
+ * with the call's device current.  Results are deterministic.
  */
 #ifndef TMAMBA_HEAD_H
 #define TMAMBA_HEAD_H

@@ -929,9 +929,11 @@ def _call(fn: str, device: torch.device, *args) -> None:
 
 
 @functools.lru_cache(maxsize=4096)
-def _ws_bytes(fn: str, *sizes) -> int:
-    """A workspace size, which is a function of the call's sizes alone."""
-    n = int(getattr(lib(), fn)(*sizes))
+def _ws_bytes(fn: str, device: int, *sizes) -> int:
+    """A workspace size, which is a function of the call's sizes and of its
+    device (the head's products are cut for the number of compute units)."""
+    with torch.cuda.device(device):
+        n = int(getattr(lib(), fn)(*sizes))
     if n < 0:
         raise ValueError(f"{fn}: sizes {sizes} out of range")
     return n
@@ -939,7 +941,7 @@ def _ws_bytes(fn: str, *sizes) -> int:
 
 def _seq_ws(fn: str, device: torch.device, *sizes):
     """Scratch of one call as (tensor or None, pointer, bytes)."""
-    n = _ws_bytes(fn, *sizes)
+    n = _ws_bytes(fn, device.index, *sizes)
     if n == 0:
         return None, None, 0
     ws = torch.empty((n,), dtype=torch.uint8, device=device)
