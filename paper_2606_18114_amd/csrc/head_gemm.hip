@@ -411,7 +411,7 @@ __device__ __forceinline__ void store_rows(const uint8_t* mine, uint16_t* to, in
 // token a block and 64 of its logits.  Lane: token 32 b + l32, words 32 a +
 // 8 (i / 4) + 4 half + i % 4.
 //
-// kStats: part[(workgroup + token tile)][wave row][256][2 or 4] = maximum and sum
+// kStats: part[(workgroup + token tile)][wave row][256][2 or 3] = maximum and sum
 // of 2^(log2e (z - maximum)) over the run's words, and the same at the temperature
 // where TEMP.  A workgroup walks many word tiles of one token tile, so
 // a step of the softmax costs no memory.
@@ -943,7 +943,8 @@ static int64_t grid_of(int64_t items) {
 // 0.52 us a workgroup of 64, 0.58 of 128 (both by their loads), 0.68 of 192, 0.80 of 256.  So
 // narrow tiles are for few words, where 256 would leave workgroups idle (300 tokens of 5000 x
 // 2048: 36 us, 51 with 256), and where they waste less of the last tile (300 of 50000: 93 us,
-// 113 with 256; 800 of 50000: 178, 208).
+// 113 with 256; 800 of 50000: 178, 208).  Dlogits are kept, in rows to the next multiple of 256, and
+// their products contract them 128 at a time: tiles of 192 would run past the last row.
 int head_tile_tokens(int64_t T, int64_t words, bool stats) {
   const int64_t P = current_cu_count(), nv = (words + kTM - 1) / kTM;
   const double us[4] = {0.52, 0.58, 0.68, 0.80};

@@ -774,7 +774,7 @@ __global__ __launch_bounds__(256) void finish_kernel(Finish f) {
 }
 
 // The same with a teacher, a workgroup of WAVES waves a token: four, or sixteen where tokens
-// are few (1 token, 64 words: 22 us, 43 of four).  Entry 0 is the label, the others
+// are few and their words many (run_finish).  Entry 0 is the label, the others
 // the teacher's words: their logits are dealt over the waves, four or five at a time; of four
 // waves each makes the softmaxes by itself.  Bound: the words' rows of W from the caches (16384 tokens of
 // 64 words of 2048 columns, 4.3 GB: 330 us).
@@ -1117,8 +1117,12 @@ static hipError_t run_teach(const Finish& f, hipStream_t stream) {
 
 template <bool F16>
 static hipError_t run_finish(const Finish& f, hipStream_t stream) {
+  // Sixteen waves while every token's workgroup finds a CU of its own, and from 28 words on (50000
+  // x 2048, sixteen and four waves: 1 token of 24 words 12.0 and 11.8 us, of 32 12.5 and 14.1, of 64
+  // 15.0 and 20.5; 256 tokens of 24 words 14.0 and 13.6, of 32 14.8 and 16.0, of 64 19.0 and 23.5;
+  // 257 tokens of 64 words 26.5 and 22.6).
   if (f.in.K > 0)
-    return f.in.T <= 512 && f.in.K >= 16 ? run_teach<F16, 16>(f, stream)
+    return f.in.T <= current_cu_count() && f.in.K >= 28 ? run_teach<F16, 16>(f, stream)
                                          : run_teach<F16, 4>(f, stream);
   hipLaunchKernelGGL(finish_kernel<F16>, dim3((unsigned)((f.in.T + 3) / 4)), dim3(256), 0, stream,
                      f);

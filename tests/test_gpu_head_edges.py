@@ -15,7 +15,7 @@ pytestmark = pytest.mark.gpu
 
 # ---------------------------------------------------------------- teachers
 
-@pytest.mark.parametrize("T,K", [(1, 1), (40, 5), (40, 20), (600, 20)])  # both launch shapes
+@pytest.mark.parametrize("T,K", [(1, 1), (40, 5), (40, 30), (600, 30)])  # both launch shapes
 @pytest.mark.parametrize("top_dtype", [torch.float32, torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("tau", [0.5, 2.0 ** -10, 1.0, 3.0])
 def test_teachers_of_the_types_ends(T, K, top_dtype, tau):
@@ -186,7 +186,9 @@ def test_gradients_of_few_tokens_at_a_temperature(T, V, D, K, tau, dtype):
 
 @pytest.mark.parametrize("T,V,D,K,tau", [(600, 900, 136, 100, 1.0), (513, 2000, 72, 1024, 2.0),
                                          (2000, 300, 64, 257, 0.5), (512, 400, 64, 15, 1.0),
-                                         (512, 400, 64, 16, 1.0), (513, 400, 64, 16, 1.0)])
+                                         (256, 400, 64, 27, 1.0), (256, 400, 64, 28, 1.0),
+                                         (256, 400, 64, 28, 2.0), (257, 400, 64, 28, 1.0),
+                                         (40, 900, 136, 75, 1.0), (1, 300, 64, 76, 0.5)])
 def test_long_teachers(T, V, D, K, tau):
     c = _inputs(T, V, D, K=K, seed=T + K, masked=0.1)
     c["tau"] = tau
