@@ -25,7 +25,8 @@ extern "C" {
  * no word no KL; neither: loss 0, and its row of h is not read.  A teacher's word is
  * kept if it lies in 0 .. V - 1 and its logit is not -infinity; words may come
  * twice (their shares add).  Infinities and NaN of a row of h that has a loss make its
- * loss NaN or infinite, those of W every loss's.
+ * loss NaN or infinite, those of W every loss's; a kept logit of +infinity or NaN makes its token's
+ * loss NaN.
  *   type       of h and W: 1 bfloat16, 2 float16
  *   h          [T, D], W [V, D] (16-byte aligned); D % 8 == 0
  *   labels     int32 (labels_i64 = 0) or int64 (1) [T]
@@ -36,7 +37,7 @@ extern "C" {
  *   loss       float32 [T]
  *   stats      float32 [T (4 + K)]: what tm_head_loss_bwd needs of this call
  *   T 1 .. 2^23, V 1 .. 2^23, D 8 .. 2^16, K 0 .. 1024, T (K + 1) < 2^31
- * Products are exact, sums and softmax statistics float32.
+ * Products of h and W are exact, sums and softmax statistics float32.
  */
 tm_status tm_head_loss(const void* h, const void* W, int32_t type, int64_t T, int64_t V, int64_t D,
                        const void* labels, int32_t labels_i64, const void* top_ids,

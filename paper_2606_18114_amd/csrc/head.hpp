@@ -70,7 +70,7 @@ HeadPlan head_plan(int64_t T, int64_t V, int64_t D);
 // How dh's contraction of nst stages is cut for the n rows in use of T: as planned for T, or,
 // where the tiles of n times those parts leave some of P workgroups idle, into as many more as
 // fill them and as the parts' place, parts T rows, has room for, in fours of stages (3001 tokens
-// of 32003 x 768, a third without a loss: 124 us as planned, 95 so).
+// of 32003 x 768, a third without a loss: 124 us as planned, 95 to 101 so).
 struct HeadCut {
   int parts, per;
 };

@@ -25,8 +25,8 @@
 // spills: accumulators leave their registers a block at a time.
 //
 // Bound: the matrix cores under the power cap (a stage of a full tile takes 0.77 us, 1.36
-// PFLOP/s, at 1.7 to 1.85 GHz).  16384 tokens of 50000 x 2048: softmax sums 2.50 ms (1.34
-// PFLOP/s), dlogits 2.85, dh 2.53, dW 2.45; a tile's epilogue adds 3 us to the sums (its first
+// PFLOP/s, at 1.7 to 1.85 GHz).  16384 tokens of 50000 x 2048: softmax sums 2.50 to 2.60 ms (1.29
+// to 1.34 PFLOP/s), dlogits 2.85 to 2.94, dh 2.53 to 2.60, dW 2.45 to 2.53; a tile's epilogue adds 3 us to the sums (its first
 // loads are then already under way) and 7 to the dlogits.  (Up to 64
 // tokens: head_dw_few_kernel below, and the softmax sums in head_loss.hip.)
 #include <type_traits>

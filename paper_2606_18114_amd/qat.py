@@ -493,8 +493,10 @@ class Head(torch.nn.Module):
     float16 [..., width] (``BlockNorm``'s output); targets int32 or int64 [...],
     a label outside the vocabulary counts nowhere.  With a teacher's top K words
     and their logits [..., K] the loss is the paper's Eq. 1, (1 - alpha) CE +
-    alpha temperature^2 KL over the teacher's words; ids outside the vocabulary
-    are places without a word.  The logits are never kept; the head's weight
+    alpha temperature^2 KL, with the teacher's softmax taken over those words
+    (the paper's runs over the vocabulary); ids outside the vocabulary are
+    places without a word.  The teacher is given: no gradient goes to its
+    logits.  The logits are never kept; the head's weight
     [vocab, width] (float32, bfloat16 or float16; ``weight`` shares one, as
     ``Embedding.weight``) is read in h's type."""
 

@@ -220,3 +220,17 @@ def test_values_at_temperatures_far_from_one(T, V, D, K, tau, dtype):
     c = _inputs(T, V, D, dtype, K=K, seed=T)
     c["tau"] = tau
     _check(c, *_run(c))
+
+
+@pytest.mark.parametrize("T,K", [(9, 3), (40, 30), (300, 5)])
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_a_teachers_infinity_or_nan_stays_with_its_token(T, K, value):
+    c = _inputs(T, 90, 72, K=K, seed=T)
+    want = _run(c)
+    c["top"][4, 1] = value
+    loss, dh, _ = _run(c)
+    rest = torch.arange(T, device="cuda") != 4
+    assert bool(torch.isnan(loss[4])) and not torch.isfinite(dh[4]).any()
+    assert torch.equal(loss[rest], want[0][rest]) and torch.equal(dh[rest], want[1][rest])
+    c["ids"][4, 1] = -1  # no word: nobody looks at it
+    assert all(bool(torch.isfinite(t.float()).all()) for t in _run(c))
